@@ -201,12 +201,15 @@ def prepare(case, seed):
 
 def _codes(X):
     """int8 codes of every row as float32 integers, and its scale: with a the
-    row's largest magnitude, scale a / 127 and round(x (127 / a))."""
+    row's largest magnitude, scale a / 127 and round(x (127 / a)), each quotient
+    rounded once (a number as a divisor or dividend is not: torch multiplies by
+    its reciprocal)."""
     x = X.float()
     a = x.abs().amax(1, keepdim=True)
     live = a > 0
-    q = torch.round(x * (127.0 / torch.where(live, a, 1.0)))
-    return torch.where(live, q, 0.0), (a / 127.0)[:, 0]
+    c = torch.full_like(a, 127.0)
+    q = torch.round(x * (c / torch.where(live, a, 1.0)))
+    return torch.where(live, q, 0.0), (a / c)[:, 0]
 
 
 def _plain_linear(s):
@@ -307,8 +310,9 @@ def exact(case, seed):
         # the codes are defined in 32 bits, everything after them is not
         X = s["X"].to(torch.float32)
         top = X.abs().max(1).values
-        inv = torch.where(top > 0, 127.0 / top, torch.zeros_like(top))
-        q = (X * inv[:, None]).round().double() * (top / 127.0).double()[:, None]
+        full = torch.full_like(top, 127.0)
+        inv = torch.where(top > 0, torch.div(full, top), torch.zeros_like(top))
+        q = (X * inv[:, None]).round().double() * torch.div(top, full).double()[:, None]
         C = s["C"].double()
         ws = s["ws"].double().reshape(case["dout"], -1)
         W = C * ws.repeat_interleave(case["din"] // ws.shape[1], dim=1)
