@@ -273,8 +273,8 @@ def run(state):
     from paper_2609_38599_gb300 import jarq
     c = state["case"]
     if kind == "linear":
-        return {"y": jarq.int8_linear(state["X"], state["C"], state["ws"], group_size=c["g"],
-                                      bias=state["bias"], dtype=str(TYPES[c["y"]])[6:])}
+        return {"y": jarq.integer_linear(state["X"], state["C"], state["ws"], group_size=c["g"],
+                                         bias=state["bias"], dtype=str(TYPES[c["y"]])[6:])}
     if kind == "score":
         r = jarq.token_logprobs(state["x"], state["tok"], top=c["top"])
         out = {"lse": r.lse, "entropy": r.entropy, "logprob": r.logprob}
