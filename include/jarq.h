@@ -31,7 +31,8 @@
  *   buffer it passes.
  * - `stream` is a cudaStream_t passed as void* (NULL = the legacy default
  *   stream).  Work is enqueued on it in order.  Calls return after the work
- *   they enqueued has finished and its status has been read back.
+ *   they enqueued has finished and its status has been read back, except the
+ *   operators that run and score a quantized model, which only enqueue.
  * - Errors are reported as jarq_status values; no exception or abort crosses
  *   the ABI.  On JARQ_ERR_ARG nothing is enqueued and no buffer is touched.
  * - A handle is not thread-safe: do not use one handle from two host threads
@@ -40,6 +41,7 @@
 #ifndef JARQ_H_
 #define JARQ_H_
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -89,7 +91,7 @@ typedef enum jarq_fit {
     JARQ_FIT_COORDINATE = 2    /* cyclic exact coordinate descent on the scales */
 } jarq_fit;
 
-/* Element types of jarq_dequantize's output. */
+/* Element types of weights, activations and logits. */
 typedef enum jarq_dtype { JARQ_F32 = 0, JARQ_F16 = 1, JARQ_BF16 = 2 } jarq_dtype;
 
 /* Per-row statistics.  Every pointer may be NULL (not collected) and may be
@@ -286,6 +288,114 @@ jarq_status jarq_pack_codes(const uint8_t *Q, int dout, int din, int bits, uint3
 jarq_status jarq_accumulate_hessian(const void *X, int n, int d, float scale, float *H,
                                     void *stream);
 
+/* ---- running and scoring a quantized model (device memory only) ----
+ * The paper judges a quantized model by the probabilities that it gives to
+ * tokens (Sec. 4, perplexity).  These operators run a layer in integers and
+ * score logits.  They differ from the calls above in three points, since a
+ * generation step takes microseconds on the device:
+ * - They only enqueue their work on `stream` and return; results are ready in
+ *   stream order, and the calls can be captured in a CUDA graph.
+ * - They allocate nothing on the device and keep no state between calls.
+ * - A failure on the device (a bounded wait that gave up) is reported by
+ *   jarq_async_status, and by every later call of these operators until
+ *   jarq_async_status has reported it.
+ * All pointers are device memory of the current device (JARQ_ERR_ARG
+ * otherwise), outputs must not overlap inputs unless stated, and a row pitch
+ * ld* is in elements and at least the row's length.  Any alignment that the
+ * element type allows is accepted; 16-byte aligned rows are fastest. */
+
+/* Waits for `stream` and returns JARQ_ERR_TIMEOUT if a device wait of these
+ * operators gave up since this was last asked (on any stream; their outputs
+ * since then are invalid), else JARQ_OK. */
+jarq_status jarq_async_status(void *stream);
+
+/* Rows of activations to 8-bit integers with a scale for each row (token):
+ * with a = max_k |X[r][k]| and every quotient and product rounded once to
+ * float32,
+ *     scale[r] = a / 127,  Q[r][k] = rint(X[r][k] * (127 / a))   (half to even),
+ * so |Q| <= 127 and X is about scale * Q.  A row whose a is below 2^-120 gets
+ * scale 0 and codes 0; a row that holds an infinity or a NaN gets scale NaN
+ * and codes 0, so that products with it are NaN.
+ *   X : [n][d] of `dtype`, pitch ldx.  Q : int8 [n][d], pitch ldq.
+ *   scale : float32 [n].  n >= 0, d >= 1. */
+jarq_status jarq_quantize_rows(const void *X, jarq_dtype dtype, int n, int d, int64_t ldx,
+                               int8_t *Q, int64_t ldq, float *scale, void *stream);
+
+/* The integer weights c = q - z of a refined layer (Sec. 3.1, Eq.
+ * quantized_group: what = s c) as int8, for jarq_integer_product; the scales S
+ * [dout][G] are its weight scales as they are.  bits <= 7, so |c| <= 127.
+ *   Q, Z : as jarq_dequantize; C : int8 [dout][din], pitch ldc.
+ * Unlike the operators around it this one checks the codes, which takes a
+ * synchronisation (JARQ_ERR_ARG before any change): it is called once a layer. */
+jarq_status jarq_integer_codes(const uint8_t *Q, const int32_t *Z, int dout, int din,
+                               int group_size, int bits, int8_t *C, int64_t ldc, void *stream);
+
+/* Product of 8-bit integers with scales for each token and channel:
+ *   Y[t][o] = xs[t] * sum_i ws[o][i] * (sum_{k in group i} X[t][k] C[o][k]) + bias[o],
+ * the groups being the G = din / group_size runs of group_size columns, or one
+ * (G = 1) for group_size = 0.
+ *   X : int8 [n][din], pitch ldx; xs : float32 [n].
+ *   C : int8 [dout][din], pitch ldc; ws : float32 [dout][G].
+ *   group_size : 0, 64 or 128 (then a divisor of din).
+ *   bias : float32 [dout] or NULL.  Y : [n][dout] of `dtype`, pitch ldy.
+ *   n >= 0, 1 <= dout, 1 <= din <= 65536.
+ * Precision: the integer sums are exact for any codes.  With G = 1 that sum is
+ * rounded once to float32; with groups the terms are added in float32.  Scales
+ * and bias are applied in float32, with one rounding to `dtype` at the end. */
+jarq_status jarq_integer_product(const int8_t *X, int64_t ldx, const float *xs, const int8_t *C,
+                                 int64_t ldc, const float *ws, int group_size, const float *bias,
+                                 int n, int dout, int din, jarq_dtype dtype, void *Y, int64_t ldy,
+                                 void *stream);
+
+/* A linear layer in 8-bit integers: jarq_quantize_rows of X [n][din] (xdtype,
+ * pitch ldx), then jarq_integer_product, in one call.  workspace: at least
+ * jarq_integer_linear_workspace(n, din) bytes of device memory, 16-byte aligned,
+ * that the stream's work may overwrite (NULL when n is 0). */
+size_t jarq_integer_linear_workspace(int n, int din);
+jarq_status jarq_integer_linear(const void *X, jarq_dtype xdtype, int64_t ldx, const int8_t *C,
+                                int64_t ldc, const float *ws, int group_size, const float *bias,
+                                int n, int dout, int din, jarq_dtype ydtype, void *Y, int64_t ldy,
+                                void *workspace, size_t workspace_bytes, void *stream);
+
+/* Log probabilities of given tokens under a softmax, with its entropy and its
+ * most probable tokens, in one pass over the logits x of every row r:
+ *   lse[r] = ln sum_v exp x_v,      logprob[r][j] = x_{tokens[r][j]} - lse,
+ *   entropy[r] = - sum_v p_v ln p_v,  p_v = exp(x_v - lse),
+ *   top_token[r][i], top_logprob[r][i], i < k: the k largest x in falling order,
+ *   of equal ones the lower token first.
+ *   logits : [n][vocab] of `dtype`, pitch ld.
+ *   tokens : int64 [n][t] (NULL when t is 0).  A negative token is ignored
+ *            (logprob 0); one >= vocab gives logprob NaN.
+ *   logprob [n][t], entropy [n], lse [n], top_logprob [n][k] : float32;
+ *   top_token [n][k] : int32.  entropy and lse may be NULL.
+ *   n >= 0, vocab >= 1, 0 <= t <= 256, 0 <= k <= 32, k <= vocab.
+ * A logit of -inf masks its token: p = 0, never an alternative (where fewer
+ * than k tokens are left the rest is token -1 with logprob -inf).  A row with
+ * all tokens masked has lse = -inf, logprob = -inf and entropy 0.  A NaN or
+ * +inf among a row's logits makes all its values NaN and its tokens -1.
+ * Maxima, sums and outputs are float32. */
+jarq_status jarq_token_logprobs(const void *logits, jarq_dtype dtype, int n, int vocab, int64_t ld,
+                                const int64_t *tokens, int t, int k, float *logprob,
+                                float *entropy, float *lse, float *top_logprob,
+                                int32_t *top_token, void *stream);
+
+/* Gradient of sum_r (sum_j g_logprob[r][j] logprob[r][j] + g_entropy[r] entropy[r])
+ * with respect to the logits of jarq_token_logprobs:
+ *   dx_v = sum_j g_j ([v = tokens_j] - p_v) - g_entropy p_v (ln p_v + entropy),
+ * the sums over tokens that are not negative (a token >= vocab makes the row
+ * NaN); 0 where the logit is -inf.
+ *   logits, dtype, n, vocab, ld, tokens, t : as there, t >= 1.
+ *   lse, entropy : float32 [n], its results; entropy may be NULL when
+ *   g_entropy is.  g_logprob : float32 [n][t].  g_entropy : float32 [n] or NULL.
+ *   dlogits : [n][vocab] of `dtype`, pitch ldd; may be `logits` itself (then
+ *   ldd = ld), otherwise must not overlap it.
+ * Computed in float32, with one rounding to `dtype`. */
+jarq_status jarq_token_logprobs_grad(const void *logits, jarq_dtype dtype, int n, int vocab,
+                                     int64_t ld, const int64_t *tokens, int t, const float *lse,
+                                     const float *entropy, const float *g_logprob,
+                                     const float *g_entropy, void *dlogits, int64_t ldd,
+                                     void *stream);
+
 /* Per-row objective without any device allocation.  The paper has no
  * counterpart: this entry point exists for callers that cannot allocate
  * device memory when they need the objective -- serving processes that
@@ -331,7 +441,8 @@ const char *jarq_status_string(jarq_status s);
  * "hr_full", "grad", "gram", "scale_solve", "symmetrize", "group_factor",
  * "slices", "slice_rows", "proj", "whw", "rhs", "htilde", "ptilde", "syrk",
  * "mu_combine", "own_rhs", "scale_fit", "probe", "sweep_product",
- * "sweep_babai"; also read: "target" and "babai" (the last two, whose launches
+ * "sweep_babai", "quantize_rows", "integer_product", "token_logprobs",
+ * "token_grad"; also read: "target" and "babai" (the last two, whose launches
  * once covered a group instead of a block of 256 columns) and "phase_hr" (no
  * launches).  Not thread-safe. */
 void jarq_profile_enable(int on);

@@ -281,6 +281,16 @@ cudaError_t launch_init_rows(int *active, int *iters, int *accepted, int *ridge,
 // Multiprocessor count of the current device (cached per device ordinal).
 int num_sms();
 
+// ---- operators that only enqueue (k_quantize.cu, k_integer*.cu, k_logprob.cu) ----
+cudaError_t launch_quantize_rows(const void *X, jarq_dtype dtype, int n, int d, int64_t ldx,
+                                 int8_t *Q, int64_t ldq, float *scale, cudaStream_t s);
+// The word in pinned host memory in which their kernels report a wait that
+// gave up (null: it could not be allocated), what it holds, and the same with
+// the word cleared.
+int *async_word();
+jarq_status async_failure();
+jarq_status take_async_failure();
+
 // Enable `bytes` of dynamic shared memory for `func` on the current device:
 // the most that any call of it needs, since the limit is the process's and a
 // smaller one, set by another thread, would refuse a launch on its way.

@@ -192,6 +192,46 @@ cudaError_t StatusWord::read(int *bits) {
     return e;
 }
 
+namespace {
+// Pinned memory is addressable by every device.  Never freed: a kernel may
+// still run while the process ends.
+int *make_async_word() {
+    void *p = nullptr;
+    if (cudaMallocHost(&p, sizeof(int)) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return nullptr;
+    }
+    *static_cast<volatile int *>(p) = 0;
+    return static_cast<int *>(p);
+}
+std::mutex g_async_mu;
+std::atomic<int *> g_async_word{nullptr};
+}  // namespace
+
+int *async_word() {
+    int *p = g_async_word.load(std::memory_order_acquire);
+    if (p) return p;
+    std::lock_guard<std::mutex> lock(g_async_mu);
+    p = g_async_word.load(std::memory_order_relaxed);
+    if (!p) {
+        p = make_async_word();          // tried again by the next call where it fails
+        g_async_word.store(p, std::memory_order_release);
+    }
+    return p;
+}
+
+jarq_status async_failure() {
+    const volatile int *p = g_async_word.load(std::memory_order_acquire);
+    return p && *p ? JARQ_ERR_TIMEOUT : JARQ_OK;
+}
+
+jarq_status take_async_failure() {
+    volatile int *p = g_async_word.load(std::memory_order_acquire);
+    if (!p || !*p) return JARQ_OK;
+    *p = 0;
+    return JARQ_ERR_TIMEOUT;
+}
+
 int num_sms() {
     constexpr int kDevs = 64;
     static std::atomic<int> cache[kDevs];

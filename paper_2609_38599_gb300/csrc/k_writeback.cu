@@ -123,6 +123,33 @@ __global__ void dequantize16_kernel(const float *__restrict__ S, const uint4 *__
     }
 }
 
+// c = q - z as int8 (bits <= 7: |c| <= 127), rows pitch ldc apart.  VEC: 16
+// codes of one group a thread (g a multiple of 16, rows of Q and C 16-byte
+// aligned).
+template <bool VEC>
+__global__ void integer_codes_kernel(const uint8_t *__restrict__ Q, const int32_t *__restrict__ Z,
+                                     int8_t *__restrict__ C, int p, int d, int g, int64_t ldc,
+                                     const int *__restrict__ status) {
+    if (*status) return;
+    constexpr int E = VEC ? 16 : 1;
+    const size_t n = (size_t)p * d / E;
+    const int G = d / g, per = d / E;
+    for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < n;
+         i += (size_t)gridDim.x * blockDim.x) {
+        const size_t j = i / per;
+        const int k = (int)(i - j * per) * E, z = Z[j * G + k / g];
+        if (VEC) {
+            const uint4 q = *reinterpret_cast<const uint4 *>(Q + j * d + k);
+            // byte-wise differences modulo 256
+            const uint32_t z4 = 0x01010101u * (uint32_t)z;
+            *reinterpret_cast<uint4 *>(C + j * ldc + k) =
+                make_uint4(__vsub4(q.x, z4), __vsub4(q.y, z4), __vsub4(q.z, z4), __vsub4(q.w, z4));
+        } else {
+            C[j * ldc + k] = (int8_t)((int)Q[j * d + k] - z);
+        }
+    }
+}
+
 // One thread per 32-bit output word: the codes whose bits [k b, k b + b)
 // overlap bits [32 w, 32 w + 32) of the row's stream.
 __global__ void pack_codes_kernel(const uint8_t *__restrict__ Q, uint32_t *__restrict__ out, int p,
@@ -302,6 +329,26 @@ jarq_status jarq_pack_codes(const uint8_t *Q, int dout, int din, int bits, uint3
     return checked_run(Q, nullptr, dout, din, 0, (1 << bits) - 1, (cudaStream_t)stream,
                        [&](cudaStream_t st, const int *status) {
                            return launch_pack<1>(Q, packed, dout, din, bits, status, st);
+                       });
+}
+
+jarq_status jarq_integer_codes(const uint8_t *Q, const int32_t *Z, int dout, int din,
+                               int group_size, int bits, int8_t *C, int64_t ldc, void *stream) {
+    if (dout < 0 || din <= 0 || group_size <= 0 || din % group_size || bits < 1 || bits > 7 || ldc < din)
+        return JARQ_ERR_ARG;
+    if (dout == 0) return JARQ_OK;
+    if (!Q || !Z || !C || !on_device(Q) || !on_device(Z) || !on_device(C)) return JARQ_ERR_ARG;
+    const int G = din / group_size;
+    return checked_run(Q, Z, dout, din, G, (1 << bits) - 1, (cudaStream_t)stream,
+                       [&](cudaStream_t st, const int *status) {
+                           const size_t n = (size_t)dout * din;
+                           if (group_size % 16 == 0 && ldc % 16 == 0 && (((uintptr_t)Q | (uintptr_t)C) & 15) == 0)
+                               integer_codes_kernel<true><<<grid_for(n / 16), 256, 0, st>>>(
+                                   Q, Z, C, dout, din, group_size, ldc, status);
+                           else
+                               integer_codes_kernel<false><<<grid_for(n), 256, 0, st>>>(
+                                   Q, Z, C, dout, din, group_size, ldc, status);
+                           return cudaGetLastError();
                        });
 }
 

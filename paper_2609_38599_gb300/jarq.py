@@ -33,7 +33,10 @@ EXPORTS = ("jarq_default_options", "jarq_prepare_hessian", "jarq_refine_layer",
            "jarq_objective_noalloc", "jarq_residual_product", "jarq_canonicalize",
            "jarq_dequantize", "jarq_pack_codes", "jarq_accumulate_hessian",
            "jarq_refine_layer_mu", "jarq_fit_scales", "jarq_multicode_probe",
-           "jarq_selftest_wait_timeout", "jarq_selftest_stalled_kernel")
+           "jarq_selftest_wait_timeout", "jarq_selftest_stalled_kernel",
+           "jarq_async_status", "jarq_quantize_rows", "jarq_integer_codes",
+           "jarq_integer_product", "jarq_integer_linear_workspace", "jarq_integer_linear",
+           "jarq_token_logprobs", "jarq_token_logprobs_grad")
 
 
 class JarqError(RuntimeError):
@@ -90,6 +93,24 @@ def _load():
     lib.jarq_pack_codes.argtypes = [vp, ci, ci, ci, vp, vp]
     lib.jarq_accumulate_hessian.restype = ci
     lib.jarq_accumulate_hessian.argtypes = [vp, ci, ci, cf, vp, vp]
+    cl = ctypes.c_int64
+    lib.jarq_async_status.restype = ci
+    lib.jarq_async_status.argtypes = [vp]
+    lib.jarq_quantize_rows.restype = ci
+    lib.jarq_quantize_rows.argtypes = [vp, ci, ci, ci, cl, vp, cl, vp, vp]
+    lib.jarq_integer_codes.restype = ci
+    lib.jarq_integer_codes.argtypes = [vp, vp, ci, ci, ci, ci, vp, cl, vp]
+    lib.jarq_integer_product.restype = ci
+    lib.jarq_integer_product.argtypes = [vp, cl, vp, vp, cl, vp, ci, vp, ci, ci, ci, ci, vp, cl, vp]
+    lib.jarq_integer_linear_workspace.restype = ctypes.c_size_t
+    lib.jarq_integer_linear_workspace.argtypes = [ci, ci]
+    lib.jarq_integer_linear.restype = ci
+    lib.jarq_integer_linear.argtypes = [vp, ci, cl, vp, cl, vp, ci, vp, ci, ci, ci, ci, vp, cl, vp,
+                                        ctypes.c_size_t, vp]
+    lib.jarq_token_logprobs.restype = ci
+    lib.jarq_token_logprobs.argtypes = [vp, ci, ci, ci, cl, vp, ci, ci, vp, vp, vp, vp, vp, vp]
+    lib.jarq_token_logprobs_grad.restype = ci
+    lib.jarq_token_logprobs_grad.argtypes = [vp, ci, ci, ci, cl, vp, ci, vp, vp, vp, vp, vp, cl, vp]
     lib.jarq_hessian_din.restype = ci
     lib.jarq_hessian_din.argtypes = [vp]
     lib.jarq_hessian_group_size.restype = ci
@@ -125,7 +146,7 @@ def library():
 KERNELS = ("validate", "residual", "init_rows", "hr_full", "grad", "gram", "scale_solve",
            "symmetrize", "group_factor", "slices", "slice_rows", "proj", "whw", "rhs", "htilde",
            "ptilde", "syrk", "mu_combine", "own_rhs", "scale_fit", "probe", "sweep_product",
-           "sweep_babai")
+           "sweep_babai", "quantize_rows", "integer_product", "token_logprobs", "token_grad")
 
 
 def profile_enable(on: bool = True):
@@ -451,3 +472,187 @@ def objective(hess: Hessian, W, S, Q, Z, bits: int, out=None):
     if status != JARQ_OK:
         raise JarqError(status, "jarq_objective")
     return F
+
+
+# ---- running and scoring a quantized model: device tensors, enqueued on torch's
+# current stream, not waited for ----
+
+def _rows(x, name, *dtypes):
+    """(pointer, row pitch) of a CUDA matrix whose rows are contiguous."""
+    if x.dtype not in dtypes or not x.is_cuda or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise TypeError(f"{name}: expected a CUDA matrix of {' or '.join(str(d) for d in dtypes)} with "
+                        f"contiguous rows, got {x.dtype} {tuple(x.shape)} on {x.device}")
+    # the pitch of a single row is never used
+    return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+
+def _flat(x, name, dtype, *shapes):
+    """Pointer of a contiguous CUDA tensor of one of the given shapes."""
+    if x.dtype != dtype or not x.is_cuda or not x.is_contiguous() or tuple(x.shape) not in shapes:
+        raise TypeError(f"{name}: expected a contiguous CUDA tensor of {dtype}, shape "
+                        f"{' or '.join(str(s) for s in shapes)}, got {x.dtype} {tuple(x.shape)} on {x.device}")
+    return x.data_ptr()
+
+
+def _float_types():
+    """jarq_dtype of every torch type of weights, activations and logits."""
+    import torch
+    return {torch.float32: JARQ_F32, torch.float16: JARQ_F16, torch.bfloat16: JARQ_BF16}
+
+
+def _named_type(dtype):
+    import torch
+    return {"float32": torch.float32, "float16": torch.float16, "bfloat16": torch.bfloat16}[dtype]
+
+
+def async_status(device=None) -> int:
+    """``jarq_async_status`` on torch's current stream: waits for it;
+    JARQ_ERR_TIMEOUT if a device wait of an enqueued operator gave up."""
+    import torch
+    return int(_lib.jarq_async_status(ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)))
+
+
+def quantize_rows(X):
+    """``jarq_quantize_rows``: (codes int8 [n][d], scale float32 [n]) of a
+    float32, float16 or bfloat16 matrix, one scale a row.  The rows of the codes
+    lie on 16-byte boundaries."""
+    import torch
+    types = _float_types()
+    ptr, ldx = _rows(X, "X", *types)
+    n, d = int(X.shape[0]), int(X.shape[1])
+    q = torch.empty(n, (d + 15) // 16 * 16, dtype=torch.int8, device=X.device)
+    scale = torch.empty(n, dtype=torch.float32, device=X.device)
+    status = _lib.jarq_quantize_rows(ptr, types[X.dtype], n, d, ldx, q.data_ptr(), q.shape[1],
+                                     scale.data_ptr(), _dev_stream(X))
+    if status != JARQ_OK:
+        raise JarqError(status, "jarq_quantize_rows")
+    return q[:, :d], scale
+
+
+def integer_codes(Q, Z, group_size: int, bits: int):
+    """``jarq_integer_codes``: q - z of a refined layer as int8 [dout][din], the
+    weights of ``integer_linear`` with the scales S and this group size."""
+    import torch
+    dout, din = int(Q.shape[0]), int(Q.shape[1])
+    C = torch.empty(dout, (din + 15) // 16 * 16, dtype=torch.int8, device=Q.device)
+    status = _lib.jarq_integer_codes(_ptr(Q, np.uint8), _ptr(Z, np.int32), dout, din, int(group_size),
+                                     int(bits), C.data_ptr(), C.shape[1], _dev_stream(Q))
+    if status != JARQ_OK:
+        raise JarqError(status, "jarq_integer_codes")
+    return C[:, :din]
+
+
+def _integer_layer(C, ws, group_size, bias, n, din, dtype, out, device):
+    """The arguments that both integer products share, and their output."""
+    import torch
+    c, ldc = _rows(C, "C", torch.int8)
+    dout = int(C.shape[0])
+    if int(C.shape[1]) != din:
+        raise ValueError(f"weights have {int(C.shape[1])} columns, activations {din}")
+    G = din // group_size if group_size else 1
+    w = _flat(ws, "ws", torch.float32, (dout, G), *([(dout,)] if G == 1 else []))
+    b = _flat(bias, "bias", torch.float32, (dout,)) if bias is not None else None
+    if out is None:
+        out = torch.empty(n, dout, dtype=dtype, device=device)
+    elif tuple(out.shape) != (n, dout):
+        raise ValueError(f"out has shape {tuple(out.shape)}, not {(n, dout)}")
+    y, ldy = _rows(out, "out", dtype)
+    return c, ldc, w, b, dout, out, y, ldy
+
+
+def integer_product(X, xs, C, ws, group_size: int = 0, bias=None, dtype: str = "float16", out=None):
+    """``jarq_integer_product``: ``xs[t] * sum_i ws[o][i] * (X_i C_i^T) + bias`` for
+    int8 codes X [n][din] and C [dout][din], as float32, float16 or bfloat16."""
+    import torch
+    x, ldx = _rows(X, "X", torch.int8)
+    n, din = int(X.shape[0]), int(X.shape[1])
+    tdt = _named_type(dtype)
+    s = _flat(xs, "xs", torch.float32, (n,))
+    c, ldc, w, b, dout, out, y, ldy = _integer_layer(C, ws, group_size, bias, n, din, tdt, out, X.device)
+    status = _lib.jarq_integer_product(x, ldx, s, c, ldc, w, int(group_size), b, n, dout, din,
+                                       _float_types()[tdt], y, ldy, _dev_stream(X))
+    if status != JARQ_OK:
+        raise JarqError(status, "jarq_integer_product")
+    return out
+
+
+def integer_linear(X, C, ws, group_size: int = 0, bias=None, dtype: str = None, out=None):
+    """``jarq_integer_linear``: the activations X [n][din] (float32, float16 or
+    bfloat16) quantized token by token and multiplied with the int8 weights C
+    [dout][din]; the result in ``dtype`` (X's own when None)."""
+    import torch
+    types = _float_types()
+    x, ldx = _rows(X, "X", *types)
+    n, din = int(X.shape[0]), int(X.shape[1])
+    tdt = X.dtype if dtype is None else _named_type(dtype)
+    c, ldc, w, b, dout, out, y, ldy = _integer_layer(C, ws, group_size, bias, n, din, tdt, out, X.device)
+    size = _lib.jarq_integer_linear_workspace(n, din)
+    work = torch.empty(size, dtype=torch.uint8, device=X.device)
+    status = _lib.jarq_integer_linear(x, types[X.dtype], ldx, c, ldc, w, int(group_size), b, n, dout, din,
+                                      types[tdt], y, ldy, work.data_ptr(), size, _dev_stream(X))
+    if status != JARQ_OK:
+        raise JarqError(status, "jarq_integer_linear")
+    return out
+
+
+@dataclass
+class TokenScores:
+    """Results of ``token_logprobs``, float32 (``top_token`` int32)."""
+    logprob: object
+    entropy: object
+    lse: object
+    top_logprob: object
+    top_token: object
+
+
+def token_logprobs(logits, tokens=None, top: int = 0) -> TokenScores:
+    """``jarq_token_logprobs``: log probabilities of ``tokens`` (int64 [n] or
+    [n][t]) under the rows of ``logits`` [n][vocab], the rows' entropies and log
+    sums of exponentials, and their ``top`` most probable tokens."""
+    import torch
+    types = _float_types()
+    x, ld = _rows(logits, "logits", *types)
+    n, vocab, k = int(logits.shape[0]), int(logits.shape[1]), int(top)
+    dev = logits.device
+    t, tok, logprob = 0, None, None
+    if tokens is not None:
+        t = 1 if tokens.dim() == 1 else int(tokens.shape[1])
+        tok = _flat(tokens, "tokens", torch.int64, (n,), (n, t))
+        logprob = torch.empty(tokens.shape, dtype=torch.float32, device=dev)
+    stats = torch.empty(2, n, dtype=torch.float32, device=dev)
+    top_logprob = torch.empty(n, k, dtype=torch.float32, device=dev) if k > 0 else None
+    top_token = torch.empty(n, k, dtype=torch.int32, device=dev) if k > 0 else None
+    entropy, lse = stats[0], stats[1]
+    status = _lib.jarq_token_logprobs(x, types[logits.dtype], n, vocab, ld, tok, t, k,
+                                      logprob.data_ptr() if t else None, stats.data_ptr(),
+                                      stats.data_ptr() + 4 * n, top_logprob.data_ptr() if k > 0 else None,
+                                      top_token.data_ptr() if k > 0 else None, _dev_stream(logits))
+    if status != JARQ_OK:
+        raise JarqError(status, "jarq_token_logprobs")
+    return TokenScores(logprob, entropy, lse, top_logprob, top_token)
+
+
+def token_logprobs_grad(logits, tokens, lse, g_logprob, entropy=None, g_entropy=None, out=None):
+    """``jarq_token_logprobs_grad``: gradient with respect to ``logits`` of
+    ``(g_logprob * logprob).sum() + (g_entropy * entropy).sum()``; ``lse`` and
+    ``entropy`` are ``token_logprobs``'s.  ``out`` may be ``logits``."""
+    import torch
+    types = _float_types()
+    x, ld = _rows(logits, "logits", *types)
+    n, vocab = int(logits.shape[0]), int(logits.shape[1])
+    t = 1 if tokens.dim() == 1 else int(tokens.shape[1])
+    tok = _flat(tokens, "tokens", torch.int64, (n,), (n, t))
+    g = _flat(g_logprob, "g_logprob", torch.float32, tuple(tokens.shape))
+    s = _flat(lse, "lse", torch.float32, (n,))
+    h = _flat(entropy, "entropy", torch.float32, (n,)) if entropy is not None else None
+    gh = _flat(g_entropy, "g_entropy", torch.float32, (n,)) if g_entropy is not None else None
+    if out is None:
+        out = torch.empty(n, vocab, dtype=logits.dtype, device=logits.device)
+    elif tuple(out.shape) != (n, vocab):
+        raise ValueError(f"out has shape {tuple(out.shape)}, not {(n, vocab)}")
+    dx, ldd = _rows(out, "out", logits.dtype)
+    status = _lib.jarq_token_logprobs_grad(x, types[logits.dtype], n, vocab, ld, tok, t, s, h, g, gh, dx,
+                                           ldd, _dev_stream(logits))
+    if status != JARQ_OK:
+        raise JarqError(status, "jarq_token_logprobs_grad")
+    return out
