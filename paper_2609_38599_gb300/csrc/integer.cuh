@@ -1,0 +1,42 @@
+// The integer product's arguments, shared by its kernels.
+#pragma once
+
+#include "jarq_internal.cuh"
+
+namespace jarq {
+
+// Y[t][o] = xs[t] sum_i ws[o][i] (sum_{k in group i} X[t][k] C[o][k]) + bias[o]
+struct ProductArgs {
+    const int8_t *X, *C;
+    const float *xs, *ws, *bias;
+    void *Y;
+    int64_t ldx, ldc, ldy;
+    int n, dout, din, g, G;      // g: group size, 0 for one scale a channel (G = 1)
+    jarq_dtype dtype;            // of Y
+};
+
+// Codes k .. k + 15 of a row of `len`; zeros beyond it, which are not read.
+template <bool VEC>
+__device__ __forceinline__ uint4 load_codes(const int8_t *row, int k, int len) {
+    if (VEC && k + 16 <= len) return *reinterpret_cast<const uint4 *>(row + k);
+    uint32_t w[4] = {0, 0, 0, 0};
+    if (k < len) {
+#pragma unroll
+        for (int b = 0; b < 16; ++b)
+            if (k + b < len) w[b / 4] |= (uint32_t)(uint8_t)row[k + b] << (8 * (b % 4));
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Whether all rows of codes lie on 16-byte boundaries.
+inline bool vector_rows(const ProductArgs &a) {
+    return (((uintptr_t)a.X | (uintptr_t)a.C) & 15) == 0 && (a.ldx % 16 == 0 || a.n == 1) &&
+           (a.ldc % 16 == 0 || a.dout == 1);
+}
+
+// More than a few tokens, on the tensor cores (k_tc_integer.cu).  `failed`: set
+// to 1 by a kernel whose waits gave up.  pdl: X and xs are the previous kernel's
+// results, and that kernel reads or writes nothing else of a's.
+cudaError_t launch_tc_integer(const ProductArgs &a, int *failed, cudaStream_t s, bool pdl);
+
+}  // namespace jarq

@@ -1,85 +1,133 @@
 // Product of 8-bit integers with scales for each token and channel:
 //   Y[t][o] = xs[t] sum_i ws[o][i] (sum_{k in group i} X[t][k] C[o][k]) + bias[o].
+//
+// Up to eight tokens: integer dot products of four, bound by reading the weights
+// once.  A block has R channels; its threads share K, 16 codes of each channel
+// at a time with 16 codes of each token, the next weights on their way while
+// these are used.  With one scale a channel the sums are int32 (exact for din <=
+// 65536); with groups (a multiple of 16) each product of 16 is scaled into a
+// float32 sum.
+#include "integer.cuh"
 #include "rows.cuh"
+#include "tc_common.cuh"
 
 namespace jarq {
 namespace {
 
 using namespace rows;
 
-struct ProductArgs {
-    const int8_t *X, *C;
-    const float *xs, *ws, *bias;
-    void *Y;
-    int64_t ldx, ldc, ldy;
-    int n, dout, din, g, G;
-};
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kFew = 8;                     // most tokens of this form
 
-constexpr int kTile = 64, kStep = 64;      // 64 x 64 outputs, 64 of K a step
-
-// Simple form: 256 threads, 4 x 4 outputs each, integer dot products of four.
-template <class T>
-__global__ void __launch_bounds__(256) integer_product_kernel(ProductArgs a) {
-    __shared__ uint32_t sx[kTile][kStep / 4 + 1], sc[kTile][kStep / 4 + 1];
-    const int t0 = blockIdx.y * kTile, o0 = blockIdx.x * kTile;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    float acc[4][4] = {};
-    int sum[4][4] = {};
-    for (int k0 = 0; k0 < a.din; k0 += kStep) {
-        for (int i = threadIdx.x; i < kTile * kStep / 4; i += 256) {
-            const int r = i / (kStep / 4), c = i % (kStep / 4);
-            uint32_t wx = 0, wc = 0;
+// Sums of V values over the lanes of a warp: value i ends in lane 32 / V i.
+template <int V>
+__device__ __forceinline__ float warp_sums(float (&v)[V], int lane) {
+    int left = V;
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const int k = k0 + 4 * c + b;
-                if (k < a.din && t0 + r < a.n) wx |= (uint32_t)(uint8_t)a.X[(size_t)(t0 + r) * a.ldx + k] << (8 * b);
-                if (k < a.din && o0 + r < a.dout)
-                    wc |= (uint32_t)(uint8_t)a.C[(size_t)(o0 + r) * a.ldc + k] << (8 * b);
-            }
-            sx[r][c] = wx;
-            sc[r][c] = wc;
-        }
-        __syncthreads();
-        for (int c = 0; c < kStep / 4; ++c) {
+    for (int off = 16; off > 0; off /= 2) {
+        if (left > 1) {
+            left /= 2;
+            const bool up = lane & off;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    sum[i][j] = __dp4a((int)sx[ty + 16 * i][c], (int)sc[tx + 16 * j][c], sum[i][j]);
-        }
-        __syncthreads();
-        if (a.g && (k0 + kStep) % a.g == 0) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int o = o0 + tx + 16 * j;
-                const float w = o < a.dout ? a.ws[(size_t)o * a.G + k0 / a.g] : 0.f;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    acc[i][j] = fmaf((float)sum[i][j], w, acc[i][j]);
-                    sum[i][j] = 0;
+            for (int i = 0; i < V / 2; ++i)
+                if (i < left) {
+                    const float give = up ? v[i] : v[i + left], keep = up ? v[i + left] : v[i];
+                    v[i] = keep + __shfl_xor_sync(0xffffffffu, give, off);
                 }
+        } else {
+            v[0] += __shfl_xor_sync(0xffffffffu, v[0], off);
+        }
+    }
+    return v[0];
+}
+
+// M: tokens (a.n <= M); R: channels of a block.
+template <int M, int R, bool GROUPS, bool VEC>
+__global__ void __launch_bounds__(kThreads) few_tokens_kernel(ProductArgs a) {
+    constexpr int V = M * R;
+    __shared__ uint32_t parts[kWarps][V];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int o0 = blockIdx.x * R, chunks = (a.din + 15) / 16;
+    uint4 w[R];
+    auto fetch = [&](int r, int c) {
+        if (o0 + r < a.dout && c < chunks) w[r] = load_codes<VEC>(a.C + (size_t)(o0 + r) * a.ldc, 16 * c, a.din);
+    };
+#pragma unroll
+    for (int r = 0; r < R; ++r) w[r] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int r = 0; r < R; ++r) fetch(r, tid);
+    // the tokens' codes may be the previous kernel's
+    tc::pdl_wait();
+    int sum[V] = {};
+    float acc[V] = {};
+    for (int c = tid; c < chunks; c += kThreads) {
+        uint4 x[M];
+#pragma unroll
+        for (int m = 0; m < M; ++m) x[m] = load_codes<VEC>(a.X + (size_t)min(m, a.n - 1) * a.ldx, 16 * c, a.din);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const uint4 wr = w[r];
+            const float s = GROUPS && o0 + r < a.dout ? a.ws[(size_t)(o0 + r) * a.G + 16 * c / a.g] : 0.f;
+            fetch(r, c + kThreads);
+#pragma unroll
+            for (int m = 0; m < M; ++m) {
+                int d = GROUPS ? 0 : sum[r * M + m];
+                d = __dp4a((int)wr.x, (int)x[m].x, d);
+                d = __dp4a((int)wr.y, (int)x[m].y, d);
+                d = __dp4a((int)wr.z, (int)x[m].z, d);
+                d = __dp4a((int)wr.w, (int)x[m].w, d);
+                if (GROUPS)
+                    acc[r * M + m] = fmaf((float)d, s, acc[r * M + m]);
+                else
+                    sum[r * M + m] = d;
             }
         }
     }
+    if (GROUPS) {
+        const float v = warp_sums(acc, lane);
+        if (V == 32 || lane % (32 / V) == 0) parts[warp][lane / (32 / V)] = __float_as_uint(v);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int t = t0 + ty + 16 * i, o = o0 + tx + 16 * j;
-            if (t >= a.n || o >= a.dout) continue;
-            const float v = a.g ? acc[i][j] : (float)sum[i][j] * a.ws[o];
-            static_cast<T *>(a.Y)[(size_t)t * a.ldy + o] = from_float<T>(fmaf(v, a.xs[t], a.bias ? a.bias[o] : 0.f));
+        for (int i = 0; i < V; ++i) {
+            const int v = __reduce_add_sync(0xffffffffu, sum[i]);
+            if (lane == i) parts[warp][i] = (uint32_t)v;
         }
+    }
+    __syncthreads();
+    const int o = o0 + tid / M, m = tid % M;
+    if (tid >= V || o >= a.dout || m >= a.n) return;
+    float f = 0.f;
+    int i = 0;
+#pragma unroll
+    for (int p = 0; p < kWarps; ++p) {
+        f += __uint_as_float(parts[p][tid]);
+        i += (int)parts[p][tid];
+    }
+    const float v = GROUPS ? f : (float)i * a.ws[o];
+    const float y = fmaf(v, a.xs[m], a.bias ? a.bias[o] : 0.f);
+    with_type_device(a.dtype, [&](auto type) {
+        using T = decltype(type);
+        static_cast<T *>(a.Y)[(size_t)m * a.ldy + o] = from_float<T>(y);
+    });
 }
 
-cudaError_t launch_product(const ProductArgs &a, jarq_dtype dtype, cudaStream_t s) {
-    const dim3 grid((a.dout + kTile - 1) / kTile, (a.n + kTile - 1) / kTile);
-    if (grid.y > 65535) return cudaErrorInvalidValue;
-    with_type(dtype, [&](auto type) {
-        integer_product_kernel<decltype(type)><<<grid, 256, 0, s>>>(a);
-        return 0;
-    });
-    return cudaGetLastError();
+template <int M, int R>
+cudaError_t launch_few(const ProductArgs &a, cudaStream_t s, bool pdl) {
+    const dim3 grid((a.dout + R - 1) / R);
+    const bool vec = vector_rows(a);
+    if (a.g)
+        return vec ? launch_k(few_tokens_kernel<M, R, true, true>, grid, dim3(kThreads), 0, s, pdl, a)
+                   : launch_k(few_tokens_kernel<M, R, true, false>, grid, dim3(kThreads), 0, s, pdl, a);
+    return vec ? launch_k(few_tokens_kernel<M, R, false, true>, grid, dim3(kThreads), 0, s, pdl, a)
+               : launch_k(few_tokens_kernel<M, R, false, false>, grid, dim3(kThreads), 0, s, pdl, a);
+}
+
+cudaError_t launch_product(const ProductArgs &a, int *failed, cudaStream_t s, bool pdl) {
+    if (a.n == 1) return launch_few<1, 8>(a, s, pdl);
+    if (a.n == 2) return launch_few<2, 8>(a, s, pdl);
+    if (a.n <= 4) return launch_few<4, 4>(a, s, pdl);
+    if (a.n <= kFew) return launch_few<8, 4>(a, s, pdl);
+    return launch_tc_integer(a, failed, s, pdl);
 }
 
 jarq_status check_layer(const int8_t *C, int64_t ldc, const float *ws, int group_size,
@@ -94,9 +142,11 @@ jarq_status check_layer(const int8_t *C, int64_t ldc, const float *ws, int group
     return JARQ_OK;
 }
 
-jarq_status run_product(const ProductArgs &a, jarq_dtype dtype, cudaStream_t st) {
+jarq_status run_product(const ProductArgs &a, cudaStream_t st, bool pdl) {
+    int *failed = async_word();
+    if (!failed) return JARQ_ERR_NOMEM;
     ProfScope ps("integer_product", st);
-    const cudaError_t e = launch_product(a, dtype, st);
+    const cudaError_t e = launch_product(a, failed, st, pdl);
     ps.done();
     count_launches(1);
     if (e != cudaSuccess) {
@@ -149,8 +199,8 @@ jarq_status jarq_integer_product(const int8_t *X, int64_t ldx, const float *xs, 
     if (!X || !xs || !on_device(X) || !on_device(xs) || (uintptr_t)xs & 3) return JARQ_ERR_ARG;
     if (const jarq_status late = async_failure()) return late;
     return run_product({X, C, xs, ws, bias, Y, ldx, ldc, ldy, n, dout, din, group_size,
-                        group_size ? din / group_size : 1},
-                       dtype, (cudaStream_t)stream);
+                        group_size ? din / group_size : 1, dtype},
+                       (cudaStream_t)stream, false);
 }
 
 size_t jarq_integer_linear_workspace(int n, int din) {
@@ -176,9 +226,10 @@ jarq_status jarq_integer_linear(const void *X, jarq_dtype xdtype, int64_t ldx, c
     float *xs = reinterpret_cast<float *>(q + (size_t)n * ldq);
     const jarq_status e = run_quantize(X, xdtype, n, din, ldx, q, ldq, xs, st);
     if (e != JARQ_OK) return e;
+    // the product starts under the quantization and reads weights meanwhile
     return run_product({q, C, xs, ws, bias, Y, ldq, ldc, ldy, n, dout, din, group_size,
-                        group_size ? din / group_size : 1},
-                       ydtype, st);
+                        group_size ? din / group_size : 1, ydtype},
+                       st, true);
 }
 
 jarq_status jarq_async_status(void *stream) {

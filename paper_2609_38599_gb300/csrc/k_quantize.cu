@@ -5,6 +5,7 @@
 // maximum is taken over the threads that share it, and the codes are formed
 // from the registers.
 #include "rows.cuh"
+#include "tc_common.cuh"
 
 namespace jarq {
 namespace {
@@ -27,6 +28,7 @@ struct QuantArgs {
 template <class T, int kPerRow>
 __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(QuantArgs a) {
     constexpr int E = kUnit<T>;
+    tc::pdl_launch_dependents();          // a product may read its weights meanwhile
     __shared__ uint32_t part[kThreads / 32];
     const int r = blockIdx.x * (kThreads / kPerRow) + threadIdx.x / kPerRow, t = threadIdx.x % kPerRow;
     if (kPerRow == 32 && r >= a.n) return;

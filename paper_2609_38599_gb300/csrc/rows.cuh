@@ -111,6 +111,15 @@ auto with_type(jarq_dtype dtype, F f) {
     if (dtype == JARQ_BF16) return f(__nv_bfloat16());
     return f(float());
 }
+template <class F>
+__device__ __forceinline__ void with_type_device(jarq_dtype dtype, F f) {
+    if (dtype == JARQ_F16)
+        f(__half());
+    else if (dtype == JARQ_BF16)
+        f(__nv_bfloat16());
+    else
+        f(float());
+}
 inline bool is_dtype(jarq_dtype t) { return t == JARQ_F32 || t == JARQ_F16 || t == JARQ_BF16; }
 inline size_t size_of(jarq_dtype t) { return t == JARQ_F32 ? 4 : 2; }
 
