@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import concurrent.futures
 import os
+import re
 import shutil
 import subprocess
 import sys
@@ -22,6 +23,22 @@ FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", 
          "-I" + os.path.join(ROOT, "include")]
 
 
+# Registers a thread that kernels with roles of different register counts must be
+# compiled for: the roles' sum would not fit a smaller block, and they would wait
+# for registers that never come.
+LAUNCH_REGISTERS = {"k_tc_integer.cu": (("tc_integer_kernelILi256E", 96), ("tc_integer_kernelILi128ELb0ELb0E", 80),
+                                        ("tc_integer_kernelILi128ELb1ELb0E", 80))}
+
+
+def check_registers(src: str, ptxas_output: str) -> None:
+    """Raises unless ptxas gave the kernels of LAUNCH_REGISTERS their count."""
+    found = re.findall(r"Compiling entry function '(\S+)'.*?Used (\d+) registers", ptxas_output, flags=re.S)
+    for part, want in LAUNCH_REGISTERS.get(os.path.basename(src), ()):
+        counts = [int(n) for name, n in found if part in name]
+        if not counts or min(counts) < want:
+            raise RuntimeError(f"{src}: {part} compiled for {counts} registers a thread, {want} are needed")
+
+
 def nvcc() -> str:
     exe = shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"
     if not os.path.exists(exe):
@@ -31,10 +48,18 @@ def nvcc() -> str:
 
 def _compile(src: str, extra) -> str:
     obj = os.path.join(BUILD, os.path.basename(src)[:-3] + ".o")
-    cmd = [nvcc(), *ARCH, *FLAGS, *extra, "-c", src, "-o", obj]
+    checked = os.path.basename(src) in LAUNCH_REGISTERS
+    info = ["-Xptxas", "-v"] if checked and not extra else []
+    cmd = [nvcc(), *ARCH, *FLAGS, *extra, *info, "-c", src, "-o", obj]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError(f"nvcc failed on {src}:\n{res.stdout}\n{res.stderr}")
+    if checked:
+        try:
+            check_registers(src, res.stdout + res.stderr)
+        except RuntimeError:
+            os.remove(obj)
+            raise
     if res.stderr.strip() and "-Xptxas" in " ".join(extra):
         sys.stderr.write(res.stderr)
     return obj

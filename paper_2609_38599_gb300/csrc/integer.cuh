@@ -15,15 +15,26 @@ struct ProductArgs {
     jarq_dtype dtype;            // of Y
 };
 
-// Codes k .. k + 15 of a row of `len`; zeros beyond it, which are not read.
+// Codes k .. k + 15 of a row of `len`; zeros beyond it, which are not read.  VEC:
+// the row and k are multiples of 16 bytes; otherwise whole words inside the row
+// are read and shifted, and single codes at its ends.
 template <bool VEC>
 __device__ __forceinline__ uint4 load_codes(const int8_t *row, int k, int len) {
-    if (VEC && k + 16 <= len) return *reinterpret_cast<const uint4 *>(row + k);
+    const int8_t *p = row + k;
+    if (VEC && k + 16 <= len) return *reinterpret_cast<const uint4 *>(p);
     uint32_t w[4] = {0, 0, 0, 0};
-    if (k < len) {
+    if (!VEC && k >= 4 && k + 20 <= len) {
+        const uint32_t off = (uint32_t)((uintptr_t)p & 3), sel = 0x3210u + 0x1111u * off;
+        const uint32_t *q = reinterpret_cast<const uint32_t *>(p - off);
+        uint32_t v[5];
+#pragma unroll
+        for (int i = 0; i < 5; ++i) v[i] = q[i];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __byte_perm(v[i], v[i + 1], sel);
+    } else if (k < len) {
 #pragma unroll
         for (int b = 0; b < 16; ++b)
-            if (k + b < len) w[b / 4] |= (uint32_t)(uint8_t)row[k + b] << (8 * (b % 4));
+            if (k + b < len) w[b / 4] |= (uint32_t)(uint8_t)p[b] << (8 * (b % 4));
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }

@@ -26,12 +26,10 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t
                                   const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// 2D tensor map of 2-byte elements (bf16 or fp16) over [rows][cols]
-// (pitch = cols), box_rows x 64 boxes with 128-byte swizzle or box_rows x 32
-// boxes with 64-byte swizzle, out-of-range elements read as zero.
-cudaError_t make_tmap_2b(CUtensorMap *m, const void *base, uint64_t rows, uint64_t cols,
-                         uint32_t box_rows, CUtensorMapDataType dtype, uint32_t box_cols) {
-    static EncodeTiledFn fn = nullptr;
+// Calls that only enqueue may meet here on several host threads.
+static cudaError_t encode_tiled(EncodeTiledFn *out) {
+    static std::atomic<EncodeTiledFn> known{nullptr};
+    EncodeTiledFn fn = known.load(std::memory_order_acquire);
     if (!fn) {
         void *ptr = nullptr;
         cudaDriverEntryPointQueryResult q;
@@ -40,7 +38,19 @@ cudaError_t make_tmap_2b(CUtensorMap *m, const void *base, uint64_t rows, uint64
         if (e != cudaSuccess || q != cudaDriverEntryPointSuccess || !ptr)
             return e != cudaSuccess ? e : cudaErrorSymbolNotFound;
         fn = (EncodeTiledFn)ptr;
+        known.store(fn, std::memory_order_release);
     }
+    *out = fn;
+    return cudaSuccess;
+}
+
+// 2D tensor map of 2-byte elements (bf16 or fp16) over [rows][cols]
+// (pitch = cols), box_rows x 64 boxes with 128-byte swizzle or box_rows x 32
+// boxes with 64-byte swizzle, out-of-range elements read as zero.
+cudaError_t make_tmap_2b(CUtensorMap *m, const void *base, uint64_t rows, uint64_t cols,
+                         uint32_t box_rows, CUtensorMapDataType dtype, uint32_t box_cols) {
+    EncodeTiledFn fn;
+    if (const cudaError_t e = encode_tiled(&fn); e != cudaSuccess) return e;
     cuuint64_t dims[2] = {cols, rows};
     cuuint64_t strides[1] = {cols * 2};
     cuuint32_t box[2] = {box_cols, box_rows};
@@ -48,6 +58,20 @@ cudaError_t make_tmap_2b(CUtensorMap *m, const void *base, uint64_t rows, uint64
     CUresult r = fn(m, dtype, 2, const_cast<void *>(base), dims, strides,
                     box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
                     box_cols == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+cudaError_t make_tmap_codes(CUtensorMap *m, const int8_t *base, uint64_t rows, uint64_t cols,
+                            uint64_t pitch, uint32_t box_rows) {
+    EncodeTiledFn fn;
+    if (const cudaError_t e = encode_tiled(&fn); e != cudaSuccess) return e;
+    cuuint64_t dims[2] = {cols, rows};
+    cuuint64_t strides[1] = {pitch};
+    cuuint32_t box[2] = {128, box_rows};
+    cuuint32_t es[2] = {1, 1};
+    CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t *>(base), dims, strides, box, es,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }

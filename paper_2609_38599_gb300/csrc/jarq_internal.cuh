@@ -364,6 +364,10 @@ class StatusWord {
 // zero.
 cudaError_t make_tmap_2b(CUtensorMap *m, const void *base, uint64_t rows, uint64_t cols,
                          uint32_t box_rows, CUtensorMapDataType dtype, uint32_t box_cols);
+// The same of int8 codes over [rows][cols], pitch a multiple of 16 bytes:
+// box_rows x 128 boxes, 128-byte swizzle.
+cudaError_t make_tmap_codes(CUtensorMap *m, const int8_t *base, uint64_t rows, uint64_t cols,
+                            uint64_t pitch, uint32_t box_rows);
 cudaError_t make_tmap_bf16(CUtensorMap *m, const void *base, uint64_t rows, uint64_t cols,
                            uint32_t box_rows, uint32_t box_cols = 64);
 cudaError_t make_tmap_f16(CUtensorMap *m, const void *base, uint64_t rows, uint64_t cols,

@@ -1,21 +1,30 @@
 // The integer product's tensor-core form, for more than a few tokens.
 //
 // GB300's 8-bit integer tensor rate is a small fraction of its fp16 rate, so
-// int8 codes become fp16 on the way into shared memory (exactly: |c| <= 128) and
-// the product runs on fp16 MMAs.  Their sums are integers of at most
-// 128 128 1024 = 2^24 over 1024 of K, exact in the float32 accumulator; after
-// that many, or after each group, they leave it: with one scale a channel for
-// an int32 sum, with groups for a float32 sum of the terms ws_i sum_i.
+// int8 codes become fp16 inside the SM (exactly: |c| <= 128) and the product
+// runs on fp16 MMAs.  Their sums are integers of at most 128 128 1024 = 2^24
+// over 1024 of K, exact in the float32 accumulator; after that many, or after
+// each group, they leave it: with one scale a channel for an int32 sum, with
+// groups for a float32 sum of the terms ws_i sum_i.
 //
 // A pair of CTAs (cta_group::2): 256 channels x NT tokens, channels on the lanes
 // of TMEM, so that a thread of the epilogue has one channel and its group's
-// scale in a register.  Per 128 of K each CTA converts its own 128 channels and
-// half of the tokens.
-//   warp 0        MMA issuer (of the pair's even CTA); warp 1: TMEM
-//   warps 4..11   loaders: 16 codes at a time from global memory to registers, a
-//                 step or two ahead, then converted and written to the ring in
-//                 the 128-byte swizzle of a K-major operand
+// scale in a register.  Per 128 of K each CTA converts its own 128 channels,
+// which go to TMEM as the A operand, and half of the tokens, which go to shared
+// memory as the B operand.  (With both operands in shared memory 192 bytes are
+// moved there per cycle of the MMAs, and the kernel took 1.6 times as long; with
+// A in TMEM it is 128.)  Tiles of 256 tokens are two accumulators of 128, one
+// read while the other's MMAs run; smaller tiles alternate two.
+//   warp 0        MMA issuer of the pair in the even CTA; in the odd one it passes
+//                 on that a stage is full (a release at cluster scope holds a warp
+//                 for long: done by the converters it doubled the time)
+//   warp 1        TMEM allocation
+//   warp 2        TMA producer: codes as they are into a ring of their own
+//   warps 4..7    convert channels: a thread has one channel's row
+//   warps 8..11   convert tokens
 //   warps 12..19  drain: lane quarter w % 4, half of the columns
+//   warps 20..23  only where rows are not on 16-byte boundaries: fill the ring in
+//                 the producer's place
 // A cluster of 2 S CTAs splits K over S pairs where there are few tiles; the
 // partial sums are joined through distributed shared memory.
 #include "integer.cuh"
@@ -27,17 +36,44 @@ namespace {
 
 using namespace rows;
 
-constexpr int kThreads = 640, kLoaders = 256, kDrain = 256;
-constexpr int kStepK = 128;                   // K of a stage: two swizzled atoms of 64
-constexpr int kAtomA = 128 * 128;             // bytes: 128 channels x 64 of K, fp16
+constexpr int kThreads = 640, kAnyThreads = 768;   // rows on 16-byte boundaries; any rows
+constexpr int kConvert = 256, kDrain = 256;
+constexpr int kStepK = 128;                   // K of a stage: two atoms of 64
 constexpr int kExact = 16;                    // atoms (1024 of K) with an exact sum
+constexpr int kStages = 4;
+constexpr int kRelays = 3;                    // warps 0, 1 and 3 of the odd CTA
+constexpr int kColsA = 64;                    // TMEM columns of a stage's channels (two fp16 each)
+constexpr int kTmem = 512;                    // two accumulators of up to 128, then kStages kColsA
 
-__host__ __device__ constexpr int atom_b(int nt) { return nt / 2 * 128; }
-__host__ __device__ constexpr int stage_bytes(int nt) { return 2 * (kAtomA + atom_b(nt)); }
-__host__ __device__ constexpr int stages(int nt) { return nt == 256 ? 3 : nt == 128 ? 4 : 5; }
-__host__ __device__ constexpr int smem_bytes(int nt) { return 1024 + stages(nt) * stage_bytes(nt) + 256; }
-// steps that a loader holds in registers
-__host__ __device__ constexpr int ahead(int nt) { return nt == 256 ? 1 : 2; }
+// columns of an accumulator, and how many a tile has; two take turns
+__host__ __device__ constexpr int acc_cols(int nt) { return nt < 128 ? nt : 128; }
+__host__ __device__ constexpr int acc_parts(int nt) { return nt / acc_cols(nt); }
+constexpr int kAccs = 2;
+// a stage of tokens: NT / 2 rows x 128 of K, fp16
+__host__ __device__ constexpr int stage_bytes(int nt) { return nt / 2 * kStepK * 2; }
+// the ring of codes as they are: 128 channels and half of the tokens x 128 of K
+__host__ __device__ constexpr int raw_bytes(int nt) { return (128 + nt / 2) * kStepK; }
+__host__ __device__ constexpr int raw_stages(int nt) { return nt == 256 ? 3 : nt == 128 ? 6 : nt == 64 ? 9 : 11; }
+__host__ __device__ constexpr int ring_bytes(int nt) { return kStages * stage_bytes(nt) + raw_stages(nt) * raw_bytes(nt); }
+__host__ __device__ constexpr int smem_bytes(int nt) { return 1024 + ring_bytes(nt) + 512; }
+static_assert(8 * (2 * kStages + 2 * kAccs + 2 * raw_stages(32) + 1) + 8 <= 512, "room for the barriers");
+static_assert(smem_bytes(256) <= 227 * 1024 && smem_bytes(128) <= 227 * 1024 && smem_bytes(64) <= 227 * 1024 &&
+                  smem_bytes(32) <= 227 * 1024,
+              "the rings must fit an SM's shared memory");
+
+// Registers a thread of each role where the drain needs more than an even
+// share.  Their sum may not pass what the block is launched with, or the roles
+// would wait for registers that never come: ptxas compiles for the `launch`
+// registers that the launch bounds leave, and the build checks its count.
+__host__ __device__ constexpr bool splits_registers(int nt, bool vec) { return nt == 256 || (nt == 128 && !vec); }
+template <bool VEC>
+struct Registers {
+    static constexpr int few = 48, convert = 56, drain = VEC ? 160 : 112, fill = 72;
+    static constexpr int launch = VEC ? 96 : 80;
+    static_assert(128 * few + kConvert * convert + kDrain * drain + (VEC ? 0 : 128 * fill) <=
+                      launch * (VEC ? kThreads : kAnyThreads),
+                  "the roles' registers must fit the block's");
+};
 
 __device__ __forceinline__ bool wait_cluster(uint32_t bar, uint32_t parity) {
 #pragma unroll 1
@@ -74,6 +110,31 @@ template <int R>
 __device__ __forceinline__ void registers_up() {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R));
 }
+__device__ __forceinline__ uint4 load_shared(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ void store_shared(uint32_t addr, const uint4 &v) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+// 16 columns of this warp's 32 TMEM lanes
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+        "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// D (+)= A B^T of a pair, A in the TMEM of both CTAs (128 rows each)
+__device__ __forceinline__ void mma_tmem_pair(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
+        "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
 
 // Two codes of w as fp16: c + 128 in the low bits of 1024 + (c + 128), less 1152.
 __device__ __forceinline__ uint32_t to_half2(uint32_t w, uint32_t sel) {
@@ -81,27 +142,47 @@ __device__ __forceinline__ uint32_t to_half2(uint32_t w, uint32_t sel) {
     const __half2 d = __hsub2(*reinterpret_cast<const __half2 *>(&h), __half2half2(__ushort_as_half(0x6480)));
     return *reinterpret_cast<const uint32_t *>(&d);
 }
-__device__ __forceinline__ void convert16(const uint4 &raw, uint4 &lo, uint4 &hi) {
-    const uint32_t a = raw.x ^ 0x80808080u, b = raw.y ^ 0x80808080u, c = raw.z ^ 0x80808080u, d = raw.w ^ 0x80808080u;
-    lo = make_uint4(to_half2(a, 0x4140), to_half2(a, 0x4342), to_half2(b, 0x4140), to_half2(b, 0x4342));
-    hi = make_uint4(to_half2(c, 0x4140), to_half2(c, 0x4342), to_half2(d, 0x4140), to_half2(d, 0x4342));
-}
-__device__ __forceinline__ void store_shared(uint32_t addr, const uint4 &v) {
-    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+// 16 codes as fp16, two a word
+__device__ __forceinline__ void convert16(const uint4 &raw, uint32_t *h) {
+    const uint32_t w[4] = {raw.x ^ 0x80808080u, raw.y ^ 0x80808080u, raw.z ^ 0x80808080u, raw.w ^ 0x80808080u};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        h[2 * i] = to_half2(w[i], 0x4140);
+        h[2 * i + 1] = to_half2(w[i], 0x4342);
+    }
 }
 
-// NT: tokens of a tile.  GROUPS: group scales.  VEC: 16-byte aligned rows.
+// A position in a ring of N stages.
+template <int N>
+struct Slot {
+    int s = 0;
+    uint32_t phase;
+    __device__ explicit Slot(uint32_t first) : phase(first) {}
+    __device__ __forceinline__ void next() {
+        if (++s == N) {
+            s = 0;
+            phase ^= 1;
+        }
+    }
+};
+
+// NT: tokens of a tile.  GROUPS: group scales.  VEC: rows on 16-byte boundaries.
 template <int NT, bool GROUPS, bool VEC>
-__global__ void __launch_bounds__(kThreads, 1) tc_integer_kernel(ProductArgs a, int split, int *failed) {
-    constexpr int kStages = stages(NT), kStage = stage_bytes(NT), kAtomB = atom_b(NT);
-    constexpr int kRowsB = NT / 2;
-    constexpr int kCols = NT / 2;               // columns of a drain warp
-    constexpr uint32_t kIdesc = tc::idesc_f16_f32(256, NT);
-    constexpr uint32_t kTmem = 2 * NT;
+__global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
+    tc_integer_kernel(const __grid_constant__ CUtensorMap mapC, const __grid_constant__ CUtensorMap mapX, ProductArgs a,
+                      int split, int *failed) {
+    using Reg = Registers<VEC>;
+    constexpr int kStage = stage_bytes(NT), kRaws = raw_stages(NT), kRaw = raw_bytes(NT);
+    constexpr int kAcc = acc_cols(NT), kParts = acc_parts(NT);
+    constexpr int kRowsB = kAcc / 2;            // this CTA's tokens of an accumulator
+    constexpr int kAtomB = kRowsB * 128, kHalfB = 2 * kAtomB;
+    constexpr int kCols = kAcc / 2;             // columns of a drain warp in an accumulator
+    constexpr int kBars = 2 * kStages + 2 * kAccs + 2 * kRaws + 1;
+    constexpr uint32_t kIdesc = tc::idesc_f16_f32(256, kAcc);
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    uint64_t *bars = (uint64_t *)(smem + kStages * kStage);
-    uint32_t *tmem_slot = (uint32_t *)(bars + 2 * kStages + 5);
+    uint64_t *bars = (uint64_t *)(smem + ring_bytes(NT));
+    uint32_t *tmem_slot = (uint32_t *)(bars + kBars);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int crank = (int)tc::cluster_rank(), rank = crank & 1, part = crank >> 1;
@@ -118,18 +199,24 @@ __global__ void __launch_bounds__(kThreads, 1) tc_integer_kernel(ProductArgs a, 
     auto full = [&](int s) { return tc::smem_u32(bars + s); };
     auto empty = [&](int s) { return tc::smem_u32(bars + kStages + s); };
     auto afull = [&](int b) { return tc::smem_u32(bars + 2 * kStages + b); };
-    auto aempty = [&](int b) { return tc::smem_u32(bars + 2 * kStages + 2 + b); };
-    const uint32_t closing = tc::smem_u32(bars + 2 * kStages + 4);
-    const uint32_t ring = tc::smem_u32(smem);
+    auto aempty = [&](int b) { return tc::smem_u32(bars + 2 * kStages + kAccs + b); };
+    auto raw_full = [&](int s) { return tc::smem_u32(bars + 2 * kStages + 2 * kAccs + s); };
+    auto raw_empty = [&](int s) { return tc::smem_u32(bars + 2 * kStages + 2 * kAccs + kRaws + s); };
+    const uint32_t closing = tc::smem_u32(bars + kBars - 1);
+    const uint32_t ring = tc::smem_u32(smem), raws = ring + kStages * kStage;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
-            tc::mbar_init(full(s), 2 * kLoaders / 32);       // the even CTA's: both CTAs' loaders
+            tc::mbar_init(full(s), kConvert / 32 + (rank == 0));   // own converters; the odd CTA's relay
             tc::mbar_init(empty(s), 1);
         }
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < kAccs; ++b) {
             tc::mbar_init(afull(b), 1);
             tc::mbar_init(aempty(b), 2 * kDrain / 32);       // the even CTA's: both drains
+        }
+        for (int s = 0; s < kRaws; ++s) {
+            tc::mbar_init(raw_full(s), VEC ? 1 : 4);
+            tc::mbar_init(raw_empty(s), kConvert / 32);
         }
         tc::mbar_init(closing, 1);
         *abort_flag = 0;
@@ -143,109 +230,201 @@ __global__ void __launch_bounds__(kThreads, 1) tc_integer_kernel(ProductArgs a, 
     __syncthreads();
     tc::cluster_sync();
     tc::tc_fence_after();
-    const uint32_t tmem = *tmem_slot;
+    const uint32_t tmem = *tmem_slot, tmem_a = tmem + kAccs * 128;
 
     if (warp < 4) {
-        if constexpr (NT == 256) registers_down<40>();
-        // ---------------- MMA issuer of the pair
+        if constexpr (splits_registers(NT, VEC)) registers_down<Reg::few>();
         if (warp == 0 && rank == 0) {
+            // ---------------- MMA issuer of the pair
             bool ok = true;
-            const uint64_t ad0 = tc::sdesc_sw128(ring), bd0 = tc::sdesc_sw128(ring + 2 * kAtomA);
-            int s = 0, ph = 0, pc = 0;
-            for (int tile = cluster; tile < ntiles && ok; tile += nclusters) {
-                int left = 0;                                // atoms left in the accumulator
-                for (int at = 0; at < natoms && ok; ++at) {
-                    if ((at & 1) == 0) ok = wait_cluster(full(s), ph);
-                    const bool first = left == 0;
-                    if (first) {
-                        left = min(ua, natoms - at);
-                        ok = tc::mbar_wait(aempty(pc & 1), ((pc >> 1) & 1) ^ 1) && ok;
-                    }
-                    if (!ok) break;
-                    tc::tc_fence_after();
-                    const bool last = --left == 0, done = (at & 1) || at + 1 == natoms;
-                    if (tc::elect_one()) {
-                        const uint64_t ad = ad0 + (uint64_t)((s * kStage + (at & 1) * kAtomA) >> 4);
-                        const uint64_t bd = bd0 + (uint64_t)((s * kStage + (at & 1) * kAtomB) >> 4);
+            const uint64_t bd0 = tc::sdesc_sw128(ring);
+            const uint16_t both = (uint16_t)(3 << even);
+            const int us = GROUPS ? max(1, ua / 2) : kExact / 2;     // stages of an accumulator
+            Slot<kStages> in(0);
+            int unit = 0;                                    // accumulators so far, over all tiles
+            // `count` atoms from atom `at` of a stage into every part's accumulator
+            auto issue = [&](int at, int count, bool first, bool last, bool done) {
 #pragma unroll
-                        for (int sub = 0; sub < 4; ++sub)
-                            tc::mma_f16_pair(tmem + (pc & 1) * NT, ad + 2 * sub, bd + 2 * sub, kIdesc, !first || sub > 0);
-                        if (done) tc::mma_commit_pair(empty(s), 3 << even);
-                        if (last) tc::mma_commit_pair(afull(pc & 1), 3 << even);
+                for (int h = 0; h < kParts; ++h) {
+                    const int use = unit * kParts + h, b = use % kAccs;
+                    if (first) {
+                        ok = tc::mbar_wait(aempty(b), (use / kAccs & 1) ^ 1);
+                        if (!ok) return;
+                        tc::tc_fence_after();
+                    }
+                    if (tc::elect_one()) {
+                        const uint32_t d = tmem + b * kAcc;
+                        const uint32_t ad = tmem_a + in.s * kColsA + at * 32;
+                        const uint64_t bd = bd0 + (uint32_t)((in.s * kStage + h * kHalfB + at * kAtomB) >> 4);
+#pragma unroll
+                        for (int sub = 0; sub < 4; ++sub) mma_tmem_pair(d, ad + 8 * sub, bd + 2 * sub, kIdesc, !first || sub > 0);
+                        if (count == 2) {
+#pragma unroll
+                            for (int sub = 0; sub < 4; ++sub)
+                                mma_tmem_pair(d, ad + 32 + 8 * sub, bd + (kAtomB >> 4) + 2 * sub, kIdesc, 1);
+                        }
+                        if (last) tc::mma_commit_pair(afull(b), both);
+                        if (done && h == kParts - 1) tc::mma_commit_pair(empty(in.s), both);
                     }
                     __syncwarp();
-                    if (last) ++pc;
-                    if (done && ++s == kStages) {
-                        s = 0;
-                        ph ^= 1;
+                }
+                unit += last;
+            };
+            for (int tile = cluster; tile < ntiles && ok; tile += nclusters)
+                for (int step = 0, in_unit = 0; step < nsteps && ok; ++step, in.next()) {
+                    ok = wait_cluster(full(in.s), in.phase);
+                    if (!ok) break;
+                    tc::tc_fence_after();
+                    const int atoms = min(2, natoms - 2 * step);
+                    if (GROUPS && ua == 1) {
+                        issue(0, 1, true, true, atoms == 1);
+                        if (ok && atoms == 2) issue(1, 1, true, true, true);
+                    } else {
+                        const bool last = in_unit + 1 == us || step + 1 == nsteps;
+                        issue(0, atoms, in_unit == 0, last, true);
+                        in_unit = last ? 0 : in_unit + 1;
                     }
                 }
-            }
             if (tc::elect_one()) tc::mma_commit_pair(closing, 1 << even);
             if (!tc::mbar_wait(closing, 0) || !ok) *abort_flag = 1;
+        } else if (warp != 2 && rank == 1) {
+            // ---------------- relays of the odd CTA: its stages are full, in turn
+            const uint32_t full0 = tc::map_rank(full(0), even);
+            const int me = warp == 3 ? 2 : warp;
+            bool ok = true;
+            int turn = 0;
+            Slot<kStages> in(0);
+            for (int tile = cluster; tile < ntiles && ok; tile += nclusters)
+                for (int step = 0; step < nsteps && ok; ++step, in.next()) {
+                    if (turn == me) {
+                        ok = tc::mbar_wait(full(in.s), in.phase);
+                        tc::tc_fence_after();
+                        tc::tc_fence_before();
+                        if (ok && lane == 0) arrive_cluster(full0 + 8 * in.s);
+                        __syncwarp();
+                    }
+                    turn = turn == kRelays - 1 ? 0 : turn + 1;
+                }
+            if (!ok) *abort_flag = 1;
+        } else if (VEC && warp == 2) {
+            // ---------------- producer of the raw ring
+            tc::pdl_wait();
+            bool ok = true;
+            Slot<kRaws> out(1);
+            int filled = 0;
+            for (int tile = cluster; tile < ntiles && ok; tile += nclusters) {
+                const int o = tile % mt * 256 + 128 * rank, tk = tile / mt * NT + kRowsB * rank;
+                for (int step = 0; step < nsteps; ++step, out.next()) {
+                    ok = tc::mbar_wait(raw_empty(out.s), out.phase);
+                    if (!ok) break;
+                    if (tc::elect_one()) {
+                        const uint32_t at = raws + out.s * kRaw, bar = raw_full(out.s);
+                        const int k = (step0 + step) * kStepK;
+                        tc::mbar_expect_tx(bar, kRaw);
+                        tc::tma_load_2d(at, &mapC, bar, k, o);
+#pragma unroll
+                        for (int h = 0; h < kParts; ++h)
+                            tc::tma_load_2d(at + (128 + h * kRowsB) * kStepK, &mapX, bar, k, tk + h * kAcc);
+                    }
+                    __syncwarp();
+                    ++filled;
+                }
+            }
+            // no copy is in flight when the CTA ends
+            for (int n = max(0, filled - kRaws); n < filled && ok; ++n)
+                ok = tc::mbar_wait(raw_empty(n % kRaws), (n / kRaws) & 1);
+            if (!ok) {
+                *abort_flag = 1;
+                tc::abandon_ring(raw_full(0), kRaws, filled, true);
+            }
         }
+    } else if (warp < 8) {
+        if constexpr (splits_registers(NT, VEC)) registers_down<Reg::convert>();
+        // ---------------- channels: raw ring -> fp16 -> TMEM
+        const int q = warp - 4, r = 32 * q + lane;
+        const uint32_t from = raws + (uint32_t)(r * kStepK), sw = r & 7;
+        const uint32_t to = tmem_a + ((uint32_t)(32 * q) << 16);
+        bool ok = true;
+        Slot<kRaws> in(0);
+        Slot<kStages> out(1);
+        for (int tile = cluster; tile < ntiles && ok; tile += nclusters)
+            for (int step = 0; step < nsteps; ++step, in.next(), out.next()) {
+                ok = tc::mbar_wait(raw_full(in.s), in.phase);
+                ok = tc::mbar_wait(empty(out.s), out.phase) && ok;
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tc::tc_fence_after();
+                const uint32_t src = from + in.s * kRaw;
+                uint4 raw[4];
+#pragma unroll 1
+                for (int c = 0; c < 8; c += 4) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) raw[j] = load_shared(src + (((c + j) ^ sw) << 4));
+#pragma unroll
+                    for (int j = 0; j < 4; j += 2) {
+                        uint32_t h[16];
+                        convert16(raw[j], h);
+                        convert16(raw[j + 1], h + 8);
+                        tmem_st16(to + out.s * kColsA + 8 * (c + j), h);
+                    }
+                }
+                tmem_wait_st();
+                tc::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    tc::mbar_arrive(full(out.s));
+                    tc::mbar_arrive(raw_empty(in.s));
+                }
+            }
+        if (!ok) *abort_flag = 1;
     } else if (warp < 12) {
-        if constexpr (NT == 256) registers_down<72>();
-        // ---------------- loaders
-        constexpr int kUB = (kRowsB + 31) / 32;              // units of the tokens a thread
-        constexpr int kU = 4 + kUB, kAhead = ahead(NT);
-        const int t = threadIdx.x - 128, c = t & 7, r0 = t >> 3;
-        const bool has_b = kRowsB >= 32 || r0 < kRowsB;
+        if constexpr (splits_registers(NT, VEC)) registers_down<Reg::convert>();
+        // ---------------- tokens: raw ring -> fp16 -> K-major tiles, 128-byte swizzle
+        constexpr int kU = NT / 32;                          // 16 rows at a time
+        const int t = threadIdx.x - 256, c = t & 7, r0 = t >> 3, sw = r0 & 7;
         // 16 codes become two 16-byte chunks of a 128-byte row; threads of the
         // second atom write theirs in the other order, so that eight lanes of a
         // row always cover all banks
         const int atom = c >> 2, j0 = 2 * (c & 3) + atom;
-        const uint32_t sw0 = (uint32_t)(r0 * 128 + ((j0 ^ (r0 & 7)) << 4)), sw1 = (uint32_t)(r0 * 128 + (((j0 ^ 1) ^ (r0 & 7)) << 4));
-        const uint32_t toA = ring + atom * kAtomA, toB = ring + 2 * kAtomA + atom * kAtomB;
-        const uint32_t full0 = tc::map_rank(full(0), even);
+        const uint32_t to = ring + atom * kAtomB + r0 * 128;
+        const uint32_t sw0 = (uint32_t)((j0 ^ sw) << 4), sw1 = (uint32_t)(((j0 ^ 1) ^ sw) << 4);
+        const uint32_t from = raws + (uint32_t)((128 + r0) * kStepK + ((c ^ sw) << 4));
         bool ok = true;
-        int s = 0, ph = 1;
-        for (int tile = cluster; tile < ntiles && ok; tile += nclusters) {
-            const int o = tile % mt * 256 + 128 * rank + r0, tk = tile / mt * NT + kRowsB * rank + r0;
-            const int8_t *pa = a.C + (size_t)o * a.ldc, *pb = a.X + (size_t)tk * a.ldx;
-            const size_t sa = (size_t)32 * a.ldc, sb = (size_t)32 * a.ldx;
-            uint4 held[kAhead][kU];
-            if (tile == cluster) tc::pdl_wait();
-            auto fetch = [&](uint4 (&h)[kU], int i, int step) {
-                const int k = (step0 + step) * kStepK + c * 16;
-                const bool in = step < nsteps && (i < 4 ? o + 32 * i < a.dout : has_b && tk + 32 * (i - 4) < a.n);
-                h[i] = in ? load_codes<VEC>(i < 4 ? pa + i * sa : pb + (i - 4) * sb, k, a.din) : make_uint4(0, 0, 0, 0);
-            };
+        Slot<kRaws> in(0);
+        Slot<kStages> out(1);
+        for (int tile = cluster; tile < ntiles && ok; tile += nclusters)
+            for (int step = 0; step < nsteps; ++step, in.next(), out.next()) {
+                ok = tc::mbar_wait(raw_full(in.s), in.phase);
+                ok = tc::mbar_wait(empty(out.s), out.phase) && ok;
+                if (!ok) break;
+                const uint32_t src = from + in.s * kRaw, dst = to + out.s * kStage;
+                constexpr int kBatch = kU < 4 ? kU : 4;      // loads in flight
+                uint4 raw[kBatch];
+#pragma unroll 1
+                for (int i = 0; i < kU; i += kBatch) {
 #pragma unroll
-            for (int p = 0; p < kAhead; ++p)
+                    for (int j = 0; j < kBatch; ++j) raw[j] = load_shared(src + (i + j) * 16 * kStepK);
 #pragma unroll
-                for (int i = 0; i < kU; ++i) fetch(held[p], i, p);
-            for (int step = 0; step < nsteps && ok; step += kAhead) {
-#pragma unroll
-                for (int p = 0; p < kAhead; ++p) {
-                    if (step + p >= nsteps) break;
-                    ok = tc::mbar_wait(empty(s), ph);
-                    if (!ok) break;
-                    const uint32_t da = toA + s * kStage, db = toB + s * kStage;
-#pragma unroll
-                    for (int i = 0; i < kU; ++i) {
-                        uint4 lo, hi;
-                        convert16(held[p][i], lo, hi);
-                        fetch(held[p], i, step + p + kAhead);
-                        if (i < 4 || has_b) {
-                            const uint32_t d = i < 4 ? da + i * 32 * 128 : db + (i - 4) * 32 * 128;
-                            store_shared(d + sw0, atom ? hi : lo);
-                            store_shared(d + sw1, atom ? lo : hi);
-                        }
-                    }
-                    fence_to_async();
-                    __syncwarp();
-                    if (lane == 0) arrive_cluster(full0 + 8 * s);
-                    if (++s == kStages) {
-                        s = 0;
-                        ph ^= 1;
+                    for (int j = 0; j < kBatch; ++j) {
+                        uint32_t h[8];
+                        convert16(raw[j], h);
+                        // row 16 (i + j) + r0 of the stage: part 16 (i + j) / kRowsB
+                        const uint32_t d = dst + 16 * (i + j) / kRowsB * kHalfB + 16 * (i + j) % kRowsB * 128;
+                        const uint4 lo = make_uint4(h[0], h[1], h[2], h[3]), hi = make_uint4(h[4], h[5], h[6], h[7]);
+                        store_shared(d + sw0, atom ? hi : lo);
+                        store_shared(d + sw1, atom ? lo : hi);
                     }
                 }
+                fence_to_async();
+                __syncwarp();
+                if (lane == 0) {
+                    tc::mbar_arrive(full(out.s));
+                    tc::mbar_arrive(raw_empty(in.s));
+                }
             }
-        }
         if (!ok) *abort_flag = 1;
-    } else {
-        if constexpr (NT == 256) registers_up<144>();
+    } else if (warp < 20) {
+        if constexpr (splits_registers(NT, VEC)) registers_up<Reg::drain>();
         // ---------------- drain
         tc::pdl_wait();                                      // the tokens' scales
         const int w = warp - 12, q = w & 3, col0 = (w >> 2) * kCols;
@@ -253,61 +432,106 @@ __global__ void __launch_bounds__(kThreads, 1) tc_integer_kernel(ProductArgs a, 
         const uint32_t released = tc::map_rank(aempty(0), even);
         const uint32_t taddr = tmem + ((uint32_t)(32 * q) << 16) + col0;
         bool ok = true;
-        int pc = 0;
+        int unit = 0;
         for (int tile = cluster; tile < ntiles && ok; tile += nclusters) {
             const int o = tile % mt * 256 + 128 * rank + lrow, t0 = tile / mt * NT;
             const bool live = o < a.dout;
-            uint32_t acc[kCols];                             // int32, or float32 with groups
+            uint32_t acc[kParts][kCols];                    // int32, or float32 with groups
 #pragma unroll
-            for (int e = 0; e < kCols; ++e) acc[e] = 0;
+            for (int h = 0; h < kParts; ++h)
+#pragma unroll
+                for (int e = 0; e < kCols; ++e) acc[h][e] = 0;
             const float *wp = a.ws + (live ? (size_t)o * a.G : 0) + (GROUPS ? 2 * step0 / ua : 0);
-            for (int u = 0; u < nunits; ++u, ++pc) {
-                const int b = pc & 1;
+            for (int u = 0; u < nunits && ok; ++u, ++unit) {
                 const float wsc = GROUPS ? wp[u] : 0.f;
-                ok = __all_sync(0xffffffffu, tc::mbar_wait(afull(b), (pc >> 1) & 1));
-                if (!ok) break;
-                tc::tc_fence_after();
 #pragma unroll
-                for (int cc = 0; cc < kCols; cc += 16) {
-                    uint32_t v[16];
-                    tc::tmem_ld16(taddr + b * NT + cc, v);
-                    tc::tmem_wait_ld();
-                    if (cc + 16 == kCols) {
-                        tc::tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) tc::mbar_arrive_cluster(released + 8 * b);
-                    }
+                for (int h = 0; h < kParts; ++h) {
+                    const int use = unit * kParts + h, b = use % kAccs;
+                    ok = __all_sync(0xffffffffu, tc::mbar_wait(afull(b), use / kAccs & 1)) && ok;
+                    if (!ok) break;
+                    tc::tc_fence_after();
+                    const uint32_t at = taddr + b * kAcc;
+                    uint32_t v[2][16];
+                    tc::tmem_ld16(at, v[0]);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        if (GROUPS)
-                            acc[cc + e] = __float_as_uint(fmaf(__uint_as_float(v[e]), wsc, __uint_as_float(acc[cc + e])));
-                        else
-                            acc[cc + e] += (uint32_t)__float2int_rn(__uint_as_float(v[e]));
+                    for (int cc = 0; cc < kCols; cc += 16) {
+                        tc::tmem_wait_ld();
+                        if (cc + 16 < kCols) {
+                            tc::tmem_ld16(at + cc + 16, v[(cc / 16 + 1) & 1]);
+                        } else {
+                            tc::tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) tc::mbar_arrive_cluster(released + 8 * b);
+                        }
+                        uint32_t(&x)[16] = v[(cc / 16) & 1];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            uint32_t &s = acc[h][cc + e];
+                            if (GROUPS)
+                                s = __float_as_uint(fmaf(__uint_as_float(x[e]), wsc, __uint_as_float(s)));
+                            else
+                                s += (uint32_t)__float2int_rn(__uint_as_float(x[e]));
+                        }
                     }
                 }
             }
             if (!ok) break;
-            const float wch = GROUPS ? 1.f : wp[0], bias = a.bias && live ? a.bias[o] : 0.f;
             if (split > 1) {
                 // every MMA of the pair is done: its ring takes the partial sums
-                const uint32_t mine = ring + (uint32_t)(col0 * 128 + lrow) * 4;
 #pragma unroll
-                for (int e = 0; e < kCols; ++e)
-                    asm volatile("st.shared.u32 [%0], %1;" ::"r"(mine + e * 512), "r"(acc[e]) : "memory");
-                break;                                       // joined below: one tile a cluster
-            }
-            if (live) {
-                const int cols = min(kCols, a.n - t0 - col0);
-                with_type_device(a.dtype, [&](auto type) {
-                    using T = decltype(type);
-                    T *y = static_cast<T *>(a.Y) + (size_t)(t0 + col0) * a.ldy + o;
+                for (int h = 0; h < kParts; ++h)
 #pragma unroll
                     for (int e = 0; e < kCols; ++e)
-                        if (e < cols) {
-                            const float v = GROUPS ? __uint_as_float(acc[e]) : (float)(int)acc[e] * wch;
-                            y[(size_t)e * a.ldy] = from_float<T>(fmaf(v, a.xs[t0 + col0 + e], bias));
-                        }
+                        asm volatile("st.shared.u32 [%0], %1;" ::"r"(ring + (uint32_t)((h * kAcc + col0 + e) * 128 + lrow) * 4),
+                                     "r"(acc[h][e])
+                                     : "memory");
+                break;                                       // joined below: one tile a cluster
+            }
+            const float wch = GROUPS ? 1.f : wp[0], bias = a.bias && live ? a.bias[o] : 0.f;
+            if (live) {
+                with_type_device(a.dtype, [&](auto type) {
+                    using T = decltype(type);
+#pragma unroll
+                    for (int h = 0; h < kParts; ++h) {
+                        const int tk = t0 + h * kAcc + col0;
+                        T *y = static_cast<T *>(a.Y) + (size_t)tk * a.ldy + o;
+#pragma unroll
+                        for (int e = 0; e < kCols; ++e)
+                            if (tk + e < a.n) {
+                                const float v = GROUPS ? __uint_as_float(acc[h][e]) : (float)(int)acc[h][e] * wch;
+                                y[(size_t)e * a.ldy] = from_float<T>(fmaf(v, a.xs[tk + e], bias));
+                            }
+                    }
                 });
+            }
+        }
+        if (!ok) *abort_flag = 1;
+    } else {
+        if constexpr (splits_registers(NT, VEC)) registers_down<Reg::fill>();
+        // ---------------- rows that TMA cannot read, into the raw ring
+        tc::pdl_wait();
+        constexpr int kUnits = 8 + NT / 32;                  // 16 rows at a time: channels, tokens
+        const int t = threadIdx.x - 640, c = t & 7, r0 = t >> 3;
+        const uint32_t to = raws + (uint32_t)(r0 * kStepK + ((c ^ (r0 & 7)) << 4));
+        bool ok = true;
+        Slot<kRaws> out(1);
+        for (int tile = cluster; tile < ntiles && ok; tile += nclusters) {
+            const int o = tile % mt * 256 + 128 * rank + r0, tk = tile / mt * NT + kRowsB * rank + r0;
+            for (int step = 0; step < nsteps; ++step, out.next()) {
+                const int k = (step0 + step) * kStepK + c * 16;
+                ok = tc::mbar_wait(raw_empty(out.s), out.phase);
+                if (!ok) break;
+#pragma unroll
+                for (int i = 0; i < kUnits; ++i) {
+                    const int j = 16 * (i - 8);              // row r0 + j of the tokens
+                    const int r = i < 8 ? o + 16 * i : tk + j / kRowsB * kAcc + j % kRowsB;
+                    uint4 v = make_uint4(0, 0, 0, 0);
+                    if (r < (i < 8 ? a.dout : a.n))
+                        v = load_codes<false>(i < 8 ? a.C + (size_t)r * a.ldc : a.X + (size_t)r * a.ldx, k, a.din);
+                    store_shared(to + out.s * kRaw + i * 16 * kStepK, v);
+                }
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(raw_full(out.s));
             }
         }
         if (!ok) *abort_flag = 1;
@@ -315,7 +539,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_integer_kernel(ProductArgs a, 
     if (split > 1) {
         // join: pair `part` finishes columns part NT / split .. of its 128 channels
         cluster_barrier();
-        if (warp >= 12 && cluster < ntiles) {
+        if (warp >= 12 && warp < 20 && cluster < ntiles) {
             const int t = threadIdx.x - 384, lrow = t & 127, half = t >> 7;
             const int o = cluster % mt * 256 + 128 * rank + lrow, t0 = cluster / mt * NT;
             const int cols = NT / split;
@@ -359,14 +583,21 @@ template <int NT, bool GROUPS, bool VEC>
 cudaError_t launch(const ProductArgs &a, int split, int *failed, cudaStream_t s, bool pdl) {
     static std::atomic<unsigned long long> done;
     auto *kernel = tc_integer_kernel<NT, GROUPS, VEC>;
-    const cudaError_t e = set_max_dynamic_smem((const void *)kernel, smem_bytes(NT), done);
+    cudaError_t e = set_max_dynamic_smem((const void *)kernel, smem_bytes(NT), done);
     if (e != cudaSuccess) return e;
+    CUtensorMap mapC = {}, mapX = {};
+    if (VEC) {
+        auto pitch = [](int64_t ld, int rows) { return (uint64_t)(rows > 1 ? ld : (ld + 15) / 16 * 16); };
+        e = make_tmap_codes(&mapC, a.C, a.dout, a.din, pitch(a.ldc, a.dout), 128);
+        if (e == cudaSuccess) e = make_tmap_codes(&mapX, a.X, a.n, a.din, pitch(a.ldx, a.n), acc_cols(NT) / 2);
+        if (e != cudaSuccess) return e;
+    }
     const int64_t tiles = (int64_t)((a.dout + 255) / 256) * ((a.n + NT - 1) / NT);
     const int64_t clusters = split > 1 ? tiles : std::min<int64_t>(tiles, num_sms() / 2);
     if (tiles > 0x3FFFFFFF / (2 * split)) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(clusters * 2 * split));
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(VEC ? kThreads : kAnyThreads);
     cfg.dynamicSmemBytes = smem_bytes(NT);
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
@@ -377,14 +608,16 @@ cudaError_t launch(const ProductArgs &a, int split, int *failed, cudaStream_t s,
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = pdl ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, a, split, failed);
+    return cudaLaunchKernelEx(&cfg, kernel, mapC, mapX, a, split, failed);
 }
 
 template <int NT>
 cudaError_t launch_nt(const ProductArgs &a, int split, int *failed, cudaStream_t s, bool pdl) {
-    const bool vec = vector_rows(a);
-    if (a.g) return vec ? launch<NT, true, true>(a, split, failed, s, pdl) : launch<NT, true, false>(a, split, failed, s, pdl);
-    return vec ? launch<NT, false, true>(a, split, failed, s, pdl) : launch<NT, false, false>(a, split, failed, s, pdl);
+    if (vector_rows(a))
+        return a.g ? launch<NT, true, true>(a, split, failed, s, pdl) : launch<NT, false, true>(a, split, failed, s, pdl);
+    // four more warps fill the ring: no registers left for 256 tokens
+    constexpr int any = NT == 256 ? 128 : NT;
+    return a.g ? launch<any, true, false>(a, split, failed, s, pdl) : launch<any, false, false>(a, split, failed, s, pdl);
 }
 
 }  // namespace
