@@ -26,8 +26,8 @@ FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", 
 # Registers a thread that kernels with roles of different register counts must be
 # compiled for: the roles' sum would not fit a smaller block, and they would wait
 # for registers that never come.
-LAUNCH_REGISTERS = {"k_tc_integer.cu": (("tc_integer_kernelILi256E", 96), ("tc_integer_kernelILi128ELb0ELb0E", 80),
-                                        ("tc_integer_kernelILi128ELb1ELb0E", 80))}
+LAUNCH_REGISTERS = {"k_tc_integer.cu": (("tc_integer_kernelILi256E", 96), ("tc_integer_kernelILi128ELb0ELb0E", 72),
+                                        ("tc_integer_kernelILi128ELb1ELb0E", 72))}
 
 
 def check_registers(src: str, ptxas_output: str) -> None:

@@ -7,25 +7,27 @@
 // each group, they leave it: with one scale a channel for an int32 sum, with
 // groups for a float32 sum of the terms ws_i sum_i.
 //
-// A pair of CTAs (cta_group::2): 256 channels x NT tokens, channels on the lanes
-// of TMEM, so that a thread of the epilogue has one channel and its group's
-// scale in a register.  Per 128 of K each CTA converts its own 128 channels,
-// which go to TMEM as the A operand, and half of the tokens, which go to shared
-// memory as the B operand.  (With both operands in shared memory 192 bytes are
-// moved there per cycle of the MMAs, and the kernel took 1.6 times as long; with
-// A in TMEM it is 128.)  Tiles of 256 tokens are two accumulators of 128, one
-// read while the other's MMAs run; smaller tiles alternate two.
-//   warp 0        MMA issuer of the pair in the even CTA; in the odd one it passes
-//                 on that a stage is full (a release at cluster scope holds a warp
-//                 for long: done by the converters it doubled the time)
+// 128 channels on the lanes of TMEM x NT tokens, so that a thread of the epilogue
+// has one channel and its group's scale in a register; for more than 64 tokens a
+// pair of CTAs (cta_group::2) has 256 channels, and each CTA converts its own 128
+// and half of the tokens.  Per 128 of K the channels go to TMEM as the A operand
+// and the tokens to shared memory as the B operand.  (With both operands in shared
+// memory 192 bytes are moved there per cycle of the MMAs, and the kernel took 1.6
+// times as long; with A in TMEM it is 128.)  Tiles of 256 tokens are two
+// accumulators of 128, one read while the other's MMAs run; smaller tiles
+// alternate two.
+//   warp 0        MMA issuer (of a pair's even CTA)
+//   warps 0, 1, 3 of a pair's odd CTA pass on that a stage is full.  (A release at
+//                 cluster scope holds a warp for some 1300 cycles: done by the
+//                 converters it doubled the time, by one warp it set the pace.)
 //   warp 1        TMEM allocation
 //   warp 2        TMA producer: codes as they are into a ring of their own
 //   warps 4..7    convert channels: a thread has one channel's row
-//   warps 8..11   convert tokens
+//   warps 8..11   convert tokens, and half of the channels' K where tokens are few
 //   warps 12..19  drain: lane quarter w % 4, half of the columns
-//   warps 20..23  only where rows are not on 16-byte boundaries: fill the ring in
+//   warps 20..27  only where rows are not on 16-byte boundaries: fill the ring in
 //                 the producer's place
-// A cluster of 2 S CTAs splits K over S pairs where there are few tiles; the
+// A cluster splits K over its CTAs or pairs where there are few tiles; the
 // partial sums are joined through distributed shared memory.
 #include "integer.cuh"
 #include "rows.cuh"
@@ -36,11 +38,12 @@ namespace {
 
 using namespace rows;
 
-constexpr int kThreads = 640, kAnyThreads = 768;   // rows on 16-byte boundaries; any rows
-constexpr int kConvert = 256, kDrain = 256;
+constexpr int kThreads = 640, kAnyThreads = 896;   // rows on 16-byte boundaries; any rows
+constexpr int kConvert = 256, kDrain = 256, kFill = 256;
 constexpr int kStepK = 128;                   // K of a stage: two atoms of 64
 constexpr int kExact = 16;                    // atoms (1024 of K) with an exact sum
 constexpr int kStages = 4;
+constexpr int kMostParts = 4;                  // of K, over a cluster
 constexpr int kRelays = 3;                    // warps 0, 1 and 3 of the odd CTA
 constexpr int kColsA = 64;                    // TMEM columns of a stage's channels (two fp16 each)
 constexpr int kTmem = 512;                    // two accumulators of up to 128, then kStages kColsA
@@ -49,11 +52,15 @@ constexpr int kTmem = 512;                    // two accumulators of up to 128, 
 __host__ __device__ constexpr int acc_cols(int nt) { return nt < 128 ? nt : 128; }
 __host__ __device__ constexpr int acc_parts(int nt) { return nt / acc_cols(nt); }
 constexpr int kAccs = 2;
-// a stage of tokens: NT / 2 rows x 128 of K, fp16
-__host__ __device__ constexpr int stage_bytes(int nt) { return nt / 2 * kStepK * 2; }
-// the ring of codes as they are: 128 channels and half of the tokens x 128 of K
-__host__ __device__ constexpr int raw_bytes(int nt) { return (128 + nt / 2) * kStepK; }
-__host__ __device__ constexpr int raw_stages(int nt) { return nt == 256 ? 3 : nt == 128 ? 6 : nt == 64 ? 9 : 11; }
+// CTAs of a tile: a pair for many tokens
+__host__ __device__ constexpr int ctas(int nt) { return nt > 64 ? 2 : 1; }
+// a CTA's tokens
+__host__ __device__ constexpr int own_tokens(int nt) { return nt / ctas(nt); }
+// a stage of tokens x 128 of K, fp16
+__host__ __device__ constexpr int stage_bytes(int nt) { return own_tokens(nt) * kStepK * 2; }
+// the ring of codes as they are: 128 channels and the tokens x 128 of K
+__host__ __device__ constexpr int raw_bytes(int nt) { return (128 + own_tokens(nt)) * kStepK; }
+__host__ __device__ constexpr int raw_stages(int nt) { return nt == 256 ? 3 : nt == 32 ? 9 : 6; }
 __host__ __device__ constexpr int ring_bytes(int nt) { return kStages * stage_bytes(nt) + raw_stages(nt) * raw_bytes(nt); }
 __host__ __device__ constexpr int smem_bytes(int nt) { return 1024 + ring_bytes(nt) + 512; }
 static_assert(8 * (2 * kStages + 2 * kAccs + 2 * raw_stages(32) + 1) + 8 <= 512, "room for the barriers");
@@ -68,9 +75,9 @@ static_assert(smem_bytes(256) <= 227 * 1024 && smem_bytes(128) <= 227 * 1024 && 
 __host__ __device__ constexpr bool splits_registers(int nt, bool vec) { return nt == 256 || (nt == 128 && !vec); }
 template <bool VEC>
 struct Registers {
-    static constexpr int few = 48, convert = 56, drain = VEC ? 160 : 112, fill = 72;
-    static constexpr int launch = VEC ? 96 : 80;
-    static_assert(128 * few + kConvert * convert + kDrain * drain + (VEC ? 0 : 128 * fill) <=
+    static constexpr int few = 48, convert = 56, drain = VEC ? 160 : 112, fill = 56;
+    static constexpr int launch = VEC ? 96 : 72;
+    static_assert(128 * few + kConvert * convert + kDrain * drain + (VEC ? 0 : kFill * fill) <=
                       launch * (VEC ? kThreads : kAnyThreads),
                   "the roles' registers must fit the block's");
 };
@@ -127,7 +134,14 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16
         : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// D (+)= A B^T of a pair, A in the TMEM of both CTAs (128 rows each)
+// D (+)= A B^T, A in TMEM; of a pair in the TMEM of both CTAs (128 rows each)
+__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
+        "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
 __device__ __forceinline__ void mma_tmem_pair(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
         "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
@@ -149,6 +163,26 @@ __device__ __forceinline__ void convert16(const uint4 &raw, uint32_t *h) {
     for (int i = 0; i < 4; ++i) {
         h[2 * i] = to_half2(w[i], 0x4140);
         h[2 * i + 1] = to_half2(w[i], 0x4342);
+    }
+}
+
+// Chunks first .. last - 1 (16 of K each, multiples of four) of a stage's 128
+// channels: from the raw ring, a thread a channel, to the TMEM lanes of quarter q.
+__device__ __forceinline__ void convert_channels(uint32_t raw, uint32_t tmem, int q, int lane, int first, int last) {
+    const int r = 32 * q + lane, sw = r & 7;
+    const uint32_t src = raw + (uint32_t)(r * kStepK), to = tmem + ((uint32_t)(32 * q) << 16);
+#pragma unroll 1
+    for (int c = first; c < last; c += 4) {
+        uint4 v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = load_shared(src + (((c + j) ^ sw) << 4));
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+            uint32_t h[16];
+            convert16(v[j], h);
+            convert16(v[j + 1], h + 8);
+            tmem_st16(to + 8 * (c + j), h);
+        }
     }
 }
 
@@ -174,21 +208,24 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
     using Reg = Registers<VEC>;
     constexpr int kStage = stage_bytes(NT), kRaws = raw_stages(NT), kRaw = raw_bytes(NT);
     constexpr int kAcc = acc_cols(NT), kParts = acc_parts(NT);
-    constexpr int kRowsB = kAcc / 2;            // this CTA's tokens of an accumulator
+    constexpr bool kPair = ctas(NT) == 2;
+    constexpr int kChannels = 128 * ctas(NT);   // of a tile
+    constexpr int kRowsB = kAcc / ctas(NT);     // this CTA's tokens of an accumulator
     constexpr int kAtomB = kRowsB * 128, kHalfB = 2 * kAtomB;
     constexpr int kCols = kAcc / 2;             // columns of a drain warp in an accumulator
+    constexpr bool kShare = !kPair;             // the tokens' converters have time for channels
     constexpr int kBars = 2 * kStages + 2 * kAccs + 2 * kRaws + 1;
-    constexpr uint32_t kIdesc = tc::idesc_f16_f32(256, kAcc);
+    constexpr uint32_t kIdesc = tc::idesc_f16_f32(kChannels, kAcc);
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint64_t *bars = (uint64_t *)(smem + ring_bytes(NT));
     uint32_t *tmem_slot = (uint32_t *)(bars + kBars);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int crank = (int)tc::cluster_rank(), rank = crank & 1, part = crank >> 1;
-    const uint32_t even = crank & ~1;
-    const int nclusters = gridDim.x / (2 * split), cluster = blockIdx.x / (2 * split);
-    const int mt = (a.dout + 255) / 256, ntiles = mt * ((a.n + NT - 1) / NT);
+    const int crank = (int)tc::cluster_rank(), rank = kPair ? crank & 1 : 0, part = crank / ctas(NT);
+    const uint32_t even = crank - rank;
+    const int nclusters = gridDim.x / (ctas(NT) * split), cluster = blockIdx.x / (ctas(NT) * split);
+    const int mt = (a.dout + kChannels - 1) / kChannels, ntiles = mt * ((a.n + NT - 1) / NT);
     // this pair's part of K
     const int steps = (a.din + kStepK - 1) / kStepK, per = (steps + split - 1) / split;
     const int step0 = min(steps, part * per), nsteps = min(steps, step0 + per) - step0;
@@ -207,15 +244,15 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
-            tc::mbar_init(full(s), kConvert / 32 + (rank == 0));   // own converters; the odd CTA's relay
+            tc::mbar_init(full(s), kConvert / 32 + (kPair && rank == 0));   // own converters; the odd CTA's relay
             tc::mbar_init(empty(s), 1);
         }
         for (int b = 0; b < kAccs; ++b) {
             tc::mbar_init(afull(b), 1);
-            tc::mbar_init(aempty(b), 2 * kDrain / 32);       // the even CTA's: both drains
+            tc::mbar_init(aempty(b), ctas(NT) * kDrain / 32);   // the even CTA's: both drains
         }
         for (int s = 0; s < kRaws; ++s) {
-            tc::mbar_init(raw_full(s), VEC ? 1 : 4);
+            tc::mbar_init(raw_full(s), VEC ? 1 : kFill / 32);
             tc::mbar_init(raw_empty(s), kConvert / 32);
         }
         tc::mbar_init(closing, 1);
@@ -223,12 +260,17 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
         tc::fence_barrier_init();
     }
     if (warp == 1) {
-        tc::tmem_alloc_pair(tc::smem_u32(tmem_slot), kTmem);
-        tc::tmem_relinquish_pair();
+        if (kPair) {
+            tc::tmem_alloc_pair(tc::smem_u32(tmem_slot), kTmem);
+            tc::tmem_relinquish_pair();
+        } else {
+            tc::tmem_alloc(tc::smem_u32(tmem_slot), kTmem);
+            tc::tmem_relinquish();
+        }
     }
     tc::tc_fence_before();
     __syncthreads();
-    tc::cluster_sync();
+    if (kPair) tc::cluster_sync();
     tc::tc_fence_after();
     const uint32_t tmem = *tmem_slot, tmem_a = tmem + kAccs * 128;
 
@@ -243,6 +285,18 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
             Slot<kStages> in(0);
             int unit = 0;                                    // accumulators so far, over all tiles
             // `count` atoms from atom `at` of a stage into every part's accumulator
+            auto mma = [&](uint32_t d, uint32_t ad, uint64_t bd, uint32_t add) {
+                if (kPair)
+                    mma_tmem_pair(d, ad, bd, kIdesc, add);
+                else
+                    mma_tmem(d, ad, bd, kIdesc, add);
+            };
+            auto commit = [&](uint32_t bar) {
+                if (kPair)
+                    tc::mma_commit_pair(bar, both);
+                else
+                    tc::mma_commit(bar);
+            };
             auto issue = [&](int at, int count, bool first, bool last, bool done) {
 #pragma unroll
                 for (int h = 0; h < kParts; ++h) {
@@ -257,14 +311,14 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
                         const uint32_t ad = tmem_a + in.s * kColsA + at * 32;
                         const uint64_t bd = bd0 + (uint32_t)((in.s * kStage + h * kHalfB + at * kAtomB) >> 4);
 #pragma unroll
-                        for (int sub = 0; sub < 4; ++sub) mma_tmem_pair(d, ad + 8 * sub, bd + 2 * sub, kIdesc, !first || sub > 0);
+                        for (int sub = 0; sub < 4; ++sub) mma(d, ad + 8 * sub, bd + 2 * sub, !first || sub > 0);
                         if (count == 2) {
 #pragma unroll
                             for (int sub = 0; sub < 4; ++sub)
-                                mma_tmem_pair(d, ad + 32 + 8 * sub, bd + (kAtomB >> 4) + 2 * sub, kIdesc, 1);
+                                mma(d, ad + 32 + 8 * sub, bd + (kAtomB >> 4) + 2 * sub, 1);
                         }
-                        if (last) tc::mma_commit_pair(afull(b), both);
-                        if (done && h == kParts - 1) tc::mma_commit_pair(empty(in.s), both);
+                        if (last) commit(afull(b));
+                        if (done && h == kParts - 1) commit(empty(in.s));
                     }
                     __syncwarp();
                 }
@@ -272,7 +326,7 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
             };
             for (int tile = cluster; tile < ntiles && ok; tile += nclusters)
                 for (int step = 0, in_unit = 0; step < nsteps && ok; ++step, in.next()) {
-                    ok = wait_cluster(full(in.s), in.phase);
+                    ok = kPair ? wait_cluster(full(in.s), in.phase) : tc::mbar_wait(full(in.s), in.phase);
                     if (!ok) break;
                     tc::tc_fence_after();
                     const int atoms = min(2, natoms - 2 * step);
@@ -285,9 +339,14 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
                         in_unit = last ? 0 : in_unit + 1;
                     }
                 }
-            if (tc::elect_one()) tc::mma_commit_pair(closing, 1 << even);
+            if (tc::elect_one()) {
+                if (kPair)
+                    tc::mma_commit_pair(closing, 1 << even);
+                else
+                    tc::mma_commit(closing);
+            }
             if (!tc::mbar_wait(closing, 0) || !ok) *abort_flag = 1;
-        } else if (warp != 2 && rank == 1) {
+        } else if (kPair && warp != 2 && rank == 1) {
             // ---------------- relays of the odd CTA: its stages are full, in turn
             const uint32_t full0 = tc::map_rank(full(0), even);
             const int me = warp == 3 ? 2 : warp;
@@ -313,7 +372,7 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
             Slot<kRaws> out(1);
             int filled = 0;
             for (int tile = cluster; tile < ntiles && ok; tile += nclusters) {
-                const int o = tile % mt * 256 + 128 * rank, tk = tile / mt * NT + kRowsB * rank;
+                const int o = tile % mt * kChannels + 128 * rank, tk = tile / mt * NT + kRowsB * rank;
                 for (int step = 0; step < nsteps; ++step, out.next()) {
                     ok = tc::mbar_wait(raw_empty(out.s), out.phase);
                     if (!ok) break;
@@ -341,9 +400,6 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
     } else if (warp < 8) {
         if constexpr (splits_registers(NT, VEC)) registers_down<Reg::convert>();
         // ---------------- channels: raw ring -> fp16 -> TMEM
-        const int q = warp - 4, r = 32 * q + lane;
-        const uint32_t from = raws + (uint32_t)(r * kStepK), sw = r & 7;
-        const uint32_t to = tmem_a + ((uint32_t)(32 * q) << 16);
         bool ok = true;
         Slot<kRaws> in(0);
         Slot<kStages> out(1);
@@ -354,20 +410,7 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc::tc_fence_after();
-                const uint32_t src = from + in.s * kRaw;
-                uint4 raw[4];
-#pragma unroll 1
-                for (int c = 0; c < 8; c += 4) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) raw[j] = load_shared(src + (((c + j) ^ sw) << 4));
-#pragma unroll
-                    for (int j = 0; j < 4; j += 2) {
-                        uint32_t h[16];
-                        convert16(raw[j], h);
-                        convert16(raw[j + 1], h + 8);
-                        tmem_st16(to + out.s * kColsA + 8 * (c + j), h);
-                    }
-                }
+                convert_channels(raws + in.s * kRaw, tmem_a + out.s * kColsA, warp & 3, lane, 0, kShare ? 4 : 8);
                 tmem_wait_st();
                 tc::tc_fence_before();
                 __syncwarp();
@@ -380,7 +423,8 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
     } else if (warp < 12) {
         if constexpr (splits_registers(NT, VEC)) registers_down<Reg::convert>();
         // ---------------- tokens: raw ring -> fp16 -> K-major tiles, 128-byte swizzle
-        constexpr int kU = NT / 32;                          // 16 rows at a time
+        constexpr int kU = own_tokens(NT) / 16;              // 16 rows at a time
+        constexpr int kBatch = kU < 4 ? kU : 4;              // loads in flight
         const int t = threadIdx.x - 256, c = t & 7, r0 = t >> 3, sw = r0 & 7;
         // 16 codes become two 16-byte chunks of a 128-byte row; threads of the
         // second atom write theirs in the other order, so that eight lanes of a
@@ -396,9 +440,13 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
             for (int step = 0; step < nsteps; ++step, in.next(), out.next()) {
                 ok = tc::mbar_wait(raw_full(in.s), in.phase);
                 ok = tc::mbar_wait(empty(out.s), out.phase) && ok;
+                ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
+                if (kShare) {
+                    tc::tc_fence_after();
+                    convert_channels(raws + in.s * kRaw, tmem_a + out.s * kColsA, warp & 3, lane, 4, 8);
+                }
                 const uint32_t src = from + in.s * kRaw, dst = to + out.s * kStage;
-                constexpr int kBatch = kU < 4 ? kU : 4;      // loads in flight
                 uint4 raw[kBatch];
 #pragma unroll 1
                 for (int i = 0; i < kU; i += kBatch) {
@@ -416,6 +464,10 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
                     }
                 }
                 fence_to_async();
+                if (kShare) {
+                    tmem_wait_st();
+                    tc::tc_fence_before();
+                }
                 __syncwarp();
                 if (lane == 0) {
                     tc::mbar_arrive(full(out.s));
@@ -434,7 +486,7 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
         bool ok = true;
         int unit = 0;
         for (int tile = cluster; tile < ntiles && ok; tile += nclusters) {
-            const int o = tile % mt * 256 + 128 * rank + lrow, t0 = tile / mt * NT;
+            const int o = tile % mt * kChannels + 128 * rank + lrow, t0 = tile / mt * NT;
             const bool live = o < a.dout;
             uint32_t acc[kParts][kCols];                    // int32, or float32 with groups
 #pragma unroll
@@ -461,7 +513,12 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
                         } else {
                             tc::tc_fence_before();
                             __syncwarp();
-                            if (lane == 0) tc::mbar_arrive_cluster(released + 8 * b);
+                            if (lane == 0) {
+                                if (kPair)
+                                    tc::mbar_arrive_cluster(released + 8 * b);
+                                else
+                                    tc::mbar_arrive(aempty(b));
+                            }
                         }
                         uint32_t(&x)[16] = v[(cc / 16) & 1];
 #pragma unroll
@@ -510,25 +567,55 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
         if constexpr (splits_registers(NT, VEC)) registers_down<Reg::fill>();
         // ---------------- rows that TMA cannot read, into the raw ring
         tc::pdl_wait();
-        constexpr int kUnits = 8 + NT / 32;                  // 16 rows at a time: channels, tokens
+        constexpr int kU = (128 + own_tokens(NT) + 31) / 32;     // 32 rows at a time: channels, tokens
+        constexpr int kBatch = 4;
         const int t = threadIdx.x - 640, c = t & 7, r0 = t >> 3;
         const uint32_t to = raws + (uint32_t)(r0 * kStepK + ((c ^ (r0 & 7)) << 4));
         bool ok = true;
         Slot<kRaws> out(1);
         for (int tile = cluster; tile < ntiles && ok; tile += nclusters) {
-            const int o = tile % mt * 256 + 128 * rank + r0, tk = tile / mt * NT + kRowsB * rank + r0;
+            const int o = tile % mt * kChannels + 128 * rank + r0, tk = tile / mt * NT + kRowsB * rank;
+            // row r0 + 32 i of the stage, null where there is none
+            auto row_of = [&](int i) -> const int8_t * {
+                if (i < 4) return o + 32 * i < a.dout ? a.C + (size_t)(o + 32 * i) * a.ldc : nullptr;
+                const int j = r0 + 32 * (i - 4), r = tk + j / kRowsB * kAcc + j % kRowsB;
+                return j < own_tokens(NT) && r < a.n ? a.X + (size_t)r * a.ldx : nullptr;
+            };
             for (int step = 0; step < nsteps; ++step, out.next()) {
                 const int k = (step0 + step) * kStepK + c * 16;
                 ok = tc::mbar_wait(raw_empty(out.s), out.phase);
                 if (!ok) break;
+                const uint32_t dst = to + out.s * kRaw;
+#pragma unroll 1
+                for (int i0 = 0; i0 < kU; i0 += kBatch) {
+                    uint4 v[kBatch];
+                    if (k >= 4 && k + 20 <= a.din) {
+                        // inside the rows: whole words, all in flight
+                        uint32_t w[kBatch][5], sel[kBatch];
 #pragma unroll
-                for (int i = 0; i < kUnits; ++i) {
-                    const int j = 16 * (i - 8);              // row r0 + j of the tokens
-                    const int r = i < 8 ? o + 16 * i : tk + j / kRowsB * kAcc + j % kRowsB;
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (r < (i < 8 ? a.dout : a.n))
-                        v = load_codes<false>(i < 8 ? a.C + (size_t)r * a.ldc : a.X + (size_t)r * a.ldx, k, a.din);
-                    store_shared(to + out.s * kRaw + i * 16 * kStepK, v);
+                        for (int j = 0; j < kBatch; ++j) {
+                            const int8_t *row = row_of(i0 + j);
+                            sel[j] = row ? (uint32_t)((uintptr_t)(row + k) & 3) : 4;
+#pragma unroll
+                            for (int e = 0; e < 5; ++e)
+                                w[j][e] = row ? reinterpret_cast<const uint32_t *>(row + k - sel[j])[e] : 0;
+                        }
+#pragma unroll
+                        for (int j = 0; j < kBatch; ++j) {
+                            const uint32_t p = 0x3210u + 0x1111u * (sel[j] & 3);
+                            v[j] = make_uint4(__byte_perm(w[j][0], w[j][1], p), __byte_perm(w[j][1], w[j][2], p),
+                                              __byte_perm(w[j][2], w[j][3], p), __byte_perm(w[j][3], w[j][4], p));
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < kBatch; ++j) {
+                            const int8_t *row = row_of(i0 + j);
+                            v[j] = row ? load_codes<false>(row, k, a.din) : make_uint4(0, 0, 0, 0);
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < kBatch; ++j)
+                        if (r0 + 32 * (i0 + j) < 128 + own_tokens(NT)) store_shared(dst + (i0 + j) * 32 * kStepK, v[j]);
                 }
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(raw_full(out.s));
@@ -537,29 +624,42 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
         if (!ok) *abort_flag = 1;
     }
     if (split > 1) {
-        // join: pair `part` finishes columns part NT / split .. of its 128 channels
+        // join: part `part` of K finishes columns part cols .. of its 128 channels
         cluster_barrier();
         if (warp >= 12 && warp < 20 && cluster < ntiles) {
             const int t = threadIdx.x - 384, lrow = t & 127, half = t >> 7;
-            const int o = cluster % mt * 256 + 128 * rank + lrow, t0 = cluster / mt * NT;
-            const int cols = NT / split;
+            const int o = cluster % mt * kChannels + 128 * rank + lrow, t0 = cluster / mt * NT;
+            const int cols = (NT + split - 1) / split;       // columns past NT are skipped
             const float bias = a.bias && o < a.dout ? a.bias[o] : 0.f, wch = !GROUPS && o < a.dout ? a.ws[o] : 1.f;
-            for (int e = half; e < cols; e += 2) {
-                const int col = part * cols + e;
-                if (o >= a.dout || t0 + col >= a.n) continue;
-                const uint32_t at = ring + (uint32_t)(col * 128 + lrow) * 4;
-                float f = 0.f;
-                int i = 0;
-                for (int p = 0; p < split; ++p) {
-                    const uint32_t v = load_remote(tc::map_rank(at, 2 * p + rank));
-                    f += __uint_as_float(v);
-                    i += (int)v;
+            constexpr int kAtOnce = 4;                       // columns in flight
+#pragma unroll 1
+            for (int e0 = half; e0 < cols; e0 += 2 * kAtOnce) {
+                uint32_t v[kAtOnce][kMostParts];
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j) {
+                    const int col = part * cols + e0 + 2 * j;
+                    const uint32_t at = ring + (uint32_t)(col * 128 + lrow) * 4;
+#pragma unroll
+                    for (int p = 0; p < kMostParts; ++p)
+                        v[j][p] = p < split && e0 + 2 * j < cols ? load_remote(tc::map_rank(at, ctas(NT) * p + rank)) : 0;
                 }
-                const float v = GROUPS ? f : (float)i * wch;
-                with_type_device(a.dtype, [&](auto type) {
-                    using T = decltype(type);
-                    static_cast<T *>(a.Y)[(size_t)(t0 + col) * a.ldy + o] = from_float<T>(fmaf(v, a.xs[t0 + col], bias));
-                });
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j) {
+                    const int col = part * cols + e0 + 2 * j;
+                    if (e0 + 2 * j >= cols || col >= NT || o >= a.dout || t0 + col >= a.n) continue;
+                    float f = 0.f;
+                    int i = 0;
+#pragma unroll
+                    for (int p = 0; p < kMostParts; ++p) {
+                        f += __uint_as_float(v[j][p]);
+                        i += (int)v[j][p];
+                    }
+                    const float y = fmaf(GROUPS ? f : (float)i * wch, a.xs[t0 + col], bias);
+                    with_type_device(a.dtype, [&](auto type) {
+                        using T = decltype(type);
+                        static_cast<T *>(a.Y)[(size_t)(t0 + col) * a.ldy + o] = from_float<T>(y);
+                    });
+                }
             }
         }
     }
@@ -568,10 +668,13 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
     tc::tc_fence_before();
     __syncwarp();
     __syncthreads();
-    tc::cluster_sync();
+    if (kPair || split > 1) tc::cluster_sync();
     if (warp == 1) {
         tc::tc_fence_after();
-        tc::tmem_dealloc_pair(tmem, kTmem);
+        if (kPair)
+            tc::tmem_dealloc_pair(tmem, kTmem);
+        else
+            tc::tmem_dealloc(tmem, kTmem);
     }
     if (threadIdx.x == 0 && *abort_flag) {
         *(volatile int *)failed = 1;
@@ -589,20 +692,20 @@ cudaError_t launch(const ProductArgs &a, int split, int *failed, cudaStream_t s,
     if (VEC) {
         auto pitch = [](int64_t ld, int rows) { return (uint64_t)(rows > 1 ? ld : (ld + 15) / 16 * 16); };
         e = make_tmap_codes(&mapC, a.C, a.dout, a.din, pitch(a.ldc, a.dout), 128);
-        if (e == cudaSuccess) e = make_tmap_codes(&mapX, a.X, a.n, a.din, pitch(a.ldx, a.n), acc_cols(NT) / 2);
+        if (e == cudaSuccess) e = make_tmap_codes(&mapX, a.X, a.n, a.din, pitch(a.ldx, a.n), acc_cols(NT) / ctas(NT));
         if (e != cudaSuccess) return e;
     }
-    const int64_t tiles = (int64_t)((a.dout + 255) / 256) * ((a.n + NT - 1) / NT);
-    const int64_t clusters = split > 1 ? tiles : std::min<int64_t>(tiles, num_sms() / 2);
+    const int64_t tiles = (int64_t)((a.dout + 128 * ctas(NT) - 1) / (128 * ctas(NT))) * ((a.n + NT - 1) / NT);
+    const int64_t clusters = split > 1 ? tiles : std::min<int64_t>(tiles, num_sms() / ctas(NT));
     if (tiles > 0x3FFFFFFF / (2 * split)) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(clusters * 2 * split));
+    cfg.gridDim = dim3((unsigned)(clusters * ctas(NT) * split));
     cfg.blockDim = dim3(VEC ? kThreads : kAnyThreads);
     cfg.dynamicSmemBytes = smem_bytes(NT);
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 2 * split;
+    attr[0].val.clusterDim.x = ctas(NT) * split;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
@@ -623,26 +726,33 @@ cudaError_t launch_nt(const ProductArgs &a, int split, int *failed, cudaStream_t
 }  // namespace
 
 cudaError_t launch_tc_integer(const ProductArgs &a, int *failed, cudaStream_t s, bool pdl) {
-    // The tile's tokens and the split of K that leave the fewest steps in a
-    // row, a step of 128 of K being about as long as given (cycles)
+    // The tile's tokens and the split of K that take the least time: waves of
+    // clusters, each so many steps of 128 of K and what a tile costs besides
+    // (cycles).  Of clusters of four CTAs 36 run at a time, of six 23, of eight 15
+    // (occupancy calculator, 152 SMs: a cluster's SMs lie in one GPC).
     constexpr struct {
-        int nt, cycles;
-    } kinds[] = {{32, 400}, {64, 450}, {128, 650}, {256, 1100}};
-    const int mt = (a.dout + 255) / 256, steps = (a.din + kStepK - 1) / kStepK, pairs = std::max(1, num_sms() / 2);
+        int nt, step, tile;
+    } kinds[] = {{32, 450, 4000}, {64, 550, 4000}, {128, 800, 5000}, {256, 1300, 7000}};
+    constexpr int resident[] = {0, 152, 76, 48, 36, 0, 23, 0, 15};
+    const bool vec = vector_rows(a);
+    const int steps = (a.din + kStepK - 1) / kStepK, sms = num_sms();
     int nt = 0, split = 1;
     double best = 0;
-    for (const auto &k : kinds)
-        for (int sp = 1; sp <= 4; sp *= 2) {
-            if (sp > 1 && sp > steps) break;
-            const int64_t tiles = (int64_t)mt * ((a.n + k.nt - 1) / k.nt);
-            if (sp > 1 && tiles * sp > pairs) break;
-            const double t = (double)((tiles * sp + pairs - 1) / pairs) * ((steps + sp - 1) / sp) * k.cycles + (sp > 1 ? 2000 : 0);
+    for (const auto &k : kinds) {
+        if (k.nt == 256 && !vec) continue;
+        for (int sp = 1; sp <= std::min(kMostParts, steps); ++sp) {
+            const int channels = 128 * ctas(k.nt), at_once = std::max(1, resident[ctas(k.nt) * sp] * sms / 152);
+            const int64_t tiles = (int64_t)((a.dout + channels - 1) / channels) * ((a.n + k.nt - 1) / k.nt);
+            if (sp > 1 && tiles > at_once) break;
+            const double waves = (double)((tiles + at_once - 1) / at_once);
+            const double t = waves * ((steps + sp - 1) / sp) * k.step * (vec ? 1 : 2) + waves * k.tile + (sp > 1 ? 1500 : 0);
             if (nt == 0 || t < best) {
                 best = t;
                 nt = k.nt;
                 split = sp;
             }
         }
+    }
     switch (nt) {
         case 32: return launch_nt<32>(a, split, failed, s, pdl);
         case 64: return launch_nt<64>(a, split, failed, s, pdl);

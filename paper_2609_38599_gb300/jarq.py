@@ -475,34 +475,56 @@ def objective(hess: Hessian, W, S, Q, Z, bits: int, out=None):
 
 
 # ---- running and scoring a quantized model: device tensors, enqueued on torch's
-# current stream, not waited for ----
+# current stream, not waited for.  A call takes a few microseconds on the device,
+# so little is done here: every attribute of a tensor is looked at once. ----
 
-def _rows(x, name, *dtypes):
-    """(pointer, row pitch) of a CUDA matrix whose rows are contiguous."""
-    if x.dtype not in dtypes or not x.is_cuda or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
-        raise TypeError(f"{name}: expected a CUDA matrix of {' or '.join(str(d) for d in dtypes)} with "
-                        f"contiguous rows, got {x.dtype} {tuple(x.shape)} on {x.device}")
+class _Torch:
+    """What the calls below need of torch, looked up once."""
+
+    def __init__(self):
+        import torch
+        self.floats = {torch.float32: JARQ_F32, torch.float16: JARQ_F16, torch.bfloat16: JARQ_BF16}
+        self.named = {"float32": torch.float32, "float16": torch.float16, "bfloat16": torch.bfloat16}
+        self.bytes = {torch.int8: 0}
+        self.empty = torch.empty
+        self.f32, self.i32, self.i64, self.i8, self.u8 = (torch.float32, torch.int32, torch.int64, torch.int8,
+                                                          torch.uint8)
+        # the current stream's handle without an object around it
+        self.stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                              lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+_torch_cache = None
+
+
+def _torch() -> _Torch:
+    global _torch_cache
+    if _torch_cache is None:
+        _torch_cache = _Torch()
+    return _torch_cache
+
+
+def _matrix(x, name, types):
+    """(pointer, row pitch, rows, columns, type code) of a CUDA matrix whose rows are contiguous."""
+    code = types.get(x.dtype)
+    shape = x.shape
+    if code is None or len(shape) != 2 or not x.is_cuda:
+        raise TypeError(f"{name}: expected a CUDA matrix of {' or '.join(str(t) for t in types)}, got {x.dtype} "
+                        f"{tuple(shape)} on {x.device}")
+    n, d = shape
+    pitch, step = x.stride()
+    if step != 1 and d > 1:
+        raise TypeError(f"{name}: expected contiguous rows, got strides {(pitch, step)}")
     # the pitch of a single row is never used
-    return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else x.shape[1]
+    return x.data_ptr(), pitch if n > 1 else d, n, d, code
 
 
-def _flat(x, name, dtype, *shapes):
-    """Pointer of a contiguous CUDA tensor of one of the given shapes."""
-    if x.dtype != dtype or not x.is_cuda or not x.is_contiguous() or tuple(x.shape) not in shapes:
-        raise TypeError(f"{name}: expected a contiguous CUDA tensor of {dtype}, shape "
-                        f"{' or '.join(str(s) for s in shapes)}, got {x.dtype} {tuple(x.shape)} on {x.device}")
+def _flat(x, name, dtype, shape, also=None):
+    """Pointer of a contiguous CUDA tensor of the given shape (or the other one)."""
+    if x.dtype != dtype or not x.is_cuda or not x.is_contiguous() or (x.shape != shape and x.shape != also):
+        raise TypeError(f"{name}: expected a contiguous CUDA tensor of {dtype}, shape {shape}"
+                        f"{f' or {also}' if also else ''}, got {x.dtype} {tuple(x.shape)} on {x.device}")
     return x.data_ptr()
-
-
-def _float_types():
-    """jarq_dtype of every torch type of weights, activations and logits."""
-    import torch
-    return {torch.float32: JARQ_F32, torch.float16: JARQ_F16, torch.bfloat16: JARQ_BF16}
-
-
-def _named_type(dtype):
-    import torch
-    return {"float32": torch.float32, "float16": torch.float16, "bfloat16": torch.bfloat16}[dtype]
 
 
 def async_status(device=None) -> int:
@@ -516,14 +538,13 @@ def quantize_rows(X):
     """``jarq_quantize_rows``: (codes int8 [n][d], scale float32 [n]) of a
     float32, float16 or bfloat16 matrix, one scale a row.  The rows of the codes
     lie on 16-byte boundaries."""
-    import torch
-    types = _float_types()
-    ptr, ldx = _rows(X, "X", *types)
-    n, d = int(X.shape[0]), int(X.shape[1])
-    q = torch.empty(n, (d + 15) // 16 * 16, dtype=torch.int8, device=X.device)
-    scale = torch.empty(n, dtype=torch.float32, device=X.device)
-    status = _lib.jarq_quantize_rows(ptr, types[X.dtype], n, d, ldx, q.data_ptr(), q.shape[1],
-                                     scale.data_ptr(), _dev_stream(X))
+    T = _torch()
+    x, ldx, n, d, code = _matrix(X, "X", T.floats)
+    pitch = (d + 15) // 16 * 16
+    q = T.empty((n, pitch), dtype=T.i8, device=X.device)
+    scale = T.empty((n,), dtype=T.f32, device=X.device)
+    status = _lib.jarq_quantize_rows(x, code, n, d, ldx, q.data_ptr(), pitch, scale.data_ptr(),
+                                     T.stream(X.get_device()))
     if status != JARQ_OK:
         raise JarqError(status, "jarq_quantize_rows")
     return q[:, :d], scale
@@ -532,45 +553,44 @@ def quantize_rows(X):
 def integer_codes(Q, Z, group_size: int, bits: int):
     """``jarq_integer_codes``: q - z of a refined layer as int8 [dout][din], the
     weights of ``integer_linear`` with the scales S and this group size."""
-    import torch
-    dout, din = int(Q.shape[0]), int(Q.shape[1])
-    C = torch.empty(dout, (din + 15) // 16 * 16, dtype=torch.int8, device=Q.device)
+    T = _torch()
+    dout, din = Q.shape
+    pitch = (din + 15) // 16 * 16
+    C = T.empty((dout, pitch), dtype=T.i8, device=Q.device)
     status = _lib.jarq_integer_codes(_ptr(Q, np.uint8), _ptr(Z, np.int32), dout, din, int(group_size),
-                                     int(bits), C.data_ptr(), C.shape[1], _dev_stream(Q))
+                                     int(bits), C.data_ptr(), pitch, T.stream(Q.get_device()))
     if status != JARQ_OK:
         raise JarqError(status, "jarq_integer_codes")
     return C[:, :din]
 
 
-def _integer_layer(C, ws, group_size, bias, n, din, dtype, out, device):
+def _integer_layer(T, X, C, ws, group_size, bias, n, din, dtype, out):
     """The arguments that both integer products share, and their output."""
-    import torch
-    c, ldc = _rows(C, "C", torch.int8)
-    dout = int(C.shape[0])
-    if int(C.shape[1]) != din:
-        raise ValueError(f"weights have {int(C.shape[1])} columns, activations {din}")
+    c, ldc, dout, dc, _ = _matrix(C, "C", T.bytes)
+    if dc != din:
+        raise ValueError(f"weights have {dc} columns, activations {din}")
     G = din // group_size if group_size else 1
-    w = _flat(ws, "ws", torch.float32, (dout, G), *([(dout,)] if G == 1 else []))
-    b = _flat(bias, "bias", torch.float32, (dout,)) if bias is not None else None
+    w = _flat(ws, "ws", T.f32, (dout, G), (dout,) if G == 1 else None)
+    b = _flat(bias, "bias", T.f32, (dout,)) if bias is not None else None
     if out is None:
-        out = torch.empty(n, dout, dtype=dtype, device=device)
-    elif tuple(out.shape) != (n, dout):
-        raise ValueError(f"out has shape {tuple(out.shape)}, not {(n, dout)}")
-    y, ldy = _rows(out, "out", dtype)
+        out = T.empty((n, dout), dtype=dtype, device=X.device)
+        return c, ldc, w, b, dout, out, out.data_ptr(), dout
+    y, ldy, rows, cols, _ = _matrix(out, "out", {dtype: 0})
+    if rows != n or cols != dout:
+        raise ValueError(f"out has shape {(rows, cols)}, not {(n, dout)}")
     return c, ldc, w, b, dout, out, y, ldy
 
 
 def integer_product(X, xs, C, ws, group_size: int = 0, bias=None, dtype: str = "float16", out=None):
     """``jarq_integer_product``: ``xs[t] * sum_i ws[o][i] * (X_i C_i^T) + bias`` for
     int8 codes X [n][din] and C [dout][din], as float32, float16 or bfloat16."""
-    import torch
-    x, ldx = _rows(X, "X", torch.int8)
-    n, din = int(X.shape[0]), int(X.shape[1])
-    tdt = _named_type(dtype)
-    s = _flat(xs, "xs", torch.float32, (n,))
-    c, ldc, w, b, dout, out, y, ldy = _integer_layer(C, ws, group_size, bias, n, din, tdt, out, X.device)
-    status = _lib.jarq_integer_product(x, ldx, s, c, ldc, w, int(group_size), b, n, dout, din,
-                                       _float_types()[tdt], y, ldy, _dev_stream(X))
+    T = _torch()
+    x, ldx, n, din, _ = _matrix(X, "X", T.bytes)
+    ydt = T.named[dtype]
+    s = _flat(xs, "xs", T.f32, (n,))
+    c, ldc, w, b, dout, out, y, ldy = _integer_layer(T, X, C, ws, group_size, bias, n, din, ydt, out)
+    status = _lib.jarq_integer_product(x, ldx, s, c, ldc, w, group_size, b, n, dout, din, T.floats[ydt], y, ldy,
+                                       T.stream(X.get_device()))
     if status != JARQ_OK:
         raise JarqError(status, "jarq_integer_product")
     return out
@@ -580,16 +600,14 @@ def integer_linear(X, C, ws, group_size: int = 0, bias=None, dtype: str = None, 
     """``jarq_integer_linear``: the activations X [n][din] (float32, float16 or
     bfloat16) quantized token by token and multiplied with the int8 weights C
     [dout][din]; the result in ``dtype`` (X's own when None)."""
-    import torch
-    types = _float_types()
-    x, ldx = _rows(X, "X", *types)
-    n, din = int(X.shape[0]), int(X.shape[1])
-    tdt = X.dtype if dtype is None else _named_type(dtype)
-    c, ldc, w, b, dout, out, y, ldy = _integer_layer(C, ws, group_size, bias, n, din, tdt, out, X.device)
+    T = _torch()
+    x, ldx, n, din, code = _matrix(X, "X", T.floats)
+    ydt = X.dtype if dtype is None else T.named[dtype]
+    c, ldc, w, b, dout, out, y, ldy = _integer_layer(T, X, C, ws, group_size, bias, n, din, ydt, out)
     size = _lib.jarq_integer_linear_workspace(n, din)
-    work = torch.empty(size, dtype=torch.uint8, device=X.device)
-    status = _lib.jarq_integer_linear(x, types[X.dtype], ldx, c, ldc, w, int(group_size), b, n, dout, din,
-                                      types[tdt], y, ldy, work.data_ptr(), size, _dev_stream(X))
+    work = T.empty((size,), dtype=T.u8, device=X.device)
+    status = _lib.jarq_integer_linear(x, code, ldx, c, ldc, w, group_size, b, n, dout, din, T.floats[ydt], y, ldy,
+                                      work.data_ptr(), size, T.stream(X.get_device()))
     if status != JARQ_OK:
         raise JarqError(status, "jarq_integer_linear")
     return out
@@ -609,24 +627,23 @@ def token_logprobs(logits, tokens=None, top: int = 0) -> TokenScores:
     """``jarq_token_logprobs``: log probabilities of ``tokens`` (int64 [n] or
     [n][t]) under the rows of ``logits`` [n][vocab], the rows' entropies and log
     sums of exponentials, and their ``top`` most probable tokens."""
-    import torch
-    types = _float_types()
-    x, ld = _rows(logits, "logits", *types)
-    n, vocab, k = int(logits.shape[0]), int(logits.shape[1]), int(top)
-    dev = logits.device
-    t, tok, logprob = 0, None, None
+    T = _torch()
+    x, ld, n, vocab, code = _matrix(logits, "logits", T.floats)
+    f32, dev = T.f32, logits.device
+    t, tok, logprob, lp = 0, None, None, None
     if tokens is not None:
-        t = 1 if tokens.dim() == 1 else int(tokens.shape[1])
-        tok = _flat(tokens, "tokens", torch.int64, (n,), (n, t))
-        logprob = torch.empty(tokens.shape, dtype=torch.float32, device=dev)
-    stats = torch.empty(2, n, dtype=torch.float32, device=dev)
-    top_logprob = torch.empty(n, k, dtype=torch.float32, device=dev) if k > 0 else None
-    top_token = torch.empty(n, k, dtype=torch.int32, device=dev) if k > 0 else None
-    entropy, lse = stats[0], stats[1]
-    status = _lib.jarq_token_logprobs(x, types[logits.dtype], n, vocab, ld, tok, t, k,
-                                      logprob.data_ptr() if t else None, stats.data_ptr(),
-                                      stats.data_ptr() + 4 * n, top_logprob.data_ptr() if k > 0 else None,
-                                      top_token.data_ptr() if k > 0 else None, _dev_stream(logits))
+        shape = tokens.shape
+        t = 1 if len(shape) == 1 else shape[-1]
+        tok = _flat(tokens, "tokens", T.i64, (n,), (n, t))
+        logprob = T.empty(shape, dtype=f32, device=dev)
+        lp = logprob.data_ptr()
+    entropy, lse = T.empty((n,), dtype=f32, device=dev), T.empty((n,), dtype=f32, device=dev)
+    top_logprob, top_token, tl, tt = None, None, None, None
+    if top > 0:
+        top_logprob, top_token = T.empty((n, top), dtype=f32, device=dev), T.empty((n, top), dtype=T.i32, device=dev)
+        tl, tt = top_logprob.data_ptr(), top_token.data_ptr()
+    status = _lib.jarq_token_logprobs(x, code, n, vocab, ld, tok, t, top, lp, entropy.data_ptr(), lse.data_ptr(),
+                                      tl, tt, T.stream(logits.get_device()))
     if status != JARQ_OK:
         raise JarqError(status, "jarq_token_logprobs")
     return TokenScores(logprob, entropy, lse, top_logprob, top_token)
@@ -636,23 +653,24 @@ def token_logprobs_grad(logits, tokens, lse, g_logprob, entropy=None, g_entropy=
     """``jarq_token_logprobs_grad``: gradient with respect to ``logits`` of
     ``(g_logprob * logprob).sum() + (g_entropy * entropy).sum()``; ``lse`` and
     ``entropy`` are ``token_logprobs``'s.  ``out`` may be ``logits``."""
-    import torch
-    types = _float_types()
-    x, ld = _rows(logits, "logits", *types)
-    n, vocab = int(logits.shape[0]), int(logits.shape[1])
-    t = 1 if tokens.dim() == 1 else int(tokens.shape[1])
-    tok = _flat(tokens, "tokens", torch.int64, (n,), (n, t))
-    g = _flat(g_logprob, "g_logprob", torch.float32, tuple(tokens.shape))
-    s = _flat(lse, "lse", torch.float32, (n,))
-    h = _flat(entropy, "entropy", torch.float32, (n,)) if entropy is not None else None
-    gh = _flat(g_entropy, "g_entropy", torch.float32, (n,)) if g_entropy is not None else None
+    T = _torch()
+    x, ld, n, vocab, code = _matrix(logits, "logits", T.floats)
+    f32, shape = T.f32, tokens.shape
+    t = 1 if len(shape) == 1 else shape[-1]
+    tok = _flat(tokens, "tokens", T.i64, (n,), (n, t))
+    g = _flat(g_logprob, "g_logprob", f32, shape)
+    s = _flat(lse, "lse", f32, (n,))
+    h = _flat(entropy, "entropy", f32, (n,)) if entropy is not None else None
+    gh = _flat(g_entropy, "g_entropy", f32, (n,)) if g_entropy is not None else None
     if out is None:
-        out = torch.empty(n, vocab, dtype=logits.dtype, device=logits.device)
-    elif tuple(out.shape) != (n, vocab):
-        raise ValueError(f"out has shape {tuple(out.shape)}, not {(n, vocab)}")
-    dx, ldd = _rows(out, "out", logits.dtype)
-    status = _lib.jarq_token_logprobs_grad(x, types[logits.dtype], n, vocab, ld, tok, t, s, h, g, gh, dx,
-                                           ldd, _dev_stream(logits))
+        out = T.empty((n, vocab), dtype=logits.dtype, device=logits.device)
+        dx, ldd = out.data_ptr(), vocab
+    else:
+        dx, ldd, rows, cols, _ = _matrix(out, "out", {logits.dtype: 0})
+        if rows != n or cols != vocab:
+            raise ValueError(f"out has shape {(rows, cols)}, not {(n, vocab)}")
+    status = _lib.jarq_token_logprobs_grad(x, code, n, vocab, ld, tok, t, s, h, g, gh, dx, ldd,
+                                           T.stream(logits.get_device()))
     if status != JARQ_OK:
         raise JarqError(status, "jarq_token_logprobs_grad")
     return out
