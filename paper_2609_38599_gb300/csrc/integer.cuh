@@ -7,13 +7,17 @@ namespace jarq {
 
 // Y[t][o] = xs[t] sum_i ws[o][i] (sum_{k in group i} X[t][k] C[o][k]) + bias[o]
 struct ProductArgs {
-    const int8_t *X, *C;
+    const void *X;               // int8 codes, or (half) the same integers in fp16
+    const int8_t *C;
     const float *xs, *ws, *bias;
     void *Y;
     int64_t ldx, ldc, ldy;
     int n, dout, din, g, G;      // g: group size, 0 for one scale a channel (G = 1)
     jarq_dtype dtype;            // of Y
+    bool half;
 };
+
+constexpr int kFewTokens = 8;    // most tokens of the form without tensor cores, which takes int8 codes
 
 // Codes k .. k + 15 of a row of `len`; zeros beyond it, which are not read.  VEC:
 // the row and k are multiples of 16 bytes; otherwise whole words inside the row
@@ -39,10 +43,12 @@ __device__ __forceinline__ uint4 load_codes(const int8_t *row, int k, int len) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Whether all rows of codes lie on 16-byte boundaries.
+// Whether all rows of weight codes (of all codes) lie on 16-byte boundaries.
+inline bool vector_codes(const ProductArgs &a) {
+    return ((uintptr_t)a.C & 15) == 0 && (a.ldc % 16 == 0 || a.dout == 1);
+}
 inline bool vector_rows(const ProductArgs &a) {
-    return (((uintptr_t)a.X | (uintptr_t)a.C) & 15) == 0 && (a.ldx % 16 == 0 || a.n == 1) &&
-           (a.ldc % 16 == 0 || a.dout == 1);
+    return vector_codes(a) && ((uintptr_t)a.X & 15) == 0 && (a.ldx % 16 == 0 || a.n == 1);
 }
 
 // More than a few tokens, on the tensor cores (k_tc_integer.cu).  `failed`: set

@@ -44,36 +44,39 @@ static cudaError_t encode_tiled(EncodeTiledFn *out) {
     return cudaSuccess;
 }
 
-// 2D tensor map of 2-byte elements (bf16 or fp16) over [rows][cols]
-// (pitch = cols), box_rows x 64 boxes with 128-byte swizzle or box_rows x 32
-// boxes with 64-byte swizzle, out-of-range elements read as zero.
-cudaError_t make_tmap_2b(CUtensorMap *m, const void *base, uint64_t rows, uint64_t cols,
-                         uint32_t box_rows, CUtensorMapDataType dtype, uint32_t box_cols) {
+// 2D tensor map over [rows][cols], rows `pitch` elements apart, out-of-range
+// elements read as zero.
+static cudaError_t make_tmap(CUtensorMap *m, CUtensorMapDataType dtype, int size, const void *base, uint64_t rows,
+                             uint64_t cols, uint64_t pitch, uint32_t box_rows, uint32_t box_cols,
+                             CUtensorMapSwizzle swizzle) {
     EncodeTiledFn fn;
     if (const cudaError_t e = encode_tiled(&fn); e != cudaSuccess) return e;
     cuuint64_t dims[2] = {cols, rows};
-    cuuint64_t strides[1] = {cols * 2};
+    cuuint64_t strides[1] = {pitch * size};
     cuuint32_t box[2] = {box_cols, box_rows};
     cuuint32_t es[2] = {1, 1};
     CUresult r = fn(m, dtype, 2, const_cast<void *>(base), dims, strides,
-                    box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                    box_cols == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                    box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
+cudaError_t make_tmap_2b(CUtensorMap *m, const void *base, uint64_t rows, uint64_t cols,
+                         uint32_t box_rows, CUtensorMapDataType dtype, uint32_t box_cols) {
+    return make_tmap(m, dtype, 2, base, rows, cols, cols, box_rows, box_cols,
+                     box_cols == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
 cudaError_t make_tmap_codes(CUtensorMap *m, const int8_t *base, uint64_t rows, uint64_t cols,
                             uint64_t pitch, uint32_t box_rows) {
-    EncodeTiledFn fn;
-    if (const cudaError_t e = encode_tiled(&fn); e != cudaSuccess) return e;
-    cuuint64_t dims[2] = {cols, rows};
-    cuuint64_t strides[1] = {pitch};
-    cuuint32_t box[2] = {128, box_rows};
-    cuuint32_t es[2] = {1, 1};
-    CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t *>(base), dims, strides, box, es,
-                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+    return make_tmap(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, base, rows, cols, pitch, box_rows, 128,
+                     CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+cudaError_t make_tmap_half(CUtensorMap *m, const void *base, uint64_t rows, uint64_t cols,
+                           uint64_t pitch, uint32_t box_rows) {
+    return make_tmap(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, rows, cols, pitch, box_rows, 64,
+                     CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 cudaError_t make_tmap_bf16(CUtensorMap *m, const void *base, uint64_t rows, uint64_t cols,

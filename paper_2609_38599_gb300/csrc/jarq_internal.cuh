@@ -282,8 +282,9 @@ cudaError_t launch_init_rows(int *active, int *iters, int *accepted, int *ridge,
 int num_sms();
 
 // ---- operators that only enqueue (k_quantize.cu, k_integer*.cu, k_logprob.cu) ----
-cudaError_t launch_quantize_rows(const void *X, jarq_dtype dtype, int n, int d, int64_t ldx,
-                                 int8_t *Q, int64_t ldq, float *scale, cudaStream_t s);
+// half: the integers are written as fp16 instead of int8
+cudaError_t launch_quantize_rows(const void *X, jarq_dtype dtype, int n, int d, int64_t ldx, void *Q,
+                                 bool half, int64_t ldq, float *scale, cudaStream_t s);
 // The word in pinned host memory in which their kernels report a wait that
 // gave up (null: it could not be allocated), what it holds, and the same with
 // the word cleared.
@@ -368,6 +369,9 @@ cudaError_t make_tmap_2b(CUtensorMap *m, const void *base, uint64_t rows, uint64
 // box_rows x 128 boxes, 128-byte swizzle.
 cudaError_t make_tmap_codes(CUtensorMap *m, const int8_t *base, uint64_t rows, uint64_t cols,
                             uint64_t pitch, uint32_t box_rows);
+// The same of fp16, pitch in elements: box_rows x 64 boxes, 128-byte swizzle.
+cudaError_t make_tmap_half(CUtensorMap *m, const void *base, uint64_t rows, uint64_t cols,
+                           uint64_t pitch, uint32_t box_rows);
 cudaError_t make_tmap_bf16(CUtensorMap *m, const void *base, uint64_t rows, uint64_t cols,
                            uint32_t box_rows, uint32_t box_cols = 64);
 cudaError_t make_tmap_f16(CUtensorMap *m, const void *base, uint64_t rows, uint64_t cols,

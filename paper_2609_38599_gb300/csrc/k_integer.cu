@@ -17,7 +17,6 @@ namespace {
 using namespace rows;
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kFew = 8;                     // most tokens of this form
 
 // Sums of V values over the lanes of a warp: value i ends in lane 32 / V i.
 template <int V>
@@ -63,7 +62,7 @@ __global__ void __launch_bounds__(kThreads) few_tokens_kernel(ProductArgs a) {
     for (int c = tid; c < chunks; c += kThreads) {
         uint4 x[M];
 #pragma unroll
-        for (int m = 0; m < M; ++m) x[m] = load_codes<VEC>(a.X + (size_t)min(m, a.n - 1) * a.ldx, 16 * c, a.din);
+        for (int m = 0; m < M; ++m) x[m] = load_codes<VEC>(static_cast<const int8_t *>(a.X) + (size_t)min(m, a.n - 1) * a.ldx, 16 * c, a.din);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const uint4 wr = w[r];
@@ -126,7 +125,7 @@ cudaError_t launch_product(const ProductArgs &a, int *failed, cudaStream_t s, bo
     if (a.n == 1) return launch_few<1, 8>(a, s, pdl);
     if (a.n == 2) return launch_few<2, 8>(a, s, pdl);
     if (a.n <= 4) return launch_few<4, 4>(a, s, pdl);
-    if (a.n <= kFew) return launch_few<8, 4>(a, s, pdl);
+    if (a.n <= kFewTokens) return launch_few<8, 4>(a, s, pdl);
     return launch_tc_integer(a, failed, s, pdl);
 }
 
@@ -156,10 +155,10 @@ jarq_status run_product(const ProductArgs &a, cudaStream_t st, bool pdl) {
     return JARQ_OK;
 }
 
-jarq_status run_quantize(const void *X, jarq_dtype dtype, int n, int d, int64_t ldx, int8_t *Q,
+jarq_status run_quantize(const void *X, jarq_dtype dtype, int n, int d, int64_t ldx, void *Q, bool half,
                          int64_t ldq, float *scale, cudaStream_t st) {
     ProfScope ps("quantize_rows", st);
-    const cudaError_t e = launch_quantize_rows(X, dtype, n, d, ldx, Q, ldq, scale, st);
+    const cudaError_t e = launch_quantize_rows(X, dtype, n, d, ldx, Q, half, ldq, scale, st);
     ps.done();
     count_launches(1);
     if (e != cudaSuccess) {
@@ -169,9 +168,10 @@ jarq_status run_quantize(const void *X, jarq_dtype dtype, int n, int d, int64_t 
     return JARQ_OK;
 }
 
-// Codes of a linear layer's activations in its workspace: rows on 16-byte
-// boundaries, then the scales.
+// A linear layer's workspace: its activations' integers, int8 for a few tokens
+// and fp16 for more, rows on 16-byte boundaries; then the scales.
 int64_t code_pitch(int din) { return round_up(din, 16); }
+size_t code_bytes(int n, int din) { return (size_t)n * code_pitch(din) * (n <= kFewTokens ? 1 : 2); }
 
 }  // namespace
 }  // namespace jarq
@@ -186,7 +186,7 @@ jarq_status jarq_quantize_rows(const void *X, jarq_dtype dtype, int n, int d, in
     if (n == 0) return JARQ_OK;
     if (!X || !Q || !scale || !on_device(X) || !on_device(Q) || !on_device(scale)) return JARQ_ERR_ARG;
     if ((uintptr_t)X & (size_of(dtype) - 1) || (uintptr_t)scale & 3) return JARQ_ERR_ARG;
-    return run_quantize(X, dtype, n, d, ldx, Q, ldq, scale, (cudaStream_t)stream);
+    return run_quantize(X, dtype, n, d, ldx, Q, false, ldq, scale, (cudaStream_t)stream);
 }
 
 jarq_status jarq_integer_product(const int8_t *X, int64_t ldx, const float *xs, const int8_t *C,
@@ -199,13 +199,13 @@ jarq_status jarq_integer_product(const int8_t *X, int64_t ldx, const float *xs, 
     if (!X || !xs || !on_device(X) || !on_device(xs) || (uintptr_t)xs & 3) return JARQ_ERR_ARG;
     if (const jarq_status late = async_failure()) return late;
     return run_product({X, C, xs, ws, bias, Y, ldx, ldc, ldy, n, dout, din, group_size,
-                        group_size ? din / group_size : 1, dtype},
+                        group_size ? din / group_size : 1, dtype, false},
                        (cudaStream_t)stream, false);
 }
 
 size_t jarq_integer_linear_workspace(int n, int din) {
     if (n < 0 || din < 1) return 0;
-    return (size_t)n * (size_t)(code_pitch(din) + (int64_t)sizeof(float));
+    return code_bytes(n, din) + (size_t)n * sizeof(float);
 }
 
 jarq_status jarq_integer_linear(const void *X, jarq_dtype xdtype, int64_t ldx, const int8_t *C,
@@ -222,13 +222,13 @@ jarq_status jarq_integer_linear(const void *X, jarq_dtype xdtype, int64_t ldx, c
     if (const jarq_status late = async_failure()) return late;
     cudaStream_t st = (cudaStream_t)stream;
     const int64_t ldq = code_pitch(din);
-    int8_t *q = static_cast<int8_t *>(workspace);
-    float *xs = reinterpret_cast<float *>(q + (size_t)n * ldq);
-    const jarq_status e = run_quantize(X, xdtype, n, din, ldx, q, ldq, xs, st);
+    const bool half = n > kFewTokens;
+    float *xs = reinterpret_cast<float *>(static_cast<char *>(workspace) + code_bytes(n, din));
+    const jarq_status e = run_quantize(X, xdtype, n, din, ldx, workspace, half, ldq, xs, st);
     if (e != JARQ_OK) return e;
     // the product starts under the quantization and reads weights meanwhile
-    return run_product({q, C, xs, ws, bias, Y, ldq, ldc, ldy, n, dout, din, group_size,
-                        group_size ? din / group_size : 1, ydtype},
+    return run_product({workspace, C, xs, ws, bias, Y, ldq, ldc, ldy, n, dout, din, group_size,
+                        group_size ? din / group_size : 1, ydtype, half},
                        st, true);
 }
 

@@ -11,7 +11,8 @@
 // has one channel and its group's scale in a register; for more than 64 tokens a
 // pair of CTAs (cta_group::2) has 256 channels, and each CTA converts its own 128
 // and half of the tokens.  Per 128 of K the channels go to TMEM as the A operand
-// and the tokens to shared memory as the B operand.  (With both operands in shared
+// and the tokens to shared memory as the B operand; the linear layer's own tokens
+// are quantized to integers in fp16 and need no conversion here.  (With both operands in shared
 // memory 192 bytes are moved there per cycle of the MMAs, and the kernel took 1.6
 // times as long; with A in TMEM it is 128.)  Tiles of 256 tokens are two
 // accumulators of 128, one read while the other's MMAs run; smaller tiles
@@ -22,8 +23,10 @@
 //                 converters it doubled the time, by one warp it set the pace.)
 //   warp 1        TMEM allocation
 //   warp 2        TMA producer: codes as they are into a ring of their own
+//   warp 3        TMA producer of tokens that are fp16
 //   warps 4..7    convert channels: a thread has one channel's row
-//   warps 8..11   convert tokens, and half of the channels' K where tokens are few
+//   warps 8..11   convert tokens, and half of the channels' K where tokens are few;
+//                 with fp16 tokens, every other stage's channels
 //   warps 12..19  drain: lane quarter w % 4, half of the columns
 //   warps 20..27  only where rows are not on 16-byte boundaries: fill the ring in
 //                 the producer's place
@@ -44,7 +47,6 @@ constexpr int kStepK = 128;                   // K of a stage: two atoms of 64
 constexpr int kExact = 16;                    // atoms (1024 of K) with an exact sum
 constexpr int kStages = 4;
 constexpr int kMostParts = 4;                  // of K, over a cluster
-constexpr int kRelays = 3;                    // warps 0, 1 and 3 of the odd CTA
 constexpr int kColsA = 64;                    // TMEM columns of a stage's channels (two fp16 each)
 constexpr int kTmem = 512;                    // two accumulators of up to 128, then kStages kColsA
 
@@ -59,14 +61,22 @@ __host__ __device__ constexpr int own_tokens(int nt) { return nt / ctas(nt); }
 // a stage of tokens x 128 of K, fp16
 __host__ __device__ constexpr int stage_bytes(int nt) { return own_tokens(nt) * kStepK * 2; }
 // the ring of codes as they are: 128 channels and the tokens x 128 of K
-__host__ __device__ constexpr int raw_bytes(int nt) { return (128 + own_tokens(nt)) * kStepK; }
-__host__ __device__ constexpr int raw_stages(int nt) { return nt == 256 ? 3 : nt == 32 ? 9 : 6; }
-__host__ __device__ constexpr int ring_bytes(int nt) { return kStages * stage_bytes(nt) + raw_stages(nt) * raw_bytes(nt); }
-__host__ __device__ constexpr int smem_bytes(int nt) { return 1024 + ring_bytes(nt) + 512; }
-static_assert(8 * (2 * kStages + 2 * kAccs + 2 * raw_stages(32) + 1) + 8 <= 512, "room for the barriers");
-static_assert(smem_bytes(256) <= 227 * 1024 && smem_bytes(128) <= 227 * 1024 && smem_bytes(64) <= 227 * 1024 &&
-                  smem_bytes(32) <= 227 * 1024,
-              "the rings must fit an SM's shared memory");
+// (the channels alone where tokens are fp16)
+__host__ __device__ constexpr int raw_bytes(int nt, bool half) { return (128 + (half ? 0 : own_tokens(nt))) * kStepK; }
+__host__ __device__ constexpr int raw_stages(int nt, bool half) {
+    return half ? (nt == 256 ? 6 : nt == 32 ? 11 : 9) : nt == 256 ? 3 : nt == 32 ? 9 : 6;
+}
+__host__ __device__ constexpr int ring_bytes(int nt, bool half) {
+    return kStages * stage_bytes(nt) + raw_stages(nt, half) * raw_bytes(nt, half);
+}
+__host__ __device__ constexpr int smem_bytes(int nt, bool half) { return 1024 + ring_bytes(nt, half) + 512; }
+constexpr bool rings_fit(bool half) {
+    for (int nt : {32, 64, 128, 256})
+        if (smem_bytes(nt, half) > 227 * 1024 || 8 * (2 * kStages + 2 * kAccs + 2 * raw_stages(nt, half) + 1) + 8 > 512)
+            return false;
+    return true;
+}
+static_assert(rings_fit(false) && rings_fit(true), "rings and barriers must fit an SM's shared memory");
 
 // Registers a thread of each role where the drain needs more than an even
 // share.  Their sum may not pass what the block is launched with, or the roles
@@ -200,25 +210,28 @@ struct Slot {
     }
 };
 
-// NT: tokens of a tile.  GROUPS: group scales.  VEC: rows on 16-byte boundaries.
-template <int NT, bool GROUPS, bool VEC>
+// NT: tokens of a tile.  GROUPS: group scales.  VEC: rows of codes on 16-byte
+// boundaries.  HALF: tokens are integers in fp16, rows on 16-byte boundaries.
+template <int NT, bool GROUPS, bool VEC, bool HALF>
 __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
     tc_integer_kernel(const __grid_constant__ CUtensorMap mapC, const __grid_constant__ CUtensorMap mapX, ProductArgs a,
                       int split, int *failed) {
     using Reg = Registers<VEC>;
-    constexpr int kStage = stage_bytes(NT), kRaws = raw_stages(NT), kRaw = raw_bytes(NT);
+    constexpr int kStage = stage_bytes(NT), kRaws = raw_stages(NT, HALF), kRaw = raw_bytes(NT, HALF);
     constexpr int kAcc = acc_cols(NT), kParts = acc_parts(NT);
     constexpr bool kPair = ctas(NT) == 2;
     constexpr int kChannels = 128 * ctas(NT);   // of a tile
     constexpr int kRowsB = kAcc / ctas(NT);     // this CTA's tokens of an accumulator
     constexpr int kAtomB = kRowsB * 128, kHalfB = 2 * kAtomB;
     constexpr int kCols = kAcc / 2;             // columns of a drain warp in an accumulator
-    constexpr bool kShare = !kPair;             // the tokens' converters have time for channels
+    constexpr bool kShare = !kPair && !HALF;    // the tokens' converters have time for channels
+    // warps that convert a stage, and those of a pair's odd CTA that pass it on
+    constexpr int kConverters = HALF ? kConvert / 64 : kConvert / 32, kRelays = HALF ? 2 : 3;
     constexpr int kBars = 2 * kStages + 2 * kAccs + 2 * kRaws + 1;
     constexpr uint32_t kIdesc = tc::idesc_f16_f32(kChannels, kAcc);
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    uint64_t *bars = (uint64_t *)(smem + ring_bytes(NT));
+    uint64_t *bars = (uint64_t *)(smem + ring_bytes(NT, HALF));
     uint32_t *tmem_slot = (uint32_t *)(bars + kBars);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -244,7 +257,8 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
-            tc::mbar_init(full(s), kConvert / 32 + (kPair && rank == 0));   // own converters; the odd CTA's relay
+            // own converters; in the issuer's CTA the other's relay, and the bytes of both CTAs' fp16 tokens
+            tc::mbar_init(full(s), kConverters + (rank == 0 ? (kPair ? 1 : 0) + (HALF ? 1 : 0) : 0));
             tc::mbar_init(empty(s), 1);
         }
         for (int b = 0; b < kAccs; ++b) {
@@ -253,7 +267,7 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
         }
         for (int s = 0; s < kRaws; ++s) {
             tc::mbar_init(raw_full(s), VEC ? 1 : kFill / 32);
-            tc::mbar_init(raw_empty(s), kConvert / 32);
+            tc::mbar_init(raw_empty(s), kConverters);
         }
         tc::mbar_init(closing, 1);
         *abort_flag = 0;
@@ -346,7 +360,7 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
                     tc::mma_commit(closing);
             }
             if (!tc::mbar_wait(closing, 0) || !ok) *abort_flag = 1;
-        } else if (kPair && warp != 2 && rank == 1) {
+        } else if (kPair && rank == 1 && (warp < 2 || (warp == 3 && !HALF))) {
             // ---------------- relays of the odd CTA: its stages are full, in turn
             const uint32_t full0 = tc::map_rank(full(0), even);
             const int me = warp == 3 ? 2 : warp;
@@ -367,7 +381,7 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
             if (!ok) *abort_flag = 1;
         } else if (VEC && warp == 2) {
             // ---------------- producer of the raw ring
-            tc::pdl_wait();
+            if (!HALF) tc::pdl_wait();
             bool ok = true;
             Slot<kRaws> out(1);
             int filled = 0;
@@ -381,9 +395,11 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
                         const int k = (step0 + step) * kStepK;
                         tc::mbar_expect_tx(bar, kRaw);
                         tc::tma_load_2d(at, &mapC, bar, k, o);
+                        if (!HALF) {
 #pragma unroll
-                        for (int h = 0; h < kParts; ++h)
-                            tc::tma_load_2d(at + (128 + h * kRowsB) * kStepK, &mapX, bar, k, tk + h * kAcc);
+                            for (int h = 0; h < kParts; ++h)
+                                tc::tma_load_2d(at + (128 + h * kRowsB) * kStepK, &mapX, bar, k, tk + h * kAcc);
+                        }
                     }
                     __syncwarp();
                     ++filled;
@@ -396,15 +412,53 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
                 *abort_flag = 1;
                 tc::abandon_ring(raw_full(0), kRaws, filled, true);
             }
+        } else if (HALF && warp == 3) {
+            // ---------------- producer of the tokens, onto the issuer's barriers
+            tc::pdl_wait();
+            const uint32_t full0 = kPair ? tc::map_rank(full(0), even) : full(0);
+            bool ok = true;
+            Slot<kStages> out(1);
+            int filled = 0;
+            for (int tile = cluster; tile < ntiles && ok; tile += nclusters) {
+                const int tk = tile / mt * NT + kRowsB * rank;
+                for (int step = 0; step < nsteps; ++step, out.next()) {
+                    ok = tc::mbar_wait(empty(out.s), out.phase);
+                    if (!ok) break;
+                    if (tc::elect_one()) {
+                        const uint32_t bar = full0 + 8 * out.s;
+                        const int k = (step0 + step) * kStepK;
+                        if (rank == 0) tc::mbar_expect_tx(bar, ctas(NT) * kStage);
+#pragma unroll
+                        for (int h = 0; h < kParts; ++h)
+#pragma unroll
+                            for (int at = 0; at < 2; ++at) {
+                                const uint32_t dst = ring + out.s * kStage + h * kHalfB + at * kAtomB;
+                                if (kPair)
+                                    tc::tma_load_2d_pair(dst, &mapX, bar, k + 64 * at, tk + h * kAcc);
+                                else
+                                    tc::tma_load_2d(dst, &mapX, bar, k + 64 * at, tk + h * kAcc);
+                            }
+                    }
+                    __syncwarp();
+                    ++filled;
+                }
+            }
+            for (int n = max(0, filled - kStages); n < filled && ok; ++n)
+                ok = tc::mbar_wait(empty(n % kStages), (n / kStages) & 1);
+            if (!ok) {
+                *abort_flag = 1;
+                tc::abandon_ring(full(0), kStages, filled, rank == 0);
+            }
         }
-    } else if (warp < 8) {
+    } else if (warp < 8 || (HALF && warp < 12)) {
         if constexpr (splits_registers(NT, VEC)) registers_down<Reg::convert>();
         // ---------------- channels: raw ring -> fp16 -> TMEM
-        bool ok = true;
+        bool ok = true, turn = warp >= 8;
         Slot<kRaws> in(0);
         Slot<kStages> out(1);
         for (int tile = cluster; tile < ntiles && ok; tile += nclusters)
             for (int step = 0; step < nsteps; ++step, in.next(), out.next()) {
+                if (HALF && (turn = !turn, !turn)) continue;     // the other four warps' stage
                 ok = tc::mbar_wait(raw_full(in.s), in.phase);
                 ok = tc::mbar_wait(empty(out.s), out.phase) && ok;
                 ok = __all_sync(0xffffffffu, ok);
@@ -566,8 +620,8 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
     } else {
         if constexpr (splits_registers(NT, VEC)) registers_down<Reg::fill>();
         // ---------------- rows that TMA cannot read, into the raw ring
-        tc::pdl_wait();
-        constexpr int kU = (128 + own_tokens(NT) + 31) / 32;     // 32 rows at a time: channels, tokens
+        if (!HALF) tc::pdl_wait();
+        constexpr int kRows = 128 + (HALF ? 0 : own_tokens(NT)), kU = (kRows + 31) / 32;   // 32 rows at a time: channels, tokens
         constexpr int kBatch = 4;
         const int t = threadIdx.x - 640, c = t & 7, r0 = t >> 3;
         const uint32_t to = raws + (uint32_t)(r0 * kStepK + ((c ^ (r0 & 7)) << 4));
@@ -579,7 +633,7 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
             auto row_of = [&](int i) -> const int8_t * {
                 if (i < 4) return o + 32 * i < a.dout ? a.C + (size_t)(o + 32 * i) * a.ldc : nullptr;
                 const int j = r0 + 32 * (i - 4), r = tk + j / kRowsB * kAcc + j % kRowsB;
-                return j < own_tokens(NT) && r < a.n ? a.X + (size_t)r * a.ldx : nullptr;
+                return j < own_tokens(NT) && r < a.n ? static_cast<const int8_t *>(a.X) + (size_t)r * a.ldx : nullptr;
             };
             for (int step = 0; step < nsteps; ++step, out.next()) {
                 const int k = (step0 + step) * kStepK + c * 16;
@@ -615,7 +669,7 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
                     }
 #pragma unroll
                     for (int j = 0; j < kBatch; ++j)
-                        if (r0 + 32 * (i0 + j) < 128 + own_tokens(NT)) store_shared(dst + (i0 + j) * 32 * kStepK, v[j]);
+                        if (r0 + 32 * (i0 + j) < kRows) store_shared(dst + (i0 + j) * 32 * kStepK, v[j]);
                 }
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(raw_full(out.s));
@@ -682,26 +736,28 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
     }
 }
 
-template <int NT, bool GROUPS, bool VEC>
+template <int NT, bool GROUPS, bool VEC, bool HALF>
 cudaError_t launch(const ProductArgs &a, int split, int *failed, cudaStream_t s, bool pdl) {
     static std::atomic<unsigned long long> done;
-    auto *kernel = tc_integer_kernel<NT, GROUPS, VEC>;
-    cudaError_t e = set_max_dynamic_smem((const void *)kernel, smem_bytes(NT), done);
+    auto *kernel = tc_integer_kernel<NT, GROUPS, VEC, HALF>;
+    cudaError_t e = set_max_dynamic_smem((const void *)kernel, smem_bytes(NT, HALF), done);
     if (e != cudaSuccess) return e;
     CUtensorMap mapC = {}, mapX = {};
-    if (VEC) {
-        auto pitch = [](int64_t ld, int rows) { return (uint64_t)(rows > 1 ? ld : (ld + 15) / 16 * 16); };
-        e = make_tmap_codes(&mapC, a.C, a.dout, a.din, pitch(a.ldc, a.dout), 128);
-        if (e == cudaSuccess) e = make_tmap_codes(&mapX, a.X, a.n, a.din, pitch(a.ldx, a.n), acc_cols(NT) / ctas(NT));
-        if (e != cudaSuccess) return e;
-    }
+    auto pitch = [](int64_t ld, int rows) { return (uint64_t)(rows > 1 ? ld : (ld + 15) / 16 * 16); };
+    constexpr int rows = acc_cols(NT) / ctas(NT);
+    if (VEC) e = make_tmap_codes(&mapC, a.C, a.dout, a.din, pitch(a.ldc, a.dout), 128);
+    if (e == cudaSuccess && HALF)
+        e = make_tmap_half(&mapX, a.X, a.n, a.din, pitch(a.ldx, a.n), rows);
+    else if (e == cudaSuccess && VEC)
+        e = make_tmap_codes(&mapX, static_cast<const int8_t *>(a.X), a.n, a.din, pitch(a.ldx, a.n), rows);
+    if (e != cudaSuccess) return e;
     const int64_t tiles = (int64_t)((a.dout + 128 * ctas(NT) - 1) / (128 * ctas(NT))) * ((a.n + NT - 1) / NT);
     const int64_t clusters = split > 1 ? tiles : std::min<int64_t>(tiles, num_sms() / ctas(NT));
     if (tiles > 0x3FFFFFFF / (2 * split)) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(clusters * ctas(NT) * split));
     cfg.blockDim = dim3(VEC ? kThreads : kAnyThreads);
-    cfg.dynamicSmemBytes = smem_bytes(NT);
+    cfg.dynamicSmemBytes = smem_bytes(NT, HALF);
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -714,13 +770,18 @@ cudaError_t launch(const ProductArgs &a, int split, int *failed, cudaStream_t s,
     return cudaLaunchKernelEx(&cfg, kernel, mapC, mapX, a, split, failed);
 }
 
+template <int NT, bool VEC, bool HALF>
+cudaError_t launch_scales(const ProductArgs &a, int split, int *failed, cudaStream_t s, bool pdl) {
+    return a.g ? launch<NT, true, VEC, HALF>(a, split, failed, s, pdl) : launch<NT, false, VEC, HALF>(a, split, failed, s, pdl);
+}
 template <int NT>
 cudaError_t launch_nt(const ProductArgs &a, int split, int *failed, cudaStream_t s, bool pdl) {
-    if (vector_rows(a))
-        return a.g ? launch<NT, true, true>(a, split, failed, s, pdl) : launch<NT, false, true>(a, split, failed, s, pdl);
-    // four more warps fill the ring: no registers left for 256 tokens
-    constexpr int any = NT == 256 ? 128 : NT;
-    return a.g ? launch<any, true, false>(a, split, failed, s, pdl) : launch<any, false, false>(a, split, failed, s, pdl);
+    constexpr int any = NT == 256 ? 128 : NT;       // eight more warps fill the ring: no registers left for 256 tokens
+    if (a.half)
+        return vector_codes(a) ? launch_scales<NT, true, true>(a, split, failed, s, pdl)
+                               : launch_scales<any, false, true>(a, split, failed, s, pdl);
+    return vector_rows(a) ? launch_scales<NT, true, false>(a, split, failed, s, pdl)
+                          : launch_scales<any, false, false>(a, split, failed, s, pdl);
 }
 
 }  // namespace
@@ -734,7 +795,7 @@ cudaError_t launch_tc_integer(const ProductArgs &a, int *failed, cudaStream_t s,
         int nt, step, tile;
     } kinds[] = {{32, 450, 4000}, {64, 550, 4000}, {128, 800, 5000}, {256, 1300, 7000}};
     constexpr int resident[] = {0, 152, 76, 48, 36, 0, 23, 0, 15};
-    const bool vec = vector_rows(a);
+    const bool vec = a.half ? vector_codes(a) : vector_rows(a);
     const int steps = (a.din + kStepK - 1) / kStepK, sms = num_sms();
     int nt = 0, split = 1;
     double best = 0;
