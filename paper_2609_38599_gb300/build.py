@@ -26,8 +26,10 @@ FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", 
 # Registers a thread that kernels with roles of different register counts must be
 # compiled for: the roles' sum would not fit a smaller block, and they would wait
 # for registers that never come.
-LAUNCH_REGISTERS = {"k_tc_integer.cu": (("tc_integer_kernelILi256E", 96), ("tc_integer_kernelILi128ELb0ELb0E", 72),
-                                        ("tc_integer_kernelILi128ELb1ELb0E", 72))}
+LAUNCH_REGISTERS = {"k_tc_integer.cu": tuple(
+    (f"tc_integer_kernelILi{nt}ELb{groups}ELb{vec}ELb{half}E", registers)
+    for nt, vec, half, registers in ((256, 1, 0, 96), (256, 1, 1, 128), (128, 0, 0, 72), (128, 0, 1, 72))
+    for groups in (0, 1))}
 
 
 def check_registers(src: str, ptxas_output: str) -> None:

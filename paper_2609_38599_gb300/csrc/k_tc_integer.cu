@@ -41,8 +41,7 @@ namespace {
 
 using namespace rows;
 
-constexpr int kThreads = 640, kAnyThreads = 896;   // rows on 16-byte boundaries; any rows
-constexpr int kConvert = 256, kDrain = 256, kFill = 256;
+constexpr int kDrain = 256, kFill = 256;
 constexpr int kStepK = 128;                   // K of a stage: two atoms of 64
 constexpr int kExact = 16;                    // atoms (1024 of K) with an exact sum
 constexpr int kStages = 4;
@@ -78,17 +77,21 @@ constexpr bool rings_fit(bool half) {
 }
 static_assert(rings_fit(false) && rings_fit(true), "rings and barriers must fit an SM's shared memory");
 
-// Registers a thread of each role where the drain needs more than an even
-// share.  Their sum may not pass what the block is launched with, or the roles
-// would wait for registers that never come: ptxas compiles for the `launch`
-// registers that the launch bounds leave, and the build checks its count.
-__host__ __device__ constexpr bool splits_registers(int nt, bool vec) { return nt == 256 || (nt == 128 && !vec); }
-template <bool VEC>
-struct Registers {
-    static constexpr int few = 48, convert = 56, drain = VEC ? 160 : 112, fill = 56;
-    static constexpr int launch = VEC ? 96 : 72;
-    static_assert(128 * few + kConvert * convert + kDrain * drain + (VEC ? 0 : kFill * fill) <=
-                      launch * (VEC ? kThreads : kAnyThreads),
+// A block's threads, and registers a thread of each role where the drain needs
+// more than an even share.  The roles' sum may not pass what the block is launched
+// with, or they would wait for registers that never come: ptxas compiles for the
+// `launch` registers that the launch bounds leave, and the build checks its count.
+template <int NT, bool VEC, bool HALF>
+struct Block {
+    // one stage of fp16 tokens takes four converting warps 600 of the 1024 cycles of
+    // its MMAs at 256 tokens, and the drain can hold a whole part besides its sums
+    static constexpr bool lean = NT == 256 && HALF;
+    static constexpr int convert = lean ? 128 : 256;
+    static constexpr int threads = 128 + convert + kDrain + (VEC ? 0 : kFill);
+    static constexpr bool splits = NT == 256 || (NT == 128 && !VEC);
+    static constexpr int launch = lean ? 128 : VEC ? 96 : 72;
+    static constexpr int few = 48, conv = lean ? 64 : 56, drain = lean ? 200 : VEC ? 160 : 112, fill = 56;
+    static_assert(!splits || 128 * few + convert * conv + kDrain * drain + (VEC ? 0 : kFill * fill) <= launch * threads,
                   "the roles' registers must fit the block's");
 };
 
@@ -213,10 +216,11 @@ struct Slot {
 // NT: tokens of a tile.  GROUPS: group scales.  VEC: rows of codes on 16-byte
 // boundaries.  HALF: tokens are integers in fp16, rows on 16-byte boundaries.
 template <int NT, bool GROUPS, bool VEC, bool HALF>
-__global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
+__global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
     tc_integer_kernel(const __grid_constant__ CUtensorMap mapC, const __grid_constant__ CUtensorMap mapX, ProductArgs a,
                       int split, int *failed) {
-    using Reg = Registers<VEC>;
+    using B = Block<NT, VEC, HALF>;
+    constexpr int kDrain0 = 4 + B::convert / 32, kFill0 = kDrain0 + kDrain / 32;   // first warps
     constexpr int kStage = stage_bytes(NT), kRaws = raw_stages(NT, HALF), kRaw = raw_bytes(NT, HALF);
     constexpr int kAcc = acc_cols(NT), kParts = acc_parts(NT);
     constexpr bool kPair = ctas(NT) == 2;
@@ -226,7 +230,7 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
     constexpr int kCols = kAcc / 2;             // columns of a drain warp in an accumulator
     constexpr bool kShare = !kPair && !HALF;    // the tokens' converters have time for channels
     // warps that convert a stage, and those of a pair's odd CTA that pass it on
-    constexpr int kConverters = HALF ? kConvert / 64 : kConvert / 32, kRelays = HALF ? 2 : 3;
+    constexpr int kConverters = HALF ? 4 : B::convert / 32, kRelays = HALF ? 2 : 3;
     constexpr int kBars = 2 * kStages + 2 * kAccs + 2 * kRaws + 1;
     constexpr uint32_t kIdesc = tc::idesc_f16_f32(kChannels, kAcc);
     extern __shared__ uint8_t smem_raw[];
@@ -289,7 +293,7 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
     const uint32_t tmem = *tmem_slot, tmem_a = tmem + kAccs * 128;
 
     if (warp < 4) {
-        if constexpr (splits_registers(NT, VEC)) registers_down<Reg::few>();
+        if constexpr (B::splits) registers_down<B::few>();
         if (warp == 0 && rank == 0) {
             // ---------------- MMA issuer of the pair
             bool ok = true;
@@ -450,15 +454,15 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
                 tc::abandon_ring(full(0), kStages, filled, rank == 0);
             }
         }
-    } else if (warp < 8 || (HALF && warp < 12)) {
-        if constexpr (splits_registers(NT, VEC)) registers_down<Reg::convert>();
+    } else if (warp < 8 || (HALF && warp < kDrain0)) {
+        if constexpr (B::splits) registers_down<B::conv>();
         // ---------------- channels: raw ring -> fp16 -> TMEM
         bool ok = true, turn = warp >= 8;
         Slot<kRaws> in(0);
         Slot<kStages> out(1);
         for (int tile = cluster; tile < ntiles && ok; tile += nclusters)
             for (int step = 0; step < nsteps; ++step, in.next(), out.next()) {
-                if (HALF && (turn = !turn, !turn)) continue;     // the other four warps' stage
+                if (HALF && B::convert == 256 && (turn = !turn, !turn)) continue;     // the other four warps' stage
                 ok = tc::mbar_wait(raw_full(in.s), in.phase);
                 ok = tc::mbar_wait(empty(out.s), out.phase) && ok;
                 ok = __all_sync(0xffffffffu, ok);
@@ -474,8 +478,8 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
                 }
             }
         if (!ok) *abort_flag = 1;
-    } else if (warp < 12) {
-        if constexpr (splits_registers(NT, VEC)) registers_down<Reg::convert>();
+    } else if (warp < kDrain0) {
+        if constexpr (B::splits) registers_down<B::conv>();
         // ---------------- tokens: raw ring -> fp16 -> K-major tiles, 128-byte swizzle
         constexpr int kU = own_tokens(NT) / 16;              // 16 rows at a time
         constexpr int kBatch = kU < 4 ? kU : 4;              // loads in flight
@@ -529,11 +533,11 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
                 }
             }
         if (!ok) *abort_flag = 1;
-    } else if (warp < 20) {
-        if constexpr (splits_registers(NT, VEC)) registers_up<Reg::drain>();
+    } else if (warp < kFill0) {
+        if constexpr (B::splits) registers_up<B::drain>();
         // ---------------- drain
         tc::pdl_wait();                                      // the tokens' scales
-        const int w = warp - 12, q = w & 3, col0 = (w >> 2) * kCols;
+        const int w = warp - kDrain0, q = w & 3, col0 = (w >> 2) * kCols;
         const int lrow = 32 * q + lane;
         const uint32_t released = tc::map_rank(aempty(0), even);
         const uint32_t taddr = tmem + ((uint32_t)(32 * q) << 16) + col0;
@@ -557,13 +561,21 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
                     if (!ok) break;
                     tc::tc_fence_after();
                     const uint32_t at = taddr + b * kAcc;
-                    uint32_t v[2][16];
-                    tc::tmem_ld16(at, v[0]);
+                    // the accumulator is handed back once it is in registers: at
+                    // once where they allow, else with its last 16 columns
+                    constexpr int kHeld = B::lean ? kCols : 16;
+                    uint32_t v[kHeld < kCols ? 2 : 1][kHeld];
+                    auto load = [&](int cc) {
 #pragma unroll
-                    for (int cc = 0; cc < kCols; cc += 16) {
+                        for (int i = 0; i < kHeld; i += 16)
+                            tc::tmem_ld16(at + cc + i, *reinterpret_cast<uint32_t(*)[16]>(&v[cc / kHeld & (kHeld < kCols)][i]));
+                    };
+                    load(0);
+#pragma unroll
+                    for (int cc = 0; cc < kCols; cc += kHeld) {
                         tc::tmem_wait_ld();
-                        if (cc + 16 < kCols) {
-                            tc::tmem_ld16(at + cc + 16, v[(cc / 16 + 1) & 1]);
+                        if (cc + kHeld < kCols) {
+                            load(cc + kHeld);
                         } else {
                             tc::tc_fence_before();
                             __syncwarp();
@@ -574,9 +586,9 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
                                     tc::mbar_arrive(aempty(b));
                             }
                         }
-                        uint32_t(&x)[16] = v[(cc / 16) & 1];
+                        uint32_t *x = v[cc / kHeld & (kHeld < kCols)];
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
+                        for (int e = 0; e < kHeld; ++e) {
                             uint32_t &s = acc[h][cc + e];
                             if (GROUPS)
                                 s = __float_as_uint(fmaf(__uint_as_float(x[e]), wsc, __uint_as_float(s)));
@@ -618,12 +630,12 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
         }
         if (!ok) *abort_flag = 1;
     } else {
-        if constexpr (splits_registers(NT, VEC)) registers_down<Reg::fill>();
+        if constexpr (B::splits) registers_down<B::fill>();
         // ---------------- rows that TMA cannot read, into the raw ring
         if (!HALF) tc::pdl_wait();
         constexpr int kRows = 128 + (HALF ? 0 : own_tokens(NT)), kU = (kRows + 31) / 32;   // 32 rows at a time: channels, tokens
         constexpr int kBatch = 4;
-        const int t = threadIdx.x - 640, c = t & 7, r0 = t >> 3;
+        const int t = threadIdx.x - 32 * kFill0, c = t & 7, r0 = t >> 3;
         const uint32_t to = raws + (uint32_t)(r0 * kStepK + ((c ^ (r0 & 7)) << 4));
         bool ok = true;
         Slot<kRaws> out(1);
@@ -680,8 +692,8 @@ __global__ void __launch_bounds__(VEC ? kThreads : kAnyThreads, 1)
     if (split > 1) {
         // join: part `part` of K finishes columns part cols .. of its 128 channels
         cluster_barrier();
-        if (warp >= 12 && warp < 20 && cluster < ntiles) {
-            const int t = threadIdx.x - 384, lrow = t & 127, half = t >> 7;
+        if (warp >= kDrain0 && warp < kFill0 && cluster < ntiles) {
+            const int t = threadIdx.x - 32 * kDrain0, lrow = t & 127, half = t >> 7;
             const int o = cluster % mt * kChannels + 128 * rank + lrow, t0 = cluster / mt * NT;
             const int cols = (NT + split - 1) / split;       // columns past NT are skipped
             const float bias = a.bias && o < a.dout ? a.bias[o] : 0.f, wch = !GROUPS && o < a.dout ? a.ws[o] : 1.f;
@@ -756,7 +768,7 @@ cudaError_t launch(const ProductArgs &a, int split, int *failed, cudaStream_t s,
     if (tiles > 0x3FFFFFFF / (2 * split)) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(clusters * ctas(NT) * split));
-    cfg.blockDim = dim3(VEC ? kThreads : kAnyThreads);
+    cfg.blockDim = dim3(Block<NT, VEC, HALF>::threads);
     cfg.dynamicSmemBytes = smem_bytes(NT, HALF);
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
