@@ -610,20 +610,24 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
                                      : "memory");
                 break;                                       // joined below: one tile a cluster
             }
+            // the tokens' scales, a lane a column, shared by shuffles: a load of
+            // each beside the stores took 230 cycles a column
             const float wch = GROUPS ? 1.f : wp[0], bias = a.bias && live ? a.bias[o] : 0.f;
-            if (live) {
+#pragma unroll
+            for (int h = 0; h < kParts; ++h) {
+                const int tk = t0 + h * kAcc + col0;
+                constexpr int kLanes = (kCols + 31) / 32;
+                float xs[kLanes];
+#pragma unroll
+                for (int i = 0; i < kLanes; ++i) xs[i] = tk + 32 * i + lane < a.n ? a.xs[tk + 32 * i + lane] : 0.f;
                 with_type_device(a.dtype, [&](auto type) {
                     using T = decltype(type);
+                    T *y = static_cast<T *>(a.Y) + (size_t)tk * a.ldy + o;
 #pragma unroll
-                    for (int h = 0; h < kParts; ++h) {
-                        const int tk = t0 + h * kAcc + col0;
-                        T *y = static_cast<T *>(a.Y) + (size_t)tk * a.ldy + o;
-#pragma unroll
-                        for (int e = 0; e < kCols; ++e)
-                            if (tk + e < a.n) {
-                                const float v = GROUPS ? __uint_as_float(acc[h][e]) : (float)(int)acc[h][e] * wch;
-                                y[(size_t)e * a.ldy] = from_float<T>(fmaf(v, a.xs[tk + e], bias));
-                            }
+                    for (int e = 0; e < kCols; ++e) {
+                        const float x = __shfl_sync(0xffffffffu, xs[e / 32], e % 32);
+                        const float v = GROUPS ? __uint_as_float(acc[h][e]) : (float)(int)acc[h][e] * wch;
+                        if (live && tk + e < a.n) y[(size_t)e * a.ldy] = from_float<T>(fmaf(v, x, bias));
                     }
                 });
             }
