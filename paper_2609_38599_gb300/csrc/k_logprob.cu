@@ -4,28 +4,35 @@
 // Forward, one pass over a row's logits x: every thread keeps its own maximum m
 // and the sums s = sum e^(x - m), u = sum e^(x - m) (x - m), rescaled when m
 // grows; joined over threads they give lse = m + ln s, logprob = (x - m) - ln s
-// and entropy = ln s - u / s (no difference of large numbers).
+// and entropy = ln s - u / s (no difference of large numbers).  Each thread has
+// four 16-byte units in flight.
 //
-// Alternatives.  A thread also remembers the 16-byte unit in which its maximum
-// stands, so (maximum, unit) orders the threads without ties, in the order of
-// (logit falling, token rising).  The k largest of these pairs are k different
-// elements, and every element of another thread comes after all of them:
-// the k largest elements of the row lie in the k threads with the largest
-// pairs.  Only those threads' elements, about k / 256 of the row, are read a
-// second time (from L2).
+// Alternatives.  Lower bounds of a row's k-th largest logit: the k-th largest of the
+// 32 thread maxima of any warp, and, with W warps, the least of all warps'
+// ceil(k / W)-th largest ones.  A thread also remembers the unit of its maximum and
+// the maximum of its other units.  The threads whose maximum reaches the larger
+// bound read that unit again and list its logits above the bound; the k-th largest
+// of the list is a bound close to the k-th largest logit itself, and only threads
+// whose second maximum reaches that one, hardly any, read their other units again
+// (from L2).  Where the list is too short for the logits above the bound (rows with
+// many equal logits), every warp keeps a sorted list of its own instead.
 #include <math.h>
 
+#include <algorithm>
+#include <type_traits>
+
 #include "rows.cuh"
+#include "tc_common.cuh"
 
 namespace jarq {
 namespace {
 
 using namespace rows;
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxTop = 32, kMaxTokens = 256;
 constexpr int kMaxSplit = 8;         // CTAs of a cluster that share a row
 constexpr int kAhead = 4;            // units of a thread in flight
+constexpr int kList = 512;           // candidates
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct ScoreArgs {
@@ -51,6 +58,11 @@ __device__ __forceinline__ float max_nan(float a, float b) {
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 // float32 as an integer in the same order (-0 as +0); 0 is below -inf
 __device__ __forceinline__ uint32_t ordered(float x) {
     const uint32_t b = __float_as_uint(x + 0.f);
@@ -71,11 +83,11 @@ struct Sums {
     float m, s, u;
     // the same sums with respect to M >= m
     __device__ void to(float M) {
-        if (m == neg_inf()) return;
-        if (m == M) return;
+        if (m == neg_inf() || m == M) return;
         const float d = fmaxf(m - M, -1e30f), f = exp2_fast(d * kLog2e);   // s d stays finite
         u = (u + s * d) * f;
         s *= f;
+        m = M;
     }
     __device__ void add(Sums o) {
         const float M = fmaxf(m, o.m);
@@ -87,20 +99,26 @@ struct Sums {
     }
 };
 
-__device__ __forceinline__ Sums shuffled(const Sums &a, int mask) {
-    return {__shfl_xor_sync(0xffffffffu, a.m, mask), __shfl_xor_sync(0xffffffffu, a.s, mask),
-            __shfl_xor_sync(0xffffffffu, a.u, mask)};
+// The sums of a warp's lanes, in every lane.
+__device__ __forceinline__ Sums warp_sums(Sums a) {
+    const float M = unordered(__reduce_max_sync(0xffffffffu, ordered(a.m)));
+    a.to(M);
+#pragma unroll
+    for (int i = 16; i > 0; i /= 2) {
+        a.s += __shfl_xor_sync(0xffffffffu, a.s, i);
+        a.u += __shfl_xor_sync(0xffffffffu, a.u, i);
+    }
+    return {M, a.s, a.u};
 }
 
 // Sorted over the warp's lanes, the largest in lane 0.
-__device__ __forceinline__ uint64_t warp_sorted(uint64_t key, int lane) {
+__device__ __forceinline__ uint32_t warp_sorted(uint32_t key, int lane) {
 #pragma unroll
     for (int k = 2; k <= 32; k *= 2)
 #pragma unroll
         for (int j = k / 2; j > 0; j /= 2) {
-            const uint64_t o = __shfl_xor_sync(0xffffffffu, key, j);
-            const bool larger = ((lane & j) == 0) == ((lane & k) == 0);
-            if ((o > key) == larger) key = o;
+            const uint32_t o = __shfl_xor_sync(0xffffffffu, key, j);
+            key = ((lane & j) == 0) == ((lane & k) == 0) ? max(key, o) : min(key, o);
         }
     return key;
 }
@@ -114,21 +132,26 @@ __device__ __forceinline__ int count_larger(const uint64_t *list, uint64_t key) 
     return c + (list[c] > key);
 }
 
-struct Shared {
-    uint64_t lists[kWarps][32];
-    uint64_t seg[kMaxTop], best[kMaxTop];
-    Sums sums[kWarps];
-    Sums total;
-};
-
-// Position of the calling thread's key, lists[warp][lane], among all lists.
-__device__ __forceinline__ int rank_of(const Shared &sh, uint64_t key, int warp, int lane) {
-    int r = lane;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w)
-        if (w != warp) r += count_larger(sh.lists[w], key);
-    return r;
+// `key` into a falling list held one a lane.
+__device__ __forceinline__ uint64_t inserted(uint64_t list, uint64_t key, int lane) {
+    const int pos = __popc(__ballot_sync(0xffffffffu, list > key));
+    const uint64_t up = __shfl_up_sync(0xffffffffu, list, 1);
+    return lane < pos ? list : lane == pos ? key : up;
 }
+
+template <int kThreads>
+struct Shared {
+    static constexpr int kWarps = kThreads / 32, kLists = kWarps > kMaxSplit ? kWarps : kMaxSplit;
+    union {
+        uint64_t list[kList];
+        uint64_t lists[kLists][32];
+    };
+    uint64_t best[kMaxTop];
+    Sums sums[kWarps], total;
+    uint32_t kth[kWarps], share[kWarps];    // of a warp's maxima: the k-th and the ceil(k / W)-th largest
+    uint32_t near;                          // the k-th largest of the list
+    int count;
+};
 
 // Address of a shared variable in CTA `rank` of the cluster.
 template <class V>
@@ -142,148 +165,266 @@ __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-template <class T, bool kTop>
-__global__ void __launch_bounds__(kThreads) token_logprobs_kernel(ScoreArgs a) {
-    constexpr int E = kUnit<T>;
-    __shared__ Shared sh;
+// A CTA's part of a row: units u0 .. u1 - 1, those of a thread kThreads apart, of
+// which lo .. lo + n - 1 lie in the row as a whole.
+template <class T, int kThreads>
+struct Part {
+    Row<T> row;
+    int u0, u1, lo, n;
+    __device__ Part(const T *x, int vocab, int split, int rank) : row(x, vocab) {
+        const int units = row.units(), per = (units + split - 1) / split;
+        u0 = min(units, rank * per);
+        u1 = min(units, u0 + per);
+        lo = u0 + (u0 < u1 && !row.whole(u0));
+        n = max(0, u1 - lo - (lo < u1 && !row.whole(u1 - 1)));
+    }
+    // a whole unit; elsewhere -inf, as if masked
+    __device__ uint4 load(int u) const {
+        constexpr uint32_t m = sizeof(T) == 4 ? 0xFF800000u : std::is_same_v<T, __half> ? 0xFC00FC00u : 0xFF80FF80u;
+        uint4 r = make_uint4(m, m, m, m);
+        if ((unsigned)(u - lo) < (unsigned)n) r = *reinterpret_cast<const uint4 *>(row.p + row.first(u));
+        return r;
+    }
+    // the first or last unit, if it is cut and this thread's
+    __device__ bool cut(int u) const {
+        return u0 < u1 && u >= u0 && u < u1 && !row.whole(u) && (u - u0) % kThreads == (int)threadIdx.x;
+    }
+};
+
+// A thread's largest logit with its unit, and the largest of its other units.
+struct Heads {
+    float first, second;
+    int unit;
+};
+
+// Ranks the listed candidates by counting; those below k go to sh.best, the k-th
+// is the new bound.
+template <int kThreads>
+__device__ __forceinline__ void rank_list(Shared<kThreads> &sh, int count, int k) {
+    for (int i = threadIdx.x; i < count; i += kThreads) {
+        const uint64_t key = sh.list[i];
+        int r = 0;
+        for (int j = 0; j < count; ++j) r += sh.list[j] > key;
+        if (r < k) sh.best[r] = key;
+        if (r == k - 1) sh.near = (uint32_t)(key >> 32);
+    }
+}
+
+// The k largest of a CTA's part into sh.best (0: none).  All threads; ends
+// without a barrier.
+template <class T, int kThreads>
+__device__ __forceinline__ void select_top(Shared<kThreads> &sh, const Part<T, kThreads> &part, const Heads &h, int k) {
+    constexpr int E = kUnit<T>, kWarps = kThreads / 32;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const T masked = from_float<T>(neg_inf());
+    uint32_t bound = max(__reduce_max_sync(0xffffffffu, sh.kth[lane % kWarps]),
+                         __reduce_min_sync(0xffffffffu, sh.share[lane % kWarps]));
+    auto list = [&](int u) {
+        float v[E];
+        unpack(part.row.load(u, masked), v, T());
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (v[e] > neg_inf() && ordered(v[e]) >= bound) {
+                const int at = atomicAdd(&sh.count, 1);
+                if (at < kList) sh.list[at] = key_of(v[e], part.row.first(u) + e);
+            }
+    };
+    if (h.first > neg_inf() && ordered(h.first) >= bound) list(h.unit);
+    if (tid == 0) sh.near = bound;              // fewer than k listed: the bound stays
+    __syncthreads();
+    int count = sh.count;
+    if (count <= kList) {
+        rank_list(sh, count, k);
+        __syncthreads();
+        bound = sh.near;
+        unsigned more = __ballot_sync(0xffffffffu, h.second > neg_inf() && ordered(h.second) >= bound);
+        if (!__syncthreads_or(more != 0)) return;
+        while (more) {
+            // the other units of a thread, 32 at a time
+            const int i = __ffs(more) - 1, skip = __shfl_sync(0xffffffffu, h.unit, i);
+            more &= more - 1;
+            for (int u = part.u0 + 32 * warp + i + lane * kThreads; u < part.u1; u += 32 * kThreads)
+                if (u != skip) list(u);
+            __syncwarp();
+        }
+        __syncthreads();
+        count = sh.count;
+        if (count <= kList) {
+            rank_list(sh, count, k);
+            return;
+        }
+    }
+    __syncthreads();
+    uint64_t best = 0;                      // the warp's largest so far, falling over the lanes
+    for (int b = part.u0 + 32 * warp; b < part.u1; b += kThreads) {
+        float v[E];
+        unpack(b + lane < part.u1 ? part.row.load(b + lane, masked) : part.load(-1), v, T());
+        const int f = part.row.first(b + lane);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const uint64_t c = v[e] > neg_inf() && ordered(v[e]) >= bound ? key_of(v[e], f + e) : 0;
+            unsigned more = __ballot_sync(0xffffffffu, c > __shfl_sync(0xffffffffu, best, k - 1));
+            while (more) {
+                best = inserted(best, __shfl_sync(0xffffffffu, c, __ffs(more) - 1), lane);
+                more &= more - 1;
+            }
+        }
+    }
+    if (tid < kMaxTop) sh.best[tid] = 0;
+    sh.lists[warp][lane] = best;
+    __syncthreads();
+    if (best) {
+        int r = lane;
+        for (int w = 0; w < kWarps; ++w)
+            if (w != warp) r += count_larger(sh.lists[w], best);
+        if (r < k) sh.best[r] = best;
+    }
+}
+
+template <class T, int kThreads, bool kTop>
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_logprobs_kernel(ScoreArgs a) {
+    constexpr int E = kUnit<T>, kWarps = kThreads / 32;
+    __shared__ Shared<kThreads> sh;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     uint32_t split, rank;
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(split));
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     const int r = blockIdx.x / split;
     const T *x = static_cast<const T *>(a.x) + (size_t)r * a.ld;
-    const Row<T> row(x, a.vocab);
-    const int units = row.units(), per = (units + split - 1) / split;
-    const int u0 = min(units, (int)rank * per), u1 = min(units, u0 + per);
-    const T masked = from_float<T>(neg_inf());      // what lies outside the row counts as masked
-
-    Sums a0{neg_inf(), 0.f, 0.f};
-    int best = -1;
-    auto take = [&](const uint4 &raw, int u) {
+    const Part<T, kThreads> part(x, a.vocab, split, rank);
+    uint4 raw[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) raw[i] = part.load(part.u0 + tid + i * kThreads);
+    // the given tokens' logits, on their way under the row
+    int64_t tok = -1;
+    float xt = 0.f;
+    if (rank == 0 && tid < a.t) {
+        tok = a.tokens[(size_t)r * a.t + tid];
+        if (tok >= 0 && tok < a.vocab) xt = to_float(x[tok]);
+    }
+    float m = neg_inf();
+    Heads heads{neg_inf(), neg_inf(), -1};
+    tc::F2 s2 = tc::f2(0.f), u2 = tc::f2(0.f);
+    auto take = [&](const uint4 &w, int unit) {
         float v[E];
-        unpack(raw, v, T());
-        float top = v[0];
+        unpack(w, v, T());
+        float top = max_nan(v[0], v[1], v[2]);
 #pragma unroll
-        for (int e = 1; e < E; ++e) top = max_nan(top, v[e]);
-        if (top > a0.m) {
-            a0.to(top);
-            a0.m = top;
-            best = u;
-        }
+        for (int e = 3; e < E; e += 2) top = e + 1 < E ? max_nan(top, v[e], v[e + 1]) : max_nan(top, v[e]);
         if (top == neg_inf()) return;
+        if (kTop) heads.second = fmaxf(heads.second, fminf(top, m));
+        if (top > m) {
+            Sums lo{m, 0.f, 0.f}, hi{m, 0.f, 0.f};
+            tc::f2_get(s2, lo.s, hi.s);
+            tc::f2_get(u2, lo.u, hi.u);
+            lo.to(top);
+            hi.to(top);
+            s2 = tc::f2(lo.s, hi.s);
+            u2 = tc::f2(lo.u, hi.u);
+            m = top;
+            heads.unit = unit;
+        }
+        tc::F2 d[E / 2], all = tc::f2(0.f);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float d = v[e] - a0.m, w = exp2_fast(d * kLog2e);
-            a0.s += w;
-            a0.u += w * fmaxf(d, -1e30f);       // 0, not NaN, for a masked element
+        for (int i = 0; i < E / 2; ++i) {
+            d[i] = tc::f2_add(tc::f2(v[2 * i], v[2 * i + 1]), tc::f2(-m));
+            all = i ? tc::f2_add(all, d[i]) : d[i];
+        }
+        float a0, a1;
+        tc::f2_get(all, a0, a1);
+        const bool far = a0 + a1 < -1e30f;      // a difference may be -inf: it adds 0, not NaN
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+            float t0, t1, d0, d1;
+            tc::f2_get(tc::f2_mul(d[i], tc::f2(kLog2e)), t0, t1);
+            const tc::F2 w2 = tc::f2(exp2_fast(t0), exp2_fast(t1));
+            s2 = tc::f2_add(s2, w2);
+            if (far) {
+                tc::f2_get(d[i], d0, d1);
+                d[i] = tc::f2(fmaxf(d0, -1e30f), fmaxf(d1, -1e30f));
+            }
+            u2 = tc::f2_fma(w2, d[i], u2);
         }
     };
-    int u = u0 + tid;
-    for (; u + (kAhead - 1) * kThreads < u1; u += kAhead * kThreads) {
-        uint4 raw[kAhead];
+    for (int u = part.u0 + tid; u < part.u1; u += kAhead * kThreads) {
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) raw[i] = row.load(u + i * kThreads, masked);
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) take(raw[i], u + i * kThreads);
+        for (int i = 0; i < kAhead; ++i) {
+            const uint4 w = raw[i];
+            raw[i] = part.load(u + (kAhead + i) * kThreads);
+            take(w, u + i * kThreads);
+        }
     }
-    for (; u < u1; u += kThreads) take(row.load(u, masked), u);
-    const float own_max = a0.m;
-
-    if (kTop) sh.lists[warp][lane] = warp_sorted(best < 0 ? (uint64_t)tid : key_of(own_max, best), lane);
-#pragma unroll
-    for (int i = 16; i > 0; i /= 2) a0.add(shuffled(a0, i));
-    if (lane == 0) sh.sums[warp] = a0;
-    if (kTop && tid < kMaxTop) sh.best[tid] = 0;
+    if (part.cut(part.u0)) take(part.row.load(part.u0, from_float<T>(neg_inf())), part.u0);
+    if (part.u1 - 1 != part.u0 && part.cut(part.u1 - 1)) take(part.row.load(part.u1 - 1, from_float<T>(neg_inf())), part.u1 - 1);
+    if (kTop) {
+        const uint32_t sorted = warp_sorted(ordered(m), lane);
+        if (lane == a.k - 1) sh.kth[warp] = sorted;
+        if (lane == (a.k - 1) / kWarps) sh.share[warp] = sorted;
+        if (tid < kMaxTop) sh.best[tid] = 0;
+        if (tid == 0) sh.count = 0;
+    }
+    float s0, s1, u0, u1;
+    tc::f2_get(s2, s0, s1);
+    tc::f2_get(u2, u0, u1);
+    Sums c = warp_sums({m, s0 + s1, u0 + u1});
+    if (lane == 0) sh.sums[warp] = c;
     __syncthreads();
     if (kTop) {
-        const uint64_t key = sh.lists[warp][lane];
-        const int at = rank_of(sh, key, warp, lane);
-        if (at < a.k) sh.seg[at] = key;
-        __syncthreads();
-        const uint32_t least = (uint32_t)(sh.seg[a.k - 1] >> 32);
-        uint64_t list = 0;                      // the warp's largest so far, falling over the lanes
-        for (int i = warp; i < a.k; i += kWarps) {
-            const uint64_t head = sh.seg[i];
-            if (head >> 32 == 0) break;         // threads without a token
-            const int first = u0 + (pos_of(head) - u0) % kThreads;
-            for (int b = first; b < u1; b += 32 * kThreads) {
-                const int w = b + lane * kThreads;
-                float v[E];
-                const bool in = w < u1;
-                if (in) unpack(row.load(w, masked), v, T());
-                const int f = row.first(w);
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const uint64_t c = in && v[e] > neg_inf() && ordered(v[e]) >= least ? key_of(v[e], f + e) : 0;
-                    const uint64_t last = __shfl_sync(0xffffffffu, list, a.k - 1);
-                    unsigned more = __ballot_sync(0xffffffffu, c > last);
-                    while (more) {
-                        const uint64_t ins = __shfl_sync(0xffffffffu, c, __ffs(more) - 1);
-                        more &= more - 1;
-                        const int pos = __popc(__ballot_sync(0xffffffffu, list > ins));
-                        const uint64_t up = __shfl_up_sync(0xffffffffu, list, 1);
-                        if (lane >= pos) list = lane == pos ? ins : up;
-                    }
-                }
-            }
-        }
-        sh.lists[warp][lane] = list;
-        __syncthreads();
-        if (list) {
-            const int p = rank_of(sh, list, warp, lane);
-            if (p < a.k) sh.best[p] = list;
-        }
+        heads.first = m;
+        select_top<T, kThreads>(sh, part, heads, a.k);
     }
     if (warp == 0) {
-        Sums c = sh.sums[lane % kWarps];
-#pragma unroll
-        for (int i = kWarps / 2; i > 0; i /= 2) c.add(shuffled(c, i));
+        c = warp_sums(lane < kWarps ? sh.sums[lane] : Sums{neg_inf(), 0.f, 0.f});
         if (lane == 0) sh.total = c;
     }
     if (split > 1) {
         cluster_barrier();
-        if (rank != 0) {
-            cluster_barrier();                  // rank 0 still reads this CTA's results
-            return;
-        }
-        if (kTop) {
-            const uint64_t key = warp < (int)split ? in_cta(sh.best, warp)[lane] : 0;
-            sh.lists[warp][lane] = key;
-        }
-        Sums c = *in_cta(&sh.total, 0);
-        for (int i = 1; i < (int)split; ++i) c.add(*in_cta(&sh.total, i));
-        cluster_barrier();                      // nothing of the others is read from here on
-        if (tid == 0) sh.total = c;
-        if (kTop && tid < kMaxTop) sh.best[tid] = 0;
-        __syncthreads();
-        if (kTop) {
-            const uint64_t key = sh.lists[warp][lane];
-            if (key) {
-                const int p = rank_of(sh, key, warp, lane);
+        if (rank == 0) {
+            uint64_t key = 0;
+            if (kTop && warp < kMaxSplit) {
+                key = warp < (int)split ? in_cta(sh.best, warp)[lane] : 0;
+                sh.lists[warp][lane] = key;
+            }
+            c = *in_cta(&sh.total, 0);
+            for (int i = 1; i < (int)split; ++i) c.add(*in_cta(&sh.total, i));
+            __syncthreads();
+            if (kTop && tid < kMaxTop) sh.best[tid] = 0;
+            if (tid == 0) sh.total = c;
+            __syncthreads();
+            if (kTop && key) {
+                int p = lane;
+                for (int i = 0; i < (int)split; ++i)
+                    if (i != warp) p += count_larger(sh.lists[i], key);
                 if (p < a.k) sh.best[p] = key;
             }
         }
     }
     __syncthreads();
-    const Sums c = sh.total;
-    const bool bad = isnan(c.s), empty = !bad && c.m == neg_inf();
-    const float logz = empty ? 0.f : logf(c.s);
-    if (tid == 0) {
-        if (a.lse) a.lse[r] = bad ? not_a_number() : empty ? neg_inf() : c.m + logz;
-        if (a.entropy) a.entropy[r] = bad ? not_a_number() : empty ? 0.f : logz - c.u / c.s;
+    if (rank == 0) {
+        c = sh.total;
+        const bool bad = isnan(c.s), empty = !bad && c.m == neg_inf();
+        const float logz = empty ? 0.f : logf(c.s);
+        if (tid == 0) {
+            if (a.lse) a.lse[r] = bad ? not_a_number() : empty ? neg_inf() : c.m + logz;
+            if (a.entropy) a.entropy[r] = bad ? not_a_number() : empty ? 0.f : logz - c.u / c.s;
+        }
+        auto logprob = [&](float v) { return bad ? not_a_number() : v == neg_inf() ? v : (v - c.m) - logz; };
+        for (int j = tid; j < a.t; j += kThreads) {
+            if (j != tid) {
+                tok = a.tokens[(size_t)r * a.t + j];
+                if (tok >= 0 && tok < a.vocab) xt = to_float(x[tok]);
+            }
+            a.logprob[(size_t)r * a.t + j] = tok < 0 ? 0.f : tok >= a.vocab ? not_a_number() : logprob(xt);
+        }
+        if (kTop && tid < a.k) {
+            const uint64_t key = sh.best[tid];
+            const bool none = bad || key == 0;
+            a.top_token[(size_t)r * a.k + tid] = none ? -1 : pos_of(key);
+            a.top_logprob[(size_t)r * a.k + tid] =
+                bad ? not_a_number() : none ? neg_inf() : logprob(unordered((uint32_t)(key >> 32)));
+        }
     }
-    auto logprob = [&](float v) { return bad ? not_a_number() : v == neg_inf() ? v : (v - c.m) - logz; };
-    if (tid < a.t) {
-        const int64_t tok = a.tokens[(size_t)r * a.t + tid];
-        a.logprob[(size_t)r * a.t + tid] = tok < 0 ? 0.f : tok >= a.vocab ? not_a_number() : logprob(to_float(x[tok]));
-    }
-    if (kTop && tid < a.k) {
-        const uint64_t key = sh.best[tid];
-        const bool none = bad || key == 0;
-        a.top_token[(size_t)r * a.k + tid] = none ? -1 : pos_of(key);
-        a.top_logprob[(size_t)r * a.k + tid] =
-            bad ? not_a_number() : none ? neg_inf() : logprob(unordered((uint32_t)(key >> 32)));
-    }
+    if (split > 1) cluster_barrier();       // rank 0 reads the others' results until here
 }
 
 struct GradArgs {
@@ -299,6 +440,8 @@ struct GradArgs {
 // A CTA writes the second term of `per` 16-byte units of a row, then the tokens
 // among them with both terms.  kSame: logits and gradient have the same
 // alignment.
+constexpr int kThreads = 256;           // of the gradient
+
 template <class T, bool kSame>
 __global__ void __launch_bounds__(kThreads) token_grad_kernel(GradArgs a) {
     constexpr int E = kUnit<T>;
@@ -359,26 +502,35 @@ __global__ void __launch_bounds__(kThreads) token_grad_kernel(GradArgs a) {
     }
 }
 
+template <class T, int kThreads>
+cudaError_t launch_rows(const ScoreArgs &a, int split, cudaStream_t s) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)a.n * split);
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = split;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return a.k ? cudaLaunchKernelEx(&cfg, token_logprobs_kernel<T, kThreads, true>, a)
+               : cudaLaunchKernelEx(&cfg, token_logprobs_kernel<T, kThreads, false>, a);
+}
+
 cudaError_t launch_logprobs(const ScoreArgs &a, jarq_dtype dtype, cudaStream_t s) {
-    // few rows: several CTAs share one, as long as each has a few units a thread
+    const int64_t units = (int64_t)a.vocab * (int64_t)size_of(dtype) / 16;
+    // Few rows: the CTAs of a cluster share one, as long as each has some 900 units
+    // (48 x 50001 fp16: 11.3 us by one CTA a row, 9.9 by four, 11.3 by eight).  Of
+    // many rows or short ones a CTA of 128 threads is better, since each has its
+    // own sums to join (8192 x 32000 bf16: 109 us, 121 with 256 threads; 600 x
+    // 131072 float32: 78 us, 56 with 256).
     int split = 1;
-    while (split < kMaxSplit && (int64_t)a.n * split < 2 * num_sms() &&
-           (int64_t)a.vocab * (int64_t)size_of(dtype) / split > 2 * kThreads * 16)
-        split *= 2;
+    while (split < kMaxSplit && 2 * (int64_t)a.n * split < 3 * num_sms() && units / (2 * split) >= 900) split *= 2;
+    const bool small = split == 1 && (units <= 2048 || a.n >= 8 * num_sms());
     return with_type(dtype, [&](auto type) {
         using T = decltype(type);
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)a.n * split);
-        cfg.blockDim = dim3(kThreads);
-        cfg.stream = s;
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = split;
-        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-        return a.k ? cudaLaunchKernelEx(&cfg, token_logprobs_kernel<T, true>, a)
-                   : cudaLaunchKernelEx(&cfg, token_logprobs_kernel<T, false>, a);
+        return small ? launch_rows<T, 128>(a, 1, s) : launch_rows<T, 256>(a, split, s);
     });
 }
 
