@@ -1,7 +1,7 @@
 // Product of 8-bit integers with scales for each token and channel:
 //   Y[t][o] = xs[t] sum_i ws[o][i] (sum_{k in group i} X[t][k] C[o][k]) + bias[o].
 //
-// Up to eight tokens: integer dot products of four, bound by reading the weights
+// One or two tokens: integer dot products of four, bound by reading the weights
 // once.  A block has R channels; its threads share K, 16 codes of each channel
 // at a time with 16 codes of each token, the next weights on their way while
 // these are used.  With one scale a channel the sums are int32 (exact for din <=
@@ -47,6 +47,7 @@ __global__ void __launch_bounds__(kThreads) few_tokens_kernel(ProductArgs a) {
     __shared__ uint32_t parts[kWarps][V];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int o0 = blockIdx.x * R, chunks = (a.din + 15) / 16;
+    const int shift = a.g == 64 ? 2 : 3;      // 16-code chunks of a group: 4 or 8
     uint4 w[R];
     auto fetch = [&](int r, int c) {
         if (o0 + r < a.dout && c < chunks) w[r] = load_codes<VEC>(a.C + (size_t)(o0 + r) * a.ldc, 16 * c, a.din);
@@ -66,7 +67,7 @@ __global__ void __launch_bounds__(kThreads) few_tokens_kernel(ProductArgs a) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const uint4 wr = w[r];
-            const float s = GROUPS && o0 + r < a.dout ? a.ws[(size_t)(o0 + r) * a.G + 16 * c / a.g] : 0.f;
+            const float s = GROUPS && o0 + r < a.dout ? a.ws[(size_t)(o0 + r) * a.G + (c >> shift)] : 0.f;
             fetch(r, c + kThreads);
 #pragma unroll
             for (int m = 0; m < M; ++m) {
@@ -122,10 +123,8 @@ cudaError_t launch_few(const ProductArgs &a, cudaStream_t s, bool pdl) {
 }
 
 cudaError_t launch_product(const ProductArgs &a, int *failed, cudaStream_t s, bool pdl) {
-    if (a.n == 1) return launch_few<1, 8>(a, s, pdl);
-    if (a.n == 2) return launch_few<2, 8>(a, s, pdl);
-    if (a.n <= 4) return launch_few<4, 4>(a, s, pdl);
-    if (a.n <= kFewTokens) return launch_few<8, 4>(a, s, pdl);
+    if (a.n == 1) return launch_few<1, 4>(a, s, pdl);
+    if (a.n <= kFewTokens) return launch_few<2, 8>(a, s, pdl);
     return launch_tc_integer(a, failed, s, pdl);
 }
 

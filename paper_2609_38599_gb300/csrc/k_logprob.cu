@@ -1,11 +1,14 @@
 // Log probabilities of given tokens under a softmax over the vocabulary, its
 // entropy and its most probable tokens, and their gradient.
 //
-// Forward, one pass over a row's logits x: every thread keeps its own maximum m
-// and the sums s = sum e^(x - m), u = sum e^(x - m) (x - m), rescaled when m
-// grows; joined over threads they give lse = m + ln s, logprob = (x - m) - ln s
-// and entropy = ln s - u / s (no difference of large numbers).  Each thread has
-// four 16-byte units in flight.
+// Forward, one pass over a row's logits x: every thread keeps its own maximum m,
+// M = m log2 e rounded to float32, and with t = x log2 e - M (one fused operation)
+// the sums s = sum 2^t and u = sum 2^t t, rescaled when m grows.  Joined over
+// threads, with the rounding left out of M, r = m log2 e - M, they give
+// z = sum e^(x - m) = s 2^-r, logprob = (x - m) - ln z, lse = m + ln z and
+// entropy = ln z - (u / s - r) ln 2 (no difference of large numbers).  Each thread
+// has four 16-byte units in flight.  Bound by issue slots for 16-bit logits (8 to
+// 9 instructions a logit), by memory for float32.
 //
 // Alternatives.  Lower bounds of a row's k-th largest logit: the k-th largest of the
 // 32 thread maxima of any warp, and, with W warps, the least of all warps'
@@ -19,7 +22,6 @@
 #include <math.h>
 
 #include <algorithm>
-#include <type_traits>
 
 #include "rows.cuh"
 #include "tc_common.cuh"
@@ -33,7 +35,7 @@ constexpr int kMaxTop = 32, kMaxTokens = 256;
 constexpr int kMaxSplit = 8;         // CTAs of a cluster that share a row
 constexpr int kAhead = 4;            // units of a thread in flight
 constexpr int kList = 512;           // candidates
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct ScoreArgs {
     const void *x;
@@ -77,23 +79,30 @@ __device__ __forceinline__ uint64_t key_of(float x, int pos) {
 }
 __device__ __forceinline__ int pos_of(uint64_t key) { return (int)(0xFFFFFFFFu - (uint32_t)key); }
 
-// m, s, u of some of a row's elements.  m = -inf: none that is not masked (s is
+// The reference M of a maximum m, and what its rounding leaves out.  Above 10^6
+// that would be too much: t is then (x - m) log2 e, and nothing is left out.
+__device__ __forceinline__ bool big(float m) { return !(fabsf(m) <= 1e6f); }
+__device__ __forceinline__ float reference(float m) { return __fmul_rn(m, kLog2e); }
+__device__ __forceinline__ float left_out(float m) { return big(m) ? 0.f : fmaf(m, kLog2e, -reference(m)); }
+
+// m, s and u of some of a row's elements.  m = -inf: none that is not masked (s is
 // 0, or NaN where one is NaN).
 struct Sums {
     float m, s, u;
-    // the same sums with respect to M >= m
-    __device__ void to(float M) {
-        if (m == neg_inf() || m == M) return;
-        const float d = fmaxf(m - M, -1e30f), f = exp2_fast(d * kLog2e);   // s d stays finite
+    // the same sums with the reference of top >= m
+    __device__ void to(float top) {
+        if (m == neg_inf() || m == top) return;
+        // s d stays finite
+        const float d = fmaxf((m - top) * kLog2e - left_out(m) + left_out(top), -1e30f), f = exp2_fast(d);
         u = (u + s * d) * f;
         s *= f;
-        m = M;
+        m = top;
     }
     __device__ void add(Sums o) {
-        const float M = fmaxf(m, o.m);
-        to(M);
-        o.to(M);
-        m = M;
+        const float top = fmaxf(m, o.m);
+        to(top);
+        o.to(top);
+        m = top;
         s += o.s;
         u += o.u;
     }
@@ -101,14 +110,14 @@ struct Sums {
 
 // The sums of a warp's lanes, in every lane.
 __device__ __forceinline__ Sums warp_sums(Sums a) {
-    const float M = unordered(__reduce_max_sync(0xffffffffu, ordered(a.m)));
-    a.to(M);
+    const float top = unordered(__reduce_max_sync(0xffffffffu, ordered(a.m)));
+    a.to(top);
 #pragma unroll
     for (int i = 16; i > 0; i /= 2) {
         a.s += __shfl_xor_sync(0xffffffffu, a.s, i);
         a.u += __shfl_xor_sync(0xffffffffu, a.u, i);
     }
-    return {M, a.s, a.u};
+    return {top, a.s, a.u};
 }
 
 // Sorted over the warp's lanes, the largest in lane 0.
@@ -165,29 +174,28 @@ __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// A CTA's part of a row: units u0 .. u1 - 1, those of a thread kThreads apart, of
-// which lo .. lo + n - 1 lie in the row as a whole.
+// A CTA's part of a row: units u0 .. u1 - 1, of which lo .. hi - 1 lie in the row
+// as a whole and are shared out kThreads apart; a cut first unit is thread 0's, a
+// cut last one thread 1's.
 template <class T, int kThreads>
 struct Part {
     Row<T> row;
-    int u0, u1, lo, n;
+    int u0, u1, lo, hi;
     __device__ Part(const T *x, int vocab, int split, int rank) : row(x, vocab) {
         const int units = row.units(), per = (units + split - 1) / split;
         u0 = min(units, rank * per);
         u1 = min(units, u0 + per);
         lo = u0 + (u0 < u1 && !row.whole(u0));
-        n = max(0, u1 - lo - (lo < u1 && !row.whole(u1 - 1)));
+        hi = max(lo, u1 - (lo < u1 && !row.whole(u1 - 1)));
     }
-    // a whole unit; elsewhere -inf, as if masked
-    __device__ uint4 load(int u) const {
-        constexpr uint32_t m = sizeof(T) == 4 ? 0xFF800000u : std::is_same_v<T, __half> ? 0xFC00FC00u : 0xFF80FF80u;
-        uint4 r = make_uint4(m, m, m, m);
-        if ((unsigned)(u - lo) < (unsigned)n) r = *reinterpret_cast<const uint4 *>(row.p + row.first(u));
-        return r;
-    }
-    // the first or last unit, if it is cut and this thread's
-    __device__ bool cut(int u) const {
-        return u0 < u1 && u >= u0 && u < u1 && !row.whole(u) && (u - u0) % kThreads == (int)threadIdx.x;
+    // the whole units, and any unit with -inf, as if masked, outside the row
+    __device__ const uint4 *units() const { return reinterpret_cast<const uint4 *>(row.p - row.skip); }
+    __device__ uint4 load(int u) const { return row.load(u, from_float<T>(neg_inf())); }
+    // f(u) for the cut units of thread `tid`
+    template <class F>
+    __device__ void cut(int tid, F f) const {
+        if (tid == 0 && lo > u0) f(u0);
+        if (tid == 1 && hi < u1) f(u1 - 1);
     }
 };
 
@@ -216,12 +224,11 @@ template <class T, int kThreads>
 __device__ __forceinline__ void select_top(Shared<kThreads> &sh, const Part<T, kThreads> &part, const Heads &h, int k) {
     constexpr int E = kUnit<T>, kWarps = kThreads / 32;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const T masked = from_float<T>(neg_inf());
     uint32_t bound = max(__reduce_max_sync(0xffffffffu, sh.kth[lane % kWarps]),
                          __reduce_min_sync(0xffffffffu, sh.share[lane % kWarps]));
     auto list = [&](int u) {
         float v[E];
-        unpack(part.row.load(u, masked), v, T());
+        unpack(part.load(u), v, T());
 #pragma unroll
         for (int e = 0; e < E; ++e)
             if (v[e] > neg_inf() && ordered(v[e]) >= bound) {
@@ -243,8 +250,12 @@ __device__ __forceinline__ void select_top(Shared<kThreads> &sh, const Part<T, k
             // the other units of a thread, 32 at a time
             const int i = __ffs(more) - 1, skip = __shfl_sync(0xffffffffu, h.unit, i);
             more &= more - 1;
-            for (int u = part.u0 + 32 * warp + i + lane * kThreads; u < part.u1; u += 32 * kThreads)
+            for (int u = part.lo + 32 * warp + i + lane * kThreads; u < part.hi; u += 32 * kThreads)
                 if (u != skip) list(u);
+            if (lane == i)
+                part.cut(tid, [&](int u) {
+                    if (u != skip) list(u);
+                });
             __syncwarp();
         }
         __syncthreads();
@@ -258,7 +269,9 @@ __device__ __forceinline__ void select_top(Shared<kThreads> &sh, const Part<T, k
     uint64_t best = 0;                      // the warp's largest so far, falling over the lanes
     for (int b = part.u0 + 32 * warp; b < part.u1; b += kThreads) {
         float v[E];
-        unpack(b + lane < part.u1 ? part.row.load(b + lane, masked) : part.load(-1), v, T());
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = neg_inf();
+        if (b + lane < part.u1) unpack(part.load(b + lane), v, T());
         const int f = part.row.first(b + lane);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
@@ -292,9 +305,14 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_logprobs_kern
     const int r = blockIdx.x / split;
     const T *x = static_cast<const T *>(a.x) + (size_t)r * a.ld;
     const Part<T, kThreads> part(x, a.vocab, split, rank);
+    constexpr int kChunk = kAhead * kThreads;
+    const int chunks = (part.hi - part.lo) / kChunk;       // whole ones
+    const uint4 *next = part.units() + part.lo + tid;
     uint4 raw[kAhead];
+    if (chunks > 0) {
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) raw[i] = part.load(part.u0 + tid + i * kThreads);
+        for (int i = 0; i < kAhead; ++i) raw[i] = next[i * kThreads];
+    }
     // the given tokens' logits, on their way under the row
     int64_t tok = -1;
     float xt = 0.f;
@@ -302,7 +320,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_logprobs_kern
         tok = a.tokens[(size_t)r * a.t + tid];
         if (tok >= 0 && tok < a.vocab) xt = to_float(x[tok]);
     }
-    float m = neg_inf();
+    float m = neg_inf(), ref = 0.f;
     Heads heads{neg_inf(), neg_inf(), -1};
     tc::F2 s2 = tc::f2(0.f), u2 = tc::f2(0.f);
     auto take = [&](const uint4 &w, int unit) {
@@ -311,7 +329,6 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_logprobs_kern
         float top = max_nan(v[0], v[1], v[2]);
 #pragma unroll
         for (int e = 3; e < E; e += 2) top = e + 1 < E ? max_nan(top, v[e], v[e + 1]) : max_nan(top, v[e]);
-        if (top == neg_inf()) return;
         if (kTop) heads.second = fmaxf(heads.second, fminf(top, m));
         if (top > m) {
             Sums lo{m, 0.f, 0.f}, hi{m, 0.f, 0.f};
@@ -322,40 +339,63 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_logprobs_kern
             s2 = tc::f2(lo.s, hi.s);
             u2 = tc::f2(lo.u, hi.u);
             m = top;
+            ref = big(m) ? not_a_number() : reference(m);
             heads.unit = unit;
         }
-        tc::F2 d[E / 2], all = tc::f2(0.f);
+        const tc::F2 scale = tc::f2(kLog2e), minus = tc::f2(-ref);
+        tc::F2 t[E / 2], all = tc::f2(0.f);
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) {
-            d[i] = tc::f2_add(tc::f2(v[2 * i], v[2 * i + 1]), tc::f2(-m));
-            all = i ? tc::f2_add(all, d[i]) : d[i];
+            t[i] = tc::f2_fma(tc::f2(v[2 * i], v[2 * i + 1]), scale, minus);
+            all = i ? tc::f2_add(all, t[i]) : t[i];
         }
         float a0, a1;
         tc::f2_get(all, a0, a1);
-        const bool far = a0 + a1 < -1e30f;      // a difference may be -inf: it adds 0, not NaN
+        if (!(fabsf(a0 + a1) <= 1e30f)) {       // -inf among them adds 0, not NaN; a large maximum
+            const bool large = big(m) && m > neg_inf();
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) {
+                tc::f2_get(t[i], a0, a1);
+                if (large) {
+                    a0 = (v[2 * i] - m) * kLog2e;
+                    a1 = (v[2 * i + 1] - m) * kLog2e;
+                }
+                t[i] = tc::f2(a0 < -1e30f ? -1e30f : a0, a1 < -1e30f ? -1e30f : a1);     // NaN stays
+            }
+        }
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) {
-            float t0, t1, d0, d1;
-            tc::f2_get(tc::f2_mul(d[i], tc::f2(kLog2e)), t0, t1);
+            float t0, t1;
+            tc::f2_get(t[i], t0, t1);
             const tc::F2 w2 = tc::f2(exp2_fast(t0), exp2_fast(t1));
             s2 = tc::f2_add(s2, w2);
-            if (far) {
-                tc::f2_get(d[i], d0, d1);
-                d[i] = tc::f2(fmaxf(d0, -1e30f), fmaxf(d1, -1e30f));
-            }
-            u2 = tc::f2_fma(w2, d[i], u2);
+            u2 = tc::f2_fma(w2, t[i], u2);
         }
     };
-    for (int u = part.u0 + tid; u < part.u1; u += kAhead * kThreads) {
+    int u = part.lo + tid;
+    for (int c = 1; c < chunks; ++c) {
+        next += kChunk;
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             const uint4 w = raw[i];
-            raw[i] = part.load(u + (kAhead + i) * kThreads);
+            raw[i] = next[i * kThreads];
             take(w, u + i * kThreads);
         }
+        u += kChunk;
     }
-    if (part.cut(part.u0)) take(part.row.load(part.u0, from_float<T>(neg_inf())), part.u0);
-    if (part.u1 - 1 != part.u0 && part.cut(part.u1 - 1)) take(part.row.load(part.u1 - 1, from_float<T>(neg_inf())), part.u1 - 1);
+    if (chunks > 0) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) take(raw[i], u + i * kThreads);
+        u += kChunk;
+    }
+    // what is left: up to kAhead units a thread
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+        if (u + i * kThreads < part.hi) raw[i] = part.units()[u + i * kThreads];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+        if (u + i * kThreads < part.hi) take(raw[i], u + i * kThreads);
+    part.cut(tid, [&](int cut) { take(part.load(cut), cut); });
     if (kTop) {
         const uint32_t sorted = warp_sorted(ordered(m), lane);
         if (lane == a.k - 1) sh.kth[warp] = sorted;
@@ -403,10 +443,10 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_logprobs_kern
     if (rank == 0) {
         c = sh.total;
         const bool bad = isnan(c.s), empty = !bad && c.m == neg_inf();
-        const float logz = empty ? 0.f : logf(c.s);
+        const float rest = left_out(c.m), logz = empty ? 0.f : logf(c.s * exp2_fast(-rest));
         if (tid == 0) {
             if (a.lse) a.lse[r] = bad ? not_a_number() : empty ? neg_inf() : c.m + logz;
-            if (a.entropy) a.entropy[r] = bad ? not_a_number() : empty ? 0.f : logz - c.u / c.s;
+            if (a.entropy) a.entropy[r] = bad ? not_a_number() : empty ? 0.f : logz - (c.u / c.s - rest) * kLn2;
         }
         auto logprob = [&](float v) { return bad ? not_a_number() : v == neg_inf() ? v : (v - c.m) - logz; };
         for (int j = tid; j < a.t; j += kThreads) {
