@@ -294,7 +294,8 @@ jarq_status jarq_accumulate_hessian(const void *X, int n, int d, float scale, fl
  * score logits.  They differ from the calls above in three points, since a
  * generation step takes microseconds on the device:
  * - They only enqueue their work on `stream` and return; results are ready in
- *   stream order, and the calls can be captured in a CUDA graph.
+ *   stream order, and the calls can be captured in a CUDA graph (a process's
+ *   first product, which allocates the word of the third point, cannot).
  * - They allocate nothing on the device and keep no state between calls.
  * - A failure on the device (a bounded wait that gave up) is reported by
  *   jarq_async_status, and by every later call of these operators until
@@ -465,7 +466,8 @@ long long jarq_launch_count(void);
 jarq_status jarq_selftest_wait_timeout(void *stream);
 
 /* The same for the tensor-core kernels: one of them ("target", "gram",
- * "proj", "ptilde", "hr_full" or "syrk") on a small layer of its own, with a
+ * "proj", "ptilde", "hr_full", "syrk" or "integer_product", whose timeout
+ * jarq_async_status reports and so clears) on a small layer of its own, with a
  * short poll limit and its issuing warp told to stop after the first unit of
  * work, so that the waits of the other warps run out while copies lie
  * unused in shared memory.  Returns what that launch reports:

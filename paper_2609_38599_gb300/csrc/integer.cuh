@@ -58,5 +58,7 @@ inline bool vector_rows(const ProductArgs &a) {
 // to 1 by a kernel whose waits gave up.  pdl: X and xs are the previous kernel's
 // results, and that kernel reads or writes nothing else of a's.
 cudaError_t launch_tc_integer(const ProductArgs &a, int *failed, cudaStream_t s, bool pdl);
+// The self-test's form (256 tokens, fp16, aligned), whose issuer stops early and whose waits give up.
+cudaError_t launch_tc_integer_stalled(const ProductArgs &a, int *failed, cudaStream_t s);
 
 }  // namespace jarq

@@ -17,7 +17,7 @@
 
 #include <new>
 
-#include "jarq_internal.cuh"
+#include "integer.cuh"
 
 namespace jarq {
 
@@ -709,6 +709,24 @@ jarq_status jarq_selftest_stalled_kernel(const char *kernel, void *stream) try {
     // its kernel reads
     constexpr int d = 512, g = 128, G = d / g, p = 300, bits = 3, n = 1200;
     cudaStream_t st = (cudaStream_t)stream;
+    if (is("integer_product")) {
+        // fp16 tokens, codes, scales and outputs of a call that only enqueues
+        constexpr int k = 4096;                  // four accumulators a tile
+        const size_t xb = (size_t)p * k * 2, cb = (size_t)n * k, yb = (size_t)p * n * 4;
+        int *failed = async_word();
+        if (!failed) return JARQ_ERR_NOMEM;
+        char *m = nullptr;
+        CK(dalloc(&m, xb + cb + yb + 4 * (p + n)));
+        cudaError_t e = cudaMemsetAsync(m, 0, xb + cb + yb + 4 * (p + n), st);
+        const float *xs = reinterpret_cast<const float *>(m + xb + cb + yb);
+        const ProductArgs a{m, reinterpret_cast<int8_t *>(m + xb), xs, xs + p, nullptr, m + xb + cb, k, k, n, p, n, k, 0, 1,
+                            JARQ_F32, true};
+        if (e == cudaSuccess) e = launch_tc_integer_stalled(a, failed, st);
+        const jarq_status got = jarq_async_status(stream);
+        cudaFree(m);
+        CK(e);
+        return got;
+    }
     std::vector<float> H((size_t)d * d), W((size_t)p * d), S((size_t)p * G, 0.1f);
     std::vector<uint8_t> Q((size_t)p * d);
     std::vector<int32_t> Z((size_t)p * G, 3);

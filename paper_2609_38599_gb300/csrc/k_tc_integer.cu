@@ -95,9 +95,10 @@ struct Block {
                   "the roles' registers must fit the block's");
 };
 
+template <uint32_t kPolls>
 __device__ __forceinline__ bool wait_cluster(uint32_t bar, uint32_t parity) {
 #pragma unroll 1
-    for (uint32_t i = 0; i < tc::kWaitIters; ++i) {
+    for (uint32_t i = 0; i < kPolls; ++i) {
         uint32_t ok;
         asm volatile(
             "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
@@ -215,10 +216,12 @@ struct Slot {
 
 // NT: tokens of a tile.  GROUPS: group scales.  VEC: rows of codes on 16-byte
 // boundaries.  HALF: tokens are integers in fp16, rows on 16-byte boundaries.
-template <int NT, bool GROUPS, bool VEC, bool HALF>
+// kStalled: for the self-test, the issuer stops after one accumulator.
+template <int NT, bool GROUPS, bool VEC, bool HALF, bool kStalled>
 __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
     tc_integer_kernel(const __grid_constant__ CUtensorMap mapC, const __grid_constant__ CUtensorMap mapX, ProductArgs a,
                       int split, int *failed) {
+    constexpr uint32_t kPolls = tc::wait_polls(kStalled);
     using B = Block<NT, VEC, HALF>;
     constexpr int kDrain0 = 4 + B::convert / 32, kFill0 = kDrain0 + kDrain / 32;   // first warps
     constexpr int kStage = stage_bytes(NT), kRaws = raw_stages(NT, HALF), kRaw = raw_bytes(NT, HALF);
@@ -320,7 +323,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
                 for (int h = 0; h < kParts; ++h) {
                     const int use = unit * kParts + h, b = use % kAccs;
                     if (first) {
-                        ok = tc::mbar_wait(aempty(b), (use / kAccs & 1) ^ 1);
+                        ok = tc::mbar_wait<kPolls>(aempty(b), (use / kAccs & 1) ^ 1);
                         if (!ok) return;
                         tc::tc_fence_after();
                     }
@@ -344,7 +347,8 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
             };
             for (int tile = cluster; tile < ntiles && ok; tile += nclusters)
                 for (int step = 0, in_unit = 0; step < nsteps && ok; ++step, in.next()) {
-                    ok = kPair ? wait_cluster(full(in.s), in.phase) : tc::mbar_wait(full(in.s), in.phase);
+                    if (kStalled && unit > 0) break;
+                    ok = kPair ? wait_cluster<kPolls>(full(in.s), in.phase) : tc::mbar_wait<kPolls>(full(in.s), in.phase);
                     if (!ok) break;
                     tc::tc_fence_after();
                     const int atoms = min(2, natoms - 2 * step);
@@ -363,7 +367,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
                 else
                     tc::mma_commit(closing);
             }
-            if (!tc::mbar_wait(closing, 0) || !ok) *abort_flag = 1;
+            if (!tc::mbar_wait<kPolls>(closing, 0) || !ok) *abort_flag = 1;
         } else if (kPair && rank == 1 && (warp < 2 || (warp == 3 && !HALF))) {
             // ---------------- relays of the odd CTA: its stages are full, in turn
             const uint32_t full0 = tc::map_rank(full(0), even);
@@ -374,7 +378,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
             for (int tile = cluster; tile < ntiles && ok; tile += nclusters)
                 for (int step = 0; step < nsteps && ok; ++step, in.next()) {
                     if (turn == me) {
-                        ok = tc::mbar_wait(full(in.s), in.phase);
+                        ok = tc::mbar_wait<kPolls>(full(in.s), in.phase);
                         tc::tc_fence_after();
                         tc::tc_fence_before();
                         if (ok && lane == 0) arrive_cluster(full0 + 8 * in.s);
@@ -392,7 +396,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
             for (int tile = cluster; tile < ntiles && ok; tile += nclusters) {
                 const int o = tile % mt * kChannels + 128 * rank, tk = tile / mt * NT + kRowsB * rank;
                 for (int step = 0; step < nsteps; ++step, out.next()) {
-                    ok = tc::mbar_wait(raw_empty(out.s), out.phase);
+                    ok = tc::mbar_wait<kPolls>(raw_empty(out.s), out.phase);
                     if (!ok) break;
                     if (tc::elect_one()) {
                         const uint32_t at = raws + out.s * kRaw, bar = raw_full(out.s);
@@ -411,7 +415,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
             }
             // no copy is in flight when the CTA ends
             for (int n = max(0, filled - kRaws); n < filled && ok; ++n)
-                ok = tc::mbar_wait(raw_empty(n % kRaws), (n / kRaws) & 1);
+                ok = tc::mbar_wait<kPolls>(raw_empty(n % kRaws), (n / kRaws) & 1);
             if (!ok) {
                 *abort_flag = 1;
                 tc::abandon_ring(raw_full(0), kRaws, filled, true);
@@ -426,7 +430,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
             for (int tile = cluster; tile < ntiles && ok; tile += nclusters) {
                 const int tk = tile / mt * NT + kRowsB * rank;
                 for (int step = 0; step < nsteps; ++step, out.next()) {
-                    ok = tc::mbar_wait(empty(out.s), out.phase);
+                    ok = tc::mbar_wait<kPolls>(empty(out.s), out.phase);
                     if (!ok) break;
                     if (tc::elect_one()) {
                         const uint32_t bar = full0 + 8 * out.s;
@@ -448,7 +452,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
                 }
             }
             for (int n = max(0, filled - kStages); n < filled && ok; ++n)
-                ok = tc::mbar_wait(empty(n % kStages), (n / kStages) & 1);
+                ok = tc::mbar_wait<kPolls>(empty(n % kStages), (n / kStages) & 1);
             if (!ok) {
                 *abort_flag = 1;
                 tc::abandon_ring(full(0), kStages, filled, rank == 0);
@@ -463,8 +467,8 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
         for (int tile = cluster; tile < ntiles && ok; tile += nclusters)
             for (int step = 0; step < nsteps; ++step, in.next(), out.next()) {
                 if (HALF && B::convert == 256 && (turn = !turn, !turn)) continue;     // the other four warps' stage
-                ok = tc::mbar_wait(raw_full(in.s), in.phase);
-                ok = tc::mbar_wait(empty(out.s), out.phase) && ok;
+                ok = tc::mbar_wait<kPolls>(raw_full(in.s), in.phase);
+                ok = tc::mbar_wait<kPolls>(empty(out.s), out.phase) && ok;
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc::tc_fence_after();
@@ -496,8 +500,8 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
         Slot<kStages> out(1);
         for (int tile = cluster; tile < ntiles && ok; tile += nclusters)
             for (int step = 0; step < nsteps; ++step, in.next(), out.next()) {
-                ok = tc::mbar_wait(raw_full(in.s), in.phase);
-                ok = tc::mbar_wait(empty(out.s), out.phase) && ok;
+                ok = tc::mbar_wait<kPolls>(raw_full(in.s), in.phase);
+                ok = tc::mbar_wait<kPolls>(empty(out.s), out.phase) && ok;
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 if (kShare) {
@@ -557,7 +561,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
 #pragma unroll
                 for (int h = 0; h < kParts; ++h) {
                     const int use = unit * kParts + h, b = use % kAccs;
-                    ok = __all_sync(0xffffffffu, tc::mbar_wait(afull(b), use / kAccs & 1)) && ok;
+                    ok = __all_sync(0xffffffffu, tc::mbar_wait<kPolls>(afull(b), use / kAccs & 1)) && ok;
                     if (!ok) break;
                     tc::tc_fence_after();
                     const uint32_t at = taddr + b * kAcc;
@@ -662,7 +666,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
             };
             for (int step = 0; step < nsteps; ++step, out.next()) {
                 const int k = (step0 + step) * kStepK + c * 16;
-                ok = tc::mbar_wait(raw_empty(out.s), out.phase);
+                ok = tc::mbar_wait<kPolls>(raw_empty(out.s), out.phase);
                 if (!ok) break;
                 const uint32_t dst = to + out.s * kRaw;
 #pragma unroll 1
@@ -761,10 +765,10 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
     }
 }
 
-template <int NT, bool GROUPS, bool VEC, bool HALF>
+template <int NT, bool GROUPS, bool VEC, bool HALF, bool kStalled = false>
 cudaError_t launch(const ProductArgs &a, int split, int *failed, cudaStream_t s, bool pdl) {
     static std::atomic<unsigned long long> done;
-    auto *kernel = tc_integer_kernel<NT, GROUPS, VEC, HALF>;
+    auto *kernel = tc_integer_kernel<NT, GROUPS, VEC, HALF, kStalled>;
     cudaError_t e = set_max_dynamic_smem((const void *)kernel, smem_bytes(NT, HALF), done);
     if (e != cudaSuccess) return e;
     CUtensorMap mapC = {}, mapX = {};
@@ -810,6 +814,10 @@ cudaError_t launch_nt(const ProductArgs &a, int split, int *failed, cudaStream_t
 }
 
 }  // namespace
+
+cudaError_t launch_tc_integer_stalled(const ProductArgs &a, int *failed, cudaStream_t s) {
+    return launch<256, false, true, true, true>(a, 1, failed, s, false);
+}
 
 cudaError_t launch_tc_integer(const ProductArgs &a, int *failed, cudaStream_t s, bool pdl) {
     // The tile's tokens and the split of K that take the least time: waves of

@@ -307,3 +307,45 @@ def test_refusals(jarq):
                 linear(w=p(work) + 4), linear(x=None)):
         assert got == jarq.JARQ_ERR_ARG
     torch.cuda.synchronize()
+
+
+def test_a_wait_that_gives_up_is_reported_once(jarq):
+    """The product's form whose issuer stops early: its waits run out, the call
+    reports it, and the next products are right."""
+    assert jarq.async_status() == jarq.JARQ_OK
+    assert jarq.selftest_stalled_kernel("integer_product") == jarq.JARQ_ERR_TIMEOUT
+    assert jarq.async_status() == jarq.JARQ_OK
+    rng = np.random.default_rng(8)
+    X, C = _codes(rng, 300, 1024), _codes(rng, 700, 1024)
+    xs, ws = rng.random(300).astype(np.float32), rng.random(700).astype(np.float32)
+    t = lambda a: torch.as_tensor(a).cuda()
+    _check(jarq.integer_product(t(X), t(xs), t(C), t(ws), dtype="float32"), X, xs, C, ws, 0, None, "float32")
+
+
+# every form of the product: tiles of 32 to 256 tokens, K split over a cluster or
+# not, one or several tiles a cluster, rows on 16-byte boundaries or not
+@pytest.mark.parametrize("pitch", [0, 1])
+@pytest.mark.parametrize("g", [0, 64, 128])
+@pytest.mark.parametrize("n,din,dout", [(3, 512, 300), (20, 2048, 140), (30, 256, 20000), (50, 1152, 200), (60, 384, 20500),
+                                        (110, 2560, 300), (128, 256, 20000), (250, 4096, 260), (700, 384, 2900),
+                                        (1500, 256, 5000)])
+def test_linear_in_every_form(jarq, n, din, dout, g, pitch):
+    rng = np.random.default_rng(n + g)
+    C = _codes(rng, dout, din, 15)
+    X = torch.as_tensor((rng.standard_normal((n, din)) * 2).astype(np.float32)).cuda().half()
+    ws = rng.standard_normal((dout, din // g if g else 1)).astype(np.float32)
+    c, w = _rows(C, din + 16 * (1 - pitch) + pitch), torch.as_tensor(ws).cuda()
+    q, xs = jarq.quantize_rows(X)
+    y = jarq.integer_linear(X, c, w, g, dtype="float32")
+    # in 64 bits on the device; the bound of _check
+    x64, c64 = q.double() * xs.double()[:, None], c.double()
+    w64 = w.double().repeat_interleave(g or din, dim=1)
+    want = x64 @ (c64 * w64).T
+    if g:
+        size = sum((x64[:, i * g:(i + 1) * g] @ (c64 * w64)[:, i * g:(i + 1) * g].T).abs() for i in range(din // g))
+    else:
+        size = want.abs()
+    terms = din // g + 11 if g else 3
+    assert ((y.double() - want).abs() <= terms * 2.0 ** -24 * 1.01 * size + 2.0 ** -24 * want.abs() + 1e-12 * x64.abs().max() * din).all()
+    p = jarq.integer_product(q, xs, c, w, g, dtype="float32")
+    assert ((p.double() - want).abs() <= terms * 2.0 ** -24 * 1.01 * size + 2.0 ** -24 * want.abs() + 1e-12 * x64.abs().max() * din).all()
