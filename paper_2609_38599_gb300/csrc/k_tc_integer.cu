@@ -18,9 +18,11 @@
 // accumulators of 128, one read while the other's MMAs run; smaller tiles
 // alternate two.
 //   warp 0        MMA issuer (of a pair's even CTA)
-//   warps 0, 1, 3 of a pair's odd CTA pass on that a stage is full.  (A release at
-//                 cluster scope holds a warp for some 1300 cycles: done by the
-//                 converters it doubled the time, by one warp it set the pace.)
+//   warps 0, 1, 3 of a pair's odd CTA pass on that a stage is full, where tokens are
+//                 converted.  (Shared memory written for the other CTA's MMAs takes a
+//                 release at cluster scope, which holds a warp for some 1300 cycles:
+//                 done by the converters it doubled the time, by one warp it set the
+//                 pace.  TMEM alone is ordered by the tcgen05 fences and an arrival.)
 //   warp 1        TMEM allocation
 //   warp 2        TMA producer: codes as they are into a ring of their own
 //   warp 3        TMA producer of tokens that are fp16
@@ -233,7 +235,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
     constexpr int kCols = kAcc / 2;             // columns of a drain warp in an accumulator
     constexpr bool kShare = !kPair && !HALF;    // the tokens' converters have time for channels
     // warps that convert a stage, and those of a pair's odd CTA that pass it on
-    constexpr int kConverters = HALF ? 4 : B::convert / 32, kRelays = HALF ? 2 : 3;
+    constexpr int kConverters = HALF ? 4 : B::convert / 32, kRelays = 3;
     constexpr int kBars = 2 * kStages + 2 * kAccs + 2 * kRaws + 1;
     constexpr uint32_t kIdesc = tc::idesc_f16_f32(kChannels, kAcc);
     extern __shared__ uint8_t smem_raw[];
@@ -264,8 +266,9 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
-            // own converters; in the issuer's CTA the other's relay, and the bytes of both CTAs' fp16 tokens
-            tc::mbar_init(full(s), kConverters + (rank == 0 ? (kPair ? 1 : 0) + (HALF ? 1 : 0) : 0));
+            // own converters and the other CTA's relay; with fp16 tokens, in the
+            // issuer's CTA only, both CTAs' converters and the tokens' bytes
+            tc::mbar_init(full(s), HALF ? ctas(NT) * kConverters + 1 : kConverters + (kPair && rank == 0));
             tc::mbar_init(empty(s), 1);
         }
         for (int b = 0; b < kAccs; ++b) {
@@ -348,7 +351,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
             for (int tile = cluster; tile < ntiles && ok; tile += nclusters)
                 for (int step = 0, in_unit = 0; step < nsteps && ok; ++step, in.next()) {
                     if (kStalled && unit > 0) break;
-                    ok = kPair ? wait_cluster<kPolls>(full(in.s), in.phase) : tc::mbar_wait<kPolls>(full(in.s), in.phase);
+                    ok = kPair && !HALF ? wait_cluster<kPolls>(full(in.s), in.phase) : tc::mbar_wait<kPolls>(full(in.s), in.phase);
                     if (!ok) break;
                     tc::tc_fence_after();
                     const int atoms = min(2, natoms - 2 * step);
@@ -368,7 +371,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
                     tc::mma_commit(closing);
             }
             if (!tc::mbar_wait<kPolls>(closing, 0) || !ok) *abort_flag = 1;
-        } else if (kPair && rank == 1 && (warp < 2 || (warp == 3 && !HALF))) {
+        } else if (kPair && !HALF && rank == 1 && warp != 2) {
             // ---------------- relays of the odd CTA: its stages are full, in turn
             const uint32_t full0 = tc::map_rank(full(0), even);
             const int me = warp == 3 ? 2 : warp;
@@ -461,6 +464,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
     } else if (warp < 8 || (HALF && warp < kDrain0)) {
         if constexpr (B::splits) registers_down<B::conv>();
         // ---------------- channels: raw ring -> fp16 -> TMEM
+        const uint32_t full0 = tc::map_rank(full(0), even);
         bool ok = true, turn = warp >= 8;
         Slot<kRaws> in(0);
         Slot<kStages> out(1);
@@ -477,7 +481,10 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
                 tc::tc_fence_before();
                 __syncwarp();
                 if (lane == 0) {
-                    tc::mbar_arrive(full(out.s));
+                    if (kPair && HALF)
+                        tc::mbar_arrive_cluster(full0 + 8 * out.s);
+                    else
+                        tc::mbar_arrive(full(out.s));
                     tc::mbar_arrive(raw_empty(in.s));
                 }
             }
