@@ -28,7 +28,7 @@ FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", 
 # for registers that never come.
 LAUNCH_REGISTERS = {"k_tc_integer.cu": tuple(
     (f"tc_integer_kernelILi{nt}ELb{groups}ELb{vec}ELb{half}E", registers)
-    for nt, vec, half, registers in ((256, 1, 0, 96), (256, 1, 1, 128), (128, 0, 0, 72), (128, 0, 1, 72))
+    for nt, vec, half, registers in ((256, 1, 1, 128), (128, 0, 0, 72), (128, 0, 1, 72))
     for groups in (0, 1))}
 
 

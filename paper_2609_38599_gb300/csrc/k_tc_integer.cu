@@ -65,14 +65,18 @@ __host__ __device__ constexpr int stage_bytes(int nt) { return own_tokens(nt) * 
 // (the channels alone where tokens are fp16)
 __host__ __device__ constexpr int raw_bytes(int nt, bool half) { return (128 + (half ? 0 : own_tokens(nt))) * kStepK; }
 __host__ __device__ constexpr int raw_stages(int nt, bool half) {
-    return half ? (nt == 256 ? 6 : nt == 32 ? 11 : 9) : nt == 256 ? 3 : nt == 32 ? 9 : 6;
+    return half ? (nt == 256 ? 4 : nt == 32 ? 11 : 9) : nt == 32 ? 8 : 6;
 }
+// columns of a drain warp that are written out at a time, and the room for those
+// of all: 128 channels x two halves, float32
+__host__ __device__ constexpr int out_cols(int nt) { return nt == 256 ? 32 : 16; }
+__host__ __device__ constexpr int out_bytes(int nt) { return 2 * out_cols(nt) * 128 * 4; }
 __host__ __device__ constexpr int ring_bytes(int nt, bool half) {
     return kStages * stage_bytes(nt) + raw_stages(nt, half) * raw_bytes(nt, half);
 }
-__host__ __device__ constexpr int smem_bytes(int nt, bool half) { return 1024 + ring_bytes(nt, half) + 512; }
+__host__ __device__ constexpr int smem_bytes(int nt, bool half) { return 1024 + ring_bytes(nt, half) + out_bytes(nt) + 512; }
 constexpr bool rings_fit(bool half) {
-    for (int nt : {32, 64, 128, 256})
+    for (int nt = 32; nt <= (half ? 256 : 128); nt *= 2)
         if (smem_bytes(nt, half) > 227 * 1024 || 8 * (2 * kStages + 2 * kAccs + 2 * raw_stages(nt, half) + 1) + 8 > 512)
             return false;
     return true;
@@ -85,14 +89,15 @@ static_assert(rings_fit(false) && rings_fit(true), "rings and barriers must fit 
 // `launch` registers that the launch bounds leave, and the build checks its count.
 template <int NT, bool VEC, bool HALF>
 struct Block {
-    // one stage of fp16 tokens takes four converting warps 600 of the 1024 cycles of
-    // its MMAs at 256 tokens, and the drain can hold a whole part besides its sums
-    static constexpr bool lean = NT == 256 && HALF;
+    // 256 tokens, fp16 only: a stage takes four converting warps 600 of the 1024
+    // cycles of its MMAs, and the drain can hold a whole part besides its sums
+    static constexpr bool lean = NT == 256;
+    static_assert(!lean || (VEC && HALF), "tiles of 256 tokens: fp16 tokens and aligned channels");
     static constexpr int convert = lean ? 128 : 256;
     static constexpr int threads = 128 + convert + kDrain + (VEC ? 0 : kFill);
-    static constexpr bool splits = NT == 256 || (NT == 128 && !VEC);
+    static constexpr bool splits = lean || (NT == 128 && !VEC);
     static constexpr int launch = lean ? 128 : VEC ? 96 : 72;
-    static constexpr int few = 48, conv = lean ? 64 : 56, drain = lean ? 200 : VEC ? 160 : 112, fill = 56;
+    static constexpr int few = 48, conv = lean ? 64 : 56, drain = lean ? 200 : 112, fill = 56;
     static_assert(!splits || 128 * few + convert * conv + kDrain * drain + (VEC ? 0 : kFill * fill) <= launch * threads,
                   "the roles' registers must fit the block's");
 };
@@ -202,6 +207,56 @@ __device__ __forceinline__ void convert_channels(uint32_t raw, uint32_t tmem, in
     }
 }
 
+// The drain warps meet; all of them go on only if `ok` in each.
+__device__ __forceinline__ void drain_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(kDrain) : "memory"); }
+__device__ __forceinline__ bool all_drain_warps(bool ok) {
+    uint32_t r;
+    asm volatile(
+        "{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.and.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(r)
+        : "r"((uint32_t)ok), "n"(kDrain)
+        : "memory");
+    return r != 0;
+}
+
+// 2 kOut tokens x 128 channels of staged sums (float32, or int32 without groups),
+// scaled, to Y: rows e < kOut are tokens first + e, the others kCols further on.
+// Thread t of 256: channels oc .. oc + 7 of every 16th token.
+template <bool GROUPS, int kOut, int kCols>
+__device__ __forceinline__ void write_out(const ProductArgs &a, uint32_t staged, int t, int first, int oc,
+                                          const float (&scale)[8], const float (&bias)[8]) {
+    const size_t size = a.dtype == JARQ_F32 ? 4 : 2;
+    const bool vector = oc + 8 <= a.dout && (((uintptr_t)a.Y | (size_t)a.ldy * size) & 15) == 0;
+#pragma unroll 1
+    for (int r = t >> 4; r < 2 * kOut; r += 16) {
+        const int tk = first + (r < kOut ? r : r - kOut + kCols);
+        if (tk >= a.n || oc >= a.dout) continue;
+        const uint32_t at = staged + (uint32_t)(r * 128 + 8 * (t & 15)) * 4;
+        const uint4 lo = load_shared(at), hi = load_shared(at + 16);
+        const uint32_t raw[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+        const float xs = a.xs[tk];
+        float y[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            y[j] = fmaf(GROUPS ? __uint_as_float(raw[j]) : (float)(int)raw[j] * scale[j], xs, bias[j]);
+        char *p = static_cast<char *>(a.Y) + ((size_t)tk * a.ldy + oc) * size;
+        if (vector && a.dtype == JARQ_F32) {
+            reinterpret_cast<float4 *>(p)[0] = make_float4(y[0], y[1], y[2], y[3]);
+            reinterpret_cast<float4 *>(p)[1] = make_float4(y[4], y[5], y[6], y[7]);
+        } else if (vector) {
+            *reinterpret_cast<uint4 *>(p) = a.dtype == JARQ_F16 ? pack(y, __half()) : pack(y, __nv_bfloat16());
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (oc + j < a.dout)
+                    with_type_device(a.dtype, [&](auto type) {
+                        using T = decltype(type);
+                        reinterpret_cast<T *>(p)[j] = from_float<T>(y[j]);
+                    });
+        }
+    }
+}
+
 // A position in a ring of N stages.
 template <int N>
 struct Slot {
@@ -240,7 +295,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
     constexpr uint32_t kIdesc = tc::idesc_f16_f32(kChannels, kAcc);
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    uint64_t *bars = (uint64_t *)(smem + ring_bytes(NT, HALF));
+    uint64_t *bars = (uint64_t *)(smem + ring_bytes(NT, HALF) + out_bytes(NT));
     uint32_t *tmem_slot = (uint32_t *)(bars + kBars);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -262,7 +317,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
     auto raw_full = [&](int s) { return tc::smem_u32(bars + 2 * kStages + 2 * kAccs + s); };
     auto raw_empty = [&](int s) { return tc::smem_u32(bars + 2 * kStages + 2 * kAccs + kRaws + s); };
     const uint32_t closing = tc::smem_u32(bars + kBars - 1);
-    const uint32_t ring = tc::smem_u32(smem), raws = ring + kStages * kStage;
+    const uint32_t ring = tc::smem_u32(smem), raws = ring + kStages * kStage, staged = ring + ring_bytes(NT, HALF);
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
@@ -618,6 +673,8 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
                     }
                 }
             }
+            // all drain warps or none go on: the rest meets at barriers
+            ok = all_drain_warps(ok);
             if (!ok) break;
             if (split > 1) {
                 // every MMA of the pair is done: its ring takes the partial sums
@@ -630,27 +687,30 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
                                      : "memory");
                 break;                                       // joined below: one tile a cluster
             }
-            // the tokens' scales, a lane a column, shared by shuffles: a load of
-            // each beside the stores took 230 cycles a column
-            const float wch = GROUPS ? 1.f : wp[0], bias = a.bias && live ? a.bias[o] : 0.f;
+            // Out through shared memory, a few columns of each warp at a time: a
+            // thread scales eight channels of a token.  (Each value scaled and stored
+            // from its register, code without a loop, took 16000 cycles a tile.)
+            constexpr int kOut = out_cols(NT);
+            const int t = threadIdx.x - 32 * kDrain0, oc = tile % mt * kChannels + 128 * rank + 8 * (t & 15);
+            float scale[8], bias[8];
 #pragma unroll
-            for (int h = 0; h < kParts; ++h) {
-                const int tk = t0 + h * kAcc + col0;
-                constexpr int kLanes = (kCols + 31) / 32;
-                float xs[kLanes];
-#pragma unroll
-                for (int i = 0; i < kLanes; ++i) xs[i] = tk + 32 * i + lane < a.n ? a.xs[tk + 32 * i + lane] : 0.f;
-                with_type_device(a.dtype, [&](auto type) {
-                    using T = decltype(type);
-                    T *y = static_cast<T *>(a.Y) + (size_t)tk * a.ldy + o;
-#pragma unroll
-                    for (int e = 0; e < kCols; ++e) {
-                        const float x = __shfl_sync(0xffffffffu, xs[e / 32], e % 32);
-                        const float v = GROUPS ? __uint_as_float(acc[h][e]) : (float)(int)acc[h][e] * wch;
-                        if (live && tk + e < a.n) y[(size_t)e * a.ldy] = from_float<T>(fmaf(v, x, bias));
-                    }
-                });
+            for (int j = 0; j < 8; ++j) {
+                scale[j] = !GROUPS && oc + j < a.dout ? a.ws[oc + j] : 1.f;
+                bias[j] = a.bias && oc + j < a.dout ? a.bias[oc + j] : 0.f;
             }
+#pragma unroll
+            for (int h = 0; h < kParts; ++h)
+#pragma unroll
+                for (int c0 = 0; c0 < kCols; c0 += kOut) {
+#pragma unroll
+                    for (int e = 0; e < kOut; ++e)
+                        asm volatile("st.shared.u32 [%0], %1;" ::"r"(staged + (uint32_t)(((w >> 2) * kOut + e) * 128 + lrow) * 4),
+                                     "r"(acc[h][c0 + e])
+                                     : "memory");
+                    drain_barrier();
+                    write_out<GROUPS, kOut, kCols>(a, staged, t, t0 + h * kAcc + c0, oc, scale, bias);
+                    drain_barrier();
+                }
         }
         if (!ok) *abort_flag = 1;
     } else {
@@ -812,12 +872,13 @@ cudaError_t launch_scales(const ProductArgs &a, int split, int *failed, cudaStre
 }
 template <int NT>
 cudaError_t launch_nt(const ProductArgs &a, int split, int *failed, cudaStream_t s, bool pdl) {
-    constexpr int any = NT == 256 ? 128 : NT;       // eight more warps fill the ring: no registers left for 256 tokens
-    if (a.half)
+    if constexpr (NT == 256) return launch_scales<256, true, true>(a, split, failed, s, pdl);
+    else if (a.half)
         return vector_codes(a) ? launch_scales<NT, true, true>(a, split, failed, s, pdl)
-                               : launch_scales<any, false, true>(a, split, failed, s, pdl);
-    return vector_rows(a) ? launch_scales<NT, true, false>(a, split, failed, s, pdl)
-                          : launch_scales<any, false, false>(a, split, failed, s, pdl);
+                               : launch_scales<NT, false, true>(a, split, failed, s, pdl);
+    else
+        return vector_rows(a) ? launch_scales<NT, true, false>(a, split, failed, s, pdl)
+                              : launch_scales<NT, false, false>(a, split, failed, s, pdl);
 }
 
 }  // namespace
@@ -840,7 +901,7 @@ cudaError_t launch_tc_integer(const ProductArgs &a, int *failed, cudaStream_t s,
     int nt = 0, split = 1;
     double best = 0;
     for (const auto &k : kinds) {
-        if (k.nt == 256 && !vec) continue;
+        if (k.nt == 256 && !(vec && a.half)) continue;
         for (int sp = 1; sp <= std::min(kMostParts, steps); ++sp) {
             const int channels = 128 * ctas(k.nt), at_once = std::max(1, resident[ctas(k.nt) * sp] * sms / 152);
             const int64_t tiles = (int64_t)((a.dout + channels - 1) / channels) * ((a.n + k.nt - 1) / k.nt);
