@@ -74,7 +74,7 @@ __host__ __device__ constexpr int out_bytes(int nt) { return 2 * out_cols(nt) * 
 __host__ __device__ constexpr int ring_bytes(int nt, bool half) {
     return kStages * stage_bytes(nt) + raw_stages(nt, half) * raw_bytes(nt, half);
 }
-__host__ __device__ constexpr int smem_bytes(int nt, bool half) { return 1024 + ring_bytes(nt, half) + out_bytes(nt) + 512; }
+__host__ __device__ constexpr int smem_bytes(int nt, bool half) { return 1024 + ring_bytes(nt, half) + out_bytes(nt) + nt * 4 + 512; }
 constexpr bool rings_fit(bool half) {
     for (int nt = 32; nt <= (half ? 256 : 128); nt *= 2)
         if (smem_bytes(nt, half) > 227 * 1024 || 8 * (2 * kStages + 2 * kAccs + 2 * raw_stages(nt, half) + 1) + 8 > 512)
@@ -219,42 +219,76 @@ __device__ __forceinline__ bool all_drain_warps(bool ok) {
     return r != 0;
 }
 
+// Whether eight channels of a token, the first a multiple of eight, are whole 16 bytes of Y.
+__device__ __forceinline__ bool vector_out(const ProductArgs &a) {
+    return (((uintptr_t)a.Y | (size_t)a.ldy * (a.dtype == JARQ_F32 ? 4 : 2)) & 15) == 0;
+}
+// Channel j of drain thread t in write_out: eight in a row, or four 32 apart.
+__device__ __forceinline__ int out_channel(bool vector, int t, int j) {
+    return vector ? 8 * (t & 15) + j : (t & 31) + 32 * (j & 3);
+}
+
 // 2 kOut tokens x 128 channels of staged sums (float32, or int32 without groups),
-// scaled, to Y: rows e < kOut are tokens first + e, the others kCols further on.
-// Thread t of 256: channels oc .. oc + 7 of every 16th token.
+// scaled, to Y: rows r < kOut are tokens first + r, the others kCols further on.
+// Threads t of 256; o: the first channel; xs: of token first.
 template <bool GROUPS, int kOut, int kCols>
-__device__ __forceinline__ void write_out(const ProductArgs &a, uint32_t staged, int t, int first, int oc,
-                                          const float (&scale)[8], const float (&bias)[8]) {
+__device__ __forceinline__ void write_out(const ProductArgs &a, uint32_t staged, const float *xs, int t, int first, int o,
+                                          bool vector, const float (&scale)[8], const float (&bias)[8]) {
+    auto token = [&](int r) { return r < kOut ? r : r - kOut + kCols; };
+    auto value = [&](uint32_t raw, float x, int j) {
+        return fmaf(GROUPS ? __uint_as_float(raw) : (float)(int)raw * scale[j], x, bias[j]);
+    };
     const size_t size = a.dtype == JARQ_F32 ? 4 : 2;
-    const bool vector = oc + 8 <= a.dout && (((uintptr_t)a.Y | (size_t)a.ldy * size) & 15) == 0;
+    if (vector) {
+        const int oc = o + 8 * (t & 15);
 #pragma unroll 1
-    for (int r = t >> 4; r < 2 * kOut; r += 16) {
-        const int tk = first + (r < kOut ? r : r - kOut + kCols);
-        if (tk >= a.n || oc >= a.dout) continue;
-        const uint32_t at = staged + (uint32_t)(r * 128 + 8 * (t & 15)) * 4;
-        const uint4 lo = load_shared(at), hi = load_shared(at + 16);
-        const uint32_t raw[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-        const float xs = a.xs[tk];
-        float y[8];
+        for (int r = t >> 4; r < 2 * kOut; r += 16) {
+            const int c = token(r), tk = first + c;
+            if (tk >= a.n || oc >= a.dout) continue;
+            const uint32_t at = staged + (uint32_t)(r * 128 + 8 * (t & 15)) * 4;
+            const uint4 lo = load_shared(at), hi = load_shared(at + 16);
+            const uint32_t raw[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+            const float x = xs[c];
+            float y[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            y[j] = fmaf(GROUPS ? __uint_as_float(raw[j]) : (float)(int)raw[j] * scale[j], xs, bias[j]);
-        char *p = static_cast<char *>(a.Y) + ((size_t)tk * a.ldy + oc) * size;
-        if (vector && a.dtype == JARQ_F32) {
-            reinterpret_cast<float4 *>(p)[0] = make_float4(y[0], y[1], y[2], y[3]);
-            reinterpret_cast<float4 *>(p)[1] = make_float4(y[4], y[5], y[6], y[7]);
-        } else if (vector) {
-            *reinterpret_cast<uint4 *>(p) = a.dtype == JARQ_F16 ? pack(y, __half()) : pack(y, __nv_bfloat16());
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (oc + j < a.dout)
+            for (int j = 0; j < 8; ++j) y[j] = value(raw[j], x, j);
+            char *p = static_cast<char *>(a.Y) + ((size_t)tk * a.ldy + oc) * size;
+            if (oc + 8 > a.dout) {
+#pragma unroll 1
+                for (int j = 0; oc + j < a.dout; ++j)
                     with_type_device(a.dtype, [&](auto type) {
                         using T = decltype(type);
-                        reinterpret_cast<T *>(p)[j] = from_float<T>(y[j]);
+                        float v = y[0];
+#pragma unroll
+                        for (int i = 1; i < 8; ++i) v = i == j ? y[i] : v;
+                        reinterpret_cast<T *>(p)[j] = from_float<T>(v);
                     });
+            } else if (a.dtype == JARQ_F32) {
+                reinterpret_cast<float4 *>(p)[0] = make_float4(y[0], y[1], y[2], y[3]);
+                reinterpret_cast<float4 *>(p)[1] = make_float4(y[4], y[5], y[6], y[7]);
+            } else {
+                *reinterpret_cast<uint4 *>(p) = a.dtype == JARQ_F16 ? pack(y, __half()) : pack(y, __nv_bfloat16());
+            }
         }
+        return;
     }
+    with_type_device(a.dtype, [&](auto type) {
+        using T = decltype(type);
+#pragma unroll 1
+        for (int r = t >> 5; r < 2 * kOut; r += 8) {
+            const int c = token(r), tk = first + c;
+            if (tk >= a.n) continue;
+            const float x = xs[c];
+            T *p = static_cast<T *>(a.Y) + (size_t)tk * a.ldy + o;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int ch = (t & 31) + 32 * j;
+                uint32_t raw;
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(raw) : "r"(staged + (uint32_t)(r * 128 + ch) * 4) : "memory");
+                if (o + ch < a.dout) p[ch] = from_float<T>(value(raw, x, j));
+            }
+        }
+    });
 }
 
 // A position in a ring of N stages.
@@ -295,7 +329,8 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
     constexpr uint32_t kIdesc = tc::idesc_f16_f32(kChannels, kAcc);
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    uint64_t *bars = (uint64_t *)(smem + ring_bytes(NT, HALF) + out_bytes(NT));
+    float *sxs = (float *)(smem + ring_bytes(NT, HALF) + out_bytes(NT));   // the tile's token scales
+    uint64_t *bars = (uint64_t *)(sxs + NT);
     uint32_t *tmem_slot = (uint32_t *)(bars + kBars);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -603,7 +638,8 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
         if constexpr (B::splits) registers_up<B::drain>();
         // ---------------- drain
         tc::pdl_wait();                                      // the tokens' scales
-        const int w = warp - kDrain0, q = w & 3, col0 = (w >> 2) * kCols;
+        float *factors = (float *)(smem + ring_bytes(NT, HALF));   // scale and bias; then staged outputs
+        const int t = threadIdx.x - 32 * kDrain0, w = warp - kDrain0, q = w & 3, col0 = (w >> 2) * kCols;
         const int lrow = 32 * q + lane;
         const uint32_t released = tc::map_rank(aempty(0), even);
         const uint32_t taddr = tmem + ((uint32_t)(32 * q) << 16) + col0;
@@ -612,6 +648,13 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
         for (int tile = cluster; tile < ntiles && ok; tile += nclusters) {
             const int o = tile % mt * kChannels + 128 * rank + lrow, t0 = tile / mt * NT;
             const bool live = o < a.dout;
+            // what the outputs are scaled with, under the products
+            if (t < NT) sxs[t] = t0 + t < a.n ? a.xs[t0 + t] : 0.f;
+            if (t < 128) {
+                const int ch = tile % mt * kChannels + 128 * rank + t;
+                factors[t] = !GROUPS && ch < a.dout ? a.ws[ch] : 1.f;
+                factors[128 + t] = a.bias && ch < a.dout ? a.bias[ch] : 0.f;
+            }
             uint32_t acc[kParts][kCols];                    // int32, or float32 with groups
 #pragma unroll
             for (int h = 0; h < kParts; ++h)
@@ -691,13 +734,14 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
             // thread scales eight channels of a token.  (Each value scaled and stored
             // from its register, code without a loop, took 16000 cycles a tile.)
             constexpr int kOut = out_cols(NT);
-            const int t = threadIdx.x - 32 * kDrain0, oc = tile % mt * kChannels + 128 * rank + 8 * (t & 15);
+            const bool vector = vector_out(a);
             float scale[8], bias[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                scale[j] = !GROUPS && oc + j < a.dout ? a.ws[oc + j] : 1.f;
-                bias[j] = a.bias && oc + j < a.dout ? a.bias[oc + j] : 0.f;
+                scale[j] = factors[out_channel(vector, t, j)];
+                bias[j] = factors[128 + out_channel(vector, t, j)];
             }
+            drain_barrier();
 #pragma unroll
             for (int h = 0; h < kParts; ++h)
 #pragma unroll
@@ -708,7 +752,8 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
                                      "r"(acc[h][c0 + e])
                                      : "memory");
                     drain_barrier();
-                    write_out<GROUPS, kOut, kCols>(a, staged, t, t0 + h * kAcc + c0, oc, scale, bias);
+                    write_out<GROUPS, kOut, kCols>(a, staged, sxs + h * kAcc + c0, t, t0 + h * kAcc + c0, tile % mt * kChannels + 128 * rank,
+                                                   vector, scale, bias);
                     drain_barrier();
                 }
         }
@@ -890,11 +935,12 @@ cudaError_t launch_tc_integer_stalled(const ProductArgs &a, int *failed, cudaStr
 cudaError_t launch_tc_integer(const ProductArgs &a, int *failed, cudaStream_t s, bool pdl) {
     // The tile's tokens and the split of K that take the least time: waves of
     // clusters, each so many steps of 128 of K and what a tile costs besides
-    // (cycles).  Of clusters of four CTAs 36 run at a time, of six 23, of eight 15
+    // (cycles, fitted to 28 layers of 8 to 8000 tokens; within 3 % of the best of
+    // all choices).  Of clusters of four CTAs 36 run at a time, of six 23, of eight 15
     // (occupancy calculator, 152 SMs: a cluster's SMs lie in one GPC).
     constexpr struct {
         int nt, step, tile;
-    } kinds[] = {{32, 450, 4000}, {64, 550, 4000}, {128, 800, 5000}, {256, 1300, 7000}};
+    } kinds[] = {{32, 530, 5000}, {64, 530, 7500}, {128, 530, 10000}, {256, 940, 17000}};
     constexpr int resident[] = {0, 152, 76, 48, 36, 0, 23, 0, 15};
     const bool vec = a.half ? vector_codes(a) : vector_rows(a);
     const int steps = (a.din + kStepK - 1) / kStepK, sms = num_sms();
@@ -907,7 +953,7 @@ cudaError_t launch_tc_integer(const ProductArgs &a, int *failed, cudaStream_t s,
             const int64_t tiles = (int64_t)((a.dout + channels - 1) / channels) * ((a.n + k.nt - 1) / k.nt);
             if (sp > 1 && tiles > at_once) break;
             const double waves = (double)((tiles + at_once - 1) / at_once);
-            const double t = waves * ((steps + sp - 1) / sp) * k.step * (vec ? 1 : 2) + waves * k.tile + (sp > 1 ? 1500 : 0);
+            const double t = waves * ((steps + sp - 1) / sp) * k.step * (vec ? 1 : 2) + waves * k.tile + (sp > 1 ? 500 : 0);
             if (nt == 0 || t < best) {
                 best = t;
                 nt = k.nt;
