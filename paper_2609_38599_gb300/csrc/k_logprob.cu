@@ -473,17 +473,18 @@ struct GradArgs {
     const float *lse, *entropy, *g_logprob, *g_entropy;
     void *dx;
     int64_t ld, ldd;
-    int n, vocab, t, chunks, per;       // CTAs of a row, units of each
+    int n, vocab, t, chunks;            // CTAs of a row
 };
 
 // dx_v = sum_j g_j [v = tokens_j] - p_v (G + g_H (ln p_v + H)), G = sum_j g_j.
-// A CTA writes the second term of `per` 16-byte units of a row, then the tokens
-// among them with both terms.  kSame: logits and gradient have the same
+// A CTA writes the second term of its 16-byte units of a row, four a thread, then
+// the tokens among them with both terms; all its logits are read first.  Bound by
+// memory: 8192 x 32000 bf16 take 1.05 GB.  kSame: logits and gradient have the same
 // alignment.
-constexpr int kThreads = 256;           // of the gradient
+constexpr int kGradThreads = 256, kGradUnits = kAhead * kGradThreads;
 
 template <class T, bool kSame>
-__global__ void __launch_bounds__(kThreads) token_grad_kernel(GradArgs a) {
+__global__ void __launch_bounds__(kGradThreads) token_grad_kernel(GradArgs a) {
     constexpr int E = kUnit<T>;
     __shared__ float sg[kMaxTokens];
     __shared__ int stok[kMaxTokens];
@@ -491,7 +492,13 @@ __global__ void __launch_bounds__(kThreads) token_grad_kernel(GradArgs a) {
     const T *x = static_cast<const T *>(a.x) + (size_t)r * a.ld;
     T *dx = static_cast<T *>(a.dx) + (size_t)r * a.ldd;
     const Row<T> row(x, a.vocab);
-    const int u0 = c * a.per, u1 = min(row.units(), u0 + a.per);
+    const int u0 = c * kGradUnits, u1 = min(row.units(), u0 + kGradUnits);
+    uint4 raw[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+        const int u = u0 + tid + i * kGradThreads;
+        if (u < u1) raw[i] = row.load(u, from_float<T>(0.f));
+    }
     const float lse = a.lse[r], gh = a.g_entropy ? a.g_entropy[r] : 0.f, h = a.g_entropy ? a.entropy[r] : 0.f;
     // the row's tokens: their weights, and the logits of those in this chunk
     // before they may be overwritten
@@ -519,9 +526,12 @@ __global__ void __launch_bounds__(kThreads) token_grad_kernel(GradArgs a) {
         if (a.g_entropy) d -= gh * (p * (lp + h));
         return v == neg_inf() ? 0.f : d;
     };
-    for (int u = u0 + tid; u < u1; u += kThreads) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+        const int u = u0 + tid + i * kGradThreads;
+        if (u >= u1) break;
         float v[E];
-        unpack(row.load(u, from_float<T>(0.f)), v, T());
+        unpack(raw[i], v, T());
 #pragma unroll
         for (int e = 0; e < E; ++e) v[e] = soft(v[e]);
         const int f = row.first(u);
@@ -577,17 +587,16 @@ cudaError_t launch_logprobs(const ScoreArgs &a, jarq_dtype dtype, cudaStream_t s
 cudaError_t launch_grad(GradArgs a, jarq_dtype dtype, cudaStream_t s) {
     const size_t b = size_of(dtype);
     const int units = (int)(((size_t)a.vocab * b + 15) / 16 + 1);
-    a.per = 4 * kThreads;
-    a.chunks = (units + a.per - 1) / a.per;
+    a.chunks = (units + kGradUnits - 1) / kGradUnits;
     const int64_t grid = (int64_t)a.n * a.chunks;
     if (grid > 0x7FFFFFFF) return cudaErrorInvalidValue;
     const bool same = (((uintptr_t)a.x ^ (uintptr_t)a.dx) & 15) == 0 && (a.n == 1 || ((a.ld - a.ldd) * (int64_t)b) % 16 == 0);
     with_type(dtype, [&](auto type) {
         using T = decltype(type);
         if (same)
-            token_grad_kernel<T, true><<<(unsigned)grid, kThreads, 0, s>>>(a);
+            token_grad_kernel<T, true><<<(unsigned)grid, kGradThreads, 0, s>>>(a);
         else
-            token_grad_kernel<T, false><<<(unsigned)grid, kThreads, 0, s>>>(a);
+            token_grad_kernel<T, false><<<(unsigned)grid, kGradThreads, 0, s>>>(a);
         return 0;
     });
     return cudaGetLastError();
@@ -653,7 +662,7 @@ jarq_status jarq_token_logprobs_grad(const void *logits, jarq_dtype dtype, int n
     if (const jarq_status late = async_failure()) return late;
     cudaStream_t st = (cudaStream_t)stream;
     ProfScope ps("token_grad", st);
-    const cudaError_t e = launch_grad({logits, tokens, lse, entropy, g_logprob, g_entropy, dlogits, ld, ldd, n, vocab, t, 0, 0},
+    const cudaError_t e = launch_grad({logits, tokens, lse, entropy, g_logprob, g_entropy, dlogits, ld, ldd, n, vocab, t, 0},
                                       dtype, st);
     ps.done();
     return finish(e);
