@@ -29,7 +29,8 @@
 //   warps 4..7    convert channels: a thread has one channel's row
 //   warps 8..11   convert tokens, and half of the channels' K where tokens are few;
 //                 with fp16 tokens, every other stage's channels
-//   warps 12..19  drain: lane quarter w % 4, half of the columns
+//   warps 12..19  drain: lane quarter w % 4, half of the columns (with kBrief one
+//                 part of a tile)
 //   warps 20..27  only where rows are not on 16-byte boundaries: fill the ring in
 //                 the producer's place
 // A cluster splits K over its CTAs or pairs where there are few tiles; the
@@ -38,23 +39,25 @@
 // Measured from a graph, the quantization of float16 tokens included where tokens
 // x K -> channels is given:
 //   8192 x 11008 -> 4096, one scale    430 us (the product 384: 1.92 PFLOP/s)
-//   4096 x 4096 -> 14336, groups of 128 309 us (1.56 PFLOP/s)
-//   2048 x 4096 -> 4096, groups of 64   79 us, of 128 58, one scale 55
+//   4096 x 4096 -> 14336, groups of 128 297 us (1.62 PFLOP/s)
+//   2048 x 4096 -> 4096, groups of 64   71 us, of 128 55, one scale 54
 //   64 x 4096 -> 4096 9.9 us, 24 x 11008 -> 4096 (45 MB of codes, cold) 17.5 us
 //   int8 tokens given, the product alone: 8192 x 11008 -> 4096 604 us
 // A large product with one scale runs near the rate of a library's product in
 // bfloat16.  With groups a sum leaves the accumulator eight (sixteen) times as often
-// as with one scale, and the hand-over and the scaling of those sums under the MMAs
-// are the bound (4096 x 4096 -> 4096 under a profiler: matrix pipes 60 % busy with
-// one scale, 56 % with groups of 128).
+// as with one scale, and what a scheduler's two drain warps do then (wake, read TMEM,
+// hand back, add) is the bound: at 79 (groups of 64) and 309 us (128) of the sizes
+// above, 61 and 271 were left without seven in eight additions and the scales' loads.
 // Few tokens: the latency of a cluster's chain (first copies, conversion, MMAs,
 // join), then reading the codes.  Rows off 16-byte boundaries are bound by the
 // filling warps' loads (333 x 1001 -> 1343: 13.8 us, aligned 8.7).
 //
 // Tried and dropped: four accumulators of 64 columns (the issuer's own instructions
-// take 1620 of 1024 cycles a stage), the issue loop rolled (619 us for 430), three
-// accumulators with two stages of channels (356 for 340), two sets of converters for
-// small tiles and conversion two units at a time (no gain, 5 % slower).
+// take 1620 of 1024 cycles a stage), the issue loop rolled (619 us for 430), two sets
+// of converters for small tiles and conversion two units at a time (no gain, 5 %
+// slower); in the drain, with groups: the next columns' loads under the additions (92
+// us for 78, since the accumulator is held longer), scales loaded ahead or four at a
+// time (81, 80), scalar additions (79; of 128: 325 for 309).
 #include "integer.cuh"
 #include "rows.cuh"
 #include "tc_common.cuh"
@@ -70,12 +73,19 @@ constexpr int kExact = 16;                    // atoms (1024 of K) with an exact
 constexpr int kStages = 4;
 constexpr int kMostParts = 4;                  // of K, over a cluster
 constexpr int kColsA = 64;                    // TMEM columns of a stage's channels (two fp16 each)
-constexpr int kTmem = 512;                    // two accumulators of up to 128, then kStages kColsA
+constexpr int kTmem = 512;                    // accumulators of up to 128, then stages of channels
 
-// columns of an accumulator, and how many a tile has; two take turns
+// columns of an accumulator, and how many a tile has
 __host__ __device__ constexpr int acc_cols(int nt) { return nt < 128 ? nt : 128; }
 __host__ __device__ constexpr int acc_parts(int nt) { return nt / acc_cols(nt); }
-constexpr int kAccs = 2;
+// Accumulators that take turns, and stages of channels.  With groups of 64 in tiles
+// of 256 tokens (`brief`) an accumulator's MMAs take 256 cycles, less than the way of
+// another's sums to the drain's registers and of the word back: there a third one
+// takes the room of two stages of channels, which with groups of 128 costs more than
+// it gives (2048 x 4096 -> 4096, groups of 64: 78 -> 71 us; 4096 x 4096 -> 14336, of
+// 128: 297 -> 315; with channels handed on 64 of K at a time 73 and 350).
+__host__ __device__ constexpr int accs(bool brief) { return brief ? 3 : 2; }
+__host__ __device__ constexpr int channel_stages(bool brief) { return (kTmem - 128 * accs(brief)) / kColsA; }
 // CTAs of a tile: a pair for many tokens
 __host__ __device__ constexpr int ctas(int nt) { return nt > 64 ? 2 : 1; }
 // a CTA's tokens
@@ -98,7 +108,7 @@ __host__ __device__ constexpr int ring_bytes(int nt, bool half) {
 __host__ __device__ constexpr int smem_bytes(int nt, bool half) { return 1024 + ring_bytes(nt, half) + out_bytes(nt) + nt * 4 + 512; }
 constexpr bool rings_fit(bool half) {
     for (int nt = 32; nt <= (half ? 256 : 128); nt *= 2)
-        if (smem_bytes(nt, half) > 227 * 1024 || 8 * (2 * kStages + 2 * kAccs + 2 * raw_stages(nt, half) + 1) + 8 > 512)
+        if (smem_bytes(nt, half) > 227 * 1024 || 8 * (4 * kStages + 2 * 3 + 2 * raw_stages(nt, half) + 1) + 8 > 512)
             return false;
     return true;
 }
@@ -262,7 +272,7 @@ __device__ __forceinline__ void write_out(const ProductArgs &a, uint32_t staged,
     const size_t size = a.dtype == JARQ_F32 ? 4 : 2;
     if (vector) {
         const int oc = o + 8 * (t & 15);
-#pragma unroll 1
+#pragma unroll
         for (int r = t >> 4; r < 2 * kOut; r += 16) {
             const int c = token(r), tk = first + c;
             if (tk >= a.n || oc >= a.dout) continue;
@@ -326,10 +336,28 @@ struct Slot {
     }
 };
 
+// The accumulators of a unit's parts, N taking turns, and the parity to wait for.
+template <int N, int PARTS>
+struct Turn {
+    int first = 0;
+    uint32_t phase;
+    __device__ explicit Turn(uint32_t p) : phase(p) {}
+    __device__ __forceinline__ int acc(int part) const { return first + part < N ? first + part : first + part - N; }
+    __device__ __forceinline__ uint32_t parity(int part) const { return first + part < N ? phase : phase ^ 1; }
+    __device__ __forceinline__ void next() {
+        first += PARTS;
+        if (first >= N) {
+            first -= N;
+            phase ^= 1;
+        }
+    }
+};
+
 // NT: tokens of a tile.  GROUPS: group scales.  VEC: rows of codes on 16-byte
 // boundaries.  HALF: tokens are integers in fp16, rows on 16-byte boundaries.
+// kBrief: groups of 64, NT 256.
 // kStalled: for the self-test, the issuer stops after one accumulator.
-template <int NT, bool GROUPS, bool VEC, bool HALF, bool kStalled>
+template <int NT, bool GROUPS, bool VEC, bool HALF, bool kBrief, bool kStalled>
 __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
     tc_integer_kernel(const __grid_constant__ CUtensorMap mapC, const __grid_constant__ CUtensorMap mapX, ProductArgs a,
                       int split, int *failed) {
@@ -342,11 +370,18 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
     constexpr int kChannels = 128 * ctas(NT);   // of a tile
     constexpr int kRowsB = kAcc / ctas(NT);     // this CTA's tokens of an accumulator
     constexpr int kAtomB = kRowsB * 128, kHalfB = 2 * kAtomB;
-    constexpr int kCols = kAcc / 2;             // columns of a drain warp in an accumulator
+    // Columns of a drain warp in an accumulator, and how many of a unit's it reads:
+    // half of each, or all of one, where the two warps of a scheduler so take turns
+    // at reading TMEM and at adding
+    constexpr int kCols = kBrief ? kAcc : kAcc / 2, kReads = kBrief ? 1 : kParts;
     constexpr bool kShare = !kPair && !HALF;    // the tokens' converters have time for channels
     // warps that convert a stage, and those of a pair's odd CTA that pass it on
     constexpr int kConverters = HALF ? 4 : B::convert / 32, kRelays = 3;
-    constexpr int kBars = 2 * kStages + 2 * kAccs + 2 * kRaws + 1;
+    constexpr int kAccs = accs(kBrief), kStagesA = channel_stages(kBrief);
+    constexpr bool kApart = kStagesA != kStages;   // channels have barriers of their own
+    static_assert(!kBrief || (GROUPS && B::lean), "converted tokens share their barriers with the channels");
+    constexpr int kBarsA = kApart ? 2 * kStagesA : 0;
+    constexpr int kBars = 2 * kStages + 2 * kAccs + 2 * kRaws + kBarsA + 1;
     constexpr uint32_t kIdesc = tc::idesc_f16_f32(kChannels, kAcc);
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -372,6 +407,8 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
     auto aempty = [&](int b) { return tc::smem_u32(bars + 2 * kStages + kAccs + b); };
     auto raw_full = [&](int s) { return tc::smem_u32(bars + 2 * kStages + 2 * kAccs + s); };
     auto raw_empty = [&](int s) { return tc::smem_u32(bars + 2 * kStages + 2 * kAccs + kRaws + s); };
+    auto full_a = [&](int s) { return kApart ? tc::smem_u32(bars + kBars - 1 - kBarsA + s) : full(s); };
+    auto empty_a = [&](int s) { return kApart ? tc::smem_u32(bars + kBars - 1 - kBarsA + kStagesA + s) : empty(s); };
     const uint32_t closing = tc::smem_u32(bars + kBars - 1);
     const uint32_t ring = tc::smem_u32(smem), raws = ring + kStages * kStage, staged = ring + ring_bytes(NT, HALF);
 
@@ -379,12 +416,16 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
         for (int s = 0; s < kStages; ++s) {
             // own converters and the other CTA's relay; with fp16 tokens, in the
             // issuer's CTA only, both CTAs' converters and the tokens' bytes
-            tc::mbar_init(full(s), HALF ? ctas(NT) * kConverters + 1 : kConverters + (kPair && rank == 0));
+            tc::mbar_init(full(s), kApart ? 1 : HALF ? ctas(NT) * kConverters + 1 : kConverters + (kPair && rank == 0));
             tc::mbar_init(empty(s), 1);
+        }
+        for (int s = 0; s < kBarsA / 2; ++s) {
+            tc::mbar_init(full_a(s), ctas(NT) * kConverters);
+            tc::mbar_init(empty_a(s), 1);
         }
         for (int b = 0; b < kAccs; ++b) {
             tc::mbar_init(afull(b), 1);
-            tc::mbar_init(aempty(b), ctas(NT) * kDrain / 32);   // the even CTA's: both drains
+            tc::mbar_init(aempty(b), ctas(NT) * kDrain / 32 * kReads / kParts);   // the even CTA's: both drains
         }
         for (int s = 0; s < kRaws; ++s) {
             tc::mbar_init(raw_full(s), VEC ? 1 : kFill / 32);
@@ -418,7 +459,9 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
             const uint16_t both = (uint16_t)(3 << even);
             const int us = GROUPS ? max(1, ua / 2) : kExact / 2;     // stages of an accumulator
             Slot<kStages> in(0);
-            int unit = 0;                                    // accumulators so far, over all tiles
+            Slot<kStagesA> chan(0);
+            Turn<kAccs, kParts> turn(1);
+            int unit = 0;                                    // over all tiles
             // `count` atoms from atom `at` of a stage into every part's accumulator
             auto mma = [&](uint32_t d, uint32_t ad, uint64_t bd, uint32_t add) {
                 if (kPair)
@@ -435,15 +478,15 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
             auto issue = [&](int at, int count, bool first, bool last, bool done) {
 #pragma unroll
                 for (int h = 0; h < kParts; ++h) {
-                    const int use = unit * kParts + h, b = use % kAccs;
+                    const int b = turn.acc(h);
                     if (first) {
-                        ok = tc::mbar_wait<kPolls>(aempty(b), (use / kAccs & 1) ^ 1);
+                        ok = tc::mbar_wait<kPolls>(aempty(b), turn.parity(h));
                         if (!ok) return;
                         tc::tc_fence_after();
                     }
                     if (tc::elect_one()) {
                         const uint32_t d = tmem + b * kAcc;
-                        const uint32_t ad = tmem_a + in.s * kColsA + at * 32;
+                        const uint32_t ad = tmem_a + chan.s * kColsA + at * 32;
                         const uint64_t bd = bd0 + (uint32_t)((in.s * kStage + h * kHalfB + at * kAtomB) >> 4);
 #pragma unroll
                         for (int sub = 0; sub < 4; ++sub) mma(d, ad + 8 * sub, bd + 2 * sub, !first || sub > 0);
@@ -453,16 +496,21 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
                                 mma(d, ad + 32 + 8 * sub, bd + (kAtomB >> 4) + 2 * sub, 1);
                         }
                         if (last) commit(afull(b));
-                        if (done && h == kParts - 1) commit(empty(in.s));
+                        if (done && h == kParts - 1) {
+                            commit(empty(in.s));
+                            if (kApart) commit(empty_a(chan.s));
+                        }
                     }
                     __syncwarp();
                 }
                 unit += last;
+                if (last) turn.next();
             };
             for (int tile = cluster; tile < ntiles && ok; tile += nclusters)
-                for (int step = 0, in_unit = 0; step < nsteps && ok; ++step, in.next()) {
+                for (int step = 0, in_unit = 0; step < nsteps && ok; ++step, in.next(), chan.next()) {
                     if (kStalled && unit > 0) break;
                     ok = kPair && !HALF ? wait_cluster<kPolls>(full(in.s), in.phase) : tc::mbar_wait<kPolls>(full(in.s), in.phase);
+                    if (kApart) ok = tc::mbar_wait<kPolls>(full_a(chan.s), chan.phase) && ok;
                     if (!ok) break;
                     tc::tc_fence_after();
                     const int atoms = min(2, natoms - 2 * step);
@@ -575,15 +623,15 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
     } else if (warp < 8 || (HALF && warp < kDrain0)) {
         if constexpr (B::splits) registers_down<B::conv>();
         // ---------------- channels: raw ring -> fp16 -> TMEM
-        const uint32_t full0 = tc::map_rank(full(0), even);
+        const uint32_t full0 = tc::map_rank(full_a(0), even);
         bool ok = true, turn = warp >= 8;
         Slot<kRaws> in(0);
-        Slot<kStages> out(1);
+        Slot<kStagesA> out(1);
         for (int tile = cluster; tile < ntiles && ok; tile += nclusters)
             for (int step = 0; step < nsteps; ++step, in.next(), out.next()) {
                 if (HALF && B::convert == 256 && (turn = !turn, !turn)) continue;     // the other four warps' stage
                 ok = tc::mbar_wait<kPolls>(raw_full(in.s), in.phase);
-                ok = tc::mbar_wait<kPolls>(empty(out.s), out.phase) && ok;
+                ok = tc::mbar_wait<kPolls>(empty_a(out.s), out.phase) && ok;
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc::tc_fence_after();
@@ -595,7 +643,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
                     if (kPair && HALF)
                         tc::mbar_arrive_cluster(full0 + 8 * out.s);
                     else
-                        tc::mbar_arrive(full(out.s));
+                        tc::mbar_arrive(full_a(out.s));
                     tc::mbar_arrive(raw_empty(in.s));
                 }
             }
@@ -660,12 +708,12 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
         // ---------------- drain
         tc::pdl_wait();                                      // the tokens' scales
         float *factors = (float *)(smem + ring_bytes(NT, HALF));   // scale and bias; then staged outputs
-        const int t = threadIdx.x - 32 * kDrain0, w = warp - kDrain0, q = w & 3, col0 = (w >> 2) * kCols;
+        const int t = threadIdx.x - 32 * kDrain0, w = warp - kDrain0, q = w & 3, col0 = (w >> 2) * kCols, mine = kBrief ? w >> 2 : 0;
         const int lrow = 32 * q + lane;
         const uint32_t released = tc::map_rank(aempty(0), even);
-        const uint32_t taddr = tmem + ((uint32_t)(32 * q) << 16) + col0;
+        const uint32_t taddr = tmem + ((uint32_t)(32 * q) << 16) + (kBrief ? 0 : col0);
         bool ok = true;
-        int unit = 0;
+        Turn<kAccs, kParts> turn(0);
         for (int tile = cluster; tile < ntiles && ok; tile += nclusters) {
             const int o = tile % mt * kChannels + 128 * rank + lrow, t0 = tile / mt * NT;
             const bool live = o < a.dout;
@@ -676,24 +724,24 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
                 factors[t] = !GROUPS && ch < a.dout ? a.ws[ch] : 1.f;
                 factors[128 + t] = a.bias && ch < a.dout ? a.bias[ch] : 0.f;
             }
-            uint32_t acc[kParts][kCols];                    // int32, or float32 with groups
+            uint32_t acc[kReads][kCols];                    // int32, or float32 with groups
 #pragma unroll
-            for (int h = 0; h < kParts; ++h)
+            for (int h = 0; h < kReads; ++h)
 #pragma unroll
                 for (int e = 0; e < kCols; ++e) acc[h][e] = 0;
             const float *wp = a.ws + (live ? (size_t)o * a.G : 0) + (GROUPS ? 2 * step0 / ua : 0);
-            for (int u = 0; u < nunits && ok; ++u, ++unit) {
+            for (int u = 0; u < nunits && ok; ++u, turn.next()) {
                 const float wsc = GROUPS ? wp[u] : 0.f;
 #pragma unroll
-                for (int h = 0; h < kParts; ++h) {
-                    const int use = unit * kParts + h, b = use % kAccs;
-                    ok = __all_sync(0xffffffffu, tc::mbar_wait<kPolls>(afull(b), use / kAccs & 1)) && ok;
+                for (int h = 0; h < kReads; ++h) {
+                    const int b = turn.acc(h + mine);
+                    ok = __all_sync(0xffffffffu, tc::mbar_wait<kPolls>(afull(b), turn.parity(h + mine))) && ok;
                     if (!ok) break;
                     tc::tc_fence_after();
                     const uint32_t at = taddr + b * kAcc;
                     // the accumulator is handed back once it is in registers: at
-                    // once where they allow, else with its last 16 columns
-                    constexpr int kHeld = B::lean ? kCols : 16;
+                    // once where they allow, else with its last columns
+                    constexpr int kHeld = kBrief ? 32 : B::lean ? kCols : 16;
                     uint32_t v[kHeld < kCols ? 2 : 1][kHeld];
                     auto load = [&](int cc) {
 #pragma unroll
@@ -743,7 +791,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
             if (split > 1) {
                 // every MMA of the pair is done: its ring takes the partial sums
 #pragma unroll
-                for (int h = 0; h < kParts; ++h)
+                for (int h = 0; h < kReads; ++h)
 #pragma unroll
                     for (int e = 0; e < kCols; ++e)
                         asm volatile("st.shared.u32 [%0], %1;" ::"r"(ring + (uint32_t)((h * kAcc + col0 + e) * 128 + lrow) * 4),
@@ -764,7 +812,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
             }
             drain_barrier();
 #pragma unroll
-            for (int h = 0; h < kParts; ++h)
+            for (int h = 0; h < kReads; ++h)
 #pragma unroll
                 for (int c0 = 0; c0 < kCols; c0 += kOut) {
 #pragma unroll
@@ -898,10 +946,10 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
     }
 }
 
-template <int NT, bool GROUPS, bool VEC, bool HALF, bool kStalled = false>
+template <int NT, bool GROUPS, bool VEC, bool HALF, bool kBrief = false, bool kStalled = false>
 cudaError_t launch(const ProductArgs &a, int split, int *failed, cudaStream_t s, bool pdl) {
     static std::atomic<unsigned long long> done;
-    auto *kernel = tc_integer_kernel<NT, GROUPS, VEC, HALF, kStalled>;
+    auto *kernel = tc_integer_kernel<NT, GROUPS, VEC, HALF, kBrief, kStalled>;
     cudaError_t e = set_max_dynamic_smem((const void *)kernel, smem_bytes(NT, HALF), done);
     if (e != cudaSuccess) return e;
     CUtensorMap mapC = {}, mapX = {};
@@ -934,6 +982,8 @@ cudaError_t launch(const ProductArgs &a, int split, int *failed, cudaStream_t s,
 
 template <int NT, bool VEC, bool HALF>
 cudaError_t launch_scales(const ProductArgs &a, int split, int *failed, cudaStream_t s, bool pdl) {
+    if constexpr (NT == 256)
+        if (a.g == 64) return launch<NT, true, VEC, HALF, true>(a, split, failed, s, pdl);
     return a.g ? launch<NT, true, VEC, HALF>(a, split, failed, s, pdl) : launch<NT, false, VEC, HALF>(a, split, failed, s, pdl);
 }
 template <int NT>
@@ -950,7 +1000,7 @@ cudaError_t launch_nt(const ProductArgs &a, int split, int *failed, cudaStream_t
 }  // namespace
 
 cudaError_t launch_tc_integer_stalled(const ProductArgs &a, int *failed, cudaStream_t s) {
-    return launch<256, false, true, true, true>(a, 1, failed, s, false);
+    return launch<256, false, true, true, false, true>(a, 1, failed, s, false);
 }
 
 cudaError_t launch_tc_integer(const ProductArgs &a, int *failed, cudaStream_t s, bool pdl) {

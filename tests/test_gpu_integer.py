@@ -349,3 +349,29 @@ def test_linear_in_every_form(jarq, n, din, dout, g, pitch):
     assert ((y.double() - want).abs() <= terms * 2.0 ** -24 * 1.01 * size + 2.0 ** -24 * want.abs() + 1e-12 * x64.abs().max() * din).all()
     p = jarq.integer_product(q, xs, c, w, g, dtype="float32")
     assert ((p.double() - want).abs() <= terms * 2.0 ** -24 * 1.01 * size + 2.0 ** -24 * want.abs() + 1e-12 * x64.abs().max() * din).all()
+
+
+# groups of 64 with many tokens: an odd number of groups, one and several tiles a
+# cluster, K split or not; every output against 64 bits on the device.  The bound is
+# _check's: G products and G - 1 additions in float32, and the three roundings of
+# the token's scale, the bias and the output.
+@pytest.mark.parametrize("n,din,dout", [(600, 64, 2900), (1500, 192, 5000), (700, 1088, 1300), (2100, 320, 5003), (513, 4160, 520),
+                                        (4000, 576, 9000)])
+def test_odd_numbers_of_groups(jarq, n, din, dout):
+    g = 64
+    rng = np.random.default_rng(n + din)
+    c = _rows(_codes(rng, dout, din, 15))
+    w = torch.as_tensor(rng.standard_normal((dout, din // g)).astype(np.float32)).cuda()
+    X = torch.as_tensor((rng.standard_normal((n, din)) * 2).astype(np.float32)).cuda().half()
+    q, xs = jarq.quantize_rows(X)
+    y = jarq.integer_linear(X, c, w, g, dtype="float32").double()
+    want, size = torch.zeros_like(y), torch.zeros_like(y)
+    for i in range(din // g):
+        part = (q[:, i * g:(i + 1) * g].double() @ c[:, i * g:(i + 1) * g].double().T) * w[:, i].double()
+        want += part
+        size += part.abs()
+    want *= xs.double()[:, None]
+    size *= xs.double()[:, None]
+    bound = (2 * (din // g) + 3) * 2.0 ** -24 * 1.01 * size + 1e-30
+    assert ((y - want).abs() <= bound).all()
+    assert torch.equal(y, jarq.integer_linear(X, c, w, g, dtype="float32").double())
