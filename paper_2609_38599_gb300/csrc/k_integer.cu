@@ -7,9 +7,11 @@
 // of these channels or the following ones, on their way while these are used and
 // their sums joined.  With one scale a channel the sums are int32 (exact for din <=
 // 65536); with groups (a multiple of 16) each product of 16 is scaled into a float32
-// sum.  One token, 4096 -> 11008 (45 MB), quantization included: 11.1 us from cold
-// memory (4.1 TB/s), 7.3 us from L2; 4096 -> 4096 6.1 and 4.7 us.
+// sum.  A linear layer's single token is quantized by every block for itself, under
+// its first weights' loads.  One token, 4096 -> 11008 (45 MB), quantization included:
+// 10.0 us from cold memory (4.5 TB/s), 7.3 us from L2; 4096 -> 4096 5.9 and 4.7 us.
 #include "integer.cuh"
+#include "quantize.cuh"
 #include "rows.cuh"
 #include "tc_common.cuh"
 
@@ -19,6 +21,12 @@ namespace {
 using namespace rows;
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
+// Longest row that a single token's blocks quantize for themselves (from a graph,
+// cold and warm, against a launch of its own: 4096 -> 11008 10.0 and 7.3 us, 11.1 and
+// 7.3; 6144 -> 8192 12.0 and 8.1, 14.1 and 8.0; 8192 -> 4096 9.1 and 7.1, 9.2 and 6.3;
+// 11008 -> 4096 15.5 and 10.9, 14.5 and 9.3).  The host's time of a call falls by
+// 4 us of 18.  Two tokens' blocks would lose (2 x 4096 -> 1000: 4.6 us for 3.6).
+constexpr int kOwnCodes = 6144;
 
 // Sums of V values over the lanes of a warp: value i ends in lane 32 / V i.
 template <int V>
@@ -42,11 +50,31 @@ __device__ __forceinline__ float warp_sums(float (&v)[V], int lane) {
     return v[0];
 }
 
-// M: tokens (a.n <= M); R: channels that a block has at a time.
-template <int M, int R, bool GROUPS, bool VEC>
-__global__ void __launch_bounds__(kThreads) few_tokens_kernel(ProductArgs a) {
+// A row of activations to codes q in shared memory, by a block; its scale.
+template <class T>
+__device__ __forceinline__ float quantize_row(const T *x, int d, int8_t *q, uint32_t (&part)[kWarps]) {
+    const Row<T> row(x, d);
+    const int units = row.units();
+    quant::Largest<T> largest;
+    for (int u = threadIdx.x; u < units; u += kThreads) largest.take(row.load(u, T(0.f)));
+    uint32_t top = __reduce_max_sync(0xffffffffu, largest.bits());
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) top = max(top, part[w]);
+    const quant::RowScale by(top);
+    for (int u = threadIdx.x; u < units; u += kThreads) quant::put_codes(row, u, row.load(u, T(0.f)), by, q);
+    __syncthreads();
+    return by.scale;
+}
+
+// M: tokens (a.n <= M); R: channels that a block has at a time.  OWN: the token
+// is activations of type `xtype`, which each block quantizes for itself.
+template <int M, int R, bool GROUPS, bool VEC, bool OWN>
+__global__ void __launch_bounds__(kThreads) few_tokens_kernel(ProductArgs a, jarq_dtype xtype) {
     constexpr int V = M * R;
     __shared__ uint32_t parts[2][kWarps][V];
+    __shared__ uint32_t tops[kWarps];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int chunks = (a.din + 15) / 16, step = gridDim.x * R;
     const int shift = a.g == 64 ? 2 : 3;      // 16-code chunks of a group: 4 or 8
@@ -58,8 +86,22 @@ __global__ void __launch_bounds__(kThreads) few_tokens_kernel(ProductArgs a) {
     for (int r = 0; r < R; ++r) w[r] = make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int r = 0; r < R; ++r) fetch(r, blockIdx.x * R + r, tid);
-    // the tokens' codes may be the previous kernel's
-    tc::pdl_wait();
+    extern __shared__ __align__(16) int8_t own[];
+    const int8_t *X = static_cast<const int8_t *>(a.X);
+    float scale[M];
+    static_assert(M == 1 || !OWN, "one token");
+    if constexpr (OWN) {
+        X = own;
+        with_type_device(xtype, [&](auto type) {
+            using T = decltype(type);
+            scale[0] = quantize_row(static_cast<const T *>(a.X), a.din, own, tops);
+        });
+    } else {
+        // the tokens' codes may be the previous kernel's
+        tc::pdl_wait();
+#pragma unroll
+        for (int m = 0; m < M; ++m) scale[m] = a.xs[min(m, a.n - 1)];
+    }
     for (int o0 = blockIdx.x * R, turn = 0; o0 < a.dout; o0 += step, turn ^= 1) {
         int sum[V] = {};
         float acc[V] = {};
@@ -71,7 +113,7 @@ __global__ void __launch_bounds__(kThreads) few_tokens_kernel(ProductArgs a) {
             uint4 x[M];
 #pragma unroll
             for (int m = 0; m < M; ++m)
-                x[m] = load_codes<VEC>(static_cast<const int8_t *>(a.X) + (size_t)min(m, a.n - 1) * a.ldx, 16 * c, a.din);
+                x[m] = load_codes<VEC || OWN>(X + min(m, a.n - 1) * (size_t)a.ldx, 16 * c, a.din);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const uint4 wr = w[r];
@@ -112,7 +154,10 @@ __global__ void __launch_bounds__(kThreads) few_tokens_kernel(ProductArgs a) {
                 i += (int)parts[turn][p][tid];
             }
             const float v = GROUPS ? f : (float)i * a.ws[o];
-            const float y = fmaf(v, a.xs[m], a.bias ? a.bias[o] : 0.f);
+            float xs = scale[0];
+#pragma unroll
+            for (int j = 1; j < M; ++j) xs = j == m ? scale[j] : xs;
+            const float y = fmaf(v, xs, a.bias ? a.bias[o] : 0.f);
             with_type_device(a.dtype, [&](auto type) {
                 using T = decltype(type);
                 static_cast<T *>(a.Y)[(size_t)m * a.ldy + o] = from_float<T>(y);
@@ -121,23 +166,24 @@ __global__ void __launch_bounds__(kThreads) few_tokens_kernel(ProductArgs a) {
     }
 }
 
-template <int M, int R>
-cudaError_t launch_few(const ProductArgs &a, cudaStream_t s, bool pdl) {
+template <int M, int R, bool OWN>
+cudaError_t launch_few(const ProductArgs &a, jarq_dtype xtype, cudaStream_t s, bool pdl) {
     // no more blocks than stay resident (cold weights, one token, 4096 -> 11008 with
     // quantization: 11.1 us, 12.7 with a block for each four channels)
     const int groups = (a.dout + R - 1) / R, resident = (M == 1 ? 4 : 2) * num_sms();
     const dim3 grid(groups < resident ? groups : resident);
-    const bool vec = vector_rows(a);
-    if (a.g)
-        return vec ? launch_k(few_tokens_kernel<M, R, true, true>, grid, dim3(kThreads), 0, s, pdl, a)
-                   : launch_k(few_tokens_kernel<M, R, true, false>, grid, dim3(kThreads), 0, s, pdl, a);
-    return vec ? launch_k(few_tokens_kernel<M, R, false, true>, grid, dim3(kThreads), 0, s, pdl, a)
-               : launch_k(few_tokens_kernel<M, R, false, false>, grid, dim3(kThreads), 0, s, pdl, a);
+    const size_t smem = OWN ? round_up(a.din, 16) : 0;
+    const bool vec = OWN ? vector_codes(a) : vector_rows(a);
+    auto run = [&](auto kernel) { return launch_k(kernel, grid, dim3(kThreads), smem, s, pdl, a, xtype); };
+    if (a.g) return vec ? run(few_tokens_kernel<M, R, true, true, OWN>) : run(few_tokens_kernel<M, R, true, false, OWN>);
+    return vec ? run(few_tokens_kernel<M, R, false, true, OWN>) : run(few_tokens_kernel<M, R, false, false, OWN>);
 }
 
-cudaError_t launch_product(const ProductArgs &a, int *failed, cudaStream_t s, bool pdl) {
-    if (a.n == 1) return launch_few<1, 4>(a, s, pdl);
-    if (a.n <= kFewTokens) return launch_few<2, 8>(a, s, pdl);
+// xtype: of one token's activations in the codes' place, or null
+cudaError_t launch_product(const ProductArgs &a, const jarq_dtype *xtype, int *failed, cudaStream_t s, bool pdl) {
+    if (xtype) return launch_few<1, 4, true>(a, *xtype, s, false);
+    if (a.n == 1) return launch_few<1, 4, false>(a, JARQ_F32, s, pdl);
+    if (a.n <= kFewTokens) return launch_few<2, 8, false>(a, JARQ_F32, s, pdl);
     return launch_tc_integer(a, failed, s, pdl);
 }
 
@@ -153,11 +199,11 @@ jarq_status check_layer(const int8_t *C, int64_t ldc, const float *ws, int group
     return JARQ_OK;
 }
 
-jarq_status run_product(const ProductArgs &a, cudaStream_t st, bool pdl) {
+jarq_status run_product(const ProductArgs &a, const jarq_dtype *xtype, cudaStream_t st, bool pdl) {
     int *failed = async_word();
     if (!failed) return JARQ_ERR_NOMEM;
     ProfScope ps("integer_product", st);
-    const cudaError_t e = launch_product(a, failed, st, pdl);
+    const cudaError_t e = launch_product(a, xtype, failed, st, pdl);
     ps.done();
     count_launches(1);
     if (e != cudaSuccess) {
@@ -212,7 +258,7 @@ jarq_status jarq_integer_product(const int8_t *X, int64_t ldx, const float *xs, 
     if (const jarq_status late = async_failure()) return late;
     return run_product({X, C, xs, ws, bias, Y, ldx, ldc, ldy, n, dout, din, group_size,
                         group_size ? din / group_size : 1, dtype, false},
-                       (cudaStream_t)stream, false);
+                       nullptr, (cudaStream_t)stream, false);
 }
 
 size_t jarq_integer_linear_workspace(int n, int din) {
@@ -235,13 +281,17 @@ jarq_status jarq_integer_linear(const void *X, jarq_dtype xdtype, int64_t ldx, c
     cudaStream_t st = (cudaStream_t)stream;
     const int64_t ldq = code_pitch(din);
     const bool half = n > kFewTokens;
+    if (n == 1 && din <= kOwnCodes)
+        return run_product({X, C, nullptr, ws, bias, Y, ldx, ldc, ldy, n, dout, din, group_size,
+                            group_size ? din / group_size : 1, ydtype, false},
+                           &xdtype, st, false);
     float *xs = reinterpret_cast<float *>(static_cast<char *>(workspace) + code_bytes(n, din));
     const jarq_status e = run_quantize(X, xdtype, n, din, ldx, workspace, half, ldq, xs, st);
     if (e != JARQ_OK) return e;
     // the product starts under the quantization and reads weights meanwhile
     return run_product({workspace, C, xs, ws, bias, Y, ldq, ldc, ldy, n, dout, din, group_size,
                         group_size ? din / group_size : 1, ydtype, half},
-                       st, true);
+                       nullptr, st, true);
 }
 
 jarq_status jarq_async_status(void *stream) {

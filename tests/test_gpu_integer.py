@@ -375,3 +375,25 @@ def test_odd_numbers_of_groups(jarq, n, din, dout):
     bound = (2 * (din // g) + 3) * 2.0 ** -24 * 1.01 * size + 1e-30
     assert ((y - want).abs() <= bound).all()
     assert torch.equal(y, jarq.integer_linear(X, c, w, g, dtype="float32").double())
+
+
+# a single token, which shorter rows' blocks quantize for themselves: the same bits
+# as quantization and product apart, on both sides of the change, at lengths that
+# are no multiple of 16, from any alignment, and with rows that hold no number
+@pytest.mark.parametrize("xdtype", list(DT))
+@pytest.mark.parametrize("din,dout,g,offset", [(1, 1, 0, 0), (17, 5, 0, 1), (1001, 1343, 0, 3), (4096, 2500, 64, 0), (6143, 40, 0, 2),
+                                               (6144, 700, 128, 1), (6145, 40, 0, 0), (6272, 300, 128, 0)])
+def test_single_token(jarq, xdtype, din, dout, g, offset):
+    rng = np.random.default_rng(din)
+    c = _rows(_codes(rng, dout, din, 15), din + offset, offset)
+    w = torch.as_tensor(rng.standard_normal((dout, din // g if g else 1)).astype(np.float32)).cuda()
+    x = torch.as_tensor(rng.standard_normal((1, din)).astype(np.float32)).to(DT[xdtype])
+    for last in (None, 0.0, float("inf"), float("nan")):
+        if last is not None:
+            x[0, -1] = last
+            if last == 0.0:
+                x.zero_()
+        X = _rows(x, None, offset)
+        q, xs = jarq.quantize_rows(X)
+        y = jarq.integer_linear(X, c, w, g, dtype="float32")
+        assert torch.equal(y.view(torch.int32), jarq.integer_product(q, xs, c, w, g, dtype="float32").view(torch.int32))
