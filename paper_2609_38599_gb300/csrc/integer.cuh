@@ -17,9 +17,10 @@ struct ProductArgs {
     bool half;
 };
 
-// Most tokens of the form without tensor cores, which takes int8 codes.  4096 x
-// 4096: two tokens 6.5 us, 9.0 on the tensor cores; four tokens of 11008 x 4096 with
-// groups of 128: 22.4 us (by dot products of four tokens at a time) against 14.0.
+// Most tokens of the form without tensor cores, which takes int8 codes.  Two tokens,
+// cold and from L2: 4096 -> 11008 12.3 and 9.0 us, on the tensor cores 16.4 and 14.6;
+// 11008 -> 4096 with groups of 128 15.4 and 12.0, there 16.3 and 14.0.  Four tokens of
+// the latter, by dot products of four tokens at a time: 22.4 against 14.0.
 constexpr int kFewTokens = 2;
 
 // Codes k .. k + 15 of a row of `len`; zeros beyond it, which are not read.  VEC:

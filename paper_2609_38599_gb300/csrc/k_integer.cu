@@ -24,7 +24,7 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 // Longest row that a single token's blocks quantize for themselves (from a graph,
 // cold and warm, against a launch of its own: 4096 -> 11008 10.0 and 7.3 us, 11.1 and
 // 7.3; 6144 -> 8192 12.0 and 8.1, 14.1 and 8.0; 8192 -> 4096 9.1 and 7.1, 9.2 and 6.3;
-// 11008 -> 4096 15.5 and 10.9, 14.5 and 9.3).  The host's time of a call falls by
+// 11008 -> 4096, groups of 128, 15.5 and 10.9, 14.5 and 9.3).  The host's time of a call falls by
 // 4 us of 18.  Two tokens' blocks would lose (2 x 4096 -> 1000: 4.6 us for 3.6).
 constexpr int kOwnCodes = 6144;
 
@@ -71,7 +71,7 @@ __device__ __forceinline__ float quantize_row(const T *x, int d, int8_t *q, uint
 // M: tokens (a.n <= M); R: channels that a block has at a time.  OWN: the token
 // is activations of type `xtype`, which each block quantizes for itself.
 template <int M, int R, bool GROUPS, bool VEC, bool OWN>
-__global__ void __launch_bounds__(kThreads) few_tokens_kernel(ProductArgs a, jarq_dtype xtype) {
+__global__ void __launch_bounds__(kThreads, M == 1 ? 4 : 2) few_tokens_kernel(ProductArgs a, jarq_dtype xtype) {
     constexpr int V = M * R;
     __shared__ uint32_t parts[2][kWarps][V];
     __shared__ uint32_t tops[kWarps];
@@ -79,11 +79,20 @@ __global__ void __launch_bounds__(kThreads) few_tokens_kernel(ProductArgs a, jar
     const int chunks = (a.din + 15) / 16, step = gridDim.x * R;
     const int shift = a.g == 64 ? 2 : 3;      // 16-code chunks of a group: 4 or 8
     uint4 w[R];
+    // and their groups' scales, on their way with them: cold, 2 x 11008 -> 4096 with
+    // groups of 128 take 15.4 us for 20.8, one token 13.0 for 14.5 (from L2, where the
+    // registers count, 12.0 for 12.3 and 10.4 for 9.4)
+    float ws[R];
     auto fetch = [&](int r, int o, int c) {
-        if (o < a.dout && c < chunks) w[r] = load_codes<VEC>(a.C + (size_t)o * a.ldc, 16 * c, a.din);
+        if (o >= a.dout || c >= chunks) return;
+        w[r] = load_codes<VEC>(a.C + (size_t)o * a.ldc, 16 * c, a.din);
+        if (GROUPS) ws[r] = a.ws[(size_t)o * a.G + (c >> shift)];
     };
 #pragma unroll
-    for (int r = 0; r < R; ++r) w[r] = make_uint4(0, 0, 0, 0);
+    for (int r = 0; r < R; ++r) {
+        w[r] = make_uint4(0, 0, 0, 0);
+        ws[r] = 0.f;
+    }
 #pragma unroll
     for (int r = 0; r < R; ++r) fetch(r, blockIdx.x * R + r, tid);
     extern __shared__ __align__(16) int8_t own[];
@@ -117,7 +126,7 @@ __global__ void __launch_bounds__(kThreads) few_tokens_kernel(ProductArgs a, jar
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const uint4 wr = w[r];
-                const float s = GROUPS && o0 + r < a.dout ? a.ws[(size_t)(o0 + r) * a.G + (c >> shift)] : 0.f;
+                const float s = ws[r];
                 fetch(r, on + r, cn);
 #pragma unroll
                 for (int m = 0; m < M; ++m) {
