@@ -61,6 +61,7 @@
 #include "integer.cuh"
 #include "rows.cuh"
 #include "tc_common.cuh"
+#include "turns.cuh"
 
 namespace jarq {
 namespace {
@@ -108,7 +109,7 @@ __host__ __device__ constexpr int ring_bytes(int nt, bool half) {
 __host__ __device__ constexpr int smem_bytes(int nt, bool half) { return 1024 + ring_bytes(nt, half) + out_bytes(nt) + nt * 4 + 512; }
 constexpr bool rings_fit(bool half) {
     for (int nt = 32; nt <= (half ? 256 : 128); nt *= 2)
-        if (smem_bytes(nt, half) > 227 * 1024 || 8 * (4 * kStages + 2 * 3 + 2 * raw_stages(nt, half) + 1) + 8 > 512)
+        if (smem_bytes(nt, half) > 227 * 1024 || 8 * (4 * kStages + 3 * 3 + 2 * raw_stages(nt, half) + 1) + 8 > 512)
             return false;
     return true;
 }
@@ -322,37 +323,6 @@ __device__ __forceinline__ void write_out(const ProductArgs &a, uint32_t staged,
     });
 }
 
-// A position in a ring of N stages.
-template <int N>
-struct Slot {
-    int s = 0;
-    uint32_t phase;
-    __device__ explicit Slot(uint32_t first) : phase(first) {}
-    __device__ __forceinline__ void next() {
-        if (++s == N) {
-            s = 0;
-            phase ^= 1;
-        }
-    }
-};
-
-// The accumulators of a unit's parts, N taking turns, and the parity to wait for.
-template <int N, int PARTS>
-struct Turn {
-    int first = 0;
-    uint32_t phase;
-    __device__ explicit Turn(uint32_t p) : phase(p) {}
-    __device__ __forceinline__ int acc(int part) const { return first + part < N ? first + part : first + part - N; }
-    __device__ __forceinline__ uint32_t parity(int part) const { return first + part < N ? phase : phase ^ 1; }
-    __device__ __forceinline__ void next() {
-        first += PARTS;
-        if (first >= N) {
-            first -= N;
-            phase ^= 1;
-        }
-    }
-};
-
 // NT: tokens of a tile.  GROUPS: group scales.  VEC: rows of codes on 16-byte
 // boundaries.  HALF: tokens are integers in fp16, rows on 16-byte boundaries.
 // kBrief: groups of 64, NT 256.
@@ -381,7 +351,9 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
     constexpr bool kApart = kStagesA != kStages;   // channels have barriers of their own
     static_assert(!kBrief || (GROUPS && B::lean), "converted tokens share their barriers with the channels");
     constexpr int kBarsA = kApart ? 2 * kStagesA : 0;
-    constexpr int kBars = 2 * kStages + 2 * kAccs + 2 * kRaws + kBarsA + 1;
+    using Accs = Turn<kAccs, kParts, kBrief>;
+    constexpr int kReports = Accs::kReports;
+    constexpr int kBars = 2 * kStages + kReports + kAccs + 2 * kRaws + kBarsA + 1;
     constexpr uint32_t kIdesc = tc::idesc_f16_f32(kChannels, kAcc);
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -404,9 +376,9 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
     auto full = [&](int s) { return tc::smem_u32(bars + s); };
     auto empty = [&](int s) { return tc::smem_u32(bars + kStages + s); };
     auto afull = [&](int b) { return tc::smem_u32(bars + 2 * kStages + b); };
-    auto aempty = [&](int b) { return tc::smem_u32(bars + 2 * kStages + kAccs + b); };
-    auto raw_full = [&](int s) { return tc::smem_u32(bars + 2 * kStages + 2 * kAccs + s); };
-    auto raw_empty = [&](int s) { return tc::smem_u32(bars + 2 * kStages + 2 * kAccs + kRaws + s); };
+    auto aempty = [&](int b) { return tc::smem_u32(bars + 2 * kStages + kReports + b); };
+    auto raw_full = [&](int s) { return tc::smem_u32(bars + 2 * kStages + kReports + kAccs + s); };
+    auto raw_empty = [&](int s) { return tc::smem_u32(bars + 2 * kStages + kReports + kAccs + kRaws + s); };
     auto full_a = [&](int s) { return kApart ? tc::smem_u32(bars + kBars - 1 - kBarsA + s) : full(s); };
     auto empty_a = [&](int s) { return kApart ? tc::smem_u32(bars + kBars - 1 - kBarsA + kStagesA + s) : empty(s); };
     const uint32_t closing = tc::smem_u32(bars + kBars - 1);
@@ -423,10 +395,9 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
             tc::mbar_init(full_a(s), ctas(NT) * kConverters);
             tc::mbar_init(empty_a(s), 1);
         }
-        for (int b = 0; b < kAccs; ++b) {
-            tc::mbar_init(afull(b), 1);
+        for (int b = 0; b < kReports; ++b) tc::mbar_init(afull(b), 1);
+        for (int b = 0; b < kAccs; ++b)
             tc::mbar_init(aempty(b), ctas(NT) * kDrain / 32 * kReads / kParts);   // the even CTA's: both drains
-        }
         for (int s = 0; s < kRaws; ++s) {
             tc::mbar_init(raw_full(s), VEC ? 1 : kFill / 32);
             tc::mbar_init(raw_empty(s), kConverters);
@@ -460,7 +431,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
             const int us = GROUPS ? max(1, ua / 2) : kExact / 2;     // stages of an accumulator
             Slot<kStages> in(0);
             Slot<kStagesA> chan(0);
-            Turn<kAccs, kParts> turn(1);
+            Accs turn(1);
             int unit = 0;                                    // over all tiles
             // `count` atoms from atom `at` of a stage into every part's accumulator
             auto mma = [&](uint32_t d, uint32_t ad, uint64_t bd, uint32_t add) {
@@ -495,7 +466,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
                             for (int sub = 0; sub < 4; ++sub)
                                 mma(d, ad + 32 + 8 * sub, bd + (kAtomB >> 4) + 2 * sub, 1);
                         }
-                        if (last) commit(afull(b));
+                        if (last) commit(afull(turn.report(h)));
                         if (done && h == kParts - 1) {
                             commit(empty(in.s));
                             if (kApart) commit(empty_a(chan.s));
@@ -713,7 +684,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
         const uint32_t released = tc::map_rank(aempty(0), even);
         const uint32_t taddr = tmem + ((uint32_t)(32 * q) << 16) + (kBrief ? 0 : col0);
         bool ok = true;
-        Turn<kAccs, kParts> turn(0);
+        Accs turn(0);
         for (int tile = cluster; tile < ntiles && ok; tile += nclusters) {
             const int o = tile % mt * kChannels + 128 * rank + lrow, t0 = tile / mt * NT;
             const bool live = o < a.dout;
@@ -735,7 +706,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
 #pragma unroll
                 for (int h = 0; h < kReads; ++h) {
                     const int b = turn.acc(h + mine);
-                    ok = __all_sync(0xffffffffu, tc::mbar_wait<kPolls>(afull(b), turn.parity(h + mine))) && ok;
+                    ok = __all_sync(0xffffffffu, tc::mbar_wait<kPolls>(afull(turn.report(h + mine)), turn.report_parity(h + mine))) && ok;
                     if (!ok) break;
                     tc::tc_fence_after();
                     const uint32_t at = taddr + b * kAcc;
