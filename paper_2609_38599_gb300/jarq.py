@@ -554,11 +554,19 @@ def integer_codes(Q, Z, group_size: int, bits: int):
     """``jarq_integer_codes``: q - z of a refined layer as int8 [dout][din], the
     weights of ``integer_linear`` with the scales S and this group size."""
     T = _torch()
+    if len(Q.shape) != 2:
+        raise TypeError(f"Q: expected a CUDA matrix of {T.u8}, got {Q.dtype} {tuple(Q.shape)}")
     dout, din = Q.shape
+    group_size = int(group_size)
+    if group_size <= 0 or din % group_size:
+        raise JarqError(JARQ_ERR_ARG, "jarq_integer_codes")
+    G = din // group_size
+    q = _flat(Q, "Q", T.u8, (dout, din))
+    z = _flat(Z, "Z", T.i32, (dout, G), (dout * G,))
     pitch = (din + 15) // 16 * 16
     C = T.empty((dout, pitch), dtype=T.i8, device=Q.device)
-    status = _lib.jarq_integer_codes(_ptr(Q, np.uint8), _ptr(Z, np.int32), dout, din, int(group_size),
-                                     int(bits), C.data_ptr(), pitch, T.stream(Q.get_device()))
+    status = _lib.jarq_integer_codes(q, z, dout, din, group_size, int(bits), C.data_ptr(), pitch,
+                                     T.stream(Q.get_device()))
     if status != JARQ_OK:
         raise JarqError(status, "jarq_integer_codes")
     return C[:, :din]
