@@ -318,7 +318,7 @@ jarq_status jarq_async_status(void *stream);
  * scale 0 and codes 0; a row that holds an infinity or a NaN gets scale NaN
  * and codes 0, so that products with it are NaN.
  *   X : [n][d] of `dtype`, pitch ldx.  Q : int8 [n][d], pitch ldq.
- *   scale : float32 [n].  n >= 0, d >= 1. */
+ *   scale : float32 [n].  n >= 0, d >= 1, both at most 2^31 - 4096. */
 jarq_status jarq_quantize_rows(const void *X, jarq_dtype dtype, int n, int d, int64_t ldx,
                                int8_t *Q, int64_t ldq, float *scale, void *stream);
 
@@ -339,7 +339,7 @@ jarq_status jarq_integer_codes(const uint8_t *Q, const int32_t *Z, int dout, int
  *   C : int8 [dout][din], pitch ldc; ws : float32 [dout][G].
  *   group_size : 0, 64 or 128 (then a divisor of din).
  *   bias : float32 [dout] or NULL.  Y : [n][dout] of `dtype`, pitch ldy.
- *   n >= 0, 1 <= dout, 1 <= din <= 65536.
+ *   n >= 0, 1 <= dout, both at most 2^31 - 4096, 1 <= din <= 65536.
  * Precision: the integer sums are exact for any codes.  With G = 1 that sum is
  * rounded once to float32; with groups the terms are added in float32.  Scales
  * and bias are applied in float32, with one rounding to `dtype` at the end. */
@@ -369,7 +369,7 @@ jarq_status jarq_integer_linear(const void *X, jarq_dtype xdtype, int64_t ldx, c
  *            (logprob 0); one >= vocab gives logprob NaN.
  *   logprob [n][t], entropy [n], lse [n], top_logprob [n][k] : float32;
  *   top_token [n][k] : int32.  entropy and lse may be NULL.
- *   n >= 0, vocab >= 1, 0 <= t <= 256, 0 <= k <= 32, k <= vocab.
+ *   n >= 0, 1 <= vocab <= 2^30, 0 <= t <= 256, 0 <= k <= 32, k <= vocab.
  * A logit of -inf masks its token: p = 0, never an alternative (where fewer
  * than k tokens are left the rest is token -1 with logprob -inf).  A row with
  * all tokens masked has lse = -inf, logprob = -inf and entropy 0.  A NaN or

@@ -17,6 +17,10 @@ struct ProductArgs {
     bool half;
 };
 
+// Most tokens, channels and elements of a row to quantize: the kernels' int indexes
+// go up to a wave of tiles (4096) beyond them.
+constexpr int kMostIndex = 0x7FFFFFFF - 4095;
+
 // Most tokens of the form without tensor cores, which takes int8 codes.  Two tokens,
 // cold and from L2: 4096 -> 11008 12.3 and 9.0 us, on the tensor cores 16.4 and 14.6;
 // 11008 -> 4096 with groups of 128 15.4 and 12.0, there 16.3 and 14.0.  Four tokens of

@@ -199,7 +199,9 @@ cudaError_t launch_product(const ProductArgs &a, const jarq_dtype *xtype, int *f
 jarq_status check_layer(const int8_t *C, int64_t ldc, const float *ws, int group_size,
                         const float *bias, int n, int dout, int din, jarq_dtype dtype, const void *Y,
                         int64_t ldy) {
-    if (n < 0 || dout < 1 || din < 1 || din > 65536 || ldc < din || ldy < dout || !is_dtype(dtype)) return JARQ_ERR_ARG;
+    if (n < 0 || n > kMostIndex || dout < 1 || dout > kMostIndex || din < 1 || din > 65536 || ldc < din || ldy < dout ||
+        !is_dtype(dtype))
+        return JARQ_ERR_ARG;
     if (group_size != 0 && ((group_size != 64 && group_size != 128) || din % group_size)) return JARQ_ERR_ARG;
     if (n == 0) return JARQ_OK;
     if (!C || !ws || !Y || !on_device(C) || !on_device(ws) || !on_device(Y) || (bias && !on_device(bias)))
@@ -249,7 +251,7 @@ extern "C" {
 
 jarq_status jarq_quantize_rows(const void *X, jarq_dtype dtype, int n, int d, int64_t ldx,
                                int8_t *Q, int64_t ldq, float *scale, void *stream) {
-    if (n < 0 || d < 1 || ldx < d || ldq < d || !is_dtype(dtype)) return JARQ_ERR_ARG;
+    if (n < 0 || n > kMostIndex || d < 1 || d > kMostIndex || ldx < d || ldq < d || !is_dtype(dtype)) return JARQ_ERR_ARG;
     if (n == 0) return JARQ_OK;
     if (!X || !Q || !scale || !on_device(X) || !on_device(Q) || !on_device(scale)) return JARQ_ERR_ARG;
     if ((uintptr_t)X & (size_of(dtype) - 1) || (uintptr_t)scale & 3) return JARQ_ERR_ARG;

@@ -93,3 +93,27 @@ def test_integer_codes_wants_matrices_of_the_device(jarq, calls):
             jarq.integer_codes(q, z, wrong, bits)
         assert e.value.status == jarq.JARQ_ERR_ARG
     assert not calls
+
+
+F16, MOST = 1, 2 ** 31 - 4096
+
+
+# sizes past which the kernels' 32-bit indexes would wrap; an empty batch is checked
+# like any other, and does no CUDA work
+@pytest.mark.parametrize("n,d", [(2 ** 31 - 1, 64), (MOST + 1, 64), (0, MOST + 1), (0, 2 ** 31 - 1), (1, MOST)])
+def test_rows_to_quantize_stay_within_the_indexes(jarq, n, d):
+    L = jarq.library()
+    assert L.jarq_quantize_rows(None, F16, n, d, d, None, d, None, None) == jarq.JARQ_ERR_ARG
+
+
+def test_layers_stay_within_the_indexes(jarq):
+    L = jarq.library()
+
+    def layer(n, dout):
+        return {L.jarq_integer_product(None, 64, None, None, 64, None, 0, None, n, dout, 64, F16, None, dout, None),
+                L.jarq_integer_linear(None, F16, 64, None, 64, None, 0, None, n, dout, 64, F16, None, dout, None, 0, None)}
+
+    for n, dout in ((0, MOST + 1), (0, 2 ** 31 - 1), (MOST + 1, 8), (2 ** 31 - 1, 8)):
+        assert layer(n, dout) == {jarq.JARQ_ERR_ARG}
+    assert layer(0, MOST) == {jarq.JARQ_OK}
+    assert L.jarq_quantize_rows(None, F16, 0, MOST, MOST, None, MOST, None, None) == jarq.JARQ_OK
