@@ -6,10 +6,13 @@
 // 16 codes of each channel at a time with 16 codes of each token, the next weights,
 // of these channels or the following ones, on their way while these are used and
 // their sums joined.  With one scale a channel the sums are int32 (exact for din <=
-// 65536); with groups (a multiple of 16) each product of 16 is scaled into a float32
-// sum.  A linear layer's single token is quantized by every block for itself, under
+// 65536); with groups the 4 or 8 lanes that share one add up its integer sum, which is
+// so exact, and share out the scaling into float32 sums.  A linear layer's single token is quantized by every block for itself, under
 // its first weights' loads.  One token, 4096 -> 11008 (45 MB), quantization included:
-// 10.0 us from cold memory (4.5 TB/s), 7.3 us from L2; 4096 -> 4096 5.9 and 4.7 us.
+// 10.0 us from cold memory (4.5 TB/s), 7.3 us from L2, with groups of 128 10.4 and 7.8;
+// 4096 -> 4096 5.9 and 4.7 us.  11008 -> 4096 with groups of 128: one token 12.9 and
+// 8.7, two 14.8 and 10.2.  (Each product of 16 scaled by its own lane, which rounds the
+// parts of a group's sum and loads a scale for each: 14.1 and 10.7, 16.5 and 12.3.)
 #include "integer.cuh"
 #include "quantize.cuh"
 #include "rows.cuh"
@@ -28,27 +31,33 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 // 4 us of 18.  Two tokens' blocks would lose (2 x 4096 -> 1000: 4.6 us for 3.6).
 constexpr int kOwnCodes = 6144;
 
-// Sums of V values over the lanes of a warp: value i ends in lane 32 / V i.
-template <int V>
-__device__ __forceinline__ float warp_sums(float (&v)[V], int lane) {
-    int left = V;
+// A group's 16-code chunks lie with LANES neighbouring lanes (4 or 8), which share
+// its V integer sums out: a lane has kOwn of them from kFirst on, and where there
+// are more lanes than sums, kSame lanes have the same one.
+template <int V, int LANES>
+struct Share {
+    static constexpr int kOwn = V > LANES ? V / LANES : 1, kSame = V < LANES ? LANES / V : 1;
+    __device__ static int first(int lane) { return lane % LANES / kSame * kOwn; }
+    // v[i]: this lane's part of sum i; afterwards v[0 .. kOwn - 1] are its own sums
+    __device__ static void join(int (&v)[V], int lane) {
+        int left = V;
 #pragma unroll
-    for (int off = 16; off > 0; off /= 2) {
-        if (left > 1) {
-            left /= 2;
-            const bool up = lane & off;
+        for (int off = LANES / 2; off > 0; off /= 2) {
+            if (left > 1) {
+                left /= 2;
+                const bool up = lane & off;
 #pragma unroll
-            for (int i = 0; i < V / 2; ++i)
-                if (i < left) {
-                    const float give = up ? v[i] : v[i + left], keep = up ? v[i + left] : v[i];
-                    v[i] = keep + __shfl_xor_sync(0xffffffffu, give, off);
-                }
-        } else {
-            v[0] += __shfl_xor_sync(0xffffffffu, v[0], off);
+                for (int i = 0; i < V / 2; ++i)
+                    if (i < left) {
+                        const int give = up ? v[i] : v[i + left], keep = up ? v[i + left] : v[i];
+                        v[i] = keep + __shfl_xor_sync(0xffffffffu, give, off);
+                    }
+            } else {
+                v[0] += __shfl_xor_sync(0xffffffffu, v[0], off);
+            }
         }
     }
-    return v[0];
-}
+};
 
 // A row of activations to codes q in shared memory, by a block; its scale.
 template <class T>
@@ -68,33 +77,41 @@ __device__ __forceinline__ float quantize_row(const T *x, int d, int8_t *q, uint
     return by.scale;
 }
 
-// M: tokens (a.n <= M); R: channels that a block has at a time.  OWN: the token
-// is activations of type `xtype`, which each block quantizes for itself.
-template <int M, int R, bool GROUPS, bool VEC, bool OWN>
+// M: tokens (a.n <= M); R: channels that a block has at a time.  LANES: 16-code
+// chunks of a group, 0 for one scale a channel.  OWN: the token is activations of
+// type `xtype`, which each block quantizes for itself.
+template <int M, int R, int LANES, bool VEC, bool OWN>
 __global__ void __launch_bounds__(kThreads, M == 1 ? 4 : 2) few_tokens_kernel(ProductArgs a, jarq_dtype xtype) {
     constexpr int V = M * R;
+    constexpr bool GROUPS = LANES > 0;
+    using Mine = Share<V, GROUPS ? LANES : 1>;
+    // scales of a lane: of the channels whose sums it has
+    constexpr int kScales = GROUPS ? Mine::kOwn / M : 1;
+    static_assert(!GROUPS || Mine::kOwn % M == 0, "all tokens of a channel");
     __shared__ uint32_t parts[2][kWarps][V];
     __shared__ uint32_t tops[kWarps];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int chunks = (a.din + 15) / 16, step = gridDim.x * R;
-    const int shift = a.g == 64 ? 2 : 3;      // 16-code chunks of a group: 4 or 8
     uint4 w[R];
-    // and their groups' scales, on their way with them: cold, 2 x 11008 -> 4096 with
-    // groups of 128 take 15.4 us for 20.8, one token 13.0 for 14.5 (from L2, where the
-    // registers count, 12.0 for 12.3 and 10.4 for 9.4)
-    float ws[R];
     auto fetch = [&](int r, int o, int c) {
-        if (o >= a.dout || c >= chunks) return;
-        w[r] = load_codes<VEC>(a.C + (size_t)o * a.ldc, 16 * c, a.din);
-        if (GROUPS) ws[r] = a.ws[(size_t)o * a.G + (c >> shift)];
+        if (o < a.dout && c < chunks) w[r] = load_codes<VEC>(a.C + (size_t)o * a.ldc, 16 * c, a.din);
+    };
+    // and the groups' scales of the lane's sums, on their way with them
+    float ws[kScales];
+    const int first = GROUPS ? Mine::first(lane) : 0;
+    auto fetch_scales = [&](int o, int c) {
+        if (!GROUPS || c >= chunks) return;
+#pragma unroll
+        for (int i = 0; i < kScales; ++i)
+            if (const int oi = o + first / M + i; oi < a.dout) ws[i] = a.ws[(size_t)oi * a.G + c / (GROUPS ? LANES : 1)];
     };
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        w[r] = make_uint4(0, 0, 0, 0);
-        ws[r] = 0.f;
-    }
+    for (int r = 0; r < R; ++r) w[r] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < kScales; ++i) ws[i] = 0.f;
 #pragma unroll
     for (int r = 0; r < R; ++r) fetch(r, blockIdx.x * R + r, tid);
+    fetch_scales(blockIdx.x * R, tid);
     extern __shared__ __align__(16) int8_t own[];
     const int8_t *X = static_cast<const int8_t *>(a.X);
     float scale[M];
@@ -113,20 +130,21 @@ __global__ void __launch_bounds__(kThreads, M == 1 ? 4 : 2) few_tokens_kernel(Pr
     }
     for (int o0 = blockIdx.x * R, turn = 0; o0 < a.dout; o0 += step, turn ^= 1) {
         int sum[V] = {};
-        float acc[V] = {};
-        for (int c = tid; c < chunks; c += kThreads) {
+        float acc[Mine::kOwn] = {};
+        // with groups a warp goes on together, lanes past the row with nothing
+        for (int c = tid; (GROUPS ? c - lane : c) < chunks; c += kThreads) {
             // the next weights: of these channels, else of the block's next ones,
             // which are then on their way under the sums' reduction
-            const bool more = c + kThreads < chunks;
-            const int on = more ? o0 : o0 + step, cn = more ? c + kThreads : tid;
+            const bool live = !GROUPS || c < chunks, more = c + kThreads < chunks;
+            const int on = more ? o0 : o0 + step, cn = live ? more ? c + kThreads : tid : chunks;
             uint4 x[M];
 #pragma unroll
             for (int m = 0; m < M; ++m)
                 x[m] = load_codes<VEC || OWN>(X + min(m, a.n - 1) * (size_t)a.ldx, 16 * c, a.din);
+            int group[V];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const uint4 wr = w[r];
-                const float s = ws[r];
                 fetch(r, on + r, cn);
 #pragma unroll
                 for (int m = 0; m < M; ++m) {
@@ -135,16 +153,27 @@ __global__ void __launch_bounds__(kThreads, M == 1 ? 4 : 2) few_tokens_kernel(Pr
                     d = __dp4a((int)wr.y, (int)x[m].y, d);
                     d = __dp4a((int)wr.z, (int)x[m].z, d);
                     d = __dp4a((int)wr.w, (int)x[m].w, d);
-                    if (GROUPS)
-                        acc[r * M + m] = fmaf((float)d, s, acc[r * M + m]);
-                    else
-                        sum[r * M + m] = d;
+                    (GROUPS ? group : sum)[r * M + m] = d;
                 }
             }
+            if constexpr (GROUPS) {
+                // a group's sum is an integer, rounded with its scale into the float32 sum
+                Mine::join(group, lane);
+                if (live) {
+#pragma unroll
+                    for (int i = 0; i < Mine::kOwn; ++i) acc[i] = fmaf((float)group[i], ws[i / M], acc[i]);
+                }
+                fetch_scales(on, cn);
+            }
         }
-        if (GROUPS) {
-            const float v = warp_sums(acc, lane);
-            if (V == 32 || lane % (32 / V) == 0) parts[turn][warp][lane / (32 / V)] = __float_as_uint(v);
+        if constexpr (GROUPS) {
+            // over the warp's groups
+#pragma unroll
+            for (int i = 0; i < Mine::kOwn; ++i) {
+#pragma unroll
+                for (int off = 16; off >= LANES; off /= 2) acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], off);
+                if (lane < LANES && lane % Mine::kSame == 0) parts[turn][warp][first + i] = __float_as_uint(acc[i]);
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
@@ -184,8 +213,9 @@ cudaError_t launch_few(const ProductArgs &a, jarq_dtype xtype, cudaStream_t s, b
     const size_t smem = OWN ? round_up(a.din, 16) : 0;
     const bool vec = OWN ? vector_codes(a) : vector_rows(a);
     auto run = [&](auto kernel) { return launch_k(kernel, grid, dim3(kThreads), smem, s, pdl, a, xtype); };
-    if (a.g) return vec ? run(few_tokens_kernel<M, R, true, true, OWN>) : run(few_tokens_kernel<M, R, true, false, OWN>);
-    return vec ? run(few_tokens_kernel<M, R, false, true, OWN>) : run(few_tokens_kernel<M, R, false, false, OWN>);
+    if (a.g == 64) return vec ? run(few_tokens_kernel<M, R, 4, true, OWN>) : run(few_tokens_kernel<M, R, 4, false, OWN>);
+    if (a.g) return vec ? run(few_tokens_kernel<M, R, 8, true, OWN>) : run(few_tokens_kernel<M, R, 8, false, OWN>);
+    return vec ? run(few_tokens_kernel<M, R, 0, true, OWN>) : run(few_tokens_kernel<M, R, 0, false, OWN>);
 }
 
 // xtype: of one token's activations in the codes' place, or null
