@@ -523,11 +523,15 @@ __global__ void __launch_bounds__(kGradThreads) token_grad_kernel(GradArgs a) {
     __syncthreads();
     float G = 0.f;
     for (int j = 0; j < a.t; ++j) G += sg[j];
+    // Logits up to here get 0: masked ones, and those whose p is 0 by far, where v - lse
+    // may overflow and 0 lp be NaN.  Only masked ones where a factor is not finite.
+    const bool finite = isfinite(lse) && isfinite(G) && isfinite(gh) && isfinite(h);
+    const float dead = finite ? lse - (1000.f + fabsf(lse) * 0x1p-10f) : neg_inf();
     auto soft = [&](float v) {
         const float lp = v - lse, p = exp2_fast(lp * kLog2e);
         float d = -G * p;
         if (a.g_entropy) d -= gh * (p * (lp + h));
-        return v == neg_inf() ? 0.f : d;
+        return v <= dead ? 0.f : d;
     };
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
