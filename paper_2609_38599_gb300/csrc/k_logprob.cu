@@ -446,10 +446,12 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_logprobs_kern
     if (rank == 0) {
         c = sh.total;
         const bool bad = isnan(c.s), empty = !bad && c.m == neg_inf();
-        const float rest = left_out(c.m), logz = empty ? 0.f : logf(c.s * exp2_fast(-rest));
+        // z is at least 1, its largest term: what the exponentials' rounding takes from
+        // that would make probabilities above 1, and the entropy may fall below 0 alike
+        const float rest = left_out(c.m), logz = empty ? 0.f : logf(fmaxf(c.s * exp2_fast(-rest), 1.f));
         if (tid == 0) {
             if (a.lse) a.lse[r] = bad ? not_a_number() : empty ? neg_inf() : c.m + logz;
-            if (a.entropy) a.entropy[r] = bad ? not_a_number() : empty ? 0.f : logz - (c.u / c.s - rest) * kLn2;
+            if (a.entropy) a.entropy[r] = bad ? not_a_number() : empty ? 0.f : fmaxf(logz - (c.u / c.s - rest) * kLn2, 0.f);
         }
         auto logprob = [&](float v) { return bad ? not_a_number() : v == neg_inf() ? v : (v - c.m) - logz; };
         for (int j = tid; j < a.t; j += kThreads) {
