@@ -285,6 +285,7 @@ jarq_status jarq_quantize_rows(const void *X, jarq_dtype dtype, int n, int d, in
     if (n == 0) return JARQ_OK;
     if (!X || !Q || !scale || !on_device(X) || !on_device(Q) || !on_device(scale)) return JARQ_ERR_ARG;
     if ((uintptr_t)X & (size_of(dtype) - 1) || (uintptr_t)scale & 3) return JARQ_ERR_ARG;
+    if (const jarq_status late = async_failure()) return late;
     return run_quantize(X, dtype, n, d, ldx, Q, false, ldq, scale, (cudaStream_t)stream);
 }
 

@@ -338,6 +338,7 @@ jarq_status jarq_integer_codes(const uint8_t *Q, const int32_t *Z, int dout, int
         return JARQ_ERR_ARG;
     if (dout == 0) return JARQ_OK;
     if (!Q || !Z || !C || !on_device(Q) || !on_device(Z) || !on_device(C)) return JARQ_ERR_ARG;
+    if (const jarq_status late = async_failure()) return late;
     const int G = din / group_size;
     return checked_run(Q, Z, dout, din, G, (1 << bits) - 1, (cudaStream_t)stream,
                        [&](cudaStream_t st, const int *status) {
