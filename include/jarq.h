@@ -295,7 +295,8 @@ jarq_status jarq_accumulate_hessian(const void *X, int n, int d, float scale, fl
  * generation step takes microseconds on the device:
  * - They only enqueue their work on `stream` and return; results are ready in
  *   stream order, and the calls can be captured in a CUDA graph (a process's
- *   first product, which allocates the word of the third point, cannot).
+ *   first product of more than two tokens, which allocates the word of the
+ *   third point in pinned host memory, cannot).
  * - They allocate nothing on the device and keep no state between calls.
  * - A failure on the device (a bounded wait that gave up) is reported by
  *   jarq_async_status, and by every later call of these operators until

@@ -241,8 +241,9 @@ jarq_status check_layer(const int8_t *C, int64_t ldc, const float *ws, int group
 }
 
 jarq_status run_product(const ProductArgs &a, const jarq_dtype *xtype, cudaStream_t st, bool pdl) {
-    int *failed = async_word();
-    if (!failed) return JARQ_ERR_NOMEM;
+    // one and two tokens have no wait that could give up
+    int *failed = nullptr;
+    if (a.n > kFewTokens && !(failed = async_word())) return JARQ_ERR_NOMEM;
     ProfScope ps("integer_product", st);
     const cudaError_t e = launch_product(a, xtype, failed, st, pdl);
     ps.done();

@@ -1,4 +1,9 @@
-"""Corners of the integer product on the GPU: sums that cancel inside a group."""
+"""Corners of the integer product on the GPU: sums that cancel inside a group, and
+first calls of a process."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 
@@ -8,6 +13,8 @@ pytestmark = [pytest.mark.gpu,
               pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a CUDA GPU")]
 
 from test_gpu_integer import _check, _codes, _rows  # noqa: E402
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.fixture(scope="module")
@@ -53,3 +60,30 @@ def test_sums_that_cancel_inside_a_group_are_exact(jarq, n, din, dout, g, pad):
     c = _rows(C, din + pad)
     _check(jarq.integer_product(t(X), t(xs), c, t(ws), g, dtype="float32"), X, xs, C, ws, g, None, "float32")
     _check(jarq.integer_linear(t(X.astype(np.float32)), c, t(ws), g, dtype="float32"), X, xs, C, ws, g, None, "float32")
+
+
+FIRST_CALL = """
+import sys, torch
+sys.path.insert(0, {root!r})
+from paper_2609_38599_gb300 import jarq
+gen = torch.Generator("cuda").manual_seed(0)
+X = torch.randn({n}, {din}, device="cuda", generator=gen)
+C = torch.randint(-15, 16, (300, {din}), device="cuda", generator=gen).to(torch.int8)
+ws = torch.rand(300, {din} // 64, device="cuda", generator=gen)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    y = jarq.integer_linear(X, C, ws, 64, dtype="float32")
+graph.replay()
+torch.cuda.synchronize()
+assert torch.equal(y, jarq.integer_linear(X, C, ws, 64, dtype="float32"))
+"""
+
+
+# a single token quantized by the product's own blocks, one with a launch for it, two
+@pytest.mark.parametrize("n,din", [(1, 4096), (1, 6272), (2, 1024)])
+def test_a_first_call_of_one_or_two_tokens_can_be_captured(n, din):
+    """Such a call has no wait to report, and so nothing to allocate for it."""
+    r = subprocess.run([sys.executable, "-c", FIRST_CALL.format(root=ROOT, n=n, din=din)], capture_output=True, text=True,
+                       timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
