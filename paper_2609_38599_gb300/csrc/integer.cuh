@@ -22,8 +22,8 @@ struct ProductArgs {
 constexpr int kMostIndex = 0x7FFFFFFF - 4095;
 
 // Most tokens of the form without tensor cores, which takes int8 codes.  Two tokens,
-// cold and from L2: 4096 -> 11008 13.3 and 9.4 us, on the tensor cores 16.4 and 14.6;
-// 11008 -> 4096 with groups of 128 14.8 and 10.2, there 16.3 and 14.0.  Four tokens of
+// cold and from L2: 4096 -> 11008 13.3 and 9.4 us, on the tensor cores 17.0 and 15.0;
+// 11008 -> 4096 with groups of 128 14.8 and 10.2, there 17.1 and 14.0.  Four tokens of
 // the latter, by dot products of four tokens at a time: 22.4 against 14.0.
 constexpr int kFewTokens = 2;
 

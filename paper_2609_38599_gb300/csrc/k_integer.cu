@@ -7,12 +7,13 @@
 // of these channels or the following ones, on their way while these are used and
 // their sums joined.  With one scale a channel the sums are int32 (exact for din <=
 // 65536); with groups the 4 or 8 lanes that share one add up its integer sum, which is
-// so exact, and share out the scaling into float32 sums.  A linear layer's single token is quantized by every block for itself, under
-// its first weights' loads.  One token, 4096 -> 11008 (45 MB), quantization included:
-// 10.0 us from cold memory (4.5 TB/s), 7.3 us from L2, with groups of 128 10.4 and 7.8;
-// 4096 -> 4096 5.9 and 4.7 us.  11008 -> 4096 with groups of 128: one token 12.9 and
-// 8.7, two 14.8 and 10.2.  (Each product of 16 scaled by its own lane, which rounds the
-// parts of a group's sum and loads a scale for each: 14.1 and 10.7, 16.5 and 12.3.)
+// so exact, and share out the scaling into float32 sums.  A linear layer's single token
+// is quantized by every block for itself, under its first weights' loads.  One token,
+// 4096 -> 11008 (45 MB), quantization included: 10.0 us from cold memory (4.5 TB/s),
+// 7.3 us from L2, with groups of 128 10.4 and 7.8; 4096 -> 4096 5.9 and 4.7 us.  11008 ->
+// 4096 with groups of 128: one token 12.9 and 8.7, two 14.8 and 10.2.  (Each product of
+// 16 scaled by its own lane, which rounds the parts of a group's sum and loads a scale
+// for each: 14.1 and 10.7, 16.5 and 12.3.)
 #include "integer.cuh"
 #include "quantize.cuh"
 #include "rows.cuh"
@@ -25,14 +26,15 @@ using namespace rows;
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 // Longest row that a single token's blocks quantize for themselves (from a graph,
-// cold and warm, against a launch of its own: 4096 -> 11008 10.0 and 7.3 us, 11.1 and
-// 7.3; 6144 -> 8192 12.0 and 8.1, 14.1 and 8.0; 8192 -> 4096 9.1 and 7.1, 9.2 and 6.3;
-// 11008 -> 4096, groups of 128, 15.5 and 10.9, 14.5 and 9.3).  The host's time of a call falls by
-// 4 us of 18.  Two tokens' blocks would lose (2 x 4096 -> 1000: 4.6 us for 3.6).
+// cold and warm, against a launch of its own: 4096 -> 11008 10.1 and 7.3 us, 11.1 and
+// 7.0, with groups of 128 10.5 and 7.8, 11.9 and 7.7; 6144 -> 8192 12.4 and 8.1, 14.5
+// and 8.0; 8192 -> 4096 9.5 and 7.3, 9.7 and 6.3; 11008 -> 4096, groups of 128, 12.6 and
+// 9.9, 12.7 and 8.5).  The host's time of a call falls by 4 us of 18.  Two tokens'
+// blocks would lose (2 x 4096 -> 1000: 4.6 us for 3.6).
 constexpr int kOwnCodes = 6144;
 
 // A group's 16-code chunks lie with LANES neighbouring lanes (4 or 8), which share
-// its V integer sums out: a lane has kOwn of them from kFirst on, and where there
+// its V integer sums out: a lane has kOwn of them from first() on, and where there
 // are more lanes than sums, kSame lanes have the same one.
 template <int V, int LANES>
 struct Share {

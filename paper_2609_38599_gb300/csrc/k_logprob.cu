@@ -21,7 +21,7 @@
 // whose second maximum reaches that one, hardly any, read their other units again
 // (from L2).  Where the list is too short for the logits above the bound (rows with
 // many equal logits), every warp keeps a sorted list of its own instead.  Five
-// of 32000 take 123 us for the 97, 32 take 160; five of 131072 168 for 157.
+// of 32000 take 123 us for the 97, 32 take 160; five of 131072 168 to 170 for 157.
 #include <math.h>
 
 #include <algorithm>
@@ -484,8 +484,9 @@ struct GradArgs {
 // dx_v = sum_j g_j [v = tokens_j] - p_v (G + g_H (ln p_v + H)), G = sum_j g_j.
 // A CTA writes the second term of its 16-byte units of a row, four a thread, then
 // the tokens among them with both terms; all its logits are read first.  Bound by
-// memory: 8192 x 32000 bf16, 1.05 GB, take 155 us (6.8 TB/s).  kSame: logits
-// and gradient have the same alignment.
+// memory: 8192 x 32000 bf16, 1.05 GB, take 166 to 169 us with three sets of inputs in
+// turn (6.2 TB/s); near issue slots too, and with the entropy's term 176.  kSame:
+// logits and gradient have the same alignment.
 constexpr int kGradThreads = 256, kGradUnits = kAhead * kGradThreads;
 
 template <class T, bool kSame>

@@ -1,9 +1,9 @@
 // The integer product's tensor-core form, for more than a few tokens.
 //
-// GB300's 8-bit integer tensor rate is a small fraction of its fp16 rate, so
-// int8 codes become fp16 inside the SM (exactly: |c| <= 128) and the product
-// runs on fp16 MMAs.  Their sums are integers of at most 128 128 1024 = 2^24 over
-// 1024 of K, exact in the float32 accumulator; after that many, or after each
+// GB300's 8-bit integer tensor rate is a small fraction of its fp16 rate (a library's
+// products of 8192^3: 155 TOP/s in int8, 1823 TFLOP/s in fp16), so int8 codes become
+// fp16 inside the SM (exactly: |c| <= 128) and the product runs on fp16 MMAs.  Their
+// sums are integers of at most 128 128 1024 = 2^24 over 1024 of K, exact in the float32 accumulator; after that many, or after each
 // group, they leave it: with one scale a channel for an int32 sum, with groups for
 // a float32 sum of the terms ws_i sum_i.
 //
@@ -40,9 +40,11 @@
 // x K -> channels is given:
 //   8192 x 11008 -> 4096, one scale    430 us (the product 384: 1.92 PFLOP/s)
 //   4096 x 4096 -> 14336, groups of 128 297 us (1.62 PFLOP/s)
-//   2048 x 4096 -> 4096, groups of 64   71 us, of 128 55, one scale 54
-//   64 x 4096 -> 4096 9.9 us, 24 x 11008 -> 4096 (45 MB of codes, cold) 17.5 us
-//   int8 tokens given, the product alone: 8192 x 11008 -> 4096 604 us
+//   2048 x 4096 -> 4096, groups of 64   71 us, of 128 55, one scale 54 (with three sets
+//                                       of inputs in turn 74, 57, 56)
+//   64 x 4096 -> 4096 9.9 us from L2, 11.6 cold; 24 x 11008 -> 4096 (45 MB, cold) 18.5 us
+//   int8 tokens given, the product alone: 8192 x 11008 -> 4096 608 us (converted in
+//                                       every tile, and their stages relayed)
 // A large product with one scale runs near the rate of a library's product in
 // bfloat16.  With groups a sum leaves the accumulator eight (sixteen) times as often
 // as with one scale, and what a scheduler's two drain warps do then (wake, read TMEM,
@@ -50,7 +52,8 @@
 // above, 61 and 271 were left without seven in eight additions and the scales' loads.
 // Few tokens: the latency of a cluster's chain (first copies, conversion, MMAs,
 // join), then reading the codes.  Rows off 16-byte boundaries are bound by the
-// filling warps' loads (333 x 1001 -> 1343: 13.8 us, aligned 8.7).
+// filling warps' loads (333 x 1001 -> 1343: 14.2 us, 1008 aligned 8.2; 4096 x 4001 -> 4096
+// 236 us, 4096 x 4096 -> 4096 106, where every tile of tokens fills the channels again).
 //
 // Tried and dropped: four accumulators of 64 columns (the issuer's own instructions
 // take 1620 of 1024 cycles a stage), the issue loop rolled (619 us for 430), two sets
