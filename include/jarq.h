@@ -288,7 +288,7 @@ jarq_status jarq_pack_codes(const uint8_t *Q, int dout, int din, int bits, uint3
 jarq_status jarq_accumulate_hessian(const void *X, int n, int d, float scale, float *H,
                                     void *stream);
 
-/* ---- running and scoring a quantized model (device memory only) ----
+/* ---- running, scoring and tuning a quantized model (device memory only) ----
  * The paper judges a quantized model by the probabilities that it gives to
  * tokens (Sec. 4, perplexity).  These operators run a layer in integers and
  * score logits.  They differ from the calls above in three points, since a
@@ -398,6 +398,86 @@ jarq_status jarq_token_logprobs_grad(const void *logits, jarq_dtype dtype, int n
                                      const float *g_entropy, void *dlogits, int64_t ldd,
                                      void *stream);
 
+/* Root-mean-square norm of rows, with the residual's addition before it and an
+ * output in 8-bit integers after it.  With T the rows' type:
+ *     h = X + R rounded to T (X itself where R is NULL),
+ *     rstd[r] = 1 / sqrt(mean_k h_k^2 + eps),   v_k = h_k gain_k  in float32,
+ *     Y[r][k] = v_k rstd  rounded to T,
+ *     scale[r] = (a / 127) rstd,  Q[r][k] = rint(v_k (127 / a)),  a = max_k |v_k|,
+ * quotients and products in float32 as in jarq_quantize_rows: Q and scale are what
+ * jarq_integer_product takes, and scale * Q is about the norm.  (rstd is common to
+ * a row, so the integers are those of v.)  A row whose a is below 2^-120 gets scale
+ * 0 and codes 0; one whose v hold an infinity or a NaN gets scale NaN and codes 0.
+ *   X, R, H, Y : [n][d] of `dtype`, pitches ldx, ldr, ldh, ldy.  R and H are both
+ *                given or both NULL; H receives h and may be R itself (ldh = ldr).
+ *   gain : [d] of gain_dtype (`dtype` or JARQ_F32), or NULL for ones.
+ *   eps : > 0, finite.  Y may be NULL.  Q : int8 [n][d], pitch ldq, and scale :
+ *   float32 [n], both or neither.  rstd : float32 [n], may be NULL.
+ *   n >= 0, d >= 1, both at most 2^31 - 4096. */
+jarq_status jarq_rms_norm(const void *X, jarq_dtype dtype, int n, int d, int64_t ldx, const void *R,
+                          int64_t ldr, void *H, int64_t ldh, const void *gain, jarq_dtype gain_dtype,
+                          float eps, void *Y, int64_t ldy, int8_t *Q, int64_t ldq, float *scale,
+                          float *rstd, void *stream);
+
+/* Gradient of the norm's values Y with respect to h and the gains, from its rstd:
+ * with u = dY gain,
+ *     dX[r][k] = dH[r][k] + rstd (u_k - h_k rstd^2 mean_j u_j h_j)  rounded to T,
+ *     dgain[k] = sum_r dY[r][k] h[r][k] rstd[r],
+ * dX being the gradient of X and of R alike.
+ *   H : the normed rows h (X where there was no residual), pitch ldh.
+ *   dY, dX : [n][d] of `dtype`, pitches ldy, ldx.  dH : the gradient that reaches h
+ *   by the residual stream, pitch lds, or NULL.  dX may be NULL, and may be dY or dH
+ *   itself (same pitch).  dgain : float32 [d], overwritten (zeros for n = 0), or NULL.
+ *   workspace : at least jarq_rms_norm_grad_workspace(n, d) bytes of device memory,
+ *   16-byte aligned, that the stream's work may overwrite; NULL without dgain.
+ * Sums are float32, always added in the same order. */
+size_t jarq_rms_norm_grad_workspace(int n, int d);
+jarq_status jarq_rms_norm_grad(const void *H, jarq_dtype dtype, int n, int d, int64_t ldh,
+                               const void *gain, jarq_dtype gain_dtype, const float *rstd,
+                               const void *dY, int64_t ldy, const void *dH, int64_t lds, void *dX,
+                               int64_t ldx, float *dgain, void *workspace, size_t workspace_bytes,
+                               void *stream);
+
+/* Softmax cross entropy of an output head, without its logits in memory: with the
+ * logits l = X W^T of every row r,
+ *     lse[r] = ln sum_v exp l_v,   loss[r] = lse[r] - l_{tokens[r]}  (not below 0).
+ *   X : hidden states [n][d], W : head [vocab][d], both of `dtype` (JARQ_F16 or
+ *   JARQ_BF16), pitches ldx, ldw.  tokens : int64 [n].  A negative token is ignored
+ *   (loss 0); one >= vocab gives loss NaN.  loss, lse : float32 [n]; lse may be NULL.
+ *   0 <= n <= 2^22, 1 <= d <= 2^20, 1 <= vocab <= 2^30.
+ *   workspace : at least jarq_cross_entropy_workspace(...) bytes of device memory,
+ *   16-byte aligned, that the stream's work may overwrite.  rows_aligned: 1 where
+ *   all rows of X and of W begin on 16-byte boundaries; else 0, which leaves room
+ *   for copies that do.
+ * A NaN or +inf among a row's logits makes its loss and lse NaN; a row with all
+ * logits -inf has lse = -inf and loss +inf.  Products are exact, their sums, the
+ * softmax's statistics and the outputs float32. */
+size_t jarq_cross_entropy_workspace(int n, int d, int vocab, int rows_aligned);
+jarq_status jarq_cross_entropy(const void *X, jarq_dtype dtype, int n, int d, int64_t ldx,
+                               const void *W, int vocab, int64_t ldw, const int64_t *tokens,
+                               float *loss, float *lse, void *workspace, size_t workspace_bytes,
+                               void *stream);
+
+/* Gradient of sum_r g_loss[r] loss[r] of jarq_cross_entropy with respect to the
+ * hidden states and the head: with D_rv = g_loss[r] (exp(l_rv - lse[r]) - [v =
+ * tokens[r]]),  dX = D W  and  dW = D^T X.  The logits are formed once more and D a
+ * piece of the vocabulary at a time (of up to 512 MB, at least 4096 tokens), rounded
+ * to 16 bits with full relative precision; sums are float32.
+ *   X to tokens : as there.  lse : its result.  g_loss : float32 [n].
+ *   dX : [n][d], dW : [vocab][d] of `dtype`, pitches lddx, lddw, overwritten (dW with
+ *   zeros for n = 0); one of them may be NULL.
+ *   workspace, rows_aligned : as there; hidden, head : whether dX, dW are given.
+ * An ignored row gets gradient 0 and adds nothing to dW, whatever X holds there; a
+ * token >= vocab makes its row of dX, and all of dW, NaN.  For float16, rows whose
+ * |g_loss| lies more than 2^14 below the largest lose precision in dW. */
+size_t jarq_cross_entropy_grad_workspace(int n, int d, int vocab, int rows_aligned, int hidden,
+                                         int head);
+jarq_status jarq_cross_entropy_grad(const void *X, jarq_dtype dtype, int n, int d, int64_t ldx,
+                                    const void *W, int vocab, int64_t ldw, const int64_t *tokens,
+                                    const float *lse, const float *g_loss, void *dX, int64_t lddx,
+                                    void *dW, int64_t lddw, void *workspace, size_t workspace_bytes,
+                                    void *stream);
+
 /* Per-row objective without any device allocation.  The paper has no
  * counterpart: this entry point exists for callers that cannot allocate
  * device memory when they need the objective -- serving processes that
@@ -444,7 +524,8 @@ const char *jarq_status_string(jarq_status s);
  * "slices", "slice_rows", "proj", "whw", "rhs", "htilde", "ptilde", "syrk",
  * "mu_combine", "own_rhs", "scale_fit", "probe", "sweep_product",
  * "sweep_babai", "quantize_rows", "integer_product", "token_logprobs",
- * "token_grad"; also read: "target" and "babai" (the last two, whose launches
+ * "token_grad", "rms_norm", "norm_grad", "cross_entropy",
+ * "cross_entropy_grad", "adapters"; also read: "target" and "babai" (the last two, whose launches
  * once covered a group instead of a block of 256 columns) and "phase_hr" (no
  * launches).  Not thread-safe. */
 void jarq_profile_enable(int on);
@@ -467,8 +548,8 @@ long long jarq_launch_count(void);
 jarq_status jarq_selftest_wait_timeout(void *stream);
 
 /* The same for the tensor-core kernels: one of them ("target", "gram",
- * "proj", "ptilde", "hr_full", "syrk" or "integer_product", whose timeout
- * jarq_async_status reports and so clears) on a small layer of its own, with a
+ * "proj", "ptilde", "hr_full", "syrk", or "integer_product" or
+ * "cross_entropy", whose timeout jarq_async_status reports and so clears) on a small layer of its own, with a
  * short poll limit and its issuing warp told to stop after the first unit of
  * work, so that the waits of the other warps run out while copies lie
  * unused in shared memory.  Returns what that launch reports:

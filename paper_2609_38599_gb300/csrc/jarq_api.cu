@@ -17,6 +17,7 @@
 
 #include <new>
 
+#include "head.cuh"
 #include "integer.cuh"
 
 namespace jarq {
@@ -722,6 +723,18 @@ jarq_status jarq_selftest_stalled_kernel(const char *kernel, void *stream) try {
         const ProductArgs a{m, reinterpret_cast<int8_t *>(m + xb), xs, xs + p, nullptr, m + xb + cb, k, k, n, p, n, k, 0, 1,
                             JARQ_F32, true};
         if (e == cudaSuccess) e = launch_tc_integer_stalled(a, failed, st);
+        const jarq_status got = jarq_async_status(stream);
+        cudaFree(m);
+        CK(e);
+        return got;
+    }
+    if (is("cross_entropy")) {
+        int *failed = async_word();
+        if (!failed) return JARQ_ERR_NOMEM;
+        char *m = nullptr;
+        CK(dalloc(&m, head::stalled_bytes()));
+        cudaError_t e = cudaMemsetAsync(m, 0, head::stalled_bytes(), st);
+        if (e == cudaSuccess) e = head::launch_stalled(m, failed, st);
         const jarq_status got = jarq_async_status(stream);
         cudaFree(m);
         CK(e);

@@ -1,0 +1,462 @@
+// Softmax cross entropy of an output head over hidden states, and its gradient, in
+// pieces of the vocabulary:
+//   l = X W^T,  lse_r = ln sum_v exp l_rv,  loss_r = lse_r - l_r,token,
+//   D_rv = g_r (exp(l_rv - lse_r) - [v = token_r]),  dX = D W,  dW = D^T X.
+// The products run on the tensor cores (k_tc_head.cu); here are the join of the
+// loss's parts, copies of rows that TMA cannot read, and the calls.
+#include <algorithm>
+
+#include "head.cuh"
+#include "integer.cuh"
+
+namespace jarq {
+namespace head {
+namespace {
+
+using namespace rows;
+
+constexpr int kPairs = 76;                  // of CTAs that run at one time
+constexpr size_t kPieceBytes = 512u << 20;  // of D at a time
+constexpr int kLeastPiece = 4096;           // but at least so many tokens
+constexpr int kMostRows = 1 << 22, kMostWidth = 1 << 20, kMostVocab = 1 << 30;
+
+// loss and lse of a row from the maxima m and sums s of its parts: with M the
+// largest m and S = sum s exp(m - M), lse = M + ln S, and the loss is ln S + (M -
+// logit), neither below 0.  PER: threads of a row, over its parts.
+template <int PER>
+__global__ void __launch_bounds__(256) loss_join_kernel(const float2 *parts, int count, const float *target,
+                                                        const int64_t *tokens, int n, int vocab, float *loss, float *lse) {
+    constexpr int kRows = 256 / PER;
+    __shared__ float2 all[PER][kRows + 1];
+    const int i = threadIdx.x % kRows, t = threadIdx.x / kRows;
+    const int r = blockIdx.x * kRows + i;
+    float m = -INFINITY, s = 0.f;
+    auto take = [&](float2 p) {
+        const float top = fmaxf(m, p.x), ref = top == -INFINITY ? 0.f : top;
+        s = s * expf(m - ref) + p.y * expf(p.x - ref);
+        m = top;
+    };
+    if (r < n)
+        for (int p = t; p < count; p += PER) take(parts[(size_t)p * n + r]);
+    all[t][i] = make_float2(m, s);
+    for (int left = PER / 2; left; left /= 2) {
+        __syncthreads();
+        if (t < left) {
+            take(all[t + left][i]);
+            all[t][i] = make_float2(m, s);
+        }
+    }
+    if (t || r >= n) return;
+    const float logs = logf(s);
+    if (lse) lse[r] = m + logs;
+    if (loss) {
+        const int64_t tok = tokens[r];
+        float v = 0.f;
+        if (tok >= vocab) v = __int_as_float(0x7FC00000);
+        else if (tok >= 0) v = m == -INFINITY ? INFINITY + s : logs + (m - target[r]);   // s: 0, or NaN
+        loss[r] = v;
+    }
+}
+
+// 16-bit rows of any alignment to rows on 16-byte boundaries, pitch a multiple of 8.
+// WEIGH: those of ignored tokens become zero, whatever they hold, and of float16
+// row r is multiplied by 2^(e_r - top), as head.cuh has D's rows.
+template <class T, bool WEIGH>
+__global__ void __launch_bounds__(256) copy_rows_kernel(const T *x, int64_t ld, int n, int d, T *out, int pitch,
+                                                        const int64_t *tokens, const float *g, const int *top) {
+    const int per = pitch / 8;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t r = i / per;
+    const int k = (int)(i % per) * 8;
+    if (r >= n) return;
+    const T *p = x + r * ld + k;
+    uint4 raw = make_uint4(0, 0, 0, 0);
+    const bool live = !WEIGH || tokens[r] >= 0;
+    if (live) {
+        if (((uintptr_t)p & 15) == 0 && k + 8 <= d) {
+            raw = *reinterpret_cast<const uint4 *>(p);
+        } else {
+            alignas(16) T t[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) t[e] = k + e < d ? p[e] : T(0.f);
+            raw = *reinterpret_cast<const uint4 *>(t);
+        }
+        if constexpr (WEIGH && std::is_same_v<T, __half>) {
+            const float by = ldexpf(1.f, exponent(g[r]) - *top);
+            float v[8];
+            unpack(raw, v, T());
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= by;
+            raw = pack(v, T());
+        }
+    }
+    *reinterpret_cast<uint4 *>(out + r * pitch + k) = raw;
+}
+
+// The largest exponent among the rows' gradients that count.
+__global__ void __launch_bounds__(1024) top_exponent_kernel(const int64_t *tokens, const float *g, int n, int *top) {
+    __shared__ int part[32];
+    int e = -126;
+    for (int r = threadIdx.x; r < n; r += 1024)
+        if (tokens[r] >= 0) e = max(e, exponent(g[r]));
+    e = __reduce_max_sync(0xffffffffu, e);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = e;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        e = __reduce_max_sync(0xffffffffu, part[threadIdx.x]);
+        if (threadIdx.x == 0) *top = e;
+    }
+}
+
+// The splits' sums, added in their order, scaled and rounded.
+template <class T>
+__global__ void __launch_bounds__(256) sum_splits_kernel(const float *slab, int splits, int n, int d, int pitch, T *out,
+                                                         int64_t ld, const float *g, const int *top) {
+    const int per = pitch / 4;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t r = i / per;
+    const int k = (int)(i % per) * 4;
+    if (r >= n || k >= d) return;
+    float4 y = *reinterpret_cast<const float4 *>(slab + r * pitch + k);
+    for (int s = 1; s < splits; ++s) {
+        const float4 o = *reinterpret_cast<const float4 *>(slab + ((int64_t)s * n + r) * pitch + k);
+        y.x += o.x, y.y += o.y, y.z += o.z, y.w += o.w;
+    }
+    float by = 1.f;
+    if (std::is_same_v<T, __half>) by = ldexpf(1.f, (g ? exponent(g[r]) : *top) - 14);
+    const float v[4] = {y.x * by, y.y * by, y.z * by, y.w * by};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (k + e < d) out[r * ld + k + e] = from_float<T>(v[e]);
+}
+
+template <class T>
+__global__ void __launch_bounds__(256) zero_rows_kernel(T *out, int64_t ld, int n, int d) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i / d < n) out[i / d * ld + i % d] = T(0.f);
+}
+
+int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+// Splits of K for a product of few tiles: as many as fill the pairs, each at least
+// four chunks.
+int splits_of(int m, int n, int chunks) {
+    const int64_t tiles = (int64_t)ceil_div(m, 256) * ceil_div(n, 256);
+    const int s = (int)std::min<int64_t>({std::max<int64_t>(1, kPairs / tiles), std::max(1, chunks / 4), 16});
+    return ceil_div(chunks, ceil_div(chunks, s));
+}
+
+// The parts of a workspace, each on a 256-byte boundary.
+struct Layout {
+    size_t bytes = 0;
+    size_t take(size_t n) {
+        const size_t at = bytes;
+        bytes += (n + 255) / 256 * 256;
+        return at;
+    }
+};
+
+struct Plan {
+    int pitch, pieces, width;            // of copies and sums; pieces of the vocabulary
+    int split_x, split_w;
+    bool slab_x, slab_w;
+    size_t copy_x, copy_w, parts, target, weighed, top, D, sums_x, sums_w, bytes;
+
+    // the loss
+    Plan(int n, int d, int vocab, bool aligned) : pitch(round_up(d, 8)) {
+        Layout l;
+        parts = l.take((size_t)2 * ceil_div(vocab, 256) * n * sizeof(float2));
+        target = l.take((size_t)n * sizeof(float));
+        copies(l, n, vocab, aligned);
+        bytes = l.bytes;
+    }
+    // its gradient
+    Plan(int n, int d, int vocab, bool aligned, bool hidden, bool head) : pitch(round_up(d, 8)) {
+        const int64_t most = std::max<int64_t>(kLeastPiece, (int64_t)(kPieceBytes / 2 / std::max(n, 1)) / 256 * 256);
+        const int even = ceil_div(vocab, ceil_div(vocab, most));
+        width = round_up(even, 256);
+        pieces = ceil_div(vocab, width);
+        split_x = splits_of(n, d, ceil_div(std::min(width, vocab), 64));
+        split_w = splits_of(std::min(width, vocab), d, ceil_div(n, 64));
+        slab_x = hidden && (split_x > 1 || pieces > 1);
+        slab_w = head && split_w > 1;
+        Layout l;
+        D = l.take((size_t)n * width * 2);
+        sums_x = l.take(slab_x ? (size_t)split_x * n * pitch * sizeof(float) : 0);
+        sums_w = l.take(slab_w ? (size_t)split_w * width * pitch * sizeof(float) : 0);
+        weighed = l.take(head ? (size_t)n * pitch * 2 : 0);
+        top = l.take(sizeof(int));
+        copies(l, n, vocab, aligned);
+        bytes = l.bytes;
+    }
+    void copies(Layout &l, int n, int vocab, bool aligned) {
+        copy_x = l.take(aligned ? 0 : (size_t)n * pitch * 2);
+        copy_w = l.take(aligned ? 0 : (size_t)vocab * pitch * 2);
+    }
+};
+
+bool is_aligned(const void *p, size_t b) { return ((uintptr_t)p & (b - 1)) == 0; }
+bool rows_aligned(const void *p, int64_t ld, int n) { return is_aligned(p, 16) && (n == 1 || ld % 8 == 0); }
+bool usable(const void *p, size_t size) { return p && on_device(p) && is_aligned(p, size); }
+
+// A 16-bit matrix with rows on 16-byte boundaries.
+struct Matrix {
+    const char *p;
+    int64_t ld;
+    const char *row(int64_t r) const { return p + r * ld * 2; }
+};
+// boxes of `box` rows x 64 elements, moved as they are whatever the type
+cudaError_t tensor_map(CUtensorMap *map, const char *p, int rows, int cols, int64_t ld, int box) {
+    return make_tmap_half(map, p, rows, cols, rows > 1 ? ld : round_up(cols, 8), box);
+}
+
+// A call's arguments and the launches that it makes, one after the other.
+struct Call {
+    jarq_dtype dtype;
+    int n, d, vocab;
+    const int64_t *tokens;
+    char *work;
+    cudaStream_t s;
+    int *failed;
+    int launches = 0;
+
+    template <class F>
+    cudaError_t typed(F f) {
+        ++launches;
+        return dtype == JARQ_F16 ? f(__half()) : f(__nv_bfloat16());
+    }
+    cudaError_t copy(const void *x, int64_t ld, int rows, char *out, int pitch) {
+        return typed([&](auto type) {
+            using T = decltype(type);
+            copy_rows_kernel<T, false><<<ceil_div((int64_t)rows * (pitch / 8), 256), 256, 0, s>>>(
+                static_cast<const T *>(x), ld, rows, d, reinterpret_cast<T *>(out), pitch, nullptr, nullptr, nullptr);
+            return cudaGetLastError();
+        });
+    }
+    cudaError_t weigh(const void *x, int64_t ld, char *out, int pitch, const float *g, const int *top) {
+        return typed([&](auto type) {
+            using T = decltype(type);
+            copy_rows_kernel<T, true><<<ceil_div((int64_t)n * (pitch / 8), 256), 256, 0, s>>>(
+                static_cast<const T *>(x), ld, n, d, reinterpret_cast<T *>(out), pitch, tokens, g, top);
+            return cudaGetLastError();
+        });
+    }
+    cudaError_t sum_splits(const float *slab, int splits, int rows, int pitch, void *out, int64_t ld, const float *g,
+                           const int *top) {
+        return typed([&](auto type) {
+            using T = decltype(type);
+            sum_splits_kernel<T><<<ceil_div((int64_t)rows * (pitch / 4), 256), 256, 0, s>>>(
+                slab, splits, rows, d, pitch, static_cast<T *>(out), ld, g, top);
+            return cudaGetLastError();
+        });
+    }
+    // the rows of x as TMA can read them: themselves, or a copy of them
+    cudaError_t readable(const void *x, int64_t ld, int rows, char *room, int pitch, Matrix *m) {
+        *m = {static_cast<const char *>(x), ld};
+        if (rows_aligned(x, ld, rows)) return cudaSuccess;
+        *m = {room, pitch};
+        return copy(x, ld, rows, room, pitch);
+    }
+    ProductArgs shape(int m, int cols, int k, int splits) const {
+        ProductArgs a{};
+        a.m = m, a.n = cols;
+        a.chunks = ceil_div(k, 64);
+        a.per = ceil_div(a.chunks, splits);
+        a.splits = ceil_div(a.chunks, a.per);
+        a.mt = ceil_div(m, 256), a.nt = ceil_div(cols, 256);
+        a.half = dtype == JARQ_F16;
+        a.tokens = tokens, a.vocab = vocab;
+        a.last = true;
+        a.failed = failed;
+        return a;
+    }
+    cudaError_t product(Product which, const CUtensorMap &a, const CUtensorMap &b, const ProductArgs &args) {
+        ++launches;
+        return launch_product(which, a, b, args, s);
+    }
+};
+
+#define TRY(x)                                                  \
+    do {                                                        \
+        if (const cudaError_t e_ = (x); e_ != cudaSuccess) return e_; \
+    } while (0)
+
+cudaError_t run_loss(Call &c, const void *X, int64_t ldx, const void *W, int64_t ldw, const Plan &p, float *loss, float *lse) {
+    Matrix x, w;
+    TRY(c.readable(X, ldx, c.n, c.work + p.copy_x, p.pitch, &x));
+    TRY(c.readable(W, ldw, c.vocab, c.work + p.copy_w, p.pitch, &w));
+    CUtensorMap mx, mw;
+    TRY(tensor_map(&mx, x.p, c.n, c.d, x.ld, 128));
+    TRY(tensor_map(&mw, w.p, c.vocab, c.d, w.ld, 128));
+    ProductArgs a = c.shape(c.n, c.vocab, c.d, 1);
+    a.part = reinterpret_cast<float2 *>(c.work + p.parts);
+    a.target = reinterpret_cast<float *>(c.work + p.target);
+    TRY(c.product(kLoss, mx, mw, a));
+    ++c.launches;
+    // few rows: more threads for each
+    if (c.n < 8 * kPairs)
+        loss_join_kernel<64><<<ceil_div(c.n, 4), 256, 0, c.s>>>(a.part, 2 * a.nt, a.target, c.tokens, c.n, c.vocab, loss, lse);
+    else
+        loss_join_kernel<8><<<ceil_div(c.n, 32), 256, 0, c.s>>>(a.part, 2 * a.nt, a.target, c.tokens, c.n, c.vocab, loss, lse);
+    return cudaGetLastError();
+}
+
+cudaError_t run_grad(Call &c, const void *X, int64_t ldx, const void *W, int64_t ldw, const Plan &p, const float *lse,
+                     const float *g, void *dX, int64_t lddx, void *dW, int64_t lddw) {
+    Matrix x, w;
+    TRY(c.readable(X, ldx, c.n, c.work + p.copy_x, p.pitch, &x));
+    TRY(c.readable(W, ldw, c.vocab, c.work + p.copy_w, p.pitch, &w));
+    int *top = reinterpret_cast<int *>(c.work + p.top);
+    CUtensorMap mx, mw, md, mb;
+    if (dW) {
+        if (c.dtype == JARQ_F16) {
+            ++c.launches;
+            top_exponent_kernel<<<1, 1024, 0, c.s>>>(c.tokens, g, c.n, top);
+            TRY(cudaGetLastError());
+        }
+        TRY(c.weigh(X, ldx, c.work + p.weighed, p.pitch, g, top));
+    }
+    char *D = c.work + p.D;
+    float *sums_x = p.slab_x ? reinterpret_cast<float *>(c.work + p.sums_x) : nullptr;
+    float *sums_w = p.slab_w ? reinterpret_cast<float *>(c.work + p.sums_w) : nullptr;
+    for (int i = 0; i < p.pieces; ++i) {
+        const int v0 = i * p.width, width = std::min(p.width, c.vocab - v0);
+        {
+            TRY(tensor_map(&mx, x.p, c.n, c.d, x.ld, 128));
+            TRY(tensor_map(&mw, w.row(v0), width, c.d, w.ld, 128));
+            ProductArgs a = c.shape(c.n, width, c.d, 1);
+            a.lse = lse, a.g = g, a.first = v0;
+            a.out = D, a.ldo = p.width;
+            TRY(c.product(kLogits, mx, mw, a));
+        }
+        if (dX) {
+            TRY(tensor_map(&md, D, c.n, width, p.width, 128));
+            TRY(tensor_map(&mb, w.row(v0), width, c.d, w.ld, 64));
+            ProductArgs a = c.shape(c.n, c.d, width, p.split_x);
+            a.g = g;
+            a.out = dX, a.ldo = lddx;
+            a.slab = sums_x, a.pitch = p.pitch;
+            a.add = i > 0;
+            a.last = p.split_x == 1 && i + 1 == p.pieces;
+            TRY(c.product(kHidden, md, mb, a));
+        }
+        if (dW) {
+            void *out = static_cast<char *>(dW) + (int64_t)v0 * lddw * 2;
+            TRY(tensor_map(&md, D, c.n, width, p.width, 64));
+            TRY(tensor_map(&mb, c.work + p.weighed, c.n, c.d, p.pitch, 64));
+            ProductArgs a = c.shape(width, c.d, c.n, p.split_w);
+            a.out = out, a.ldo = lddw;
+            a.slab = sums_w, a.pitch = p.pitch;
+            a.last = !p.slab_w;
+            a.top = top;
+            TRY(c.product(kHead, md, mb, a));
+            if (p.slab_w) TRY(c.sum_splits(sums_w, a.splits, width, p.pitch, out, lddw, nullptr, top));
+        }
+    }
+    if (dX && p.split_x > 1) TRY(c.sum_splits(sums_x, p.split_x, c.n, p.pitch, dX, lddx, g, nullptr));
+    return cudaSuccess;
+}
+
+jarq_status check(const void *X, jarq_dtype dtype, int n, int d, int64_t ldx, const void *W, int vocab, int64_t ldw,
+                  const int64_t *tokens) {
+    if ((dtype != JARQ_F16 && dtype != JARQ_BF16) || n < 0 || n > kMostRows || d < 1 || d > kMostWidth || vocab < 1 ||
+        vocab > kMostVocab || ldx < d || ldw < d)
+        return JARQ_ERR_ARG;
+    if (n == 0) return JARQ_OK;
+    if (!usable(X, 2) || !usable(W, 2) || !usable(tokens, 8)) return JARQ_ERR_ARG;
+    return JARQ_OK;
+}
+
+jarq_status finish(cudaError_t e, int launches) {
+    count_launches(launches);
+    if (e == cudaSuccess) return JARQ_OK;
+    (void)cudaGetLastError();
+    return JARQ_ERR_CUDA;
+}
+
+// More tiles than pairs, so that some have a second one, which is never summed.
+constexpr int kStalledRows = 2048, kStalledTokens = 4096, kStalledWidth = 256;
+
+}  // namespace
+
+size_t stalled_bytes() {
+    return (size_t)(kStalledRows + kStalledTokens) * kStalledWidth * 2 + kStalledRows * (sizeof(int64_t) + sizeof(float)) +
+           (size_t)2 * (kStalledTokens / 256) * kStalledRows * sizeof(float2);
+}
+cudaError_t launch_stalled(char *zeros, int *failed, cudaStream_t s) {
+    char *w = zeros + (size_t)kStalledRows * kStalledWidth * 2, *rest = w + (size_t)kStalledTokens * kStalledWidth * 2;
+    Call c{JARQ_F16, kStalledRows, kStalledWidth, kStalledTokens, reinterpret_cast<const int64_t *>(rest), zeros, s, failed};
+    ProductArgs a = c.shape(c.n, c.vocab, c.d, 1);
+    a.part = reinterpret_cast<float2 *>(rest + kStalledRows * sizeof(int64_t));
+    a.target = reinterpret_cast<float *>(a.part + (size_t)2 * a.nt * c.n);
+    CUtensorMap mx, mw;
+    TRY(tensor_map(&mx, zeros, c.n, c.d, c.d, 128));
+    TRY(tensor_map(&mw, w, c.vocab, c.d, c.d, 128));
+    return launch_product(kLoss, mx, mw, a, s, true);
+}
+
+}  // namespace head
+}  // namespace jarq
+
+using namespace jarq;
+using namespace jarq::head;
+
+extern "C" {
+
+size_t jarq_cross_entropy_workspace(int n, int d, int vocab, int rows_aligned) {
+    if (n < 1 || n > kMostRows || d < 1 || d > kMostWidth || vocab < 1 || vocab > kMostVocab) return 0;
+    return Plan(n, d, vocab, rows_aligned != 0).bytes;
+}
+
+jarq_status jarq_cross_entropy(const void *X, jarq_dtype dtype, int n, int d, int64_t ldx, const void *W,
+                               int vocab, int64_t ldw, const int64_t *tokens, float *loss, float *lse,
+                               void *workspace, size_t workspace_bytes, void *stream) {
+    const jarq_status ok = check(X, dtype, n, d, ldx, W, vocab, ldw, tokens);
+    if (ok != JARQ_OK || n == 0) return ok;
+    if (!usable(loss, 4) || (lse && !usable(lse, 4))) return JARQ_ERR_ARG;
+    const Plan plan(n, d, vocab, rows_aligned(X, ldx, n) && rows_aligned(W, ldw, vocab));
+    if (!usable(workspace, 16) || workspace_bytes < plan.bytes) return JARQ_ERR_ARG;
+    if (const jarq_status late = async_failure()) return late;
+    Call c{dtype, n, d, vocab, tokens, static_cast<char *>(workspace), (cudaStream_t)stream, async_word()};
+    if (!c.failed) return JARQ_ERR_NOMEM;
+    ProfScope ps("cross_entropy", c.s);
+    const cudaError_t e = run_loss(c, X, ldx, W, ldw, plan, loss, lse);
+    ps.done();
+    return finish(e, c.launches);
+}
+
+size_t jarq_cross_entropy_grad_workspace(int n, int d, int vocab, int rows_aligned, int hidden, int head) {
+    if (n < 1 || n > kMostRows || d < 1 || d > kMostWidth || vocab < 1 || vocab > kMostVocab) return 0;
+    return Plan(n, d, vocab, rows_aligned != 0, hidden != 0, head != 0).bytes;
+}
+
+jarq_status jarq_cross_entropy_grad(const void *X, jarq_dtype dtype, int n, int d, int64_t ldx, const void *W,
+                                    int vocab, int64_t ldw, const int64_t *tokens, const float *lse,
+                                    const float *g_loss, void *dX, int64_t lddx, void *dW, int64_t lddw,
+                                    void *workspace, size_t workspace_bytes, void *stream) {
+    const jarq_status ok = check(X, dtype, n, d, ldx, W, vocab, ldw, tokens);
+    if (ok != JARQ_OK || (!dX && !dW) || (dX && lddx < d) || (dW && lddw < d)) return JARQ_ERR_ARG;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (n == 0) {
+        // no rows: no gradient reaches the head
+        if (!dW) return JARQ_OK;
+        if (!usable(dW, 2)) return JARQ_ERR_ARG;
+        const int64_t blocks = ((int64_t)vocab * d + 255) / 256;
+        if (blocks > 0x7FFFFFFF) return JARQ_ERR_ARG;
+        if (const jarq_status late = async_failure()) return late;
+        zero_rows_kernel<<<(unsigned)blocks, 256, 0, st>>>(static_cast<__half *>(dW), lddw, vocab, d);
+        return finish(cudaGetLastError(), 1);
+    }
+    if (!usable(lse, 4) || !usable(g_loss, 4) || (dX && !usable(dX, 2)) || (dW && !usable(dW, 2))) return JARQ_ERR_ARG;
+    const Plan plan(n, d, vocab, rows_aligned(X, ldx, n) && rows_aligned(W, ldw, vocab), dX != nullptr, dW != nullptr);
+    if (!usable(workspace, 16) || workspace_bytes < plan.bytes) return JARQ_ERR_ARG;
+    if (const jarq_status late = async_failure()) return late;
+    Call c{dtype, n, d, vocab, tokens, static_cast<char *>(workspace), st, async_word()};
+    if (!c.failed) return JARQ_ERR_NOMEM;
+    ProfScope ps("cross_entropy_grad", st);
+    const cudaError_t e = run_grad(c, X, ldx, W, ldw, plan, lse, g_loss, dX, lddx, dW, lddw);
+    ps.done();
+    return finish(e, c.launches);
+}
+
+}  // extern "C"

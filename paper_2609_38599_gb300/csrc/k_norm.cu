@@ -1,0 +1,521 @@
+// Root-mean-square norm of rows with the residual's addition, its outputs in the
+// rows' type and in 8-bit integers, and its gradient.
+//
+//   h = round(x + r),  rstd = (mean_k h_k^2 + eps)^(-1/2),  v = h gain,
+//   y = round(v rstd),  a = max_k |v_k|,  scale = (a / 127) rstd,  q = rint(v (127 / a)).
+// rstd is one number a row, so it goes into the row's scale and the integers do
+// not depend on the order of the sum behind it.  With u = dy gain,
+//   dx = dh + rstd (u - h rstd^2 mean_k u_k h_k),   dgain = sum_t dy h rstd.
+//
+// One pass over memory: a row's threads hold it in registers from the loads to the
+// outputs.  Rows are read 16 bytes at a time where every array's rows lie on
+// 16-byte boundaries, else an element at a time, neighbouring threads reading
+// neighbouring elements.
+#include <math.h>
+
+#include <algorithm>
+
+#include "integer.cuh"
+#include "quantize.cuh"
+#include "rows.cuh"
+
+namespace jarq {
+namespace {
+
+using namespace rows;
+
+constexpr int kMostGradBlocks = 608;       // four for each of 152 SMs
+
+// Elements that a thread reads at a time, how often it does so and keeps them, and
+// so the longest row that P threads hold.  (1024 threads have 64 registers each.)
+template <class T, bool VEC, int P>
+struct Shape {
+    static constexpr int E = VEC ? kUnit<T> : 1, held = !VEC ? 8 : P == 1024 ? 16 / E : 4, row = P * E * held;
+};
+
+// Elements k .. k + E - 1 of a row of d.
+template <int E, class T>
+__device__ __forceinline__ void load(const T *p, int k, int d, float (&v)[E]) {
+    if constexpr (E == 1) {
+        v[0] = to_float(p[k]);
+    } else if (k + E <= d) {
+        if constexpr (E == kUnit<T>) {
+            unpack(*reinterpret_cast<const uint4 *>(p + k), v, T());
+        } else {                            // float32 beside a 16-bit type
+            static_assert(E == 2 * kUnit<T>, "two units of float32");
+            const float4 lo = reinterpret_cast<const float4 *>(p + k)[0], hi = reinterpret_cast<const float4 *>(p + k)[1];
+            v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w;
+            v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = k + e < d ? to_float(p[k + e]) : 0.f;
+    }
+}
+template <int E, class T>
+__device__ __forceinline__ void store(T *p, int k, int d, const float (&v)[E]) {
+    if constexpr (E == 1) {
+        p[k] = from_float<T>(v[0]);
+    } else if (k + E <= d) {
+        *reinterpret_cast<uint4 *>(p + k) = pack(v, T());
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (k + e < d) p[k + e] = from_float<T>(v[e]);
+    }
+}
+template <int E>
+__device__ __forceinline__ void store_codes(int8_t *p, int k, int d, const int (&q)[E]) {
+    if constexpr (E == 1) {
+        p[k] = (int8_t)q[0];
+    } else if (k + E <= d) {
+        uint32_t w[E / 4];
+#pragma unroll
+        for (int i = 0; i < E / 4; ++i)
+            w[i] = __byte_perm(__byte_perm(q[4 * i], q[4 * i + 1], 0x0040), __byte_perm(q[4 * i + 2], q[4 * i + 3], 0x0040), 0x5410);
+        if constexpr (E == 8)
+            *reinterpret_cast<uint2 *>(p + k) = make_uint2(w[0], w[1]);
+        else
+            *reinterpret_cast<uint32_t *>(p + k) = w[0];
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (k + e < d) p[k + e] = (int8_t)q[e];
+    }
+}
+// The gains of elements k ..: 1 where there are none, float32 or of the rows' type.
+template <int E, class T>
+__device__ __forceinline__ void load_gain(const void *gain, bool wide, int k, int d, float (&g)[E]) {
+    if (!gain) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) g[e] = 1.f;
+    } else if (wide) {
+        load<E>(static_cast<const float *>(gain), k, d, g);
+    } else {
+        load<E>(static_cast<const T *>(gain), k, d, g);
+    }
+}
+
+__device__ __forceinline__ float warp_sum(float x) {
+#pragma unroll
+    for (int off = 16; off; off /= 2) x += __shfl_xor_sync(0xffffffffu, x, off);
+    return x;
+}
+// The sum over a row's P threads, in all of them, the same bits in each.
+// `part`: P / 32 floats; two sums in a row need two of them.
+template <int P>
+__device__ __forceinline__ float row_sum(float x, float *part) {
+    x = warp_sum(x);
+    if constexpr (P > 32) {
+        if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = x;
+        __syncthreads();
+        x = warp_sum((threadIdx.x & 31) < P / 32 ? part[threadIdx.x & 31] : 0.f);
+    }
+    return x;
+}
+
+struct NormArgs {
+    const void *X, *R, *gain;
+    void *H, *Y;
+    int8_t *Q;
+    float *scale, *rstd;
+    int64_t ldx, ldr, ldh, ldy, ldq;
+    int n, d;
+    float eps;
+    bool wide_gain;
+};
+
+// T: element type; VEC: rows on 16-byte boundaries; P: threads of a row (a block of
+// 256 has several rows where P is 32).
+template <class T, bool VEC, int P>
+__global__ void __launch_bounds__(P == 32 ? 256 : P) norm_kernel(NormArgs a) {
+    constexpr int E = Shape<T, VEC, P>::E, kHeld = Shape<T, VEC, P>::held;
+    __shared__ float sums[2][32];
+    __shared__ uint32_t tops[32];
+    const int t = P == 32 ? threadIdx.x & 31 : threadIdx.x;
+    const int64_t r = P == 32 ? (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x;
+    if (r >= a.n) return;
+    const T *x = static_cast<const T *>(a.X) + r * a.ldx, *res = static_cast<const T *>(a.R) + r * a.ldr;
+    T *h = static_cast<T *>(a.H) + r * a.ldh, *y = static_cast<T *>(a.Y) + r * a.ldy;
+    int8_t *q = a.Q + r * a.ldq;
+    // what a later pass over the row reads
+    const T *again = a.R ? h : x;
+
+    auto read = [&](int k, float (&v)[E]) {
+        load<E>(x, k, a.d, v);
+        if (a.R) {
+            float o[E];
+            load<E>(res, k, a.d, o);
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] = to_float(from_float<T>(v[e] + o[e]));
+            store<E>(h, k, a.d, v);
+        }
+    };
+    float held[kHeld][E];
+    float sum = 0.f;
+    uint32_t top = 0;
+    auto take = [&](int k, float (&v)[E]) {
+        float g[E];
+        load_gain<E, T>(a.gain, a.wide_gain, k, a.d, g);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            sum = fmaf(v[e], v[e], sum);
+            v[e] = __fmul_rn(v[e], g[e]);
+            top = max(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+        if ((t + i * P) * E < a.d) read((t + i * P) * E, held[i]);
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+        if ((t + i * P) * E < a.d) take((t + i * P) * E, held[i]);
+    for (int64_t k = (int64_t)(t + kHeld * P) * E; k < a.d; k += P * E) {
+        float v[E];
+        read((int)k, v);
+        take((int)k, v);
+    }
+    sum = warp_sum(sum);
+    top = __reduce_max_sync(0xffffffffu, top);
+    if constexpr (P > 32) {
+        if ((threadIdx.x & 31) == 0) {
+            sums[0][threadIdx.x >> 5] = sum;
+            tops[threadIdx.x >> 5] = top;
+        }
+        __syncthreads();
+        const int w = threadIdx.x & 31;
+        sum = warp_sum(w < P / 32 ? sums[0][w] : 0.f);
+        top = __reduce_max_sync(0xffffffffu, w < P / 32 ? tops[w] : 0u);
+    }
+    float rstd = 1.f / sqrtf(sum / (float)a.d + a.eps);
+    if (isinf(sum)) {
+        // squares past float32's range: the row scaled by 2^-80 (the row is read
+        // once more; an infinity in it stays one, and rstd is 0)
+        float small = 0.f;
+        for (int64_t k = (int64_t)t * E; k < a.d; k += P * E) {
+            float v[E];
+            load<E>(again, (int)k, a.d, v);
+#pragma unroll
+            for (int e = 0; e < E; ++e) small = fmaf(v[e] * 0x1p-80f, v[e] * 0x1p-80f, small);
+        }
+        rstd = 0x1p-80f / sqrtf(row_sum<P>(small, sums[1]) / (float)a.d);
+    }
+    const quant::RowScale by(top);
+    if (t == 0) {
+        if (a.rstd) a.rstd[r] = rstd;
+        if (a.scale) a.scale[r] = __fmul_rn(by.scale, rstd);
+    }
+    auto put = [&](int k, const float (&v)[E]) {
+        if (a.Y) {
+            float o[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = v[e] * rstd;
+            store<E>(y, k, a.d, o);
+        }
+        if (a.Q) {
+            int c[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) c[e] = by.bad ? 0 : __float2int_rn(__fmul_rn(v[e], by.inv));
+            store_codes<E>(q, k, a.d, c);
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+        if ((t + i * P) * E < a.d) put((t + i * P) * E, held[i]);
+    for (int64_t k = (int64_t)(t + kHeld * P) * E; k < a.d; k += P * E) {
+        float v[E], g[E];
+        load<E>(again, (int)k, a.d, v);
+        load_gain<E, T>(a.gain, a.wide_gain, (int)k, a.d, g);
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = __fmul_rn(v[e], g[e]);
+        put((int)k, v);
+    }
+}
+
+struct GradArgs {
+    const void *H, *gain, *dY, *dH;
+    void *dX;
+    const float *rstd;
+    float *part;               // [blocks][d] sums of the gains' gradient, or null
+    int64_t ldh, ldy, lds, ldx;
+    int n, d;
+    bool wide_gain;
+};
+
+// A block goes from row to row; a thread has the same columns of each, and so their
+// part of the gains' gradient in registers.  GAIN: it is wanted, and a row fits
+// what the threads hold.
+template <class T, bool VEC, int P, bool GAIN>
+__global__ void __launch_bounds__(P) norm_grad_kernel(GradArgs a) {
+    constexpr int E = Shape<T, VEC, P>::E, kHeld = Shape<T, VEC, P>::held;
+    __shared__ float part[2][32];
+    const int t = threadIdx.x;
+    float acc[GAIN ? kHeld : 1][E];
+    if constexpr (GAIN)
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[i][e] = 0.f;
+    int turn = 0;
+    for (int64_t r = blockIdx.x; r < a.n; r += gridDim.x, turn ^= 1) {
+        const T *h = static_cast<const T *>(a.H) + r * a.ldh, *dy = static_cast<const T *>(a.dY) + r * a.ldy;
+        const T *dh = static_cast<const T *>(a.dH) + r * a.lds;
+        T *dx = static_cast<T *>(a.dX) + r * a.ldx;
+        const float rstd = a.rstd[r];
+        float hv[kHeld][E], u[kHeld][E], dot = 0.f;
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            const int k = (t + i * P) * E;
+            if (k >= a.d) continue;
+            load<E>(h, k, a.d, hv[i]);
+            load<E>(dy, k, a.d, u[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            const int k = (t + i * P) * E;
+            if (k >= a.d) continue;
+            float g[E];
+            load_gain<E, T>(a.gain, a.wide_gain, k, a.d, g);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                if constexpr (GAIN) acc[i][e] = fmaf(u[i][e] * hv[i][e], rstd, acc[i][e]);
+                u[i][e] *= g[e];
+                dot = fmaf(u[i][e], hv[i][e], dot);
+            }
+        }
+        if constexpr (!GAIN)
+            for (int64_t k = (int64_t)(t + kHeld * P) * E; k < a.d; k += P * E) {
+                float v[E], w[E], g[E];
+                load<E>(h, (int)k, a.d, v);
+                load<E>(dy, (int)k, a.d, w);
+                load_gain<E, T>(a.gain, a.wide_gain, (int)k, a.d, g);
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    dot = fmaf(w[e] * g[e], v[e], dot);
+            }
+        if (!a.dX) continue;
+        // the two rows of `part` take turns: one is written while the other may still be read
+        const float along = rstd * rstd * (row_sum<P>(dot, part[turn]) / (float)a.d);
+        auto put = [&](int k, const float (&v)[E], const float (&w)[E]) {
+            float o[E], s[E];
+            if (a.dH) load<E>(dh, k, a.d, s);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                o[e] = rstd * fmaf(-v[e], along, w[e]);
+                if (a.dH) o[e] += s[e];
+            }
+            store<E>(dx, k, a.d, o);
+        };
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            const int k = (t + i * P) * E;
+            if (k < a.d) put(k, hv[i], u[i]);
+        }
+        if constexpr (!GAIN)
+            for (int64_t k = (int64_t)(t + kHeld * P) * E; k < a.d; k += P * E) {
+                float v[E], w[E], g[E];
+                load<E>(h, (int)k, a.d, v);
+                load<E>(dy, (int)k, a.d, w);
+                load_gain<E, T>(a.gain, a.wide_gain, (int)k, a.d, g);
+#pragma unroll
+                for (int e = 0; e < E; ++e) w[e] *= g[e];
+                put((int)k, v, w);
+            }
+    }
+    if constexpr (GAIN) {
+        float *to = a.part + (size_t)blockIdx.x * a.d;
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if ((t + i * P) * E + e < a.d) to[(t + i * P) * E + e] = acc[i][e];
+    }
+}
+
+// The gains' gradient of rows too long to be held: 32 columns a block, its parts of
+// `rows_each` rows written for gain_join_kernel.
+template <class T>
+__global__ void __launch_bounds__(256) gain_columns_kernel(GradArgs a, int rows_each) {
+    __shared__ float part[8][32];
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const int64_t k = (int64_t)blockIdx.x * 32 + lane;
+    const int64_t r0 = (int64_t)blockIdx.y * rows_each, r1 = min((int64_t)a.n, r0 + rows_each);
+    float acc = 0.f;
+    if (k < a.d)
+        for (int64_t r = r0 + w; r < r1; r += 8)
+            acc = fmaf(to_float(static_cast<const T *>(a.dY)[r * a.ldy + k]) * to_float(static_cast<const T *>(a.H)[r * a.ldh + k]),
+                       a.rstd[r], acc);
+    part[w][lane] = acc;
+    __syncthreads();
+    if (w == 0 && k < a.d) {
+#pragma unroll
+        for (int i = 1; i < 8; ++i) acc += part[i][lane];
+        a.part[(size_t)blockIdx.y * a.d + k] = acc;
+    }
+}
+
+// dgain[k] = sum of its parts, always in the same order.
+__global__ void __launch_bounds__(1024) gain_join_kernel(const float *parts, int count, int d, float *dgain) {
+    __shared__ float part[32][33];
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const int64_t k = (int64_t)blockIdx.x * 32 + lane;
+    float acc = 0.f;
+    if (k < d)
+        for (int i = w; i < count; i += 32) acc += parts[(size_t)i * d + k];
+    part[w][lane] = acc;
+    __syncthreads();
+    acc = warp_sum(part[lane][w]);                 // column w of the block's 32
+    const int64_t c = (int64_t)blockIdx.x * 32 + w;
+    if (lane == 0 && c < d) dgain[c] = acc;
+}
+
+template <class T, bool VEC, int P>
+cudaError_t launch_norm_p(const NormArgs &a, cudaStream_t s) {
+    const int64_t blocks = P == 32 ? ((int64_t)a.n + 7) / 8 : a.n;
+    norm_kernel<T, VEC, P><<<(unsigned)blocks, P == 32 ? 256 : P, 0, s>>>(a);
+    return cudaGetLastError();
+}
+template <class T, bool VEC>
+cudaError_t launch_norm_t(const NormArgs &a, cudaStream_t s) {
+    // the fewest threads that hold a row; for few rows one unit a thread
+    const int64_t d = a.n <= num_sms() ? (int64_t)a.d * Shape<T, VEC, 256>::held : a.d;
+    if (d <= Shape<T, VEC, 32>::row) return launch_norm_p<T, VEC, 32>(a, s);
+    if (d <= Shape<T, VEC, 128>::row) return launch_norm_p<T, VEC, 128>(a, s);
+    if (d <= Shape<T, VEC, 256>::row) return launch_norm_p<T, VEC, 256>(a, s);
+    if (d <= Shape<T, VEC, 512>::row) return launch_norm_p<T, VEC, 512>(a, s);
+    return launch_norm_p<T, VEC, 1024>(a, s);
+}
+
+template <class T, bool VEC, int P>
+cudaError_t launch_grad_p(const GradArgs &a, int blocks, cudaStream_t s) {
+    if (a.part)
+        norm_grad_kernel<T, VEC, P, true><<<blocks, P, 0, s>>>(a);
+    else
+        norm_grad_kernel<T, VEC, P, false><<<blocks, P, 0, s>>>(a);
+    return cudaGetLastError();
+}
+
+template <class T, bool VEC>
+cudaError_t launch_grad_t(GradArgs a, float *dgain, cudaStream_t s) {
+    int parts = std::min(a.n, kMostGradBlocks);
+    float *const part = a.part;
+    cudaError_t e = cudaSuccess;
+    if (part && a.d > Shape<T, VEC, 1024>::row) {
+        // rows that no block holds: the columns' sums apart, and first, since dX may be dY
+        const int each = (a.n + std::min(parts, 32) - 1) / std::min(parts, 32);
+        parts = (a.n + each - 1) / each;
+        gain_columns_kernel<T><<<dim3((unsigned)(((int64_t)a.d + 31) / 32), parts), 256, 0, s>>>(a, each);
+        count_launches(1);
+        e = cudaGetLastError();
+        a.part = nullptr;
+    }
+    if (e == cudaSuccess && (a.dX || a.part)) {
+        const int blocks = std::min(a.n, kMostGradBlocks);
+        if (a.d <= Shape<T, VEC, 128>::row) e = launch_grad_p<T, VEC, 128>(a, blocks, s);
+        else if (a.d <= Shape<T, VEC, 256>::row) e = launch_grad_p<T, VEC, 256>(a, blocks, s);
+        else if (a.d <= Shape<T, VEC, 512>::row) e = launch_grad_p<T, VEC, 512>(a, blocks, s);
+        else e = launch_grad_p<T, VEC, 1024>(a, blocks, s);
+        count_launches(1);
+    }
+    if (e == cudaSuccess && dgain) {
+        gain_join_kernel<<<(unsigned)(((int64_t)a.d + 31) / 32), 1024, 0, s>>>(part, parts, a.d, dgain);
+        count_launches(1);
+        e = cudaGetLastError();
+    }
+    return e;
+}
+
+bool aligned(const void *p, size_t b) { return ((uintptr_t)p & (b - 1)) == 0; }
+// Whether all rows begin on 16-byte boundaries (n/a: no such array).
+bool vector(const void *p, int64_t ld, int n, size_t size) {
+    return !p || (aligned(p, 16) && (n == 1 || ld * (int64_t)size % 16 == 0));
+}
+bool usable(const void *p, size_t size) { return p && on_device(p) && aligned(p, size); }
+bool usable_or_null(const void *p, size_t size) { return !p || usable(p, size); }
+
+jarq_status finish(cudaError_t e) {
+    if (e == cudaSuccess) return JARQ_OK;
+    (void)cudaGetLastError();
+    return JARQ_ERR_CUDA;
+}
+
+}  // namespace
+}  // namespace jarq
+
+using namespace jarq;
+
+extern "C" {
+
+jarq_status jarq_rms_norm(const void *X, jarq_dtype dtype, int n, int d, int64_t ldx, const void *R,
+                          int64_t ldr, void *H, int64_t ldh, const void *gain, jarq_dtype gain_dtype,
+                          float eps, void *Y, int64_t ldy, int8_t *Q, int64_t ldq, float *scale,
+                          float *rstd, void *stream) {
+    if (n < 0 || n > kMostIndex || d < 1 || d > kMostIndex || ldx < d || !is_dtype(dtype) || !(eps > 0.f) || isinf(eps))
+        return JARQ_ERR_ARG;
+    if (gain && gain_dtype != dtype && gain_dtype != JARQ_F32) return JARQ_ERR_ARG;
+    if ((R != nullptr) != (H != nullptr) || (Q != nullptr) != (scale != nullptr)) return JARQ_ERR_ARG;
+    if ((R && (ldr < d || ldh < d)) || (Y && ldy < d) || (Q && ldq < d) || (R == H && R && n > 1 && ldr != ldh))
+        return JARQ_ERR_ARG;
+    if (n == 0) return JARQ_OK;
+    const size_t size = size_of(dtype);
+    if (!usable(X, size) || !usable_or_null(R, size) || !usable_or_null(H, size) || !usable_or_null(Y, size) ||
+        !usable_or_null(Q, 1) || !usable_or_null(scale, 4) || !usable_or_null(rstd, 4) ||
+        !usable_or_null(gain, gain ? size_of(gain_dtype) : 1))
+        return JARQ_ERR_ARG;
+    if (const jarq_status late = async_failure()) return late;
+    cudaStream_t st = (cudaStream_t)stream;
+    const NormArgs a{X, R, gain, H, Y, Q, scale, rstd, ldx, ldr, ldh, ldy, ldq, n, d, eps, gain_dtype != dtype};
+    const bool vec = vector(X, ldx, n, size) && vector(R, ldr, n, size) && vector(H, ldh, n, size) &&
+                     vector(Y, ldy, n, size) && vector(gain, 0, 1, 1) &&
+                     (!Q || (aligned(Q, 8) && (n == 1 || ldq % 8 == 0)));
+    ProfScope ps("rms_norm", st);
+    const cudaError_t e = with_type(dtype, [&](auto type) {
+        using T = decltype(type);
+        return vec ? launch_norm_t<T, true>(a, st) : launch_norm_t<T, false>(a, st);
+    });
+    ps.done();
+    count_launches(1);
+    return finish(e);
+}
+
+size_t jarq_rms_norm_grad_workspace(int n, int d) {
+    if (n < 0 || d < 1) return 0;
+    return (size_t)std::min(n, kMostGradBlocks) * d * sizeof(float);
+}
+
+jarq_status jarq_rms_norm_grad(const void *H, jarq_dtype dtype, int n, int d, int64_t ldh,
+                               const void *gain, jarq_dtype gain_dtype, const float *rstd,
+                               const void *dY, int64_t ldy, const void *dH, int64_t lds, void *dX,
+                               int64_t ldx, float *dgain, void *workspace, size_t workspace_bytes,
+                               void *stream) {
+    if (n < 0 || n > kMostIndex || d < 1 || d > kMostIndex || ldh < d || ldy < d || !is_dtype(dtype)) return JARQ_ERR_ARG;
+    if ((gain && gain_dtype != dtype && gain_dtype != JARQ_F32) || (dH && lds < d) || (dX && ldx < d)) return JARQ_ERR_ARG;
+    if (!dX && !dgain) return JARQ_ERR_ARG;
+    if (n > 1 && dX && ((dX == dY && ldx != ldy) || (dX == dH && ldx != lds))) return JARQ_ERR_ARG;
+    cudaStream_t st = (cudaStream_t)stream;
+    const size_t size = size_of(dtype);
+    if (n == 0) {
+        // no rows: no gradient reaches the gains
+        if (!dgain) return JARQ_OK;
+        if (!usable(dgain, 4)) return JARQ_ERR_ARG;
+        return finish(cudaMemsetAsync(dgain, 0, (size_t)d * sizeof(float), st));
+    }
+    if (!usable(H, size) || !usable(dY, size) || !usable(rstd, 4) || !usable_or_null(dH, size) || !usable_or_null(dX, size) ||
+        !usable_or_null(dgain, 4) || !usable_or_null(gain, gain ? size_of(gain_dtype) : 1))
+        return JARQ_ERR_ARG;
+    if (dgain && (!usable(workspace, 16) || workspace_bytes < jarq_rms_norm_grad_workspace(n, d))) return JARQ_ERR_ARG;
+    if (const jarq_status late = async_failure()) return late;
+    const GradArgs a{H, gain, dY, dH, dX, rstd, dgain ? static_cast<float *>(workspace) : nullptr, ldh, ldy, lds, ldx, n, d,
+                     gain_dtype != dtype};
+    const bool vec = vector(H, ldh, n, size) && vector(dY, ldy, n, size) && vector(dH, lds, n, size) &&
+                     vector(dX, ldx, n, size) && vector(gain, 0, 1, 1);
+    ProfScope ps("norm_grad", st);
+    const cudaError_t e = with_type(dtype, [&](auto type) {
+        using T = decltype(type);
+        return vec ? launch_grad_t<T, true>(a, dgain, st) : launch_grad_t<T, false>(a, dgain, st);
+    });
+    ps.done();
+    return finish(e);
+}
+
+}  // extern "C"

@@ -1,0 +1,424 @@
+// The products of an output head's loss and its gradient on the tensor cores:
+//   logits = X W^T            reduced to a maximum and a sum of exponentials a row,
+//   D = g (softmax - onehot)  from the same product once more, in the inputs' type,
+//   dX = D W,  dW = D^T X.
+// Logits exist in the accumulators alone.
+//
+// A pair of CTAs (cta_group::2) computes tiles of 256 x 256, K in chunks of 64, over
+// a ring that TMA fills; an operand is read as it lies in memory, along K or (W of
+// dX, D and X of dW) along MN, so that nothing is transposed.  In each CTA:
+//   warp 0      TMA producer: its own 128 rows of A and 128 of B's 256 columns
+//   warp 1      TMEM allocation; in the even CTA the MMA issuer
+//   warps 2..9  drain: lane quarter w % 4, half of the columns, of one accumulator
+//               while the MMAs of the next tile fill the other
+// A row of the loss lies in one thread: its maximum and sum need no exchange.
+// Results leave through 4 KB of shared memory a warp, 128 bytes of a row at a time.
+#include <algorithm>
+
+#include "head.cuh"
+#include "tc_common.cuh"
+#include "turns.cuh"
+
+namespace jarq {
+namespace head {
+namespace {
+
+using namespace rows;
+
+constexpr int kBox = 64 * 64 * 2;          // a TMA box of an operand along MN
+constexpr int kTile = 128 * 64 * 2;        // a CTA's part of an operand's chunk
+constexpr int kStage = 2 * kTile;
+constexpr int kStages = 6;
+constexpr int kDrainWarps = 8;
+constexpr int kPart = 32 * 128;            // bytes that a drain warp stages
+constexpr int kBars = 2 * kStages + 5;     // full, empty, afull[2], aempty[2], closing
+constexpr int kSmem = 1024 + kStages * kStage + kDrainWarps * kPart + 8 * kBars + 16;
+constexpr int kThreads = 32 * (2 + kDrainWarps);
+constexpr int kBand = 16;                  // tiles of rows that share the columns' panels in L2
+static_assert(kSmem <= 227 * 1024, "ring and staged parts must fit an SM's shared memory");
+
+// Descriptor of an operand along MN (128-byte swizzle): 64 elements of MN a row,
+// rows of K 128 bytes apart, 8 of them 1024, the next 64 of MN one box further.
+__device__ __forceinline__ uint64_t sdesc_mn(uint32_t saddr) {
+    uint64_t d = 0;
+    d |= (uint64_t)((saddr >> 4) & 0x3FFFu);
+    d |= (uint64_t)(kBox >> 4) << 16;
+    d |= (uint64_t)(1024 >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+
+// A pair's units of work: tiles in bands of kBand tiles of rows, column after column
+// of a band, for one split of K after the other.
+struct Unit {
+    int ri, cj, split;
+    __device__ Unit(int64_t u, const ProductArgs &a) {
+        const int64_t tiles = (int64_t)a.mt * a.nt;
+        split = (int)(u / tiles);
+        u -= split * tiles;
+        const int band = (int)(u / ((int64_t)kBand * a.nt));
+        u -= (int64_t)band * kBand * a.nt;
+        const int rows = min(kBand, a.mt - band * kBand);
+        cj = (int)(u / rows);
+        ri = band * kBand + (int)(u - (int64_t)cj * rows);
+    }
+};
+
+__device__ __forceinline__ uint4 load_shared(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ void store_shared(uint32_t addr, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+// 32 columns of this warp's lanes
+__device__ __forceinline__ void load_columns(uint32_t taddr, float (&x)[32]) {
+    uint32_t v[2][16];
+    tc::tmem_ld16(taddr, v[0]);
+    tc::tmem_ld16(taddr + 16, v[1]);
+    tc::tmem_wait_ld();
+#pragma unroll
+    for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(v[e / 16][e % 16]);
+}
+// This lane's 128 bytes of 32 rows to shared memory, and 16 bytes of four rows at a
+// time back: row 4 i + lane / 8, bytes 16 (lane % 8) ..
+__device__ __forceinline__ void stage_row(uint32_t part, int lane, const uint32_t (&w)[32]) {
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        store_shared(part + lane * 128 + ((i ^ (lane & 7)) << 4), w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    __syncwarp();
+}
+__device__ __forceinline__ uint4 staged(uint32_t part, int lane, int i) {
+    const int row = 4 * i + (lane >> 3);
+    return load_shared(part + row * 128 + (((lane & 7) ^ (row & 7)) << 4));
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi, bool half) {
+    if (half) {
+        const __half2 h = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&h);
+    }
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// A row of 128 columns of logits: maximum, sum of exponentials less the maximum, and
+// the token's logit where it is among them.
+__device__ __forceinline__ void drain_loss(uint32_t acc, const ProductArgs &a, int row, int col, int part) {
+    const int64_t tok = row < a.m ? a.tokens[row] : -1;
+    const int64_t mine = tok - col;
+    float m = -INFINITY, s = 0.f;
+#pragma unroll 1
+    for (int c = 0; c < 128; c += 32) {
+        float x[32];
+        load_columns(acc + c, x);
+        if (col + c + 32 > a.n) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+                if (col + c + e >= a.n) x[e] = -INFINITY;
+        }
+        if (mine >= c && mine < c + 32) {
+            float t = 0.f;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) t = mine == c + e ? x[e] : t;
+            a.target[row] = t;
+        }
+        float top = m;
+#pragma unroll
+        for (int e = 0; e < 32; ++e) top = fmaxf(top, x[e]);
+        const float ref = top == -INFINITY ? 0.f : top;
+        s *= __expf(m - ref);
+        float t[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < 32; ++e) t[e % 4] += __expf(x[e] - ref);
+        s += (t[0] + t[1]) + (t[2] + t[3]);
+        m = top;
+    }
+    if (row < a.m) a.part[(size_t)part * a.m + row] = make_float2(m, s);
+}
+
+// 128 columns of logits to D.
+__device__ __forceinline__ void drain_logits(uint32_t acc, const ProductArgs &a, int row0, int lane, int col, uint32_t part) {
+    const int row = row0 + lane;
+    const bool in = row < a.m;
+    const int64_t tok = in ? a.tokens[row] : -1;
+    const int64_t mine = tok - a.first - col;
+    const float lse = in ? a.lse[row] : 0.f, g0 = in ? a.g[row] : 0.f;
+    const float g = tok >= a.vocab ? __int_as_float(0x7FC00000) : a.half ? scaled(g0) : g0;
+    const bool live = tok >= 0;
+    uint16_t *out = static_cast<uint16_t *>(a.out) + (size_t)row0 * a.ldo + col;
+#pragma unroll 1
+    for (int c = 0; c < 128; c += 64) {
+        uint32_t w[32];
+#pragma unroll
+        for (int h = 0; h < 64; h += 32) {
+            float x[32];
+            load_columns(acc + c + h, x);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+                const float p = x[e] == -INFINITY ? 0.f : __expf(x[e] - lse);
+                x[e] = live ? g * (mine == c + h + e ? p - 1.f : p) : 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) w[(h + e) / 2] = pack2(x[e], x[e + 1], a.half);
+        }
+        stage_row(part, lane, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = 4 * i + (lane >> 3), k = c + 8 * (lane & 7);
+            // whole units up to the pitch: what lies past column n is not read
+            if (row0 + r < a.m && col + k < a.n)
+                *reinterpret_cast<uint4 *>(out + (size_t)r * a.ldo + k) = staged(part, lane, i);
+        }
+    }
+}
+
+// 128 columns of dX or dW: into the float32 sums, or to the result.
+template <bool kRows>
+__device__ __forceinline__ void drain_result(uint32_t acc, const ProductArgs &a, int row0, int lane, int col, int split,
+                                             uint32_t part) {
+    const bool vec = ((uintptr_t)a.out & 7) == 0 && a.ldo % 4 == 0;
+    const int top = !kRows && a.half ? *a.top : 0;
+#pragma unroll 1
+    for (int c = 0; c < 128; c += 32) {
+        if (col + c >= a.n) break;
+        float x[32];
+        load_columns(acc + c, x);
+        uint32_t w[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(x[e]);
+        stage_row(part, lane, w);
+        const int k = col + c + 4 * (lane & 7);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = row0 + 4 * i + (lane >> 3);
+            if (r >= a.m || k >= a.n) continue;
+            const uint4 u = staged(part, lane, i);
+            float y[4] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
+            if (a.slab) {
+                float4 *to = reinterpret_cast<float4 *>(a.slab + ((size_t)split * a.m + r) * a.pitch + k);
+                if (a.add) {
+                    const float4 o = *to;
+                    y[0] += o.x, y[1] += o.y, y[2] += o.z, y[3] += o.w;
+                }
+                if (!a.last) {
+                    *to = make_float4(y[0], y[1], y[2], y[3]);
+                    continue;
+                }
+            }
+            if (a.half) {
+                const float by = ldexpf(1.f, (kRows ? exponent(a.g[r]) : top) - 14);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] *= by;
+            }
+            uint16_t *to = static_cast<uint16_t *>(a.out) + (size_t)r * a.ldo + k;
+            const uint32_t lo = pack2(y[0], y[1], a.half), hi = pack2(y[2], y[3], a.half);
+            if (vec && k + 4 <= a.n) {
+                *reinterpret_cast<uint2 *>(to) = make_uint2(lo, hi);
+            } else {
+                to[0] = (uint16_t)lo;
+                if (k + 1 < a.n) to[1] = (uint16_t)(lo >> 16);
+                if (k + 2 < a.n) to[2] = (uint16_t)hi;
+                if (k + 3 < a.n) to[3] = (uint16_t)(hi >> 16);
+            }
+        }
+    }
+}
+
+// kStalled: for the self-test, the issuer stops after one tile.
+template <Product kWhich, bool kStalled>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    tc_head_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, ProductArgs a) {
+    constexpr uint32_t kPolls = tc::wait_polls(kStalled);
+    constexpr bool kAmn = kWhich == kHead, kBmn = kWhich == kHead || kWhich == kHidden;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    uint64_t *bars = (uint64_t *)(smem + kStages * kStage + kDrainWarps * kPart);
+    uint32_t *tmem_slot = (uint32_t *)(bars + kBars);
+    volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = (int)tc::cluster_rank();
+    const int64_t pair = blockIdx.x / 2, npairs = gridDim.x / 2;
+    const int64_t units = (int64_t)a.mt * a.nt * a.splits;
+
+    auto full = [&](int s) { return tc::smem_u32(bars + s); };
+    auto empty = [&](int s) { return tc::smem_u32(bars + kStages + s); };
+    auto afull = [&](int b) { return tc::smem_u32(bars + 2 * kStages + b); };
+    auto aempty = [&](int b) { return tc::smem_u32(bars + 2 * kStages + 2 + b); };
+    const uint32_t closing = tc::smem_u32(bars + 2 * kStages + 4);
+    auto tileA = [&](int s) { return tc::smem_u32(smem + s * kStage); };
+    auto tileB = [&](int s) { return tc::smem_u32(smem + s * kStage + kTile); };
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            tc::mbar_init(full(s), 1);      // the even CTA's: bytes of both CTAs
+            tc::mbar_init(empty(s), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            tc::mbar_init(afull(b), 1);
+            tc::mbar_init(aempty(b), 2 * kDrainWarps);   // the even CTA's: both drains
+        }
+        tc::mbar_init(closing, 1);
+        *abort_flag = 0;
+        tc::fence_barrier_init();
+    }
+    if (warp == 1) {
+        tc::tmem_alloc_pair(tc::smem_u32(tmem_slot), 512);
+        tc::tmem_relinquish_pair();
+    }
+    if (warp == 0 && lane == 0) {
+        tc::prefetch_tmap(&mapA);
+        tc::prefetch_tmap(&mapB);
+    }
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::cluster_sync();
+    tc::tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    if (warp == 0) {
+        // ---------------- producer
+        bool ok = true;
+        const uint32_t full0 = tc::map_rank(full(0), 0);
+        Slot<kStages> slot(1);
+        int filled = 0;
+        for (int64_t u = pair; u < units && ok; u += npairs) {
+            const Unit unit(u, a);
+            const int ra = unit.ri * 256 + 128 * rank, cb = unit.cj * 256 + 128 * rank;
+            const int c1 = min(a.chunks, (unit.split + 1) * a.per);
+            for (int c = unit.split * a.per; c < c1; ++c, slot.next()) {
+                ok = tc::mbar_wait<kPolls>(empty(slot.s), slot.phase);
+                if (!ok) break;
+                if (tc::elect_one()) {
+                    if (rank == 0) tc::mbar_expect_tx(full(slot.s), 2 * kStage);
+                    const uint32_t bar = full0 + 8 * slot.s;
+                    if (kAmn) {
+#pragma unroll
+                        for (int m = 0; m < 2; ++m)
+                            tc::tma_load_2d_pair(tileA(slot.s) + m * kBox, &mapA, bar, ra + 64 * m, c * 64);
+                    } else {
+                        tc::tma_load_2d_pair(tileA(slot.s), &mapA, bar, c * 64, ra);
+                    }
+                    if (kBmn) {
+#pragma unroll
+                        for (int m = 0; m < 2; ++m)
+                            tc::tma_load_2d_pair(tileB(slot.s) + m * kBox, &mapB, bar, cb + 64 * m, c * 64);
+                    } else {
+                        tc::tma_load_2d_pair(tileB(slot.s), &mapB, bar, c * 64, cb);
+                    }
+                }
+                __syncwarp();
+                ++filled;
+            }
+        }
+        // do not leave before the MMAs have consumed the stages filled here:
+        // no copy or commit is in flight afterwards
+        for (int n = max(0, filled - kStages); n < filled && ok; ++n)
+            ok = tc::mbar_wait<kPolls>(empty(n % kStages), (n / kStages) & 1);
+        if (!ok) {
+            *abort_flag = 1;
+            tc::abandon_ring(full(0), kStages, filled, rank == 0);
+        }
+    } else if (warp == 1) {
+        // ---------------- MMA issuer of the pair
+        if (rank == 0) {
+            bool ok = true;
+            const uint64_t a0 = kAmn ? sdesc_mn(tileA(0)) : tc::sdesc_sw128(tileA(0));
+            const uint64_t b0 = kBmn ? sdesc_mn(tileB(0)) : tc::sdesc_sw128(tileB(0));
+            // 16 of K: 32 bytes along K, two 8-row atoms (2048 bytes) along MN
+            constexpr uint64_t kA = kAmn ? 128 : 2, kB = kBmn ? 128 : 2;
+            const uint32_t idesc = (a.half ? tc::idesc_f16_f32(256, 256) : tc::idesc_bf16_f32(256, 256)) |
+                                   (kAmn ? 1u << 15 : 0) | (kBmn ? 1u << 16 : 0);
+            Slot<kStages> slot(0);
+            Slot<2> acc(1);
+            for (int64_t u = pair; u < units && ok && !(kStalled && u != pair); u += npairs, acc.next()) {
+                const Unit unit(u, a);
+                const int c0 = unit.split * a.per, c1 = min(a.chunks, c0 + a.per);
+                ok = tc::mbar_wait<kPolls>(aempty(acc.s), acc.phase);
+                for (int c = c0; c < c1 && ok; ++c, slot.next()) {
+                    ok = tc::mbar_wait<kPolls>(full(slot.s), slot.phase);
+                    if (!ok) break;
+                    tc::tc_fence_after();
+                    if (tc::elect_one()) {
+                        const uint64_t o = (uint64_t)(slot.s * (kStage >> 4));
+#pragma unroll
+                        for (int sub = 0; sub < 4; ++sub)
+                            tc::mma_f16_pair(tmem + acc.s * 256, a0 + o + kA * sub, b0 + o + kB * sub, idesc, c > c0 || sub > 0);
+                        tc::mma_commit_pair(empty(slot.s));
+                        if (c + 1 == c1) tc::mma_commit_pair(afull(acc.s));
+                    }
+                    __syncwarp();
+                }
+            }
+            if (!tc::mma_done_pair<kPolls>(closing, tc::elect_one()) || !ok) *abort_flag = 1;
+        }
+    } else {
+        // ---------------- drain
+        const int q = warp & 3, half = (warp - 2) >> 2;   // lane quarter, 128-column half
+        const uint32_t released = tc::map_rank(aempty(0), 0);
+        const uint32_t part = tc::smem_u32(smem + kStages * kStage + (warp - 2) * kPart);
+        bool ok = true;
+        Slot<2> acc(0);
+        for (int64_t u = pair; u < units && ok; u += npairs, acc.next()) {
+            const Unit unit(u, a);
+            const int row0 = unit.ri * 256 + 128 * rank + 32 * q, col = unit.cj * 256 + half * 128;
+            ok = __all_sync(0xffffffffu, tc::mbar_wait<kPolls>(afull(acc.s), acc.phase));
+            if (!ok) break;
+            tc::tc_fence_after();
+            const uint32_t at = tmem + ((uint32_t)(32 * q) << 16) + acc.s * 256 + half * 128;
+            if constexpr (kWhich == kLoss)
+                drain_loss(at, a, row0 + lane, col, 2 * unit.cj + half);
+            else if constexpr (kWhich == kLogits)
+                drain_logits(at, a, row0, lane, col, part);
+            else
+                drain_result<kWhich == kHidden>(at, a, row0, lane, col, unit.split, part);
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive_cluster(released + 8 * acc.s);
+        }
+        if (!ok) *abort_flag = 1;
+    }
+    // neither CTA leaves while the other may still read its shared memory,
+    // signal its barriers or hold TMEM of the pair
+    tc::tc_fence_before();
+    __syncwarp();
+    __syncthreads();
+    tc::cluster_sync();
+    if (warp == 1) {
+        tc::tc_fence_after();
+        tc::tmem_dealloc_pair(tmem, 512);
+    }
+    if (threadIdx.x == 0 && *abort_flag) {
+        *(volatile int *)a.failed = 1;
+        __threadfence_system();
+    }
+}
+
+template <Product kWhich, bool kStalled = false>
+cudaError_t launch(const CUtensorMap &a, const CUtensorMap &b, const ProductArgs &args, cudaStream_t s) {
+    static std::atomic<unsigned long long> done;
+    auto *kernel = tc_head_kernel<kWhich, kStalled>;
+    const cudaError_t e = set_max_dynamic_smem((const void *)kernel, kSmem, done);
+    if (e != cudaSuccess) return e;
+    const int64_t units = (int64_t)args.mt * args.nt * args.splits;
+    return launch_k(kernel, dim3((unsigned)(2 * std::min<int64_t>(units, std::max(1, num_sms() / 2)))), dim3(kThreads),
+                    (size_t)kSmem, s, false, a, b, args);
+}
+
+}  // namespace
+
+cudaError_t launch_product(Product which, const CUtensorMap &a, const CUtensorMap &b, const ProductArgs &args,
+                           cudaStream_t s, bool stalled) {
+    if (stalled) return launch<kLoss, true>(a, b, args, s);
+    switch (which) {
+        case kLoss: return launch<kLoss>(a, b, args, s);
+        case kLogits: return launch<kLogits>(a, b, args, s);
+        case kHidden: return launch<kHidden>(a, b, args, s);
+        default: return launch<kHead>(a, b, args, s);
+    }
+}
+
+}  // namespace head
+}  // namespace jarq

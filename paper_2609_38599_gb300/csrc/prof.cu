@@ -12,7 +12,8 @@ const char *const kNames[] = {"validate", "residual", "init_rows", "hr_full", "g
                               "scale_solve", "symmetrize", "group_factor", "slices", "slice_rows",
                               "proj", "whw", "rhs", "htilde", "ptilde", "syrk", "mu_combine", "own_rhs",
                               "scale_fit", "probe", "sweep_product", "sweep_babai", "quantize_rows",
-                              "integer_product", "token_logprobs", "token_grad"};
+                              "integer_product", "token_logprobs", "token_grad", "rms_norm", "norm_grad",
+                              "cross_entropy", "cross_entropy_grad", "adapters"};
 constexpr int kNumNames = sizeof(kNames) / sizeof(kNames[0]);
 
 // Earlier names, still read: what is recorded under them now (null: nothing).

@@ -36,7 +36,9 @@ EXPORTS = ("jarq_default_options", "jarq_prepare_hessian", "jarq_refine_layer",
            "jarq_selftest_wait_timeout", "jarq_selftest_stalled_kernel",
            "jarq_async_status", "jarq_quantize_rows", "jarq_integer_codes",
            "jarq_integer_product", "jarq_integer_linear_workspace", "jarq_integer_linear",
-           "jarq_token_logprobs", "jarq_token_logprobs_grad")
+           "jarq_token_logprobs", "jarq_token_logprobs_grad", "jarq_rms_norm",
+           "jarq_rms_norm_grad_workspace", "jarq_rms_norm_grad", "jarq_cross_entropy_workspace",
+           "jarq_cross_entropy", "jarq_cross_entropy_grad_workspace", "jarq_cross_entropy_grad")
 
 
 class JarqError(RuntimeError):
@@ -111,6 +113,21 @@ def _load():
     lib.jarq_token_logprobs.argtypes = [vp, ci, ci, ci, cl, vp, ci, ci, vp, vp, vp, vp, vp, vp]
     lib.jarq_token_logprobs_grad.restype = ci
     lib.jarq_token_logprobs_grad.argtypes = [vp, ci, ci, ci, cl, vp, ci, vp, vp, vp, vp, vp, cl, vp]
+    cz = ctypes.c_size_t
+    lib.jarq_rms_norm.restype = ci
+    lib.jarq_rms_norm.argtypes = [vp, ci, ci, ci, cl, vp, cl, vp, cl, vp, ci, cf, vp, cl, vp, cl, vp, vp, vp]
+    lib.jarq_rms_norm_grad_workspace.restype = cz
+    lib.jarq_rms_norm_grad_workspace.argtypes = [ci, ci]
+    lib.jarq_rms_norm_grad.restype = ci
+    lib.jarq_rms_norm_grad.argtypes = [vp, ci, ci, ci, cl, vp, ci, vp, vp, cl, vp, cl, vp, cl, vp, vp, cz, vp]
+    lib.jarq_cross_entropy_workspace.restype = cz
+    lib.jarq_cross_entropy_workspace.argtypes = [ci, ci, ci, ci]
+    lib.jarq_cross_entropy.restype = ci
+    lib.jarq_cross_entropy.argtypes = [vp, ci, ci, ci, cl, vp, ci, cl, vp, vp, vp, vp, cz, vp]
+    lib.jarq_cross_entropy_grad_workspace.restype = cz
+    lib.jarq_cross_entropy_grad_workspace.argtypes = [ci, ci, ci, ci, ci, ci]
+    lib.jarq_cross_entropy_grad.restype = ci
+    lib.jarq_cross_entropy_grad.argtypes = [vp, ci, ci, ci, cl, vp, ci, cl, vp, vp, vp, vp, cl, vp, cl, vp, cz, vp]
     lib.jarq_hessian_din.restype = ci
     lib.jarq_hessian_din.argtypes = [vp]
     lib.jarq_hessian_group_size.restype = ci
@@ -146,7 +163,8 @@ def library():
 KERNELS = ("validate", "residual", "init_rows", "hr_full", "grad", "gram", "scale_solve",
            "symmetrize", "group_factor", "slices", "slice_rows", "proj", "whw", "rhs", "htilde",
            "ptilde", "syrk", "mu_combine", "own_rhs", "scale_fit", "probe", "sweep_product",
-           "sweep_babai", "quantize_rows", "integer_product", "token_logprobs", "token_grad")
+           "sweep_babai", "quantize_rows", "integer_product", "token_logprobs", "token_grad",
+           "rms_norm", "norm_grad", "cross_entropy", "cross_entropy_grad", "adapters")
 
 
 def profile_enable(on: bool = True):
@@ -474,7 +492,7 @@ def objective(hess: Hessian, W, S, Q, Z, bits: int, out=None):
     return F
 
 
-# ---- running and scoring a quantized model: device tensors, enqueued on torch's
+# ---- running, scoring and tuning a quantized model: device tensors, enqueued on torch's
 # current stream, not waited for.  A call takes a few microseconds on the device,
 # so little is done here: every attribute of a tensor is looked at once. ----
 
@@ -486,6 +504,7 @@ class _Torch:
         self.floats = {torch.float32: JARQ_F32, torch.float16: JARQ_F16, torch.bfloat16: JARQ_BF16}
         self.named = {"float32": torch.float32, "float16": torch.float16, "bfloat16": torch.bfloat16}
         self.bytes = {torch.int8: 0}
+        self.halves = {torch.float16: JARQ_F16, torch.bfloat16: JARQ_BF16}
         self.empty = torch.empty
         self.f32, self.i32, self.i64, self.i8, self.u8 = (torch.float32, torch.int32, torch.int64, torch.int8,
                                                           torch.uint8)
@@ -682,3 +701,152 @@ def token_logprobs_grad(logits, tokens, lse, g_logprob, entropy=None, g_entropy=
     if status != JARQ_OK:
         raise JarqError(status, "jarq_token_logprobs_grad")
     return out
+
+
+@dataclass
+class NormedRows:
+    """Results of ``rms_norm``; None where not asked for."""
+    h: object
+    y: object
+    codes: object
+    scale: object
+    rstd: object
+
+
+def _like(x, name, n, d, dtype):
+    """(pointer, row pitch) of a matrix of the shape and type of another one."""
+    p, ld, rows, cols, _ = _matrix(x, name, {dtype: 0})
+    if rows != n or cols != d:
+        raise ValueError(f"{name} has shape {(rows, cols)}, not {(n, d)}")
+    return p, ld
+
+
+def _gain(T, gain, d, dtype, code):
+    """(pointer, type code) of the gains of rows of ``dtype``."""
+    if gain is None:
+        return None, code
+    wide = gain.dtype == T.f32
+    return _flat(gain, "gain", T.f32 if wide else dtype, (d,)), JARQ_F32 if wide else code
+
+
+def rms_norm(X, gain=None, eps: float = 1e-6, residual=None, values: bool = True, codes: bool = False,
+             h=None) -> NormedRows:
+    """``jarq_rms_norm``: the rows ``h = X + residual`` (X itself without one)
+    over their root mean square, times ``gain`` [d] (of X's type or float32):
+    as ``values`` in X's type and as ``codes`` int8 with a scale a row, the
+    arguments of ``integer_product``.  ``h`` receives the sum; it may be
+    ``residual``.  The rows of the codes lie on 16-byte boundaries."""
+    T = _torch()
+    x, ldx, n, d, code = _matrix(X, "X", T.floats)
+    dtype, dev = X.dtype, X.device
+    g, gcode = _gain(T, gain, d, dtype, code)
+    r = hp = y = q = s = None
+    ldr = ldh = ldq = d
+    if residual is not None:
+        r, ldr = _like(residual, "residual", n, d, dtype)
+        if h is None:
+            h = T.empty((n, d), dtype=dtype, device=dev)
+            hp = h.data_ptr()
+        else:
+            hp, ldh = _like(h, "h", n, d, dtype)
+    elif h is not None:
+        raise ValueError("h is the sum with a residual: there is none")
+    Y = Q = scale = None
+    if values:
+        Y = T.empty((n, d), dtype=dtype, device=dev)
+        y = Y.data_ptr()
+    if codes:
+        ldq = (d + 15) // 16 * 16
+        Q = T.empty((n, ldq), dtype=T.i8, device=dev)
+        scale = T.empty((n,), dtype=T.f32, device=dev)
+        q, s = Q.data_ptr(), scale.data_ptr()
+    rstd = T.empty((n,), dtype=T.f32, device=dev)
+    status = _lib.jarq_rms_norm(x, code, n, d, ldx, r, ldr, hp, ldh, g, gcode, eps, y, d, q, ldq, s, rstd.data_ptr(),
+                                T.stream(X.get_device()))
+    if status != JARQ_OK:
+        raise JarqError(status, "jarq_rms_norm")
+    return NormedRows(X if residual is None else h, Y, Q[:, :d] if codes else None, scale, rstd)
+
+
+def rms_norm_grad(h, gain, rstd, dy, dh=None, rows: bool = True, gains: bool = True, out=None):
+    """``jarq_rms_norm_grad``: (dX, dgain float32 [d]) from the normed rows
+    ``h``, the norm's ``rstd`` and the gradient ``dy`` of its values; ``dh`` is
+    the gradient that reaches ``h`` by the residual stream.  dX, the gradient of
+    X and of the residual alike, goes to ``out``, which may be ``dy`` or ``dh``;
+    None in the place of what ``rows`` or ``gains`` does not ask for."""
+    T = _torch()
+    p, ldh, n, d, code = _matrix(h, "h", T.floats)
+    dtype, dev = h.dtype, h.device
+    g, gcode = _gain(T, gain, d, dtype, code)
+    r = _flat(rstd, "rstd", T.f32, (n,))
+    y, ldy = _like(dy, "dy", n, d, dtype)
+    s, lds = _like(dh, "dh", n, d, dtype) if dh is not None else (None, d)
+    x, ldx, dgain, gp, work, size = None, d, None, None, None, 0
+    if rows:
+        if out is None:
+            out = T.empty((n, d), dtype=dtype, device=dev)
+            x = out.data_ptr()
+        else:
+            x, ldx = _like(out, "out", n, d, dtype)
+    elif out is not None:
+        raise ValueError("out is dX, which is not asked for")
+    if gains:
+        dgain = T.empty((d,), dtype=T.f32, device=dev)
+        size = _lib.jarq_rms_norm_grad_workspace(n, d)
+        buffer = T.empty((size,), dtype=T.u8, device=dev)
+        gp, work = dgain.data_ptr(), buffer.data_ptr()
+    status = _lib.jarq_rms_norm_grad(p, code, n, d, ldh, g, gcode, r, y, ldy, s, lds, x, ldx, gp, work, size,
+                                     T.stream(h.get_device()))
+    if status != JARQ_OK:
+        raise JarqError(status, "jarq_rms_norm_grad")
+    return out, dgain
+
+
+def _head(T, X, W, tokens):
+    """What the loss of an output head and its gradient share."""
+    x, ldx, n, d, code = _matrix(X, "X", T.halves)
+    w, ldw, vocab, dw, _ = _matrix(W, "W", {X.dtype: code})
+    if dw != d:
+        raise ValueError(f"the head has {dw} columns, hidden states {d}")
+    tok = _flat(tokens, "tokens", T.i64, (n,))
+    aligned = not (x | w) & 15 and (n <= 1 or not ldx & 7) and (vocab <= 1 or not ldw & 7)
+    return x, ldx, n, d, code, w, ldw, vocab, tok, 1 if aligned else 0
+
+
+def cross_entropy(X, W, tokens):
+    """``jarq_cross_entropy``: (loss, lse), float32 [n], of ``tokens`` (int64
+    [n]; negative ones count for nothing) under the logits ``X W^T`` of hidden
+    states X [n][d] and a head W [vocab][d], both float16 or both bfloat16.
+    The logits are never in memory."""
+    T = _torch()
+    x, ldx, n, d, code, w, ldw, vocab, tok, aligned = _head(T, X, W, tokens)
+    f32, dev = T.f32, X.device
+    loss, lse = T.empty((n,), dtype=f32, device=dev), T.empty((n,), dtype=f32, device=dev)
+    size = _lib.jarq_cross_entropy_workspace(n, d, vocab, aligned)
+    work = T.empty((size,), dtype=T.u8, device=dev)
+    status = _lib.jarq_cross_entropy(x, code, n, d, ldx, w, vocab, ldw, tok, loss.data_ptr(), lse.data_ptr(),
+                                     work.data_ptr(), size, T.stream(X.get_device()))
+    if status != JARQ_OK:
+        raise JarqError(status, "jarq_cross_entropy")
+    return loss, lse
+
+
+def cross_entropy_grad(X, W, tokens, lse, g_loss, hidden: bool = True, head: bool = True):
+    """``jarq_cross_entropy_grad``: (dX, dW), the gradients of ``(g_loss *
+    loss).sum()`` with respect to the hidden states and the head, in their type;
+    None in the place of one that ``hidden`` or ``head`` does not ask for.
+    ``lse`` is ``cross_entropy``'s."""
+    T = _torch()
+    x, ldx, n, d, code, w, ldw, vocab, tok, aligned = _head(T, X, W, tokens)
+    s, g = _flat(lse, "lse", T.f32, (n,)), _flat(g_loss, "g_loss", T.f32, (n,))
+    dev, dtype = X.device, X.dtype
+    dX = T.empty((n, d), dtype=dtype, device=dev) if hidden else None
+    dW = T.empty((vocab, d), dtype=dtype, device=dev) if head else None
+    size = _lib.jarq_cross_entropy_grad_workspace(n, d, vocab, aligned, 1 if hidden else 0, 1 if head else 0)
+    work = T.empty((size,), dtype=T.u8, device=dev)
+    status = _lib.jarq_cross_entropy_grad(x, code, n, d, ldx, w, vocab, ldw, tok, s, g,
+                                          dX.data_ptr() if hidden else None, d, dW.data_ptr() if head else None, d,
+                                          work.data_ptr(), size, T.stream(X.get_device()))
+    if status != JARQ_OK:
+        raise JarqError(status, "jarq_cross_entropy_grad")
+    return dX, dW
