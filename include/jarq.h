@@ -478,6 +478,30 @@ jarq_status jarq_cross_entropy_grad(const void *X, jarq_dtype dtype, int n, int 
                                     void *dW, int64_t lddw, void *workspace, size_t workspace_bytes,
                                     void *stream);
 
+/* Low-rank adapters of many requests, added to the outputs of a projection that they
+ * share (jarq_integer_linear's, say): with i = ids[t],
+ *     Y[t] = Y0[t] + scale[i] B[i] (A[i] X[t]).
+ *   X : [n][din] of `dtype` (JARQ_F16 or JARQ_BF16), pitch ldx.
+ *   A : [adapters][rank][din], B : [adapters][dout][rank], both of `dtype`, contiguous.
+ *   scale : float32 [adapters], or NULL for ones.  ids : int32 [n], in any order; a
+ *   negative one stands for no adapter (Y = Y0), one >= adapters gives NaN.
+ *   Y0, Y : [n][dout] of ydtype (`dtype` or JARQ_F32), pitches ldy0, ldy.  Y0 may be
+ *   NULL (zeros), and may be Y itself (ldy0 = ldy).
+ *   rank : a multiple of 8, at most 128; adapters of a lower one are filled up with
+ *   zeros.  0 <= adapters <= 8192, n >= 0 and at most 2^31 - 4096, din and dout 1 ..
+ *   2^20.
+ *   workspace : at least jarq_adapters_workspace(n, din, rank) bytes of device memory,
+ *   16-byte aligned, that the stream's work may overwrite.
+ * Products are exact or kept to 2^-22 of a token's largest A[i] X[t], sums float32,
+ * with one rounding to ydtype at the end.  A token's result does not depend on the
+ * other tokens of a call of the same size. */
+size_t jarq_adapters_workspace(int n, int din, int rank);
+jarq_status jarq_apply_adapters(const void *X, jarq_dtype dtype, int64_t ldx, const void *A,
+                                const void *B, const float *scale, int adapters, int rank,
+                                const int32_t *ids, int n, int din, int dout, const void *Y0,
+                                int64_t ldy0, void *Y, int64_t ldy, jarq_dtype ydtype,
+                                void *workspace, size_t workspace_bytes, void *stream);
+
 /* Per-row objective without any device allocation.  The paper has no
  * counterpart: this entry point exists for callers that cannot allocate
  * device memory when they need the objective -- serving processes that

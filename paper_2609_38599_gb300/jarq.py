@@ -38,7 +38,8 @@ EXPORTS = ("jarq_default_options", "jarq_prepare_hessian", "jarq_refine_layer",
            "jarq_integer_product", "jarq_integer_linear_workspace", "jarq_integer_linear",
            "jarq_token_logprobs", "jarq_token_logprobs_grad", "jarq_rms_norm",
            "jarq_rms_norm_grad_workspace", "jarq_rms_norm_grad", "jarq_cross_entropy_workspace",
-           "jarq_cross_entropy", "jarq_cross_entropy_grad_workspace", "jarq_cross_entropy_grad")
+           "jarq_cross_entropy", "jarq_cross_entropy_grad_workspace", "jarq_cross_entropy_grad",
+           "jarq_adapters_workspace", "jarq_apply_adapters")
 
 
 class JarqError(RuntimeError):
@@ -128,6 +129,10 @@ def _load():
     lib.jarq_cross_entropy_grad_workspace.argtypes = [ci, ci, ci, ci, ci, ci]
     lib.jarq_cross_entropy_grad.restype = ci
     lib.jarq_cross_entropy_grad.argtypes = [vp, ci, ci, ci, cl, vp, ci, cl, vp, vp, vp, vp, cl, vp, cl, vp, cz, vp]
+    lib.jarq_adapters_workspace.restype = cz
+    lib.jarq_adapters_workspace.argtypes = [ci, ci, ci]
+    lib.jarq_apply_adapters.restype = ci
+    lib.jarq_apply_adapters.argtypes = [vp, ci, cl, vp, vp, vp, ci, ci, vp, ci, ci, ci, vp, cl, vp, cl, ci, vp, cz, vp]
     lib.jarq_hessian_din.restype = ci
     lib.jarq_hessian_din.argtypes = [vp]
     lib.jarq_hessian_group_size.restype = ci
@@ -850,3 +855,41 @@ def cross_entropy_grad(X, W, tokens, lse, g_loss, hidden: bool = True, head: boo
     if status != JARQ_OK:
         raise JarqError(status, "jarq_cross_entropy_grad")
     return dX, dW
+
+
+def apply_adapters(X, A, B, ids, scale=None, base=None, dtype: str = None, out=None):
+    """``jarq_apply_adapters``: ``base[t] + scale[i] * B[i] @ (A[i] @ X[t])`` with
+    ``i = ids[t]`` (int32 [n]; negative for no adapter), beside a projection
+    whose outputs are ``base`` [n][dout].  X [n][din], A [adapters][rank][din]
+    and B [adapters][dout][rank] are all float16 or all bfloat16; the result is
+    of base's type, X's own or float32 (without one, of ``dtype`` or X's).
+    ``out`` may be ``base``."""
+    T = _torch()
+    x, ldx, n, din, code = _matrix(X, "X", T.halves)
+    xdt, dev = X.dtype, X.device
+    if len(A.shape) != 3 or len(B.shape) != 3:
+        raise TypeError(f"A and B: expected [adapters][rank][din] and [adapters][dout][rank], got {tuple(A.shape)} and "
+                        f"{tuple(B.shape)}")
+    m, rank, da = A.shape
+    dout = B.shape[1]
+    if da != din:
+        raise ValueError(f"the adapters have {da} columns, activations {din}")
+    a, b = _flat(A, "A", xdt, (m, rank, din)), _flat(B, "B", xdt, (m, dout, rank))
+    s = _flat(scale, "scale", T.f32, (m,)) if scale is not None else None
+    i = _flat(ids, "ids", T.i32, (n,))
+    ydt = base.dtype if base is not None else xdt if dtype is None else T.named[dtype]
+    if ydt != xdt and ydt != T.f32 or (dtype is not None and ydt != T.named[dtype]):
+        raise TypeError(f"expected outputs of {xdt} or {T.f32}, got {ydt}{f' and dtype {dtype}' if dtype else ''}")
+    y0, ldy0 = _like(base, "base", n, dout, ydt) if base is not None else (None, dout)
+    if out is None:
+        out = T.empty((n, dout), dtype=ydt, device=dev)
+        y, ldy = out.data_ptr(), dout
+    else:
+        y, ldy = _like(out, "out", n, dout, ydt)
+    size = _lib.jarq_adapters_workspace(n, din, rank)
+    work = T.empty((size,), dtype=T.u8, device=dev)
+    status = _lib.jarq_apply_adapters(x, code, ldx, a, b, s, m, rank, i, n, din, dout, y0, ldy0, y, ldy,
+                                      T.floats[ydt], work.data_ptr(), size, T.stream(X.get_device()))
+    if status != JARQ_OK:
+        raise JarqError(status, "jarq_apply_adapters")
+    return out
