@@ -134,6 +134,7 @@ __global__ void __launch_bounds__(256) few_outputs_kernel(AdapterArgs a) {
 // Tokens by adapter, those without one last.  The order of an adapter's tokens is
 // any; no result depends on it.
 __global__ void __launch_bounds__(1024) order_kernel(AdapterArgs a) {
+    tc::pdl_launch_dependents();
     extern __shared__ int bins[];              // adapters + 2
     __shared__ int sums[32];
     const int count = a.adapters + 2, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -151,7 +152,18 @@ __global__ void __launch_bounds__(1024) order_kernel(AdapterArgs a) {
         if (lane == leader) at = atomicAdd(&bins[b], __popc(same));
         return __shfl_sync(same, at, leader) + __popc(same & ((1u << lane) - 1));
     };
-    for (int t = threadIdx.x; t < a.n; t += 1024) add(bin(t), __activemask());
+    // the first of a thread's tokens stay in registers between the two passes
+    constexpr int kKeep = 8;
+    int own_bin[kKeep];
+#pragma unroll
+    for (int i = 0; i < kKeep; ++i) {
+        const int t = threadIdx.x + 1024 * i;
+        own_bin[i] = t < a.n ? bin(t) : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < kKeep; ++i)
+        if (own_bin[i] >= 0) add(own_bin[i], __activemask());
+    for (int t = threadIdx.x + 1024 * kKeep; t < a.n; t += 1024) add(bin(t), __activemask());
     __syncthreads();
     // bins to their first places
     int base = 0;
@@ -178,7 +190,10 @@ __global__ void __launch_bounds__(1024) order_kernel(AdapterArgs a) {
         base += total;
         __syncthreads();
     }
-    for (int t = threadIdx.x; t < a.n; t += 1024) a.order[add(bin(t), __activemask())] = t;
+#pragma unroll
+    for (int i = 0; i < kKeep; ++i)
+        if (own_bin[i] >= 0) a.order[add(own_bin[i], __activemask())] = threadIdx.x + 1024 * i;
+    for (int t = threadIdx.x + 1024 * kKeep; t < a.n; t += 1024) a.order[add(bin(t), __activemask())] = t;
 }
 
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&x)[4], uint32_t b0, uint32_t b1, __half) {
@@ -213,6 +228,8 @@ __global__ void __launch_bounds__(256) sums_kernel(AdapterArgs a) {
     __shared__ float part[kWarps][kTokens][kCols + 1];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
     const int at = blockIdx.x * kTokens;
+    tc::pdl_launch_dependents();
+    tc::pdl_wait();
     const int tok = lane < kTokens && at + lane < a.n ? a.order[at + lane] : -1;
     const int mine = tok >= 0 ? adapter_of(a, tok) : -1;
     const T *x[2 * MT];
@@ -234,7 +251,7 @@ __global__ void __launch_bounds__(256) sums_kernel(AdapterArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[m][j][e] = 0.f;
         if (warp < kWarps) {
-#pragma unroll 2
+#pragma unroll(NT <= 2 ? 4 : 2)
             for (int ch = c0 + warp; ch < c1; ch += kWarps) {
                 const int k = ch * 32 + 8 * c;
                 uint4 xv[2 * MT];
@@ -287,16 +304,42 @@ __device__ __forceinline__ void split(float lo, float hi, uint32_t (&out)[PARTS]
     }
 }
 
-// Outputs of 16 MT tokens a warp, 32 columns at a time; KS: sixteens of the rank.
+// 16 neighbouring outputs of a token, from element o on: the sums d to what Y0 has
+// there. `held`: Y0's, read before, where the outputs are whole 16 bytes.
+template <class Out>
+constexpr int kHeld16 = 16 / kUnit<Out>;
+template <class Out>
+__device__ __forceinline__ void put16(Out *y, const Out *y0, const uint4 (&held)[kHeld16<Out>], bool vec, int left,
+                                      const float (&d)[16]) {
+    constexpr int E = kUnit<Out>;
+    if (vec && left >= 16) {
+#pragma unroll
+        for (int h = 0; h < kHeld16<Out>; ++h) {
+            float v[E];
+            unpack(held[h], v, Out());
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] += d[E * h + e];
+            *reinterpret_cast<uint4 *>(y + E * h) = pack(v, Out());
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            if (e < left) y[e] = from_float<Out>((y0 ? to_float(y0[e]) : 0.f) + d[e]);
+    }
+}
+
+// Outputs of 16 MT tokens a block: each of its warps has 64 of every 256 columns, a
+// lane 16 neighbours of a token; KS: sixteens of the rank.
 template <class T, class Out, int MT, int KS, int PARTS>
 __global__ void __launch_bounds__(128) outputs_kernel(AdapterArgs a, int columns) {
     constexpr int kTokens = 16 * MT;
     constexpr bool kHalf = std::is_same_v<T, __half>;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
-    const int at = (blockIdx.x * 4 + warp) * kTokens;
+    const int at = blockIdx.x * kTokens;
+    tc::pdl_wait();
     const int tok = lane < kTokens && at + lane < a.n ? a.order[at + lane] : -1;
     const int mine = tok >= 0 ? adapter_of(a, tok) : -3;
-    const int o0 = blockIdx.y * columns, o1 = min(a.dout, o0 + columns);
+    const int o0 = blockIdx.y * columns + 64 * warp, o1 = min(a.dout, (int)(blockIdx.y + 1) * columns);
     int t[2 * MT], id[2 * MT];
     uint32_t u[MT][KS][PARTS][4];
     float back[2 * MT];
@@ -346,75 +389,72 @@ __global__ void __launch_bounds__(128) outputs_kernel(AdapterArgs a, int columns
             }
         }
     }
-    auto put = [&](int m, int o, const float (&d)[8]) {
-        const Out *y0 = static_cast<const Out *>(a.Y0) + (size_t)t[m] * a.ldy0 + o;
-        Out *y = static_cast<Out *>(a.Y) + (size_t)t[m] * a.ldy + o;
-        if (a.vec_y && o + 8 <= o1) {
-            constexpr int E = kUnit<Out>;
+    const Out *Y0 = static_cast<const Out *>(a.Y0);
+    Out *Y = static_cast<Out *>(a.Y);
+    // Y0's 16 of token t[m]
+    auto hold = [&](int m, int o, uint4 (&held)[kHeld16<Out>]) {
 #pragma unroll
-            for (int h = 0; h < 8; h += E) {
-                float v[E];
-                if (a.Y0) {
-                    unpack(*reinterpret_cast<const uint4 *>(y0 + h), v, Out());
-#pragma unroll
-                    for (int e = 0; e < E; ++e) v[e] += d[h + e];
-                } else {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) v[e] = d[h + e];
-                }
-                *reinterpret_cast<uint4 *>(y + h) = pack(v, Out());
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (o + e < o1) y[e] = from_float<Out>((a.Y0 ? to_float(y0[e]) : 0.f) + d[e]);
-        }
+        for (int h = 0; h < kHeld16<Out>; ++h)
+            held[h] = Y0 && a.vec_y && o + 16 <= o1
+                          ? *reinterpret_cast<const uint4 *>(Y0 + (size_t)t[m] * a.ldy0 + o + kUnit<Out> * h)
+                          : make_uint4(0, 0, 0, 0);
+    };
+    auto put = [&](int m, int o, const uint4 (&held)[kHeld16<Out>], const float (&d)[16]) {
+        put16<Out>(Y + (size_t)t[m] * a.ldy + o, Y0 ? Y0 + (size_t)t[m] * a.ldy0 + o : nullptr, held, a.vec_y, o1 - o, d);
     };
     each_adapter(mine, [&](int i, uint32_t its) {
         const T *B = static_cast<const T *>(a.B) + (size_t)i * a.dout * a.rank;
         const bool vec = ((uintptr_t)B & 7) == 0;
-        for (int o = o0; o < o1; o += 32) {
-            float acc[MT][4][4];
+        for (int o = o0; o < o1; o += 256) {
+            const int mo = o + 16 * c;             // this lane's outputs
+            uint4 held[2 * MT][kHeld16<Out>];
+#pragma unroll
+            for (int m = 0; m < 2 * MT; ++m)
+                if (id[m] == i) hold(m, mo, held[m]);
+            float acc[MT][8][4];
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
+                for (int q = 0; q < 8; ++q)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[m][q][e] = 0.f;
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
                 const int j = 16 * k + 4 * c;
+                uint2 b[8];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    // column g of MMA q is output 8 (g / 2) + 2 q + g % 2: a lane's
-                    // two of each of the four are eight neighbours
-                    const int col = o + 8 * (g >> 1) + 2 * q + (g & 1);
-                    uint2 b = make_uint2(0, 0);
+                for (int q = 0; q < 8; ++q) {
+                    // column g of MMA q is output 16 (g / 2) + 2 q + g % 2: a lane's two
+                    // of each of the eight are 16 neighbours
+                    const int col = o + 16 * (g >> 1) + 2 * q + (g & 1);
+                    b[q] = make_uint2(0, 0);
                     if (j < a.rank && col < o1) {
                         const T *p = B + (size_t)col * a.rank + j;
                         if (vec) {
-                            b = *reinterpret_cast<const uint2 *>(p);
+                            b[q] = *reinterpret_cast<const uint2 *>(p);
                         } else {
                             alignas(8) T v[4] = {p[0], p[1], p[2], p[3]};
-                            b = *reinterpret_cast<const uint2 *>(v);
+                            b[q] = *reinterpret_cast<const uint2 *>(v);
                         }
                     }
+                }
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
 #pragma unroll
                     for (int m = 0; m < MT; ++m)
 #pragma unroll
-                        for (int p = 0; p < PARTS; ++p) mma(acc[m][q], u[m][k][p], b.x, b.y, T());
-                }
+                        for (int p = 0; p < PARTS; ++p) mma(acc[m][q], u[m][k][p], b[q].x, b[q].y, T());
             }
 #pragma unroll
             for (int m = 0; m < 2 * MT; ++m) {
-                if (id[m] != i) continue;
-                float d[8];
+                if (id[m] != i || mo >= o1) continue;
+                float d[16];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
+                for (int q = 0; q < 8; ++q) {
                     d[2 * q] = acc[m / 2][q][2 * (m % 2)] * back[m];
                     d[2 * q + 1] = acc[m / 2][q][2 * (m % 2) + 1] * back[m];
                 }
-                put(m, o + 8 * c, d);
+                put(m, mo, held[m], d);
             }
         }
     });
@@ -422,10 +462,14 @@ __global__ void __launch_bounds__(128) outputs_kernel(AdapterArgs a, int columns
 #pragma unroll
     for (int m = 0; m < 2 * MT; ++m) {
         if (id[m] != -1 && id[m] != -2) continue;
-        const float v = id[m] == -1 ? 0.f : __int_as_float(0x7FC00000);
-        const float d[8] = {v, v, v, v, v, v, v, v};
-        for (int o = o0; o < o1; o += 32)
-            if (o + 8 * c < o1) put(m, o + 8 * c, d);
+        float d[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) d[e] = id[m] == -1 ? 0.f : __int_as_float(0x7FC00000);
+        for (int o = o0 + 16 * c; o < o1; o += 256) {
+            uint4 held[kHeld16<Out>];
+            hold(m, o, held);
+            put(m, o, held, d);
+        }
     }
 }
 
@@ -434,8 +478,9 @@ int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 int few_splits(int din) { return ceil_div(din, kFewPiece); }
 // Splits of the width where there are few tiles of tokens.
 int many_splits(int n, int din, int rank) {
-    const int tiles = ceil_div(n, rank <= 32 ? 32 : 16);
-    return std::max(1, std::min({ceil_div(304, tiles), ceil_div(din, 512), kMostSplits}));
+    // as many blocks as run at one time
+    const int tiles = ceil_div(n, 16), at_once = 152 * (rank <= 16 ? 4 : rank <= 64 ? 2 : 1);
+    return std::max(1, std::min({at_once / tiles, ceil_div(din, 512), kMostSplits}));
 }
 
 template <class T, class Out>
@@ -451,13 +496,16 @@ template <class T, class Out, int MT, int KS>
 cudaError_t launch_many_as(const AdapterArgs &a, cudaStream_t s) {
     constexpr int kParts = std::is_same_v<Out, float> && std::is_same_v<T, __nv_bfloat16> ? 3 : 2;
     order_kernel<<<1, 1024, (a.adapters + 2) * sizeof(int), s>>>(a);
-    sums_kernel<T, MT, 2 * KS><<<dim3(ceil_div(a.n, 16 * MT), a.splits), 256, 0, s>>>(a);
-    const int tiles = ceil_div(a.n, 64 * MT);
-    // columns of a block: enough blocks for the machine, at least 64
-    const int columns = std::max(64, std::min(512, round_up(ceil_div((int64_t)a.dout * tiles, 8 * 152), 64)));
-    outputs_kernel<T, Out, MT, KS, kParts><<<dim3(tiles, ceil_div(a.dout, columns)), 128, 0, s>>>(a, columns);
+    cudaError_t e = cudaGetLastError();
+    const int tiles = ceil_div(a.n, 16 * MT);
+    if (e == cudaSuccess)
+        e = launch_pdl(sums_kernel<T, 1, 2 * KS>, dim3(ceil_div(a.n, 16), a.splits), dim3(256), 0, s, a);
+    // columns of a block: enough blocks for the machine, in whole steps of 256
+    const int columns = std::max(256, std::min(1024, round_up(ceil_div((int64_t)a.dout * tiles, 6 * 152), 256)));
+    if (e == cudaSuccess)
+        e = launch_pdl(outputs_kernel<T, Out, MT, KS, kParts>, dim3(tiles, ceil_div(a.dout, columns)), dim3(128), 0, s, a, columns);
     count_launches(3);
-    return cudaGetLastError();
+    return e;
 }
 template <class T, class Out>
 cudaError_t launch_many(const AdapterArgs &a, cudaStream_t s) {

@@ -18,6 +18,7 @@ using namespace rows;
 constexpr int kPairs = 76;                  // of CTAs that run at one time
 constexpr size_t kPieceBytes = 512u << 20;  // of D at a time
 constexpr int kLeastPiece = 4096;           // but at least so many tokens
+constexpr int kMostSplits = 16;             // of a sum over K
 constexpr int kMostRows = 1 << 22, kMostWidth = 1 << 20, kMostVocab = 1 << 30;
 
 // loss and lse of a row from the maxima m and sums s of its parts: with M the
@@ -138,13 +139,28 @@ __global__ void __launch_bounds__(256) zero_rows_kernel(T *out, int64_t ld, int 
 
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-// Splits of K for a product of few tiles: as many as fill the pairs, each at least
-// four chunks.
-int splits_of(int m, int n, int chunks) {
-    const int64_t tiles = (int64_t)ceil_div(m, 256) * ceil_div(n, 256);
-    const int s = (int)std::min<int64_t>({std::max<int64_t>(1, kPairs / tiles), std::max(1, chunks / 4), 16});
-    return ceil_div(chunks, ceil_div(chunks, s));
-}
+// A product's tiles: columns and splits of K that take the least time. Waves of pairs,
+// each so many chunks of K at a time that goes with the columns (6 of them stand for
+// what a tile costs besides), and with splits their float32 sums through memory.
+struct Tiles {
+    int cols = 256, splits = 1;
+    Tiles(int m, int n, int chunks, int most_splits) {
+        double best = 0;
+        for (int c = 256; c >= 128; c -= 32)
+            for (int s = 1; s <= std::min(most_splits, std::max(1, chunks / 8)); ++s) {
+                const int per = ceil_div(chunks, s), real = ceil_div(chunks, per);
+                const int64_t tiles = (int64_t)ceil_div(m, 256) * ceil_div(n, c) * real;
+                // two cycles a column and chunk; some 3500 bytes a cycle from memory
+                const double t = (double)((tiles + kPairs - 1) / kPairs) * per * (c + 6) +
+                                 (real > 1 ? 8.0 * real * m * n / 3500 / 2 : 0);
+                if (best == 0 || t < best) {
+                    best = t;
+                    cols = c;
+                    splits = real;
+                }
+            }
+    }
+};
 
 // The parts of a workspace, each on a 256-byte boundary.
 struct Layout {
@@ -165,7 +181,7 @@ struct Plan {
     // the loss
     Plan(int n, int d, int vocab, bool aligned) : pitch(round_up(d, 8)) {
         Layout l;
-        parts = l.take((size_t)2 * ceil_div(vocab, 256) * n * sizeof(float2));
+        parts = l.take((size_t)2 * ceil_div(vocab, Tiles(n, vocab, ceil_div(d, 64), 1).cols) * n * sizeof(float2));
         target = l.take((size_t)n * sizeof(float));
         copies(l, n, vocab, aligned);
         bytes = l.bytes;
@@ -176,8 +192,8 @@ struct Plan {
         const int even = ceil_div(vocab, ceil_div(vocab, most));
         width = round_up(even, 256);
         pieces = ceil_div(vocab, width);
-        split_x = splits_of(n, d, ceil_div(std::min(width, vocab), 64));
-        split_w = splits_of(std::min(width, vocab), d, ceil_div(n, 64));
+        split_x = Tiles(n, d, ceil_div(std::min(width, vocab), 64), kMostSplits).splits;
+        split_w = Tiles(std::min(width, vocab), d, ceil_div(n, 64), kMostSplits).splits;
         slab_x = hidden && (split_x > 1 || pieces > 1);
         slab_w = head && split_w > 1;
         Layout l;
@@ -257,13 +273,15 @@ struct Call {
         *m = {room, pitch};
         return copy(x, ld, rows, room, pitch);
     }
-    ProductArgs shape(int m, int cols, int k, int splits) const {
+    ProductArgs shape(int m, int cols, int k, int most_splits) const {
+        const Tiles tile(m, cols, ceil_div(k, 64), most_splits);
         ProductArgs a{};
         a.m = m, a.n = cols;
         a.chunks = ceil_div(k, 64);
-        a.per = ceil_div(a.chunks, splits);
-        a.splits = ceil_div(a.chunks, a.per);
-        a.mt = ceil_div(m, 256), a.nt = ceil_div(cols, 256);
+        a.splits = tile.splits;
+        a.per = ceil_div(a.chunks, a.splits);
+        a.cols = tile.cols;
+        a.mt = ceil_div(m, 256), a.nt = ceil_div(cols, a.cols);
         a.half = dtype == JARQ_F16;
         a.tokens = tokens, a.vocab = vocab;
         a.last = true;
@@ -287,17 +305,17 @@ cudaError_t run_loss(Call &c, const void *X, int64_t ldx, const void *W, int64_t
     TRY(c.readable(W, ldw, c.vocab, c.work + p.copy_w, p.pitch, &w));
     CUtensorMap mx, mw;
     TRY(tensor_map(&mx, x.p, c.n, c.d, x.ld, 128));
-    TRY(tensor_map(&mw, w.p, c.vocab, c.d, w.ld, 128));
     ProductArgs a = c.shape(c.n, c.vocab, c.d, 1);
+    TRY(tensor_map(&mw, w.p, c.vocab, c.d, w.ld, a.cols / 2));
     a.part = reinterpret_cast<float2 *>(c.work + p.parts);
     a.target = reinterpret_cast<float *>(c.work + p.target);
     TRY(c.product(kLoss, mx, mw, a));
     ++c.launches;
-    // few rows: more threads for each
-    if (c.n < 8 * kPairs)
+    // 32 threads a row (8192 rows of 250 parts: 21 us by 8); few rows: 64
+    if (c.n < kPairs)
         loss_join_kernel<64><<<ceil_div(c.n, 4), 256, 0, c.s>>>(a.part, 2 * a.nt, a.target, c.tokens, c.n, c.vocab, loss, lse);
     else
-        loss_join_kernel<8><<<ceil_div(c.n, 32), 256, 0, c.s>>>(a.part, 2 * a.nt, a.target, c.tokens, c.n, c.vocab, loss, lse);
+        loss_join_kernel<32><<<ceil_div(c.n, 8), 256, 0, c.s>>>(a.part, 2 * a.nt, a.target, c.tokens, c.n, c.vocab, loss, lse);
     return cudaGetLastError();
 }
 
@@ -319,12 +337,13 @@ cudaError_t run_grad(Call &c, const void *X, int64_t ldx, const void *W, int64_t
     char *D = c.work + p.D;
     float *sums_x = p.slab_x ? reinterpret_cast<float *>(c.work + p.sums_x) : nullptr;
     float *sums_w = p.slab_w ? reinterpret_cast<float *>(c.work + p.sums_w) : nullptr;
+    int sums = 1;                                    // splits of dX
     for (int i = 0; i < p.pieces; ++i) {
         const int v0 = i * p.width, width = std::min(p.width, c.vocab - v0);
         {
             TRY(tensor_map(&mx, x.p, c.n, c.d, x.ld, 128));
-            TRY(tensor_map(&mw, w.row(v0), width, c.d, w.ld, 128));
             ProductArgs a = c.shape(c.n, width, c.d, 1);
+            TRY(tensor_map(&mw, w.row(v0), width, c.d, w.ld, a.cols / 2));
             a.lse = lse, a.g = g, a.first = v0;
             a.out = D, a.ldo = p.width;
             TRY(c.product(kLogits, mx, mw, a));
@@ -332,12 +351,13 @@ cudaError_t run_grad(Call &c, const void *X, int64_t ldx, const void *W, int64_t
         if (dX) {
             TRY(tensor_map(&md, D, c.n, width, p.width, 128));
             TRY(tensor_map(&mb, w.row(v0), width, c.d, w.ld, 64));
-            ProductArgs a = c.shape(c.n, c.d, width, p.split_x);
+            ProductArgs a = c.shape(c.n, c.d, width, i == 0 ? p.split_x : sums);
+            if (i == 0) sums = a.splits;             // a shorter piece may have fewer
             a.g = g;
             a.out = dX, a.ldo = lddx;
             a.slab = sums_x, a.pitch = p.pitch;
             a.add = i > 0;
-            a.last = p.split_x == 1 && i + 1 == p.pieces;
+            a.last = sums == 1 && i + 1 == p.pieces;
             TRY(c.product(kHidden, md, mb, a));
         }
         if (dW) {
@@ -353,7 +373,7 @@ cudaError_t run_grad(Call &c, const void *X, int64_t ldx, const void *W, int64_t
             if (p.slab_w) TRY(c.sum_splits(sums_w, a.splits, width, p.pitch, out, lddw, nullptr, top));
         }
     }
-    if (dX && p.split_x > 1) TRY(c.sum_splits(sums_x, p.split_x, c.n, p.pitch, dX, lddx, g, nullptr));
+    if (dX && sums > 1) TRY(c.sum_splits(sums_x, sums, c.n, p.pitch, dX, lddx, g, nullptr));
     return cudaSuccess;
 }
 
@@ -381,7 +401,7 @@ constexpr int kStalledRows = 2048, kStalledTokens = 4096, kStalledWidth = 256;
 
 size_t stalled_bytes() {
     return (size_t)(kStalledRows + kStalledTokens) * kStalledWidth * 2 + kStalledRows * (sizeof(int64_t) + sizeof(float)) +
-           (size_t)2 * (kStalledTokens / 256) * kStalledRows * sizeof(float2);
+           (size_t)2 * (kStalledTokens / 128) * kStalledRows * sizeof(float2);
 }
 cudaError_t launch_stalled(char *zeros, int *failed, cudaStream_t s) {
     char *w = zeros + (size_t)kStalledRows * kStalledWidth * 2, *rest = w + (size_t)kStalledTokens * kStalledWidth * 2;
@@ -391,7 +411,7 @@ cudaError_t launch_stalled(char *zeros, int *failed, cudaStream_t s) {
     a.target = reinterpret_cast<float *>(a.part + (size_t)2 * a.nt * c.n);
     CUtensorMap mx, mw;
     TRY(tensor_map(&mx, zeros, c.n, c.d, c.d, 128));
-    TRY(tensor_map(&mw, w, c.vocab, c.d, c.d, 128));
+    TRY(tensor_map(&mw, w, c.vocab, c.d, c.d, a.cols / 2));
     return launch_product(kLoss, mx, mw, a, s, true);
 }
 

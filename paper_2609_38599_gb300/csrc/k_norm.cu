@@ -14,6 +14,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "integer.cuh"
 #include "quantize.cuh"
@@ -369,6 +370,261 @@ __global__ void __launch_bounds__(1024) gain_join_kernel(const float *parts, int
     if (lane == 0 && c < d) dgain[c] = acc;
 }
 
+// ---------------------------------------------------------------- many rows
+// A block goes from row to row.  A thread has the same units of each, which it copies
+// into its own places of a ring in shared memory rows ahead: they are read by no other
+// thread, so that a copy needs no barrier, and what a row waits for is its sum alone.
+// The gains stay in registers.  P: threads, HELD: units of 16 bytes of a thread.
+constexpr int kMostShared = 220 * 1024;
+template <int P, int HELD, int ARRAYS>
+struct Ring {
+    static constexpr int stage = P * HELD * ARRAYS * 16;
+    static constexpr int stages = 3 * stage <= kMostShared ? 3 : 2, bytes = stages * stage;
+    // blocks of an SM, by threads and by shared memory
+    static constexpr int resident = 768 / P < 1 ? 1 : 768 / P < kMostShared / bytes ? 768 / P : kMostShared / bytes;
+    __device__ static uint4 *at(uint4 *ring, int s, int array, int i) {
+        return ring + ((s * ARRAYS + array) * HELD + i) * P + threadIdx.x;
+    }
+};
+// 16 bytes, or the `bytes` that are left of a row and zeros
+__device__ __forceinline__ void copy_ahead(uint4 *to, const void *from, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(tc::smem_u32(to)), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_made() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copies_landed() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
+}
+template <class R, class T, int HELD, int P>
+__device__ __forceinline__ void copy_row(uint4 *ring, int s, int array, const T *row, int d) {
+    constexpr int E = kUnit<T>;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+        const int k = (threadIdx.x + i * P) * E;
+        if (k < d) copy_ahead(R::at(ring, s, array, i), row + k, min(E, d - k) * (int)sizeof(T));
+    }
+}
+
+template <class T, int P, int HELD, bool RES>
+__global__ void __launch_bounds__(P, Ring<P, HELD, 1 + RES>::resident) norm_rows_kernel(NormArgs a) {
+    using R = Ring<P, HELD, 1 + RES>;
+    constexpr int E = kUnit<T>;
+    extern __shared__ uint4 ring[];
+    __shared__ float sums[2][32], again[32];
+    __shared__ uint32_t tops[2][32];
+    const int t = threadIdx.x, w = t & 31;
+    const T *X = static_cast<const T *>(a.X), *S = static_cast<const T *>(a.R);
+    float g[HELD][E];
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+        if ((t + i * P) * E < a.d) load_gain<E, T>(a.gain, a.wide_gain, (t + i * P) * E, a.d, g[i]);
+    auto ahead = [&](int64_t r, int s) {
+        if (r < a.n) {
+            copy_row<R, T, HELD, P>(ring, s, 0, X + r * a.ldx, a.d);
+            if (RES) copy_row<R, T, HELD, P>(ring, s, 1, S + r * a.ldr, a.d);
+        }
+        copies_made();
+    };
+    for (int s = 0; s + 1 < R::stages; ++s) ahead(blockIdx.x + (int64_t)s * gridDim.x, s);
+    int s = 0, turn = 0;
+    for (int64_t r = blockIdx.x; r < a.n; r += gridDim.x, turn ^= 1) {
+        ahead(r + (int64_t)(R::stages - 1) * gridDim.x, s == 0 ? R::stages - 1 : s - 1);
+        copies_landed<R::stages - 1>();
+        T *h = static_cast<T *>(a.H) + r * a.ldh;
+        float v[HELD][E], sum = 0.f;
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) {
+            const int k = (t + i * P) * E;
+            if (k >= a.d) continue;
+            unpack(*R::at(ring, s, 0, i), v[i], T());
+            if (RES) {
+                float o[E];
+                unpack(*R::at(ring, s, 1, i), o, T());
+#pragma unroll
+                for (int e = 0; e < E; ++e) v[i][e] += o[e];
+                const uint4 raw = pack(v[i], T());
+                if (k + E <= a.d) {
+                    *reinterpret_cast<uint4 *>(h + k) = raw;
+                    unpack(raw, v[i], T());
+                } else {
+                    unpack(raw, v[i], T());
+                    store<E>(h, k, a.d, v[i]);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                sum = fmaf(v[i][e], v[i][e], sum);
+                v[i][e] = __fmul_rn(v[i][e], g[i][e]);
+                top = max(top, __float_as_uint(v[i][e]) & 0x7FFFFFFFu);
+            }
+        }
+        sum = warp_sum(sum);
+        top = __reduce_max_sync(0xffffffffu, top);
+        if (w == 0) {
+            sums[turn][t >> 5] = sum;
+            tops[turn][t >> 5] = top;
+        }
+        __syncthreads();
+        sum = warp_sum(w < P / 32 ? sums[turn][w] : 0.f);
+        top = __reduce_max_sync(0xffffffffu, w < P / 32 ? tops[turn][w] : 0u);
+        float rstd = 1.f / sqrtf(sum / (float)a.d + a.eps);
+        if (isinf(sum)) {
+            // as in norm_kernel: the row, still in the ring, scaled by 2^-80
+            float small = 0.f;
+#pragma unroll
+            for (int i = 0; i < HELD; ++i) {
+                if ((t + i * P) * E >= a.d) continue;
+                float x[E], o[E];
+                unpack(*R::at(ring, s, 0, i), x, T());
+                if (RES) unpack(*R::at(ring, s, 1, i), o, T());
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    if (RES) x[e] = to_float(from_float<T>(x[e] + o[e]));
+                    small = fmaf(x[e] * 0x1p-80f, x[e] * 0x1p-80f, small);
+                }
+            }
+            small = row_sum<P>(small, again);
+            __syncthreads();                       // `again` is free for the next row
+            rstd = 0x1p-80f / sqrtf(small / (float)a.d);
+        }
+        const quant::RowScale by(top);
+        if (t == 0) {
+            if (a.rstd) a.rstd[r] = rstd;
+            if (a.scale) a.scale[r] = __fmul_rn(by.scale, rstd);
+        }
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) {
+            const int k = (t + i * P) * E;
+            if (k >= a.d) continue;
+            if (a.Y) {
+                float o[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] = v[i][e] * rstd;
+                store<E>(static_cast<T *>(a.Y) + r * a.ldy, k, a.d, o);
+            }
+            if (a.Q) {
+                int c[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) c[e] = by.bad ? 0 : __float2int_rn(__fmul_rn(v[i][e], by.inv));
+                store_codes<E>(a.Q + r * a.ldq, k, a.d, c);
+            }
+        }
+        s = s + 1 == R::stages ? 0 : s + 1;
+    }
+}
+
+template <class T, int P, int HELD, bool STREAM>
+__global__ void __launch_bounds__(P, Ring<P, HELD, 2 + STREAM>::resident) norm_grad_rows_kernel(GradArgs a) {
+    using R = Ring<P, HELD, 2 + STREAM>;
+    constexpr int E = kUnit<T>;
+    extern __shared__ uint4 ring[];
+    __shared__ float part[2][32];
+    const int t = threadIdx.x;
+    const T *H = static_cast<const T *>(a.H), *Y = static_cast<const T *>(a.dY), *D = static_cast<const T *>(a.dH);
+    float g[HELD][E], acc[HELD][E];
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+        if ((t + i * P) * E < a.d) load_gain<E, T>(a.gain, a.wide_gain, (t + i * P) * E, a.d, g[i]);
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[i][e] = 0.f;
+    }
+    auto ahead = [&](int64_t r, int s) {
+        if (r < a.n) {
+            copy_row<R, T, HELD, P>(ring, s, 0, H + r * a.ldh, a.d);
+            copy_row<R, T, HELD, P>(ring, s, 1, Y + r * a.ldy, a.d);
+            if (STREAM) copy_row<R, T, HELD, P>(ring, s, 2, D + r * a.lds, a.d);
+        }
+        copies_made();
+    };
+    for (int s = 0; s + 1 < R::stages; ++s) ahead(blockIdx.x + (int64_t)s * gridDim.x, s);
+    int s = 0, turn = 0;
+    float next = a.rstd[blockIdx.x];
+    for (int64_t r = blockIdx.x; r < a.n; r += gridDim.x, turn ^= 1) {
+        ahead(r + (int64_t)(R::stages - 1) * gridDim.x, s == 0 ? R::stages - 1 : s - 1);
+        const float rstd = next;
+        if (r + gridDim.x < a.n) next = a.rstd[r + gridDim.x];
+        copies_landed<R::stages - 1>();
+        float dot = 0.f;
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) {
+            if ((t + i * P) * E >= a.d) continue;
+            float h[E], u[E];
+            unpack(*R::at(ring, s, 0, i), h, T());
+            unpack(*R::at(ring, s, 1, i), u, T());
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                acc[i][e] = fmaf(u[e] * h[e], rstd, acc[i][e]);
+                dot = fmaf(u[e] * g[i][e], h[e], dot);
+            }
+        }
+        if (a.dX) {
+            const float along = rstd * rstd * (row_sum<P>(dot, part[turn]) / (float)a.d);
+            T *dx = static_cast<T *>(a.dX) + r * a.ldx;
+#pragma unroll
+            for (int i = 0; i < HELD; ++i) {
+                const int k = (t + i * P) * E;
+                if (k >= a.d) continue;
+                float h[E], u[E], o[E];
+                unpack(*R::at(ring, s, 0, i), h, T());
+                unpack(*R::at(ring, s, 1, i), u, T());
+                if (STREAM) unpack(*R::at(ring, s, 2, i), o, T());
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float x = rstd * fmaf(-h[e], along, u[e] * g[i][e]);
+                    o[e] = STREAM ? x + o[e] : x;
+                }
+                store<E>(dx, k, a.d, o);
+            }
+        }
+        s = s + 1 == R::stages ? 0 : s + 1;
+    }
+    if (a.part) {
+        float *to = a.part + (size_t)blockIdx.x * a.d;
+#pragma unroll
+        for (int i = 0; i < HELD; ++i)
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if ((t + i * P) * E + e < a.d) to[(t + i * P) * E + e] = acc[i][e];
+    }
+}
+
+// The form for few rows holds four units a thread, so that P alone decides its sums.
+// `f(P, HELD)`, as integral constants, for the fewest threads whose units hold a row of
+// d elements of type T; false where none do.
+template <class T, class F>
+bool with_threads(int d, F f) {
+    constexpr int E = kUnit<T>;
+    using std::integral_constant;
+    auto fits = [&](auto p, auto held) {
+        if (d > p.value * held.value * E) return false;
+        f(p, held);
+        return true;
+    };
+    return fits(integral_constant<int, 128>(), integral_constant<int, 1>()) || fits(integral_constant<int, 128>(), integral_constant<int, 2>()) ||
+           fits(integral_constant<int, 256>(), integral_constant<int, 2>()) || fits(integral_constant<int, 512>(), integral_constant<int, 2>()) ||
+           fits(integral_constant<int, 512>(), integral_constant<int, 3>()) || fits(integral_constant<int, 1024>(), integral_constant<int, 2>());
+}
+// One launch of as many blocks as run at one time; `blocks`: how many those are.
+template <class R, class K, class A>
+cudaError_t launch_rows(K *kernel, std::atomic<unsigned long long> &done, int p, const A &a, int *blocks, cudaStream_t s) {
+    const cudaError_t e = set_max_dynamic_smem((const void *)kernel, R::bytes, done);
+    if (e != cudaSuccess) return e;
+    *blocks = std::min(a.n, std::min(kMostGradBlocks, R::resident * num_sms()));
+    return launch_k(kernel, dim3(*blocks), dim3(p), (size_t)R::bytes, s, false, a);
+}
+template <class T, int P, int HELD, bool RES>
+cudaError_t launch_norm_rows(const NormArgs &a, cudaStream_t s) {
+    static std::atomic<unsigned long long> done;
+    int blocks;
+    return launch_rows<Ring<P, HELD, 1 + RES>>(norm_rows_kernel<T, P, HELD, RES>, done, P, a, &blocks, s);
+}
+template <class T, int P, int HELD, bool STREAM>
+cudaError_t launch_grad_rows(const GradArgs &a, int *blocks, cudaStream_t s) {
+    static std::atomic<unsigned long long> done;
+    return launch_rows<Ring<P, HELD, 2 + STREAM>>(norm_grad_rows_kernel<T, P, HELD, STREAM>, done, P, a, blocks, s);
+}
+
 template <class T, bool VEC, int P>
 cudaError_t launch_norm_p(const NormArgs &a, cudaStream_t s) {
     const int64_t blocks = P == 32 ? ((int64_t)a.n + 7) / 8 : a.n;
@@ -377,12 +633,22 @@ cudaError_t launch_norm_p(const NormArgs &a, cudaStream_t s) {
 }
 template <class T, bool VEC>
 cudaError_t launch_norm_t(const NormArgs &a, cudaStream_t s) {
-    // the fewest threads that hold a row; for few rows one unit a thread
-    const int64_t d = a.n <= num_sms() ? (int64_t)a.d * Shape<T, VEC, 256>::held : a.d;
-    if (d <= Shape<T, VEC, 32>::row) return launch_norm_p<T, VEC, 32>(a, s);
-    if (d <= Shape<T, VEC, 128>::row) return launch_norm_p<T, VEC, 128>(a, s);
-    if (d <= Shape<T, VEC, 256>::row) return launch_norm_p<T, VEC, 256>(a, s);
-    if (d <= Shape<T, VEC, 512>::row) return launch_norm_p<T, VEC, 512>(a, s);
+    if (a.d <= Shape<T, VEC, 32>::row) return launch_norm_p<T, VEC, 32>(a, s);
+    cudaError_t e = cudaSuccess;
+    if (VEC) {
+        // the threads by the width alone, so that a row's sum is added in one order
+        if (with_threads<T>(a.d, [&](auto p, auto held) {
+                constexpr int P = p.value, HELD = held.value;
+                e = a.n <= num_sms() ? launch_norm_p<T, VEC, P>(a, s)
+                    : a.R            ? launch_norm_rows<T, P, HELD, true>(a, s)
+                                     : launch_norm_rows<T, P, HELD, false>(a, s);
+            }))
+            return e;
+    } else {
+        if (a.d <= Shape<T, VEC, 128>::row) return launch_norm_p<T, VEC, 128>(a, s);
+        if (a.d <= Shape<T, VEC, 256>::row) return launch_norm_p<T, VEC, 256>(a, s);
+        if (a.d <= Shape<T, VEC, 512>::row) return launch_norm_p<T, VEC, 512>(a, s);
+    }
     return launch_norm_p<T, VEC, 1024>(a, s);
 }
 
@@ -410,12 +676,24 @@ cudaError_t launch_grad_t(GradArgs a, float *dgain, cudaStream_t s) {
         a.part = nullptr;
     }
     if (e == cudaSuccess && (a.dX || a.part)) {
-        const int blocks = std::min(a.n, kMostGradBlocks);
-        if (a.d <= Shape<T, VEC, 128>::row) e = launch_grad_p<T, VEC, 128>(a, blocks, s);
-        else if (a.d <= Shape<T, VEC, 256>::row) e = launch_grad_p<T, VEC, 256>(a, blocks, s);
-        else if (a.d <= Shape<T, VEC, 512>::row) e = launch_grad_p<T, VEC, 512>(a, blocks, s);
-        else e = launch_grad_p<T, VEC, 1024>(a, blocks, s);
+        int blocks = std::min(a.n, kMostGradBlocks);
         count_launches(1);
+        if (VEC) {
+            if (!with_threads<T>(a.d, [&](auto p, auto held) {
+                    constexpr int P = p.value, HELD = held.value;
+                    e = a.n <= num_sms() ? launch_grad_p<T, VEC, P>(a, blocks, s)
+                        : a.dH           ? launch_grad_rows<T, P, HELD, true>(a, &blocks, s)
+                                         : launch_grad_rows<T, P, HELD, false>(a, &blocks, s);
+                }))
+                e = launch_grad_p<T, VEC, 1024>(a, blocks, s);
+        } else if (a.d <= Shape<T, VEC, 128>::row) {
+            e = launch_grad_p<T, VEC, 128>(a, blocks, s);
+        } else if (a.d <= Shape<T, VEC, 512>::row) {
+            e = launch_grad_p<T, VEC, 512>(a, blocks, s);
+        } else {
+            e = launch_grad_p<T, VEC, 1024>(a, blocks, s);
+        }
+        if (a.part) parts = blocks;
     }
     if (e == cudaSuccess && dgain) {
         gain_join_kernel<<<(unsigned)(((int64_t)a.d + 31) / 32), 1024, 0, s>>>(part, parts, a.d, dgain);

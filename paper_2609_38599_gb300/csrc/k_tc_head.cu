@@ -4,10 +4,10 @@
 //   dX = D W,  dW = D^T X.
 // Logits exist in the accumulators alone.
 //
-// A pair of CTAs (cta_group::2) computes tiles of 256 x 256, K in chunks of 64, over
+// A pair of CTAs (cta_group::2) computes tiles of 256 x up to 256, K in chunks of 64, over
 // a ring that TMA fills; an operand is read as it lies in memory, along K or (W of
 // dX, D and X of dW) along MN, so that nothing is transposed.  In each CTA:
-//   warp 0      TMA producer: its own 128 rows of A and 128 of B's 256 columns
+//   warp 0      TMA producer: its own 128 rows of A and half of B's columns
 //   warp 1      TMEM allocation; in the even CTA the MMA issuer
 //   warps 2..9  drain: lane quarter w % 4, half of the columns, of one accumulator
 //               while the MMAs of the next tile fill the other
@@ -34,6 +34,10 @@ constexpr int kPart = 32 * 128;            // bytes that a drain warp stages
 constexpr int kBars = 2 * kStages + 5;     // full, empty, afull[2], aempty[2], closing
 constexpr int kSmem = 1024 + kStages * kStage + kDrainWarps * kPart + 8 * kBars + 16;
 constexpr int kThreads = 32 * (2 + kDrainWarps);
+// Chunks of K in one accumulator of the loss: the tensor cores' float32 additions
+// round toward zero, which over a long K moves every logit the same way (K = 4096 in
+// one: lse off by 2e-6 of itself); after 512 the sum goes to the drain's registers.
+constexpr int kLossChunks = 8;
 constexpr int kBand = 16;                  // tiles of rows that share the columns' panels in L2
 static_assert(kSmem <= 227 * 1024, "ring and staged parts must fit an SM's shared memory");
 
@@ -104,22 +108,23 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi, bool half) {
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-// A row of 128 columns of logits: maximum, sum of exponentials less the maximum, and
+// A row of `cols` columns of logits: maximum, sum of exponentials less the maximum, and
 // the token's logit where it is among them.
-__device__ __forceinline__ void drain_loss(uint32_t acc, const ProductArgs &a, int row, int col, int part) {
+__device__ __forceinline__ void reduce_loss(float (&acc)[128], const ProductArgs &a, int row, int col, int cols, int part) {
     const int64_t tok = row < a.m ? a.tokens[row] : -1;
     const int64_t mine = tok - col;
+    const int limit = min(cols, a.n - col);
     float m = -INFINITY, s = 0.f;
-#pragma unroll 1
+#pragma unroll
     for (int c = 0; c < 128; c += 32) {
-        float x[32];
-        load_columns(acc + c, x);
-        if (col + c + 32 > a.n) {
+        if (c >= limit) break;
+        float *x = acc + c;
+        if (c + 32 > limit) {
 #pragma unroll
             for (int e = 0; e < 32; ++e)
-                if (col + c + e >= a.n) x[e] = -INFINITY;
+                if (c + e >= limit) x[e] = -INFINITY;
         }
-        if (mine >= c && mine < c + 32) {
+        if (mine >= c && mine < min(c + 32, limit)) {
             float t = 0.f;
 #pragma unroll
             for (int e = 0; e < 32; ++e) t = mine == c + e ? x[e] : t;
@@ -139,8 +144,9 @@ __device__ __forceinline__ void drain_loss(uint32_t acc, const ProductArgs &a, i
     if (row < a.m) a.part[(size_t)part * a.m + row] = make_float2(m, s);
 }
 
-// 128 columns of logits to D.
-__device__ __forceinline__ void drain_logits(uint32_t acc, const ProductArgs &a, int row0, int lane, int col, uint32_t part) {
+// `cols` columns of logits to D.
+__device__ __forceinline__ void drain_logits(uint32_t acc, const ProductArgs &a, int row0, int lane, int col, int cols,
+                                             uint32_t part) {
     const int row = row0 + lane;
     const bool in = row < a.m;
     const int64_t tok = in ? a.tokens[row] : -1;
@@ -149,8 +155,9 @@ __device__ __forceinline__ void drain_logits(uint32_t acc, const ProductArgs &a,
     const float g = tok >= a.vocab ? __int_as_float(0x7FC00000) : a.half ? scaled(g0) : g0;
     const bool live = tok >= 0;
     uint16_t *out = static_cast<uint16_t *>(a.out) + (size_t)row0 * a.ldo + col;
+    const int limit = min(cols, a.n - col);
 #pragma unroll 1
-    for (int c = 0; c < 128; c += 64) {
+    for (int c = 0; c < limit; c += 64) {
         uint32_t w[32];
 #pragma unroll
         for (int h = 0; h < 64; h += 32) {
@@ -169,21 +176,21 @@ __device__ __forceinline__ void drain_logits(uint32_t acc, const ProductArgs &a,
         for (int i = 0; i < 8; ++i) {
             const int r = 4 * i + (lane >> 3), k = c + 8 * (lane & 7);
             // whole units up to the pitch: what lies past column n is not read
-            if (row0 + r < a.m && col + k < a.n)
+            if (row0 + r < a.m && k < limit)
                 *reinterpret_cast<uint4 *>(out + (size_t)r * a.ldo + k) = staged(part, lane, i);
         }
     }
 }
 
-// 128 columns of dX or dW: into the float32 sums, or to the result.
+// `cols` columns of dX or dW: into the float32 sums, or to the result.
 template <bool kRows>
-__device__ __forceinline__ void drain_result(uint32_t acc, const ProductArgs &a, int row0, int lane, int col, int split,
-                                             uint32_t part) {
+__device__ __forceinline__ void drain_result(uint32_t acc, const ProductArgs &a, int row0, int lane, int col, int cols,
+                                             int split, uint32_t part) {
     const bool vec = ((uintptr_t)a.out & 7) == 0 && a.ldo % 4 == 0;
     const int top = !kRows && a.half ? *a.top : 0;
+    const int limit = min(cols, a.n - col);
 #pragma unroll 1
-    for (int c = 0; c < 128; c += 32) {
-        if (col + c >= a.n) break;
+    for (int c = 0; c < limit; c += 32) {
         float x[32];
         load_columns(acc + c, x);
         uint32_t w[32];
@@ -191,10 +198,11 @@ __device__ __forceinline__ void drain_result(uint32_t acc, const ProductArgs &a,
         for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(x[e]);
         stage_row(part, lane, w);
         const int k = col + c + 4 * (lane & 7);
+        if (c + 4 * (lane & 7) >= limit) continue;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int r = row0 + 4 * i + (lane >> 3);
-            if (r >= a.m || k >= a.n) continue;
+            if (r >= a.m) continue;
             const uint4 u = staged(part, lane, i);
             float y[4] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
             if (a.slab) {
@@ -282,17 +290,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         // ---------------- producer
         bool ok = true;
         const uint32_t full0 = tc::map_rank(full(0), 0);
+        // of both CTAs; boxes of an operand along MN are 64 wide whatever the tile
+        const uint32_t bytes = 2 * (kTile + (kBmn ? kTile : a.cols / 2 * 128));
         Slot<kStages> slot(1);
         int filled = 0;
         for (int64_t u = pair; u < units && ok; u += npairs) {
             const Unit unit(u, a);
-            const int ra = unit.ri * 256 + 128 * rank, cb = unit.cj * 256 + 128 * rank;
+            const int ra = unit.ri * 256 + 128 * rank, cb = unit.cj * a.cols + a.cols / 2 * rank;
             const int c1 = min(a.chunks, (unit.split + 1) * a.per);
             for (int c = unit.split * a.per; c < c1; ++c, slot.next()) {
                 ok = tc::mbar_wait<kPolls>(empty(slot.s), slot.phase);
                 if (!ok) break;
                 if (tc::elect_one()) {
-                    if (rank == 0) tc::mbar_expect_tx(full(slot.s), 2 * kStage);
+                    if (rank == 0) tc::mbar_expect_tx(full(slot.s), bytes);
                     const uint32_t bar = full0 + 8 * slot.s;
                     if (kAmn) {
 #pragma unroll
@@ -329,15 +339,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const uint64_t b0 = kBmn ? sdesc_mn(tileB(0)) : tc::sdesc_sw128(tileB(0));
             // 16 of K: 32 bytes along K, two 8-row atoms (2048 bytes) along MN
             constexpr uint64_t kA = kAmn ? 128 : 2, kB = kBmn ? 128 : 2;
-            const uint32_t idesc = (a.half ? tc::idesc_f16_f32(256, 256) : tc::idesc_bf16_f32(256, 256)) |
+            const uint32_t idesc = (a.half ? tc::idesc_f16_f32(256, a.cols) : tc::idesc_bf16_f32(256, a.cols)) |
                                    (kAmn ? 1u << 15 : 0) | (kBmn ? 1u << 16 : 0);
             Slot<kStages> slot(0);
             Slot<2> acc(1);
-            for (int64_t u = pair; u < units && ok && !(kStalled && u != pair); u += npairs, acc.next()) {
+            for (int64_t u = pair; u < units && ok && !(kStalled && u != pair); u += npairs) {
                 const Unit unit(u, a);
-                const int c0 = unit.split * a.per, c1 = min(a.chunks, c0 + a.per);
-                ok = tc::mbar_wait<kPolls>(aempty(acc.s), acc.phase);
-                for (int c = c0; c < c1 && ok; ++c, slot.next()) {
+                const int first = unit.split * a.per, last = min(a.chunks, first + a.per);
+                for (int c = first, c0 = first, c1 = first; c < last && ok; ++c, slot.next()) {
+                    if (c == first || c == c1) {
+                        // an accumulator's chunks of K begin
+                        c0 = c;
+                        c1 = kWhich == kLoss ? min(last, c + kLossChunks) : last;
+                        ok = tc::mbar_wait<kPolls>(aempty(acc.s), acc.phase);
+                        if (!ok) break;
+                    }
                     ok = tc::mbar_wait<kPolls>(full(slot.s), slot.phase);
                     if (!ok) break;
                     tc::tc_fence_after();
@@ -350,6 +366,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                         if (c + 1 == c1) tc::mma_commit_pair(afull(acc.s));
                     }
                     __syncwarp();
+                    if (c + 1 == c1) acc.next();
                 }
             }
             if (!tc::mma_done_pair<kPolls>(closing, tc::elect_one()) || !ok) *abort_flag = 1;
@@ -361,22 +378,49 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const uint32_t part = tc::smem_u32(smem + kStages * kStage + (warp - 2) * kPart);
         bool ok = true;
         Slot<2> acc(0);
-        for (int64_t u = pair; u < units && ok; u += npairs, acc.next()) {
-            const Unit unit(u, a);
-            const int row0 = unit.ri * 256 + 128 * rank + 32 * q, col = unit.cj * 256 + half * 128;
-            ok = __all_sync(0xffffffffu, tc::mbar_wait<kPolls>(afull(acc.s), acc.phase));
-            if (!ok) break;
-            tc::tc_fence_after();
-            const uint32_t at = tmem + ((uint32_t)(32 * q) << 16) + acc.s * 256 + half * 128;
-            if constexpr (kWhich == kLoss)
-                drain_loss(at, a, row0 + lane, col, 2 * unit.cj + half);
-            else if constexpr (kWhich == kLogits)
-                drain_logits(at, a, row0, lane, col, part);
-            else
-                drain_result<kWhich == kHidden>(at, a, row0, lane, col, unit.split, part);
+        const int cols = a.cols / 2;
+        const uint32_t mine = tmem + ((uint32_t)(32 * q) << 16) + half * cols;
+        auto filled = [&] {
+            const bool in = __all_sync(0xffffffffu, tc::mbar_wait<kPolls>(afull(acc.s), acc.phase));
+            if (in) tc::tc_fence_after();
+            return in;
+        };
+        auto release = [&] {
             tc::tc_fence_before();
             __syncwarp();
             if (lane == 0) tc::mbar_arrive_cluster(released + 8 * acc.s);
+            acc.next();
+        };
+        for (int64_t u = pair; u < units && ok; u += npairs) {
+            const Unit unit(u, a);
+            const int row0 = unit.ri * 256 + 128 * rank + 32 * q, col = unit.cj * a.cols + half * cols;
+            if constexpr (kWhich == kLoss) {
+                float x[128];
+#pragma unroll
+                for (int e = 0; e < 128; ++e) x[e] = 0.f;
+                for (int c = 0; c < a.chunks && ok; c += kLossChunks) {
+                    ok = filled();
+                    if (!ok) break;
+#pragma unroll
+                    for (int h = 0; h < 128; h += 32) {
+                        float v[32];
+                        if (h >= cols) break;
+                        load_columns(mine + acc.s * 256 + h, v);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) x[h + e] += v[e];
+                    }
+                    release();
+                }
+                if (ok) reduce_loss(x, a, row0 + lane, col, cols, 2 * unit.cj + half);
+            } else {
+                ok = filled();
+                if (!ok) break;
+                if constexpr (kWhich == kLogits)
+                    drain_logits(mine + acc.s * 256, a, row0, lane, col, cols, part);
+                else
+                    drain_result<kWhich == kHidden>(mine + acc.s * 256, a, row0, lane, col, cols, unit.split, part);
+                release();
+            }
         }
         if (!ok) *abort_flag = 1;
     }
