@@ -488,14 +488,13 @@ jarq_status jarq_cross_entropy_grad(const void *X, jarq_dtype dtype, int n, int 
  *   Y0, Y : [n][dout] of ydtype (`dtype` or JARQ_F32), pitches ldy0, ldy.  Y0 may be
  *   NULL (zeros), and may be Y itself (ldy0 = ldy).
  *   rank : a multiple of 8, at most 128; adapters of a lower one are filled up with
- *   zeros.  0 <= adapters <= 8192, n >= 0 and at most 2^31 - 4096, din and dout 1 ..
- *   2^20.
- *   workspace : at least jarq_adapters_workspace(n, din, rank) bytes of device memory,
- *   16-byte aligned, that the stream's work may overwrite.
+ *   zeros.  0 <= adapters <= 8192, 0 <= n <= 2^30, din and dout 1 .. 2^20.
+ *   workspace : at least jarq_adapters_workspace(n, din, rank, adapters) bytes of device
+ *   memory, 16-byte aligned, that the stream's work may overwrite.
  * Products are exact or kept to 2^-22 of a token's largest A[i] X[t], sums float32,
  * with one rounding to ydtype at the end.  A token's result does not depend on the
  * other tokens of a call of the same size. */
-size_t jarq_adapters_workspace(int n, int din, int rank);
+size_t jarq_adapters_workspace(int n, int din, int rank, int adapters);
 jarq_status jarq_apply_adapters(const void *X, jarq_dtype dtype, int64_t ldx, const void *A,
                                 const void *B, const float *scale, int adapters, int rank,
                                 const int32_t *ids, int n, int din, int dout, const void *Y0,

@@ -48,8 +48,9 @@ __device__ __forceinline__ float scaled(float g) {
     return __uint_as_float((__float_as_uint(g) & 0x807FFFFFu) | (140u << 23));
 }
 
+// pdl: the launch before it in the stream is one of the same call's.
 cudaError_t launch_product(Product which, const CUtensorMap &a, const CUtensorMap &b, const ProductArgs &args,
-                           cudaStream_t s, bool stalled = false);
+                           cudaStream_t s, bool pdl, bool stalled = false);
 
 // The self-test's form of the loss's product, on `stalled_bytes` of zeros, whose
 // issuer stops early and whose waits give up.

@@ -8,6 +8,7 @@
 
 #include "head.cuh"
 #include "integer.cuh"
+#include "tc_common.cuh"
 
 namespace jarq {
 namespace head {
@@ -29,21 +30,32 @@ __global__ void __launch_bounds__(256) loss_join_kernel(const float2 *parts, int
                                                         const int64_t *tokens, int n, int vocab, float *loss, float *lse) {
     constexpr int kRows = 256 / PER;
     __shared__ float2 all[PER][kRows + 1];
+    tc::pdl_launch_dependents();
+    tc::pdl_wait();
     const int i = threadIdx.x % kRows, t = threadIdx.x / kRows;
     const int r = blockIdx.x * kRows + i;
     float m = -INFINITY, s = 0.f;
-    auto take = [&](float2 p) {
-        const float top = fmaxf(m, p.x), ref = top == -INFINITY ? 0.f : top;
-        s = s * expf(m - ref) + p.y * expf(p.x - ref);
+    constexpr int kBatch = 8;
+    auto take = [&](const float2 *p, int k) {
+        float top = m;
+        for (int j = 0; j < k; ++j) top = fmaxf(top, p[j].x);
+        const float ref = top == -INFINITY ? 0.f : top;
+        s *= expf(m - ref);
+        for (int j = 0; j < k; ++j) s += p[j].y * expf(p[j].x - ref);
         m = top;
     };
     if (r < n)
-        for (int p = t; p < count; p += PER) take(parts[(size_t)p * n + r]);
+        for (int p = t; p < count; p += kBatch * PER) {
+            float2 v[kBatch];
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) v[j] = p + j * PER < count ? parts[(size_t)(p + j * PER) * n + r] : make_float2(-INFINITY, 0.f);
+            take(v, kBatch);
+        }
     all[t][i] = make_float2(m, s);
     for (int left = PER / 2; left; left /= 2) {
         __syncthreads();
         if (t < left) {
-            take(all[t + left][i]);
+            take(&all[t + left][i], 1);
             all[t][i] = make_float2(m, s);
         }
     }
@@ -69,6 +81,8 @@ __global__ void __launch_bounds__(256) copy_rows_kernel(const T *x, int64_t ld, 
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int64_t r = i / per;
     const int k = (int)(i % per) * 8;
+    tc::pdl_launch_dependents();
+    tc::pdl_wait();
     if (r >= n) return;
     const T *p = x + r * ld + k;
     uint4 raw = make_uint4(0, 0, 0, 0);
@@ -98,6 +112,8 @@ __global__ void __launch_bounds__(256) copy_rows_kernel(const T *x, int64_t ld, 
 __global__ void __launch_bounds__(1024) top_exponent_kernel(const int64_t *tokens, const float *g, int n, int *top) {
     __shared__ int part[32];
     int e = -126;
+    tc::pdl_launch_dependents();
+    tc::pdl_wait();
     for (int r = threadIdx.x; r < n; r += 1024)
         if (tokens[r] >= 0) e = max(e, exponent(g[r]));
     e = __reduce_max_sync(0xffffffffu, e);
@@ -115,6 +131,8 @@ __global__ void __launch_bounds__(256) sum_splits_kernel(const float *slab, int 
                                                          int64_t ld, const float *g, const int *top) {
     const int per = pitch / 4;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    tc::pdl_launch_dependents();
+    tc::pdl_wait();
     const int64_t r = i / per;
     const int k = (int)(i % per) * 4;
     if (r >= n || k >= d) return;
@@ -140,8 +158,8 @@ __global__ void __launch_bounds__(256) zero_rows_kernel(T *out, int64_t ld, int 
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // A product's tiles: columns and splits of K that take the least time. Waves of pairs,
-// each so many chunks of K at a time that goes with the columns (6 of them stand for
-// what a tile costs besides), and with splits their float32 sums through memory.
+// each so many chunks of K at a time that goes with the columns (64 of them stand for the
+// rows' operand and what a tile costs besides), and with splits their float32 sums through memory.
 struct Tiles {
     int cols = 256, splits = 1;
     Tiles(int m, int n, int chunks, int most_splits) {
@@ -151,7 +169,7 @@ struct Tiles {
                 const int per = ceil_div(chunks, s), real = ceil_div(chunks, per);
                 const int64_t tiles = (int64_t)ceil_div(m, 256) * ceil_div(n, c) * real;
                 // two cycles a column and chunk; some 3500 bytes a cycle from memory
-                const double t = (double)((tiles + kPairs - 1) / kPairs) * per * (c + 6) +
+                const double t = (double)((tiles + kPairs - 1) / kPairs) * per * (c + 64) +
                                  (real > 1 ? 8.0 * real * m * n / 3500 / 2 : 0);
                 if (best == 0 || t < best) {
                     best = t;
@@ -226,7 +244,8 @@ cudaError_t tensor_map(CUtensorMap *map, const char *p, int rows, int cols, int6
     return make_tmap_half(map, p, rows, cols, rows > 1 ? ld : round_up(cols, 8), box);
 }
 
-// A call's arguments and the launches that it makes, one after the other.
+// A call's arguments and the launches that it makes, one after the other: each but the
+// first may start while the one before it ends, and waits for it before it reads.
 struct Call {
     jarq_dtype dtype;
     int n, d, vocab;
@@ -238,32 +257,33 @@ struct Call {
 
     template <class F>
     cudaError_t typed(F f) {
-        ++launches;
         return dtype == JARQ_F16 ? f(__half()) : f(__nv_bfloat16());
+    }
+    template <class... KArgs, class... Args>
+    cudaError_t run(void (*kernel)(KArgs...), int64_t blocks, int threads, Args... args) {
+        return launch_k(kernel, dim3((unsigned)blocks), dim3(threads), 0, s, launches++ > 0, args...);
     }
     cudaError_t copy(const void *x, int64_t ld, int rows, char *out, int pitch) {
         return typed([&](auto type) {
             using T = decltype(type);
-            copy_rows_kernel<T, false><<<ceil_div((int64_t)rows * (pitch / 8), 256), 256, 0, s>>>(
-                static_cast<const T *>(x), ld, rows, d, reinterpret_cast<T *>(out), pitch, nullptr, nullptr, nullptr);
-            return cudaGetLastError();
+            return run(copy_rows_kernel<T, false>, ceil_div((int64_t)rows * (pitch / 8), 256), 256, static_cast<const T *>(x), ld,
+                       rows, d, reinterpret_cast<T *>(out), pitch, (const int64_t *)nullptr, (const float *)nullptr,
+                       (const int *)nullptr);
         });
     }
     cudaError_t weigh(const void *x, int64_t ld, char *out, int pitch, const float *g, const int *top) {
         return typed([&](auto type) {
             using T = decltype(type);
-            copy_rows_kernel<T, true><<<ceil_div((int64_t)n * (pitch / 8), 256), 256, 0, s>>>(
-                static_cast<const T *>(x), ld, n, d, reinterpret_cast<T *>(out), pitch, tokens, g, top);
-            return cudaGetLastError();
+            return run(copy_rows_kernel<T, true>, ceil_div((int64_t)n * (pitch / 8), 256), 256, static_cast<const T *>(x), ld, n, d,
+                       reinterpret_cast<T *>(out), pitch, tokens, g, top);
         });
     }
     cudaError_t sum_splits(const float *slab, int splits, int rows, int pitch, void *out, int64_t ld, const float *g,
                            const int *top) {
         return typed([&](auto type) {
             using T = decltype(type);
-            sum_splits_kernel<T><<<ceil_div((int64_t)rows * (pitch / 4), 256), 256, 0, s>>>(
-                slab, splits, rows, d, pitch, static_cast<T *>(out), ld, g, top);
-            return cudaGetLastError();
+            return run(sum_splits_kernel<T>, ceil_div((int64_t)rows * (pitch / 4), 256), 256, slab, splits, rows, d, pitch,
+                       static_cast<T *>(out), ld, g, top);
         });
     }
     // the rows of x as TMA can read them: themselves, or a copy of them
@@ -289,8 +309,7 @@ struct Call {
         return a;
     }
     cudaError_t product(Product which, const CUtensorMap &a, const CUtensorMap &b, const ProductArgs &args) {
-        ++launches;
-        return launch_product(which, a, b, args, s);
+        return launch_product(which, a, b, args, s, launches++ > 0);
     }
 };
 
@@ -310,13 +329,12 @@ cudaError_t run_loss(Call &c, const void *X, int64_t ldx, const void *W, int64_t
     a.part = reinterpret_cast<float2 *>(c.work + p.parts);
     a.target = reinterpret_cast<float *>(c.work + p.target);
     TRY(c.product(kLoss, mx, mw, a));
-    ++c.launches;
     // 32 threads a row (8192 rows of 250 parts: 21 us by 8); few rows: 64
-    if (c.n < kPairs)
-        loss_join_kernel<64><<<ceil_div(c.n, 4), 256, 0, c.s>>>(a.part, 2 * a.nt, a.target, c.tokens, c.n, c.vocab, loss, lse);
-    else
-        loss_join_kernel<32><<<ceil_div(c.n, 8), 256, 0, c.s>>>(a.part, 2 * a.nt, a.target, c.tokens, c.n, c.vocab, loss, lse);
-    return cudaGetLastError();
+    auto join = [&](auto *kernel, int per) {
+        return c.run(kernel, ceil_div(c.n, 256 / per), 256, (const float2 *)a.part, 2 * a.nt, (const float *)a.target, c.tokens,
+                     c.n, c.vocab, loss, lse);
+    };
+    return c.n < kPairs ? join(loss_join_kernel<64>, 64) : join(loss_join_kernel<32>, 32);
 }
 
 cudaError_t run_grad(Call &c, const void *X, int64_t ldx, const void *W, int64_t ldw, const Plan &p, const float *lse,
@@ -328,9 +346,7 @@ cudaError_t run_grad(Call &c, const void *X, int64_t ldx, const void *W, int64_t
     CUtensorMap mx, mw, md, mb;
     if (dW) {
         if (c.dtype == JARQ_F16) {
-            ++c.launches;
-            top_exponent_kernel<<<1, 1024, 0, c.s>>>(c.tokens, g, c.n, top);
-            TRY(cudaGetLastError());
+            TRY(c.run(top_exponent_kernel, 1, 1024, c.tokens, g, c.n, top));
         }
         TRY(c.weigh(X, ldx, c.work + p.weighed, p.pitch, g, top));
     }
@@ -412,7 +428,7 @@ cudaError_t launch_stalled(char *zeros, int *failed, cudaStream_t s) {
     CUtensorMap mx, mw;
     TRY(tensor_map(&mx, zeros, c.n, c.d, c.d, 128));
     TRY(tensor_map(&mw, w, c.vocab, c.d, c.d, a.cols / 2));
-    return launch_product(kLoss, mx, mw, a, s, true);
+    return launch_product(kLoss, mx, mw, a, s, false, true);
 }
 
 }  // namespace head

@@ -250,6 +250,7 @@ template <class T, bool VEC, int P, bool GAIN>
 __global__ void __launch_bounds__(P) norm_grad_kernel(GradArgs a) {
     constexpr int E = Shape<T, VEC, P>::E, kHeld = Shape<T, VEC, P>::held;
     __shared__ float part[2][32];
+    tc::pdl_launch_dependents();
     const int t = threadIdx.x;
     float acc[GAIN ? kHeld : 1][E];
     if constexpr (GAIN)
@@ -360,9 +361,16 @@ __global__ void __launch_bounds__(1024) gain_join_kernel(const float *parts, int
     __shared__ float part[32][33];
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const int64_t k = (int64_t)blockIdx.x * 32 + lane;
+    tc::pdl_wait();
     float acc = 0.f;
     if (k < d)
-        for (int i = w; i < count; i += 32) acc += parts[(size_t)i * d + k];
+        for (int i0 = w; i0 < count; i0 += 32 * 8) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = i0 + 32 * j < count ? parts[(size_t)(i0 + 32 * j) * d + k] : 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc += v[j];
+        }
     part[w][lane] = acc;
     __syncthreads();
     acc = warp_sum(part[lane][w]);                 // column w of the block's 32
@@ -520,6 +528,7 @@ __global__ void __launch_bounds__(P, Ring<P, HELD, 2 + STREAM>::resident) norm_g
     constexpr int E = kUnit<T>;
     extern __shared__ uint4 ring[];
     __shared__ float part[2][32];
+    tc::pdl_launch_dependents();
     const int t = threadIdx.x;
     const T *H = static_cast<const T *>(a.H), *Y = static_cast<const T *>(a.dY), *D = static_cast<const T *>(a.dH);
     float g[HELD][E], acc[HELD][E];
@@ -696,9 +705,9 @@ cudaError_t launch_grad_t(GradArgs a, float *dgain, cudaStream_t s) {
         if (a.part) parts = blocks;
     }
     if (e == cudaSuccess && dgain) {
-        gain_join_kernel<<<(unsigned)(((int64_t)a.d + 31) / 32), 1024, 0, s>>>(part, parts, a.d, dgain);
+        e = launch_pdl(gain_join_kernel, dim3((unsigned)(((int64_t)a.d + 31) / 32)), dim3(1024), 0, s, (const float *)part, parts,
+                       a.d, dgain);
         count_launches(1);
-        e = cudaGetLastError();
     }
     return e;
 }

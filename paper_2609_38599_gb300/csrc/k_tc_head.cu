@@ -36,9 +36,9 @@ constexpr int kSmem = 1024 + kStages * kStage + kDrainWarps * kPart + 8 * kBars 
 constexpr int kThreads = 32 * (2 + kDrainWarps);
 // Chunks of K in one accumulator of the loss: the tensor cores' float32 additions
 // round toward zero, which over a long K moves every logit the same way (K = 4096 in
-// one: lse off by 2e-6 of itself); after 512 the sum goes to the drain's registers.
-constexpr int kLossChunks = 8;
-constexpr int kBand = 16;                  // tiles of rows that share the columns' panels in L2
+// one: lse off by 2e-6 of itself); after 1024 the sum goes to the drain's registers.
+constexpr int kLossChunks = 16;
+constexpr int kBand = 9;                   // tiles of rows of a band: with as many columns' tiles at one time, the fewest panels
 static_assert(kSmem <= 227 * 1024, "ring and staged parts must fit an SM's shared memory");
 
 // Descriptor of an operand along MN (128-byte swizzle): 64 elements of MN a row,
@@ -108,23 +108,49 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi, bool half) {
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
+// exp(x - y) of two x as 2^(x L - y L), L = log2 e: with the product y L rounded first,
+// every exponential of a row is off by the same 2^rho, rho = y L - fl(y L), which the
+// caller takes out of their sum or factor.  For |y| below 2^16; rho is below 2^-7 then.
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+constexpr float kLog2e = 1.44269504f, kNear = 65536.f;
+struct Exponentials {
+    tc::F2 scale, shift;
+    float rho;
+    __device__ explicit Exponentials(float y) : scale(tc::f2(kLog2e)) {
+        const float p = __fmul_rn(y, kLog2e);
+        shift = tc::f2(-p);
+        rho = fmaf(y, kLog2e, -p);
+    }
+    __device__ tc::F2 of(tc::F2 x) const {
+        float lo, hi;
+        tc::f2_get(tc::f2_fma(x, scale, shift), lo, hi);
+        return tc::f2(exp2_approx(lo), exp2_approx(hi));
+    }
+};
+
 // A row of `cols` columns of logits: maximum, sum of exponentials less the maximum, and
 // the token's logit where it is among them.
-__device__ __forceinline__ void reduce_loss(float (&acc)[128], const ProductArgs &a, int row, int col, int cols, int part) {
-    const int64_t tok = row < a.m ? a.tokens[row] : -1;
-    const int64_t mine = tok - col;
+__device__ __forceinline__ void reduce_loss(tc::F2 (&acc)[64], const ProductArgs &a, int row, int col, int cols, int part) {
+    const int64_t tok = row < a.m ? a.tokens[row] - col : -1;
     const int limit = min(cols, a.n - col);
+    const int mine = tok >= 0 && tok < limit ? (int)tok : -1;
     float m = -INFINITY, s = 0.f;
 #pragma unroll
     for (int c = 0; c < 128; c += 32) {
         if (c >= limit) break;
-        float *x = acc + c;
+        float x[32];
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) tc::f2_get(acc[(c + e) / 2], x[e], x[e + 1]);
         if (c + 32 > limit) {
 #pragma unroll
             for (int e = 0; e < 32; ++e)
                 if (c + e >= limit) x[e] = -INFINITY;
         }
-        if (mine >= c && mine < min(c + 32, limit)) {
+        if (mine >= c && mine < c + 32) {
             float t = 0.f;
 #pragma unroll
             for (int e = 0; e < 32; ++e) t = mine == c + e ? x[e] : t;
@@ -132,13 +158,23 @@ __device__ __forceinline__ void reduce_loss(float (&acc)[128], const ProductArgs
         }
         float top = m;
 #pragma unroll
-        for (int e = 0; e < 32; ++e) top = fmaxf(top, x[e]);
+        for (int e = 0; e < 32; e += 2) top = fmaxf(fmaxf(x[e], x[e + 1]), top);
         const float ref = top == -INFINITY ? 0.f : top;
-        s *= __expf(m - ref);
-        float t[4] = {0.f, 0.f, 0.f, 0.f};
+        float sum;
+        if (fabsf(ref) < kNear) {
+            const Exponentials exps(ref);
+            tc::F2 t[2] = {tc::f2(0.f), tc::f2(0.f)};
 #pragma unroll
-        for (int e = 0; e < 32; ++e) t[e % 4] += __expf(x[e] - ref);
-        s += (t[0] + t[1]) + (t[2] + t[3]);
+            for (int e = 0; e < 32; e += 2) t[e / 2 % 2] = tc::f2_add(t[e / 2 % 2], exps.of(tc::f2(x[e], x[e + 1])));
+            float lo, hi;
+            tc::f2_get(tc::f2_add(t[0], t[1]), lo, hi);
+            sum = (lo + hi) * exp2_approx(-exps.rho);
+        } else {
+            sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) sum += __expf(x[e] - ref);
+        }
+        s = fmaf(s, __expf(m - ref), sum);
         m = top;
     }
     if (row < a.m) a.part[(size_t)part * a.m + row] = make_float2(m, s);
@@ -149,11 +185,15 @@ __device__ __forceinline__ void drain_logits(uint32_t acc, const ProductArgs &a,
                                              uint32_t part) {
     const int row = row0 + lane;
     const bool in = row < a.m;
-    const int64_t tok = in ? a.tokens[row] : -1;
-    const int64_t mine = tok - a.first - col;
-    const float lse = in ? a.lse[row] : 0.f, g0 = in ? a.g[row] : 0.f;
+    const int64_t tok = in ? a.tokens[row] : -1, at = tok - a.first - col;
+    const int mine = at >= 0 && at < cols ? (int)at : -1;
+    float lse = in ? a.lse[row] : 0.f;
+    if (lse == -INFINITY) lse = 0.f;              // every logit of the row is -inf
+    const float g0 = in ? a.g[row] : 0.f;
     const float g = tok >= a.vocab ? __int_as_float(0x7FC00000) : a.half ? scaled(g0) : g0;
-    const bool live = tok >= 0;
+    const bool live = tok >= 0, all_live = __all_sync(0xffffffffu, live), near = __all_sync(0xffffffffu, fabsf(lse) < kNear);
+    const Exponentials exps(lse);
+    const tc::F2 by = tc::f2(g * exp2_approx(-exps.rho));
     uint16_t *out = static_cast<uint16_t *>(a.out) + (size_t)row0 * a.ldo + col;
     const int limit = min(cols, a.n - col);
 #pragma unroll 1
@@ -163,10 +203,23 @@ __device__ __forceinline__ void drain_logits(uint32_t acc, const ProductArgs &a,
         for (int h = 0; h < 64; h += 32) {
             float x[32];
             load_columns(acc + c + h, x);
+            if (near) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-                const float p = x[e] == -INFINITY ? 0.f : __expf(x[e] - lse);
-                x[e] = live ? g * (mine == c + h + e ? p - 1.f : p) : 0.f;
+                for (int e = 0; e < 32; e += 2) tc::f2_get(tc::f2_mul(exps.of(tc::f2(x[e], x[e + 1])), by), x[e], x[e + 1]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 32; ++e) x[e] = g * __expf(x[e] - lse);
+            }
+            const int j = mine - c - h;
+            if (j >= 0 && j < 32) {
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                    if (e == j) x[e] -= g;
+            }
+            if (!all_live) {
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                    if (!live) x[e] = 0.f;
             }
 #pragma unroll
             for (int e = 0; e < 32; e += 2) w[(h + e) / 2] = pack2(x[e], x[e + 1], a.half);
@@ -285,6 +338,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     tc::cluster_sync();
     tc::tc_fence_after();
     const uint32_t tmem = *tmem_slot;
+    // what the launch before this one wrote, if it may still be running
+    tc::pdl_launch_dependents();
+    tc::pdl_wait();
 
     if (warp == 0) {
         // ---------------- producer
@@ -395,9 +451,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const Unit unit(u, a);
             const int row0 = unit.ri * 256 + 128 * rank + 32 * q, col = unit.cj * a.cols + half * cols;
             if constexpr (kWhich == kLoss) {
-                float x[128];
+                tc::F2 x[64];
 #pragma unroll
-                for (int e = 0; e < 128; ++e) x[e] = 0.f;
+                for (int e = 0; e < 64; ++e) x[e] = tc::f2(0.f);
                 for (int c = 0; c < a.chunks && ok; c += kLossChunks) {
                     ok = filled();
                     if (!ok) break;
@@ -407,7 +463,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                         if (h >= cols) break;
                         load_columns(mine + acc.s * 256 + h, v);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) x[h + e] += v[e];
+                        for (int e = 0; e < 32; e += 2) x[(h + e) / 2] = tc::f2_add(x[(h + e) / 2], tc::f2(v[e], v[e + 1]));
                     }
                     release();
                 }
@@ -441,26 +497,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 }
 
 template <Product kWhich, bool kStalled = false>
-cudaError_t launch(const CUtensorMap &a, const CUtensorMap &b, const ProductArgs &args, cudaStream_t s) {
+cudaError_t launch(const CUtensorMap &a, const CUtensorMap &b, const ProductArgs &args, cudaStream_t s, bool pdl) {
     static std::atomic<unsigned long long> done;
     auto *kernel = tc_head_kernel<kWhich, kStalled>;
     const cudaError_t e = set_max_dynamic_smem((const void *)kernel, kSmem, done);
     if (e != cudaSuccess) return e;
     const int64_t units = (int64_t)args.mt * args.nt * args.splits;
     return launch_k(kernel, dim3((unsigned)(2 * std::min<int64_t>(units, std::max(1, num_sms() / 2)))), dim3(kThreads),
-                    (size_t)kSmem, s, false, a, b, args);
+                    (size_t)kSmem, s, pdl, a, b, args);
 }
 
 }  // namespace
 
 cudaError_t launch_product(Product which, const CUtensorMap &a, const CUtensorMap &b, const ProductArgs &args,
-                           cudaStream_t s, bool stalled) {
-    if (stalled) return launch<kLoss, true>(a, b, args, s);
+                           cudaStream_t s, bool pdl, bool stalled) {
+    if (stalled) return launch<kLoss, true>(a, b, args, s, pdl);
     switch (which) {
-        case kLoss: return launch<kLoss>(a, b, args, s);
-        case kLogits: return launch<kLogits>(a, b, args, s);
-        case kHidden: return launch<kHidden>(a, b, args, s);
-        default: return launch<kHead>(a, b, args, s);
+        case kLoss: return launch<kLoss>(a, b, args, s, pdl);
+        case kLogits: return launch<kLogits>(a, b, args, s, pdl);
+        case kHidden: return launch<kHidden>(a, b, args, s, pdl);
+        default: return launch<kHead>(a, b, args, s, pdl);
     }
 }
 

@@ -130,7 +130,7 @@ def _load():
     lib.jarq_cross_entropy_grad.restype = ci
     lib.jarq_cross_entropy_grad.argtypes = [vp, ci, ci, ci, cl, vp, ci, cl, vp, vp, vp, vp, cl, vp, cl, vp, cz, vp]
     lib.jarq_adapters_workspace.restype = cz
-    lib.jarq_adapters_workspace.argtypes = [ci, ci, ci]
+    lib.jarq_adapters_workspace.argtypes = [ci, ci, ci, ci]
     lib.jarq_apply_adapters.restype = ci
     lib.jarq_apply_adapters.argtypes = [vp, ci, cl, vp, vp, vp, ci, ci, vp, ci, ci, ci, vp, cl, vp, cl, ci, vp, cz, vp]
     lib.jarq_hessian_din.restype = ci
@@ -743,34 +743,34 @@ def rms_norm(X, gain=None, eps: float = 1e-6, residual=None, values: bool = True
     ``residual``.  The rows of the codes lie on 16-byte boundaries."""
     T = _torch()
     x, ldx, n, d, code = _matrix(X, "X", T.floats)
-    dtype, dev = X.dtype, X.device
+    dtype, empty = X.dtype, T.empty
     g, gcode = _gain(T, gain, d, dtype, code)
-    r = hp = y = q = s = None
+    r = hp = Y = y = Q = q = scale = s = None
     ldr = ldh = ldq = d
     if residual is not None:
         r, ldr = _like(residual, "residual", n, d, dtype)
         if h is None:
-            h = T.empty((n, d), dtype=dtype, device=dev)
+            h = empty((n, d), dtype=dtype, device=X.device)
             hp = h.data_ptr()
         else:
             hp, ldh = _like(h, "h", n, d, dtype)
     elif h is not None:
         raise ValueError("h is the sum with a residual: there is none")
-    Y = Q = scale = None
     if values:
-        Y = T.empty((n, d), dtype=dtype, device=dev)
+        Y = empty((n, d), dtype=dtype, device=X.device)
         y = Y.data_ptr()
     if codes:
         ldq = (d + 15) // 16 * 16
-        Q = T.empty((n, ldq), dtype=T.i8, device=dev)
-        scale = T.empty((n,), dtype=T.f32, device=dev)
+        Q = empty((n, ldq), dtype=T.i8, device=X.device)
+        scale = empty((n,), dtype=T.f32, device=X.device)
         q, s = Q.data_ptr(), scale.data_ptr()
-    rstd = T.empty((n,), dtype=T.f32, device=dev)
+        Q = Q[:, :d]
+    rstd = empty((n,), dtype=T.f32, device=X.device)
     status = _lib.jarq_rms_norm(x, code, n, d, ldx, r, ldr, hp, ldh, g, gcode, eps, y, d, q, ldq, s, rstd.data_ptr(),
                                 T.stream(X.get_device()))
     if status != JARQ_OK:
         raise JarqError(status, "jarq_rms_norm")
-    return NormedRows(X if residual is None else h, Y, Q[:, :d] if codes else None, scale, rstd)
+    return NormedRows(X if residual is None else h, Y, Q, scale, rstd)
 
 
 def rms_norm_grad(h, gain, rstd, dy, dh=None, rows: bool = True, gains: bool = True, out=None):
@@ -886,7 +886,7 @@ def apply_adapters(X, A, B, ids, scale=None, base=None, dtype: str = None, out=N
         y, ldy = out.data_ptr(), dout
     else:
         y, ldy = _like(out, "out", n, dout, ydt)
-    size = _lib.jarq_adapters_workspace(n, din, rank)
+    size = _lib.jarq_adapters_workspace(n, din, rank, m)
     work = T.empty((size,), dtype=T.u8, device=dev)
     status = _lib.jarq_apply_adapters(x, code, ldx, a, b, s, m, rank, i, n, din, dout, y0, ldy0, y, ldy,
                                       T.floats[ydt], work.data_ptr(), size, T.stream(X.get_device()))
