@@ -18,13 +18,14 @@ enum Product {
 struct ProductArgs {
     int m, n;                   // rows and columns of the result
     int chunks, per, splits;    // 64-wide chunks of K, of a split, splits
-    int cols;                   // columns of a tile: a multiple of 32, 128 .. 256
+    int cols;                   // columns of a tile: a multiple of 32, up to 256
     int mt, nt;                 // tiles of 256 x cols
     bool half;                  // float16, else bfloat16
     // kLoss, kLogits
     const int64_t *tokens;
     const float *lse, *g;       // kLogits; g also of kHidden
     int first, vocab;           // token of column 0; tokens of the vocabulary
+    int rows;                   // of A's box of 128: fewer where the result has no more
     float2 *part;               // kLoss: [2 nt][m] maxima and sums of half a tile's columns
     float *target;              // kLoss: [m] logit of the row's token
     // kLogits: D [m][ldo].  kHidden, kHead: the result, or with `slab` float32 sums

@@ -164,7 +164,7 @@ struct Tiles {
     int cols = 256, splits = 1;
     Tiles(int m, int n, int chunks, int most_splits) {
         double best = 0;
-        for (int c = 256; c >= 128; c -= 32)
+        for (int c = 256; c >= 32; c -= 32)
             for (int s = 1; s <= std::min(most_splits, std::max(1, chunks / 8)); ++s) {
                 const int per = ceil_div(chunks, s), real = ceil_div(chunks, per);
                 const int64_t tiles = (int64_t)ceil_div(m, 256) * ceil_div(n, c) * real;
@@ -301,6 +301,7 @@ struct Call {
         a.splits = tile.splits;
         a.per = ceil_div(a.chunks, a.splits);
         a.cols = tile.cols;
+        a.rows = m < 128 ? round_up(m, 8) : 128;
         a.mt = ceil_div(m, 256), a.nt = ceil_div(cols, a.cols);
         a.half = dtype == JARQ_F16;
         a.tokens = tokens, a.vocab = vocab;
@@ -323,8 +324,8 @@ cudaError_t run_loss(Call &c, const void *X, int64_t ldx, const void *W, int64_t
     TRY(c.readable(X, ldx, c.n, c.work + p.copy_x, p.pitch, &x));
     TRY(c.readable(W, ldw, c.vocab, c.work + p.copy_w, p.pitch, &w));
     CUtensorMap mx, mw;
-    TRY(tensor_map(&mx, x.p, c.n, c.d, x.ld, 128));
     ProductArgs a = c.shape(c.n, c.vocab, c.d, 1);
+    TRY(tensor_map(&mx, x.p, c.n, c.d, x.ld, a.rows));
     TRY(tensor_map(&mw, w.p, c.vocab, c.d, w.ld, a.cols / 2));
     a.part = reinterpret_cast<float2 *>(c.work + p.parts);
     a.target = reinterpret_cast<float *>(c.work + p.target);
@@ -357,17 +358,17 @@ cudaError_t run_grad(Call &c, const void *X, int64_t ldx, const void *W, int64_t
     for (int i = 0; i < p.pieces; ++i) {
         const int v0 = i * p.width, width = std::min(p.width, c.vocab - v0);
         {
-            TRY(tensor_map(&mx, x.p, c.n, c.d, x.ld, 128));
             ProductArgs a = c.shape(c.n, width, c.d, 1);
+            TRY(tensor_map(&mx, x.p, c.n, c.d, x.ld, a.rows));
             TRY(tensor_map(&mw, w.row(v0), width, c.d, w.ld, a.cols / 2));
             a.lse = lse, a.g = g, a.first = v0;
             a.out = D, a.ldo = p.width;
             TRY(c.product(kLogits, mx, mw, a));
         }
         if (dX) {
-            TRY(tensor_map(&md, D, c.n, width, p.width, 128));
-            TRY(tensor_map(&mb, w.row(v0), width, c.d, w.ld, 64));
             ProductArgs a = c.shape(c.n, c.d, width, i == 0 ? p.split_x : sums);
+            TRY(tensor_map(&md, D, c.n, width, p.width, a.rows));
+            TRY(tensor_map(&mb, w.row(v0), width, c.d, w.ld, 64));
             if (i == 0) sums = a.splits;             // a shorter piece may have fewer
             a.g = g;
             a.out = dX, a.ldo = lddx;
@@ -417,7 +418,7 @@ constexpr int kStalledRows = 2048, kStalledTokens = 4096, kStalledWidth = 256;
 
 size_t stalled_bytes() {
     return (size_t)(kStalledRows + kStalledTokens) * kStalledWidth * 2 + kStalledRows * (sizeof(int64_t) + sizeof(float)) +
-           (size_t)2 * (kStalledTokens / 128) * kStalledRows * sizeof(float2);
+           (size_t)2 * (kStalledTokens / 32) * kStalledRows * sizeof(float2);
 }
 cudaError_t launch_stalled(char *zeros, int *failed, cudaStream_t s) {
     char *w = zeros + (size_t)kStalledRows * kStalledWidth * 2, *rest = w + (size_t)kStalledTokens * kStalledWidth * 2;
@@ -426,7 +427,7 @@ cudaError_t launch_stalled(char *zeros, int *failed, cudaStream_t s) {
     a.part = reinterpret_cast<float2 *>(rest + kStalledRows * sizeof(int64_t));
     a.target = reinterpret_cast<float *>(a.part + (size_t)2 * a.nt * c.n);
     CUtensorMap mx, mw;
-    TRY(tensor_map(&mx, zeros, c.n, c.d, c.d, 128));
+    TRY(tensor_map(&mx, zeros, c.n, c.d, c.d, a.rows));
     TRY(tensor_map(&mw, w, c.vocab, c.d, c.d, a.cols / 2));
     return launch_product(kLoss, mx, mw, a, s, false, true);
 }

@@ -134,8 +134,9 @@ struct Exponentials {
 
 // A row of `cols` columns of logits: maximum, sum of exponentials less the maximum, and
 // the token's logit where it is among them.
-__device__ __forceinline__ void reduce_loss(tc::F2 (&acc)[64], const ProductArgs &a, int row, int col, int cols, int part) {
-    const int64_t tok = row < a.m ? a.tokens[row] - col : -1;
+__device__ __forceinline__ void reduce_loss(tc::F2 (&acc)[64], const ProductArgs &a, int row, int64_t token, int col, int cols,
+                                            int part) {
+    const int64_t tok = token - col;
     const int limit = min(cols, a.n - col);
     const int mine = tok >= 0 && tok < limit ? (int)tok : -1;
     float m = -INFINITY, s = 0.f;
@@ -180,17 +181,25 @@ __device__ __forceinline__ void reduce_loss(tc::F2 (&acc)[64], const ProductArgs
     if (row < a.m) a.part[(size_t)part * a.m + row] = make_float2(m, s);
 }
 
+// What a drain warp's lane knows of its row; read before the row's sums are waited for.
+struct RowArgs {
+    int64_t token;
+    float lse, g;
+    __device__ RowArgs(const ProductArgs &a, int row, bool gradient) {
+        const bool in = row < a.m;
+        token = in ? a.tokens[row] : -1;
+        lse = in && gradient ? a.lse[row] : 0.f;
+        g = in && gradient ? a.g[row] : 0.f;
+    }
+};
+
 // `cols` columns of logits to D.
-__device__ __forceinline__ void drain_logits(uint32_t acc, const ProductArgs &a, int row0, int lane, int col, int cols,
-                                             uint32_t part) {
-    const int row = row0 + lane;
-    const bool in = row < a.m;
-    const int64_t tok = in ? a.tokens[row] : -1, at = tok - a.first - col;
+__device__ __forceinline__ void drain_logits(uint32_t acc, const ProductArgs &a, const RowArgs &of, int row0, int lane, int col,
+                                             int cols, uint32_t part) {
+    const int64_t tok = of.token, at = tok - a.first - col;
     const int mine = at >= 0 && at < cols ? (int)at : -1;
-    float lse = in ? a.lse[row] : 0.f;
-    if (lse == -INFINITY) lse = 0.f;              // every logit of the row is -inf
-    const float g0 = in ? a.g[row] : 0.f;
-    const float g = tok >= a.vocab ? __int_as_float(0x7FC00000) : a.half ? scaled(g0) : g0;
+    const float lse = of.lse == -INFINITY ? 0.f : of.lse;         // -inf: every logit of the row is
+    const float g = tok >= a.vocab ? __int_as_float(0x7FC00000) : a.half ? scaled(of.g) : of.g;
     const bool live = tok >= 0, all_live = __all_sync(0xffffffffu, live), near = __all_sync(0xffffffffu, fabsf(lse) < kNear);
     const Exponentials exps(lse);
     const tc::F2 by = tc::f2(g * exp2_approx(-exps.rho));
@@ -235,11 +244,48 @@ __device__ __forceinline__ void drain_logits(uint32_t acc, const ProductArgs &a,
     }
 }
 
-// `cols` columns of dX or dW: into the float32 sums, or to the result.
+// `cols` columns of dX or dW to the result.
 template <bool kRows>
 __device__ __forceinline__ void drain_result(uint32_t acc, const ProductArgs &a, int row0, int lane, int col, int cols,
-                                             int split, uint32_t part) {
-    const bool vec = ((uintptr_t)a.out & 7) == 0 && a.ldo % 4 == 0;
+                                             uint32_t part) {
+    const int limit = min(cols, a.n - col), rows = a.m - row0;
+    const bool vec = ((uintptr_t)a.out & 15) == 0 && a.ldo % 8 == 0;
+    const float by = !a.half ? 1.f : ldexpf(1.f, (!kRows ? *a.top : lane < rows ? exponent(a.g[row0 + lane]) : 0) - 14);
+    uint16_t *out = static_cast<uint16_t *>(a.out) + (size_t)row0 * a.ldo + col;
+#pragma unroll 1
+    for (int c = 0; c < limit; c += 64) {
+        uint32_t w[32];
+#pragma unroll
+        for (int h = 0; h < 64; h += 32) {
+            float x[32];
+            load_columns(acc + c + h, x);
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) w[(h + e) / 2] = pack2(x[e] * by, x[e + 1] * by, a.half);
+        }
+        stage_row(part, lane, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = 4 * i + (lane >> 3), k = c + 8 * (lane & 7);
+            if (r >= rows || k >= limit) continue;
+            const uint4 u = staged(part, lane, i);
+            uint16_t *to = out + (size_t)r * a.ldo + k;
+            if (vec && k + 8 <= limit) {
+                *reinterpret_cast<uint4 *>(to) = u;
+            } else {
+                const uint32_t v[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (k + e < limit) to[e] = (uint16_t)(v[e / 2] >> (e & 1 ? 16 : 0));
+            }
+        }
+    }
+}
+
+// The same to the float32 sums of a split or of several pieces; the last piece's, where
+// there is one split, to the result.
+template <bool kRows>
+__device__ __forceinline__ void drain_sums(uint32_t acc, const ProductArgs &a, int row0, int lane, int col, int cols, int split,
+                                           uint32_t part) {
     const int top = !kRows && a.half ? *a.top : 0;
     const int limit = min(cols, a.n - col);
 #pragma unroll 1
@@ -258,32 +304,21 @@ __device__ __forceinline__ void drain_result(uint32_t acc, const ProductArgs &a,
             if (r >= a.m) continue;
             const uint4 u = staged(part, lane, i);
             float y[4] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
-            if (a.slab) {
-                float4 *to = reinterpret_cast<float4 *>(a.slab + ((size_t)split * a.m + r) * a.pitch + k);
-                if (a.add) {
-                    const float4 o = *to;
-                    y[0] += o.x, y[1] += o.y, y[2] += o.z, y[3] += o.w;
-                }
-                if (!a.last) {
-                    *to = make_float4(y[0], y[1], y[2], y[3]);
-                    continue;
-                }
+            float4 *sum = reinterpret_cast<float4 *>(a.slab + ((size_t)split * a.m + r) * a.pitch + k);
+            if (a.add) {
+                const float4 o = *sum;
+                y[0] += o.x, y[1] += o.y, y[2] += o.z, y[3] += o.w;
             }
-            if (a.half) {
-                const float by = ldexpf(1.f, (kRows ? exponent(a.g[r]) : top) - 14);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] *= by;
+            if (!a.last) {
+                *sum = make_float4(y[0], y[1], y[2], y[3]);
+                continue;
             }
+            const float by = a.half ? ldexpf(1.f, (kRows ? exponent(a.g[r]) : top) - 14) : 1.f;
             uint16_t *to = static_cast<uint16_t *>(a.out) + (size_t)r * a.ldo + k;
-            const uint32_t lo = pack2(y[0], y[1], a.half), hi = pack2(y[2], y[3], a.half);
-            if (vec && k + 4 <= a.n) {
-                *reinterpret_cast<uint2 *>(to) = make_uint2(lo, hi);
-            } else {
-                to[0] = (uint16_t)lo;
-                if (k + 1 < a.n) to[1] = (uint16_t)(lo >> 16);
-                if (k + 2 < a.n) to[2] = (uint16_t)hi;
-                if (k + 3 < a.n) to[3] = (uint16_t)(hi >> 16);
-            }
+            const uint32_t v[2] = {pack2(y[0] * by, y[1] * by, a.half), pack2(y[2] * by, y[3] * by, a.half)};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (k + e < a.n) to[e] = (uint16_t)(v[e / 2] >> (e & 1 ? 16 : 0));
         }
     }
 }
@@ -347,7 +382,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         bool ok = true;
         const uint32_t full0 = tc::map_rank(full(0), 0);
         // of both CTAs; boxes of an operand along MN are 64 wide whatever the tile
-        const uint32_t bytes = 2 * (kTile + (kBmn ? kTile : a.cols / 2 * 128));
+        const int boxes = a.cols > 128 ? 2 : 1;
+        // of a single tile's rows only those that there are: the others' places in shared
+        // memory hold what they hold, and their sums are not kept
+        const bool loadsA = kAmn || a.mt > 1 || 128 * rank < a.m;
+        const uint32_t bytesA = kAmn ? 2 * kTile : a.rows * 128 * (a.mt > 1 || a.m > 128 ? 2 : 1);
+        const uint32_t bytes = bytesA + 2 * (kBmn ? boxes * kBox : a.cols / 2 * 128);
         Slot<kStages> slot(1);
         int filled = 0;
         for (int64_t u = pair; u < units && ok; u += npairs) {
@@ -364,12 +404,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
                         for (int m = 0; m < 2; ++m)
                             tc::tma_load_2d_pair(tileA(slot.s) + m * kBox, &mapA, bar, ra + 64 * m, c * 64);
-                    } else {
+                    } else if (loadsA) {
                         tc::tma_load_2d_pair(tileA(slot.s), &mapA, bar, c * 64, ra);
                     }
                     if (kBmn) {
-#pragma unroll
-                        for (int m = 0; m < 2; ++m)
+                        for (int m = 0; m < boxes; ++m)
                             tc::tma_load_2d_pair(tileB(slot.s) + m * kBox, &mapB, bar, cb + 64 * m, c * 64);
                     } else {
                         tc::tma_load_2d_pair(tileB(slot.s), &mapB, bar, c * 64, cb);
@@ -450,7 +489,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         for (int64_t u = pair; u < units && ok; u += npairs) {
             const Unit unit(u, a);
             const int row0 = unit.ri * 256 + 128 * rank + 32 * q, col = unit.cj * a.cols + half * cols;
+            const bool rows = row0 < a.m;          // else nothing is kept of this warp's rows
             if constexpr (kWhich == kLoss) {
+                const RowArgs of(a, row0 + lane, false);
                 tc::F2 x[64];
 #pragma unroll
                 for (int e = 0; e < 64; ++e) x[e] = tc::f2(0.f);
@@ -460,21 +501,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
                     for (int h = 0; h < 128; h += 32) {
                         float v[32];
-                        if (h >= cols) break;
+                        if (h >= cols || !rows) break;
                         load_columns(mine + acc.s * 256 + h, v);
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) x[(h + e) / 2] = tc::f2_add(x[(h + e) / 2], tc::f2(v[e], v[e + 1]));
                     }
                     release();
                 }
-                if (ok) reduce_loss(x, a, row0 + lane, col, cols, 2 * unit.cj + half);
+                if (ok && rows) reduce_loss(x, a, row0 + lane, of.token, col, cols, 2 * unit.cj + half);
             } else {
+                const RowArgs of(a, kWhich == kLogits ? row0 + lane : a.m, true);
                 ok = filled();
                 if (!ok) break;
-                if constexpr (kWhich == kLogits)
-                    drain_logits(mine + acc.s * 256, a, row0, lane, col, cols, part);
+                if (!rows)
+                    ;
+                else if constexpr (kWhich == kLogits)
+                    drain_logits(mine + acc.s * 256, a, of, row0, lane, col, cols, part);
+                else if (a.slab)
+                    drain_sums<kWhich == kHidden>(mine + acc.s * 256, a, row0, lane, col, cols, unit.split, part);
                 else
-                    drain_result<kWhich == kHidden>(mine + acc.s * 256, a, row0, lane, col, cols, unit.split, part);
+                    drain_result<kWhich == kHidden>(mine + acc.s * 256, a, row0, lane, col, cols, part);
                 release();
             }
         }
