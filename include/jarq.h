@@ -429,7 +429,8 @@ jarq_status jarq_rms_norm(const void *X, jarq_dtype dtype, int n, int d, int64_t
  *   by the residual stream, pitch lds, or NULL.  dX may be NULL, and may be dY or dH
  *   itself (same pitch).  dgain : float32 [d], overwritten (zeros for n = 0), or NULL.
  *   workspace : at least jarq_rms_norm_grad_workspace(n, d) bytes of device memory,
- *   16-byte aligned, that the stream's work may overwrite; NULL without dgain.
+ *   16-byte aligned, that the stream's work may overwrite; NULL without dgain and for up
+ *   to 152 rows, which need none.
  * Sums are float32, always added in the same order. */
 size_t jarq_rms_norm_grad_workspace(int n, int d);
 jarq_status jarq_rms_norm_grad(const void *H, jarq_dtype dtype, int n, int d, int64_t ldh,
@@ -490,7 +491,8 @@ jarq_status jarq_cross_entropy_grad(const void *X, jarq_dtype dtype, int n, int 
  *   rank : a multiple of 8, at most 128; adapters of a lower one are filled up with
  *   zeros.  0 <= adapters <= 8192, 0 <= n <= 2^30, din and dout 1 .. 2^20.
  *   workspace : at least jarq_adapters_workspace(n, din, rank, adapters) bytes of device
- *   memory, 16-byte aligned, that the stream's work may overwrite.
+ *   memory, 16-byte aligned, that the stream's work may overwrite; NULL for none (up to
+ *   64 tokens).
  * Products are exact or kept to 2^-22 of a token's largest A[i] X[t], sums float32,
  * with one rounding to ydtype at the end.  A token's result does not depend on the
  * other tokens of a call of the same size. */

@@ -1,12 +1,10 @@
 // Low-rank adapters of many requests, added to a shared projection's outputs:
 //   Y_t = Y0_t + s_i B_i (A_i x_t),   i = ids[t].
-// Two kernels: the sums u_t = A_i x_t over the tokens' width, and their expansion by
-// B_i with the addition.
 //
-// Few tokens: dot products, a block a token and a piece of its width (of its outputs);
-// an adapter's bytes are read as wide as they lie.
+// Few tokens: dot products, a cluster of CTAs a token, in one launch.
 //
-// More tokens: first an order in which tokens of one adapter follow one another (a
+// More tokens: two kernels, the sums u_t = A_i x_t over the tokens' width and their
+// expansion by B_i with the addition.  Before them an order in which tokens of one adapter follow one another (a
 // token's results do not depend on it: the sums of a row of an MMA are its own), then
 // 16 tokens a warp on mma.sync, whose operands go straight from memory to
 // registers: a sum over K does not depend on the order of K, so a lane takes 8
@@ -86,70 +84,109 @@ __device__ __forceinline__ int adapter_of(const AdapterArgs &a, int t) {
 }
 
 // ---------------------------------------------------------------- few tokens
-// Piece blockIdx.y of the width of token blockIdx.x: a warp has every 8th row of A.
-template <class T>
-__global__ void __launch_bounds__(256) few_sums_kernel(AdapterArgs a) {
-    tc::pdl_launch_dependents();
-    const int t = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int i = adapter_of(a, t);
-    if (i < 0) return;
-    const T *x = static_cast<const T *>(a.X) + (size_t)t * a.ldx;
-    const T *A = static_cast<const T *>(a.A) + (size_t)i * a.rank * a.din;
-    const int k0 = blockIdx.y * kFewPiece + 8 * lane;
-    float v[kFewPiece / 256][8];
-#pragma unroll
-    for (int h = 0; h < kFewPiece / 256; ++h) unpack(load8(x, k0 + 256 * h, a.din, a.vec_x), v[h], T());
-    for (int j = warp; j < a.rank; j += 8) {
-        float sum = 0.f;
-#pragma unroll
-        for (int h = 0; h < kFewPiece / 256; ++h) {
-            float w[8];
-            unpack(load8(A + (size_t)j * a.din, k0 + 256 * h, a.din, a.vec_x), w, T());
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum = fmaf(v[h][e], w[e], sum);
-        }
-        sum = warp_sum(sum);
-        if (lane == 0) a.u[((size_t)blockIdx.y * a.n + t) * a.rank + j] = sum;
-    }
+// The CTAs of a cluster share a token: pieces of its width, then, with the sums of all
+// of them, pieces of its outputs.  Bound by latencies (first loads, cluster's join, B's
+// loads) and, outside a graph, by the host: one token 4096 -> 11008 of rank 16 takes 5.9
+// us on the device, a call 17 us.  In two launches with the sums in memory between them
+// it took 4.6 and 23.  48 tokens 11008 -> 4096 8.1 us, 8.4 in two.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ float load_peer(const float *p, uint32_t rank) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(tc::map_rank(tc::smem_u32(p), rank)) : "memory");
+    return v;
 }
 
-// 256 outputs of token blockIdx.x, one a thread.
-template <class T, class Out>
-__global__ void __launch_bounds__(256) few_outputs_kernel(AdapterArgs a) {
-    __shared__ float u[kMostRank], part[256];
-    const int t = blockIdx.x, o = blockIdx.y * 256 + threadIdx.x;
-    const int i = adapter_of(a, t);
-    const float y0 = a.Y0 && o < a.dout ? to_float(static_cast<const Out *>(a.Y0)[(size_t)t * a.ldy0 + o]) : 0.f;
-    float y = i == -2 ? __int_as_float(0x7FC00000) : y0;
-    tc::pdl_wait();
+// kThreads: 512 where the CTAs leave SMs idle, with B on its way to L2 under the sums; a
+// row's sum is the same.
+template <class T, class Out, int kThreads>
+__global__ void __launch_bounds__(kThreads) few_kernel(AdapterArgs a, int ctas) {
+    constexpr int kWarps = kThreads / 32, kH = kFewPiece / 256;
+    __shared__ float mine[kMostRank], u[kMostRank];
+    const int t = blockIdx.x / ctas, part = blockIdx.x % ctas, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int i = adapter_of(a, t);            // of all of the cluster
+    const Out *y0 = static_cast<const Out *>(a.Y0) + (size_t)t * a.ldy0;
+    Out *y = static_cast<Out *>(a.Y) + (size_t)t * a.ldy;
+    const T *B = static_cast<const T *>(a.B) + (size_t)max(i, 0) * a.dout * a.rank;
+    const int first = part * kThreads + threadIdx.x, step = ctas * kThreads;   // outputs
     if (i >= 0) {
-        // the sums over the width's pieces: 256 / rank threads have a rank's
-        const int slices = 256 / a.rank, j = threadIdx.x % a.rank, s0 = threadIdx.x / a.rank;
-        float sum = 0.f;
-        if (s0 < slices)
-            for (int s = s0; s < a.splits; s += slices) sum += a.u[((size_t)s * a.n + t) * a.rank + j];
-        part[threadIdx.x] = sum;
-        __syncthreads();
-        if (threadIdx.x < a.rank) {
-            sum = 0.f;
-            for (int s = 0; s < slices; ++s) sum += part[s * a.rank + threadIdx.x];
-            u[threadIdx.x] = sum * (a.scale ? a.scale[i] : 1.f);
-        }
-        __syncthreads();
-        if (o < a.dout) {
-            const T *b = static_cast<const T *>(a.B) + ((size_t)i * a.dout + o) * a.rank;
-            const bool vec = ((uintptr_t)b & 15) == 0;
-            float d = 0.f;
-            for (int k = 0; k < a.rank; k += 8) {
-                float w[8];
-                unpack(load8(b, k, a.rank, vec), w, T());
+        for (int o = first; kThreads == 512 && o < a.dout; o += step)
+            for (int k = 0; k < a.rank; k += 64)
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(B + (size_t)o * a.rank + k) : "memory");
+        const T *x = static_cast<const T *>(a.X) + (size_t)t * a.ldx;
+        const T *A = static_cast<const T *>(a.A) + (size_t)i * a.rank * a.din;
+        for (int k0 = part * kFewPiece; k0 < a.din || k0 == part * kFewPiece; k0 += ctas * kFewPiece) {
+            const int k = k0 + 8 * lane;
+            uint4 raw[kH];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) d = fmaf(w[e], u[k + e], d);
+            for (int h = 0; h < kH; ++h) raw[h] = load8(x, k + 256 * h, a.din, a.vec_x);
+            // a warp has every kWarps-th row of A, two at a time
+            for (int j = warp; j < a.rank; j += 2 * kWarps) {
+                const bool two = j + kWarps < a.rank;
+                uint4 w[2][kH];
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int h = 0; h < kH; ++h)
+                        w[r][h] = r && !two ? make_uint4(0, 0, 0, 0)
+                                            : load8(A + (size_t)(j + r * kWarps) * a.din, k + 256 * h, a.din, a.vec_x);
+                float sum[2] = {0.f, 0.f};
+#pragma unroll
+                for (int h = 0; h < kH; ++h) {
+                    float v[8];
+                    unpack(raw[h], v, T());
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        float q[8];
+                        unpack(w[r][h], q, T());
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) sum[r] = fmaf(v[e], q[e], sum[r]);
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const int row = j + r * kWarps;
+                    sum[r] = warp_sum(sum[r]);
+                    if (lane == 0 && (r == 0 || two)) mine[row] = (k0 == part * kFewPiece ? 0.f : mine[row]) + sum[r];
+                }
             }
-            y = y0 + d;
         }
     }
-    if (o < a.dout) static_cast<Out *>(a.Y)[(size_t)t * a.ldy + o] = from_float<Out>(y);
+    __syncthreads();
+    cluster_arrive();
+    cluster_wait();
+    if (i >= 0 && threadIdx.x < a.rank) {
+        float sum = 0.f;
+        for (int c = 0; c < ctas; ++c) sum += load_peer(mine + threadIdx.x, c);
+        u[threadIdx.x] = sum * (a.scale ? a.scale[i] : 1.f);
+    }
+    __syncthreads();
+    cluster_arrive();                          // no CTA leaves while another reads its sums
+    const bool vec = ((uintptr_t)B & 15) == 0;
+#pragma unroll 2
+    for (int o = first; o < a.dout; o += step) {
+        float v = a.Y0 ? to_float(y0[o]) : 0.f;
+        if (i >= 0) {
+            const T *b = B + (size_t)o * a.rank;
+            float d = 0.f;
+            for (int k = 0; k < a.rank; k += 16) {
+                const bool two = k + 8 < a.rank;
+                const uint4 raw[2] = {load8(b, k, a.rank, vec), two ? load8(b, k + 8, a.rank, vec) : make_uint4(0, 0, 0, 0)};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (h && !two) break;
+                    float w[8];
+                    unpack(raw[h], w, T());
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) d = fmaf(w[e], u[k + 8 * h + e], d);
+                }
+            }
+            v += d;
+        }
+        y[o] = from_float<Out>(i == -2 ? __int_as_float(0x7FC00000) : v);
+    }
+    __syncwarp();
+    cluster_wait();
 }
 
 // ---------------------------------------------------------------- more tokens
@@ -693,7 +730,6 @@ __global__ void __launch_bounds__(128) outputs_kernel(AdapterArgs a, int columns
 
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-int few_splits(int din) { return ceil_div(din, kFewPiece); }
 // Splits of the width where there are few tiles of tokens: as many blocks as run at
 // one time, each at least 256 of it.
 int many_splits(int n, int din, int rank) {
@@ -703,11 +739,23 @@ int many_splits(int n, int din, int rank) {
 
 template <class T, class Out>
 cudaError_t launch_few(const AdapterArgs &a, cudaStream_t s) {
-    few_sums_kernel<T><<<dim3(a.n, a.splits), 256, 0, s>>>(a);
-    cudaError_t e = cudaGetLastError();
-    if (e == cudaSuccess) e = launch_pdl(few_outputs_kernel<T, Out>, dim3(a.n, ceil_div(a.dout, 256)), dim3(256), 0, s, a);
-    count_launches(2);
-    return e;
+    // CTAs of a token by its width and outputs alone, so that its sums do not depend on
+    // the batch
+    int ctas = 1;
+    while (ctas < 8 && ctas * kFewPiece < std::max(a.din, a.dout)) ctas *= 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.n * ctas));
+    const bool wide = a.n * ctas <= 152;
+    cfg.blockDim = dim3(wide ? 512 : 256);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ctas;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    count_launches(1);
+    return wide ? cudaLaunchKernelEx(&cfg, few_kernel<T, Out, 512>, a, ctas) : cudaLaunchKernelEx(&cfg, few_kernel<T, Out, 256>, a, ctas);
 }
 
 template <class T, class Out, int KS>
@@ -752,7 +800,7 @@ extern "C" {
 
 size_t jarq_adapters_workspace(int n, int din, int rank, int adapters) {
     if (n < 1 || adapters < 0 || adapters > kMostAdapters || n > kMostTokens || din < 1 || din > kMostWidth || rank < 8 || rank > kMostRank || rank % 8) return 0;
-    if (n <= kFew) return (size_t)few_splits(din) * n * rank * sizeof(float);
+    if (n <= kFew) return 0;
     return (size_t)many_splits(n, din, rank) * n * rank * sizeof(float) + ((size_t)tiles_at_most(n, adapters) * 17 + 16) * sizeof(int);
 }
 
@@ -770,12 +818,13 @@ jarq_status jarq_apply_adapters(const void *X, jarq_dtype dtype, int64_t ldx, co
     if (!usable(X, 2) || !usable(ids, 4) || !usable(Y, ysize) || (Y0 && !usable(Y0, ysize)) || (scale && !usable(scale, 4)))
         return JARQ_ERR_ARG;
     if (adapters && (!usable(A, 2) || !usable(B, 2))) return JARQ_ERR_ARG;
-    if (!usable(workspace, 16) || workspace_bytes < jarq_adapters_workspace(n, din, rank, adapters)) return JARQ_ERR_ARG;
+    const size_t need = jarq_adapters_workspace(n, din, rank, adapters);
+    if (need && (!usable(workspace, 16) || workspace_bytes < need)) return JARQ_ERR_ARG;
     if (const jarq_status late = async_failure()) return late;
     cudaStream_t st = (cudaStream_t)stream;
     const bool few = n <= kFew;
     AdapterArgs a{X, A, B, Y0, Y, scale, ids, static_cast<float *>(workspace), nullptr, ldx, ldy0, ldy, n, din, dout, rank,
-                  adapters, few ? few_splits(din) : many_splits(n, din, rank)};
+                  adapters, few ? 1 : many_splits(n, din, rank)};
     if (!few) a.order = reinterpret_cast<int *>(a.u + (size_t)a.splits * n * rank);
     a.vec_x = is_aligned(X, 16) && is_aligned(A, 16) && din % 8 == 0 && (n == 1 || ldx % 8 == 0);
     auto rows16 = [&](const void *p, int64_t ld) { return is_aligned(p, 16) && (n == 1 || ld * (int64_t)ysize % 16 == 0); };

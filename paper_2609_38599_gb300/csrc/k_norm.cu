@@ -26,6 +26,7 @@ namespace {
 using namespace rows;
 
 constexpr int kMostGradBlocks = 608;       // four for each of 152 SMs
+constexpr int kFewGradRows = 152;          // most rows of the gradient's form for few
 
 // Elements that a thread reads at a time, how often it does so and keeps them, and
 // so the longest row that P threads hold.  (1024 threads have 64 registers each.)
@@ -296,6 +297,8 @@ __global__ void __launch_bounds__(P) norm_grad_kernel(GradArgs a) {
                     dot = fmaf(w[e] * g[e], v[e], dot);
             }
         if (!a.dX) continue;
+        // the launch before this one may be reading dY still, where dX is dY
+        if (!GAIN && turn == 0) tc::pdl_wait();
         // the two rows of `part` take turns: one is written while the other may still be read
         const float along = rstd * rstd * (row_sum<P>(dot, part[turn]) / (float)a.d);
         auto put = [&](int k, const float (&v)[E], const float (&w)[E]) {
@@ -334,19 +337,32 @@ __global__ void __launch_bounds__(P) norm_grad_kernel(GradArgs a) {
     }
 }
 
-// The gains' gradient of rows too long to be held: 32 columns a block, its parts of
-// `rows_each` rows written for gain_join_kernel.
+// The gains' gradient by columns, 32 a block, in parts of `rows_each` rows: of rows too
+// long to be held, with gain_join_kernel after it, and of few rows in one part.
 template <class T>
 __global__ void __launch_bounds__(256) gain_columns_kernel(GradArgs a, int rows_each) {
     __shared__ float part[8][32];
+    tc::pdl_launch_dependents();
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const int64_t k = (int64_t)blockIdx.x * 32 + lane;
     const int64_t r0 = (int64_t)blockIdx.y * rows_each, r1 = min((int64_t)a.n, r0 + rows_each);
     float acc = 0.f;
-    if (k < a.d)
-        for (int64_t r = r0 + w; r < r1; r += 8)
-            acc = fmaf(to_float(static_cast<const T *>(a.dY)[r * a.ldy + k]) * to_float(static_cast<const T *>(a.H)[r * a.ldh + k]),
-                       a.rstd[r], acc);
+    if (k < a.d) {
+        constexpr int kBatch = 8;                  // rows in flight
+        for (int64_t b = r0 + w; b < r1; b += 8 * kBatch) {
+            float y[kBatch], h[kBatch], s[kBatch];
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                const int64_t r = b + 8 * j;
+                const bool in = r < r1;
+                y[j] = in ? to_float(static_cast<const T *>(a.dY)[r * a.ldy + k]) : 0.f;
+                h[j] = in ? to_float(static_cast<const T *>(a.H)[r * a.ldh + k]) : 0.f;
+                s[j] = in ? a.rstd[r] : 0.f;
+            }
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) acc = fmaf(y[j] * h[j], s[j], acc);
+        }
+    }
     part[w][lane] = acc;
     __syncthreads();
     if (w == 0 && k < a.d) {
@@ -661,13 +677,11 @@ cudaError_t launch_norm_t(const NormArgs &a, cudaStream_t s) {
     return launch_norm_p<T, VEC, 1024>(a, s);
 }
 
+// after: gain_columns_kernel is the launch before, whose results it does not need.
 template <class T, bool VEC, int P>
-cudaError_t launch_grad_p(const GradArgs &a, int blocks, cudaStream_t s) {
-    if (a.part)
-        norm_grad_kernel<T, VEC, P, true><<<blocks, P, 0, s>>>(a);
-    else
-        norm_grad_kernel<T, VEC, P, false><<<blocks, P, 0, s>>>(a);
-    return cudaGetLastError();
+cudaError_t launch_grad_p(const GradArgs &a, int blocks, bool after, cudaStream_t s) {
+    return a.part ? launch_k(norm_grad_kernel<T, VEC, P, true>, dim3(blocks), dim3(P), 0, s, false, a)
+                  : launch_k(norm_grad_kernel<T, VEC, P, false>, dim3(blocks), dim3(P), 0, s, after, a);
 }
 
 template <class T, bool VEC>
@@ -675,11 +689,15 @@ cudaError_t launch_grad_t(GradArgs a, float *dgain, cudaStream_t s) {
     int parts = std::min(a.n, kMostGradBlocks);
     float *const part = a.part;
     cudaError_t e = cudaSuccess;
-    if (part && a.d > Shape<T, VEC, 1024>::row) {
-        // rows that no block holds: the columns' sums apart, and first, since dX may be dY
-        const int each = (a.n + std::min(parts, 32) - 1) / std::min(parts, 32);
+    const bool few = a.n <= kFewGradRows, apart = dgain && (few || a.d > Shape<T, VEC, 1024>::row);
+    if (apart) {
+        // few rows, or rows that no block holds: the columns' sums apart, and first, since
+        // dX may be dY
+        const int each = few ? a.n : (a.n + std::min(parts, 32) - 1) / std::min(parts, 32);
         parts = (a.n + each - 1) / each;
-        gain_columns_kernel<T><<<dim3((unsigned)(((int64_t)a.d + 31) / 32), parts), 256, 0, s>>>(a, each);
+        GradArgs by = a;
+        if (few) by.part = dgain;
+        gain_columns_kernel<T><<<dim3((unsigned)(((int64_t)a.d + 31) / 32), parts), 256, 0, s>>>(by, each);
         count_launches(1);
         e = cudaGetLastError();
         a.part = nullptr;
@@ -690,21 +708,21 @@ cudaError_t launch_grad_t(GradArgs a, float *dgain, cudaStream_t s) {
         if (VEC) {
             if (!with_threads<T>(a.d, [&](auto p, auto held) {
                     constexpr int P = p.value, HELD = held.value;
-                    e = a.n <= num_sms() ? launch_grad_p<T, VEC, P>(a, blocks, s)
+                    e = a.n <= kFewGradRows ? launch_grad_p<T, VEC, P>(a, blocks, apart, s)
                         : a.dH           ? launch_grad_rows<T, P, HELD, true>(a, &blocks, s)
                                          : launch_grad_rows<T, P, HELD, false>(a, &blocks, s);
                 }))
-                e = launch_grad_p<T, VEC, 1024>(a, blocks, s);
+                e = launch_grad_p<T, VEC, 1024>(a, blocks, apart, s);
         } else if (a.d <= Shape<T, VEC, 128>::row) {
-            e = launch_grad_p<T, VEC, 128>(a, blocks, s);
+            e = launch_grad_p<T, VEC, 128>(a, blocks, apart, s);
         } else if (a.d <= Shape<T, VEC, 512>::row) {
-            e = launch_grad_p<T, VEC, 512>(a, blocks, s);
+            e = launch_grad_p<T, VEC, 512>(a, blocks, apart, s);
         } else {
-            e = launch_grad_p<T, VEC, 1024>(a, blocks, s);
+            e = launch_grad_p<T, VEC, 1024>(a, blocks, apart, s);
         }
         if (a.part) parts = blocks;
     }
-    if (e == cudaSuccess && dgain) {
+    if (e == cudaSuccess && dgain && !few) {
         e = launch_pdl(gain_join_kernel, dim3((unsigned)(((int64_t)a.d + 31) / 32)), dim3(1024), 0, s, (const float *)part, parts,
                        a.d, dgain);
         count_launches(1);
@@ -766,7 +784,7 @@ jarq_status jarq_rms_norm(const void *X, jarq_dtype dtype, int n, int d, int64_t
 }
 
 size_t jarq_rms_norm_grad_workspace(int n, int d) {
-    if (n < 0 || d < 1) return 0;
+    if (n <= kFewGradRows || d < 1) return 0;
     return (size_t)std::min(n, kMostGradBlocks) * d * sizeof(float);
 }
 
@@ -790,9 +808,10 @@ jarq_status jarq_rms_norm_grad(const void *H, jarq_dtype dtype, int n, int d, in
     if (!usable(H, size) || !usable(dY, size) || !usable(rstd, 4) || !usable_or_null(dH, size) || !usable_or_null(dX, size) ||
         !usable_or_null(dgain, 4) || !usable_or_null(gain, gain ? size_of(gain_dtype) : 1))
         return JARQ_ERR_ARG;
-    if (dgain && (!usable(workspace, 16) || workspace_bytes < jarq_rms_norm_grad_workspace(n, d))) return JARQ_ERR_ARG;
+    const size_t need = dgain ? jarq_rms_norm_grad_workspace(n, d) : 0;
+    if (need && (!usable(workspace, 16) || workspace_bytes < need)) return JARQ_ERR_ARG;
     if (const jarq_status late = async_failure()) return late;
-    const GradArgs a{H, gain, dY, dH, dX, rstd, dgain ? static_cast<float *>(workspace) : nullptr, ldh, ldy, lds, ldx, n, d,
+    const GradArgs a{H, gain, dY, dH, dX, rstd, need ? static_cast<float *>(workspace) : nullptr, ldh, ldy, lds, ldx, n, d,
                      gain_dtype != dtype};
     const bool vec = vector(H, ldh, n, size) && vector(dY, ldy, n, size) && vector(dH, lds, n, size) &&
                      vector(dX, ldx, n, size) && vector(gain, 0, 1, 1);

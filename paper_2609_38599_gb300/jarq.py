@@ -798,8 +798,10 @@ def rms_norm_grad(h, gain, rstd, dy, dh=None, rows: bool = True, gains: bool = T
     if gains:
         dgain = T.empty((d,), dtype=T.f32, device=dev)
         size = _lib.jarq_rms_norm_grad_workspace(n, d)
-        buffer = T.empty((size,), dtype=T.u8, device=dev)
-        gp, work = dgain.data_ptr(), buffer.data_ptr()
+        if size:
+            buffer = T.empty((size,), dtype=T.u8, device=dev)
+            work = buffer.data_ptr()
+        gp = dgain.data_ptr()
     status = _lib.jarq_rms_norm_grad(p, code, n, d, ldh, g, gcode, r, y, ldy, s, lds, x, ldx, gp, work, size,
                                      T.stream(h.get_device()))
     if status != JARQ_OK:
@@ -887,9 +889,9 @@ def apply_adapters(X, A, B, ids, scale=None, base=None, dtype: str = None, out=N
     else:
         y, ldy = _like(out, "out", n, dout, ydt)
     size = _lib.jarq_adapters_workspace(n, din, rank, m)
-    work = T.empty((size,), dtype=T.u8, device=dev)
+    buffer = T.empty((size,), dtype=T.u8, device=dev) if size else None
     status = _lib.jarq_apply_adapters(x, code, ldx, a, b, s, m, rank, i, n, din, dout, y0, ldy0, y, ldy,
-                                      T.floats[ydt], work.data_ptr(), size, T.stream(X.get_device()))
+                                      T.floats[ydt], buffer.data_ptr() if size else None, size, T.stream(X.get_device()))
     if status != JARQ_OK:
         raise JarqError(status, "jarq_apply_adapters")
     return out

@@ -68,7 +68,8 @@ def test_sizes_are_checked_first(jarq):  # noqa: F811
 def test_workspaces_of_sizes_that_are_refused(jarq):  # noqa: F811
     L = jarq.library()
     assert L.jarq_rms_norm_grad_workspace(-1, 64) == 0 and L.jarq_rms_norm_grad_workspace(4, 0) == 0
-    assert L.jarq_rms_norm_grad_workspace(4, 64) == 4 * 64 * 4 and L.jarq_rms_norm_grad_workspace(10 ** 6, 64) == 608 * 64 * 4
+    assert L.jarq_rms_norm_grad_workspace(200, 64) == 200 * 64 * 4 and L.jarq_rms_norm_grad_workspace(10 ** 6, 64) == 608 * 64 * 4
+    assert L.jarq_rms_norm_grad_workspace(152, 64) == 0 and L.jarq_adapters_workspace(64, 64, 16, 1) == 0 < L.jarq_adapters_workspace(65, 64, 16, 1)
     assert L.jarq_cross_entropy_workspace(0, 64, 100, 1) == 0 and L.jarq_cross_entropy_workspace(2 ** 22 + 1, 64, 100, 1) == 0
     assert L.jarq_adapters_workspace(0, 64, 16, 1) == 0 and L.jarq_adapters_workspace(8, 64, 20, 1) == 0
     # room for copies of rows that are not on 16-byte boundaries
@@ -142,13 +143,13 @@ def test_pointers_and_workspaces_are_checked(dev):  # noqa: F811
     odd = lambda p, k: ctypes.c_void_p(p.value + k)
     size = L.jarq_cross_entropy_workspace(8, 64, 100, 1)
     gsize = L.jarq_cross_entropy_grad_workspace(8, 64, 100, 1, 1, 1)
-    asize = L.jarq_adapters_workspace(8, 64, 16, 2)
+    asize = L.jarq_adapters_workspace(100, 64, 16, 2)
     z = ctypes.c_size_t
     made = [
         lambda X=x, T=tok, F=f, w=work, k=size: L.jarq_cross_entropy(X, F16, 8, 64, i64(64), W, 100, i64(64), T, F, f, w, z(k), s),
         lambda X=x, T=tok, F=f, w=work, k=gsize: L.jarq_cross_entropy_grad(X, F16, 8, 64, i64(64), W, 100, i64(64), T, F, f, x, i64(64), W, i64(64), w, z(k), s),
-        lambda X=x, T=tok, F=f, w=work, k=asize: L.jarq_apply_adapters(X, F16, i64(64), W, W, F, 2, 16, T, 8, 64, 32, x, i64(32), x, i64(32), F16, w, z(k), s),
-        lambda X=x, T=tok, F=f, w=work, k=8 * 64 * 4: L.jarq_rms_norm_grad(X, F16, 8, 64, i64(64), None, F16, F, x, i64(64), None, i64(64), W, i64(64), T, w, z(k), s),
+        lambda X=x, T=tok, F=f, w=work, k=asize: L.jarq_apply_adapters(X, F16, i64(64), W, W, F, 2, 16, T, 100, 64, 32, x, i64(32), x, i64(32), F16, w, z(k), s),
+        lambda X=x, T=tok, F=f, w=work, k=200 * 64 * 4: L.jarq_rms_norm_grad(X, F16, 200, 64, i64(64), None, F16, F, x, i64(64), None, i64(64), W, i64(64), T, w, z(k), s),
     ]
     for call in made:
         assert call() == 0
@@ -157,7 +158,7 @@ def test_pointers_and_workspaces_are_checked(dev):  # noqa: F811
         for wrong in (dict(X=host), dict(X=odd(x, 1)), dict(X=None), dict(T=host), dict(T=odd(tok, 2)), dict(F=odd(f, 2)),
                       dict(w=None), dict(w=odd(work, 8)), dict(w=host)):
             assert call(**wrong) == ARG, (i, wrong)
-        assert call(k=(size, gsize, asize, 8 * 64 * 4)[i] - 1) == ARG, i
+        assert call(k=(size, gsize, asize, 200 * 64 * 4)[i] - 1) == ARG, i
     assert len(dev.log()) == before
 
 
