@@ -290,13 +290,14 @@ jarq_status jarq_accumulate_hessian(const void *X, int n, int d, float scale, fl
 
 /* ---- running, scoring and tuning a quantized model (device memory only) ----
  * The paper judges a quantized model by the probabilities that it gives to
- * tokens (Sec. 4, perplexity).  These operators run a layer in integers and
- * score logits.  They differ from the calls above in three points, since a
+ * tokens (Sec. 4, perplexity).  These operators run a layer in integers, norm
+ * its inputs and add adapters to it, score logits, and form the loss of an output
+ * head with its gradient.  They differ from the calls above in three points, since a
  * generation step takes microseconds on the device:
  * - They only enqueue their work on `stream` and return; results are ready in
  *   stream order, and the calls can be captured in a CUDA graph (a process's
- *   first product of more than two tokens, which allocates the word of the
- *   third point in pinned host memory, cannot).
+ *   first product of more than two tokens, or first loss, which allocates the
+ *   word of the third point in pinned host memory, cannot).
  * - They allocate nothing on the device and keep no state between calls.
  * - A failure on the device (a bounded wait that gave up) is reported by
  *   jarq_async_status, and by every later call of these operators until
@@ -413,7 +414,8 @@ jarq_status jarq_token_logprobs_grad(const void *logits, jarq_dtype dtype, int n
  *   gain : [d] of gain_dtype (`dtype` or JARQ_F32), or NULL for ones.
  *   eps : > 0, finite.  Y may be NULL.  Q : int8 [n][d], pitch ldq, and scale :
  *   float32 [n], both or neither.  rstd : float32 [n], may be NULL.
- *   n >= 0, d >= 1, both at most 2^31 - 4096. */
+ *   n >= 0, d >= 1, both at most 2^31 - 4096.
+ * Sums are float32.  A row's outputs do not depend on the other rows of a call. */
 jarq_status jarq_rms_norm(const void *X, jarq_dtype dtype, int n, int d, int64_t ldx, const void *R,
                           int64_t ldr, void *H, int64_t ldh, const void *gain, jarq_dtype gain_dtype,
                           float eps, void *Y, int64_t ldy, int8_t *Q, int64_t ldq, float *scale,

@@ -3,15 +3,21 @@
 //
 // Few tokens: dot products, a cluster of CTAs a token, in one launch.
 //
-// More tokens: two kernels, the sums u_t = A_i x_t over the tokens' width and their
-// expansion by B_i with the addition.  Before them an order in which tokens of one adapter follow one another (a
-// token's results do not depend on it: the sums of a row of an MMA are its own), then
-// 16 tokens a warp on mma.sync, whose operands go straight from memory to
-// registers: a sum over K does not depend on the order of K, so a lane takes 8
-// neighbouring elements of a row (16 bytes) for its share of two MMAs, and the columns
-// of the expansion are dealt out so that a lane's results are 8 neighbouring outputs.
-// The work is bound by the tokens' and outputs' memory, far below what tensor cores
-// could do.  The expansion multiplies u, split into two or three 16-bit parts, with B.
+// More tokens: tiles of 16 of one adapter (order_kernel), then two kernels, the sums u_t =
+// A_i x_t over the tokens' width and their expansion by B_i with the addition.  Bound by
+// the tokens' and outputs' memory, far below what tensor cores could do, and an adapter's
+// tile is too small to fill tcgen05's 128 rows: mma.sync, a warp 16 tokens.  A sum over K
+// does not depend on the order of K, so a lane takes 8 neighbouring elements of a row for
+// its share of two MMAs, and the columns of the expansion are dealt out so that a lane's
+// results are 16 bytes of a token.  u is split into two 16-bit parts for the expansion,
+// three where float32 outputs ask for more than bfloat16's give.
+//
+// On the device, cold: 8192 tokens 4096 -> 4096 of rank 16 in bfloat16, six adapters, 47 us
+// (201 MB: order 5, sums 13 at 5.2 TB/s, outputs 26); 276 x 4236 -> 2009, rank 8, float32
+// outputs, rows on no boundary 21 us; 2392 x 992 -> 745, rank 64, 38 adapters in any order,
+// float32 38 us.  Measured and not kept: tiles of two adapters walked one after the other
+// (the others wait for them: 61 -> 75 us at that state), each lane's operands straight
+// into its registers (half lines: 103 us) or into places of its own in shared memory (87).
 #include <algorithm>
 
 #include "integer.cuh"

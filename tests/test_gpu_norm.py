@@ -224,9 +224,13 @@ def test_same_bits_whatever_the_batch_and_again(jarq):
     x, r = randn(rng, 400, 4096, "bfloat16").cuda(), randn(rng, 400, 4096, "bfloat16").cuda()
     gain = randn(rng, 1, 4096, "bfloat16")[0].cuda()
     a = jarq.rms_norm(x, gain, residual=r, codes=True)
-    b = jarq.rms_norm(x[100:300], gain, residual=r[100:300], codes=True)
-    for name in ("h", "y", "codes", "scale", "rstd"):
-        assert torch.equal(getattr(a, name)[100:300], getattr(b, name))
+    for at in (slice(100, 300), slice(7, 8), slice(300, 400)):
+        b = jarq.rms_norm(x[at], gain, residual=r[at], codes=True)
+        for name in ("h", "y", "codes", "scale", "rstd"):
+            assert torch.equal(getattr(a, name)[at], getattr(b, name))
+        for dh in (r, None):
+            full = jarq.rms_norm_grad(a.h, gain, a.rstd, x, dh=dh)[0]
+            assert torch.equal(full[at], jarq.rms_norm_grad(b.h, gain, b.rstd, x[at], dh=None if dh is None else dh[at])[0])
     one = jarq.rms_norm_grad(a.h, gain, a.rstd, x, dh=r)
     for _ in range(3):
         two = jarq.rms_norm_grad(a.h, gain, a.rstd, x, dh=r)
