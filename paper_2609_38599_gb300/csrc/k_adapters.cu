@@ -12,12 +12,13 @@
 // results are 16 bytes of a token.  u is split into two 16-bit parts for the expansion,
 // three where float32 outputs ask for more than bfloat16's give.
 //
-// On the device, cold: 8192 tokens 4096 -> 4096 of rank 16 in bfloat16, six adapters, 47 us
-// (201 MB: order 5, sums 13 at 5.2 TB/s, outputs 26); 276 x 4236 -> 2009, rank 8, float32
-// outputs, rows on no boundary 21 us; 2392 x 992 -> 745, rank 64, 38 adapters in any order,
-// float32 38 us.  Measured and not kept: tiles of two adapters walked one after the other
-// (the others wait for them: 61 -> 75 us at that state), each lane's operands straight
-// into its registers (half lines: 103 us) or into places of its own in shared memory (87).
+// On the device, cold: 8192 tokens 4096 -> 4096 of rank 16 in bfloat16, six adapters, 47
+// to 49 us (201 MB; each launch alone under a profiler: order 9, sums 15 at 4.4 TB/s, outputs
+// 26 at 5.2); 276 x 4236 -> 2009, rank 8, float32 outputs, rows on no boundary 21 us; 2392 x
+// 992 -> 745, rank 64, 38 adapters in any order, float32 38 us.  States on the way, which
+// differ in more than one thing each: operands straight into a lane's registers 74 to 103
+// us, into places of each lane's own in shared memory 87, tiles of one adapter instead
+// of two walked one after the other (the other blocks had ended) 61, whole lines 53.
 #include <algorithm>
 
 #include "integer.cuh"
@@ -93,8 +94,8 @@ __device__ __forceinline__ int adapter_of(const AdapterArgs &a, int t) {
 // The CTAs of a cluster share a token: pieces of its width, then, with the sums of all
 // of them, pieces of its outputs.  Bound by latencies (first loads, cluster's join, B's
 // loads) and, outside a graph, by the host: one token 4096 -> 11008 of rank 16 takes 5.9
-// us on the device, a call 17 us.  In two launches with the sums in memory between them
-// it took 4.6 and 23.  48 tokens 11008 -> 4096 8.1 us, 8.4 in two.
+// us on the device, a call 20 us.  In two launches with the sums in memory between them
+// it took 4.6 and 26.  48 tokens 11008 -> 4096 8.1 us, 8.4 in two.
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ float load_peer(const float *p, uint32_t rank) {

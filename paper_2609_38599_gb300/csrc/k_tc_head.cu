@@ -21,7 +21,7 @@
 //                                          pipes 93 to 97 % active
 //   1000 x 1344 -> 50001 float16           78, 84 and 80 us for logits, D and dX (1.7 PFLOP/s:
 //                                          21 chunks of K a tile, the last wave's tail)
-//   48 x 2048 -> 50001 float16             39 us (205 MB); one row, 7976 -> 86781 226 us (6.1 TB/s)
+//   48 x 2048 -> 50001 float16             40 us (205 MB); one row, 7976 -> 86781 226 us (6.1 TB/s)
 // Rows past the tokens: their boxes, filled with zeros by TMA, held the one row's call to
 // 383 us.  D's exponentials as subtract, multiply, compare for masks and token, select, an
 // element each: 113 us for 84.  Measured and not kept: sixteen drain warps with stages as
