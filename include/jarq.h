@@ -465,7 +465,8 @@ jarq_status jarq_cross_entropy(const void *X, jarq_dtype dtype, int n, int d, in
  * hidden states and the head: with D_rv = g_loss[r] (exp(l_rv - lse[r]) - [v =
  * tokens[r]]),  dX = D W  and  dW = D^T X.  The logits are formed once more and D a
  * piece of the vocabulary at a time (of up to 512 MB, at least 4096 tokens), rounded
- * to 16 bits with full relative precision; sums are float32.
+ * to 16 bits with full relative precision, and what that takes from the tokens' own
+ * entries is added to the sums, which are float32.
  *   X to tokens : as there.  lse : its result.  g_loss : float32 [n].
  *   dX : [n][d], dW : [vocab][d] of `dtype`, pitches lddx, lddw, overwritten (dW with
  *   zeros for n = 0); one of them may be NULL.

@@ -35,6 +35,14 @@ struct ProductArgs {
     int pitch;
     bool add, last;             // to what slab holds; into out
     const int *top;             // kHead of float16: exponent of the rows' scale
+    float *lost;                // [rows of X] what rounding took from D of a row's token, scaled as D is
+    // kHidden, kHead: that much more, of the tokens `first` .. `first` + `window` - 1
+    int window, count;          // count: rows of X
+    const uint16_t *w;          // kHidden: W from token `first` on
+    int64_t ldw;
+    const int *slot;            // kHead: a row of `rest` for each token; holds where tokens[slot] is the token
+    const float *rest;          // kHead: [count][rest_pitch]
+    int rest_pitch;
     int *failed;
 };
 

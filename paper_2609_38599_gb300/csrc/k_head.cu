@@ -132,6 +132,55 @@ __global__ void __launch_bounds__(1024) top_exponent_kernel(const int64_t *token
     }
 }
 
+// What dW lacks of D's entries of the tokens first .. first + window - 1 that occur: for
+// each the sum of lost_t x_t over its rows t, in their order, which the first of them
+// adds up. No atomics: the same bits every time. x: rows as dW's product reads them.
+// A row's block looks through the tokens before it, and a first one through all: n^2
+// tokens at most, which stay in L2, beside n vocab d products.
+template <class T>
+__global__ void __launch_bounds__(256) lost_rows_kernel(const int64_t *tokens, const float *lost, const T *x, int n, int d, int pitch,
+                                                        int first, int window, int *slot, float *rest) {
+    __shared__ uint32_t found[8];
+    tc::pdl_launch_dependents();
+    tc::pdl_wait();
+    const int t = blockIdx.x;
+    const int64_t tok = tokens[t];
+    if (tok < first || tok >= (int64_t)first + window) return;
+    for (int i = 0; i < t; i += 1024) {
+        bool same = false;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int r = i + 256 * j + threadIdx.x;
+            same |= r < t && tokens[r] == tok;
+        }
+        if (__syncthreads_or(same)) return;
+    }
+    if (threadIdx.x == 0) slot[tok - first] = t;
+    float *sum = rest + (size_t)t * pitch;
+    for (int i = t; i < n; i += 256) {
+        const int r = i + threadIdx.x;
+        const uint32_t mine = __ballot_sync(0xffffffffu, r < n && tokens[r] == tok);
+        if ((threadIdx.x & 31) == 0) found[threadIdx.x >> 5] = mine;
+        __syncthreads();
+        for (int w = 0; w < 8; ++w)
+            for (uint32_t left = found[w]; left; left &= left - 1) {
+                const int row = i + 32 * w + __ffs(left) - 1;
+                const float by = lost[row];
+                // a thread's columns are its own from row to row
+                for (int k = 8 * threadIdx.x; k < d; k += 8 * 256) {
+                    float v[8];
+                    unpack(*reinterpret_cast<const uint4 *>(x + (size_t)row * pitch + k), v, T());
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float y = by != 0.f && fabsf(v[e]) < INFINITY ? by * v[e] : 0.f;
+                        sum[k + e] = row == t ? y : sum[k + e] + y;
+                    }
+                }
+            }
+        __syncthreads();
+    }
+}
+
 // The splits' sums, added in their order, scaled and rounded.
 template <class T>
 __global__ void __launch_bounds__(256) sum_splits_kernel(const float *slab, int splits, int n, int d, int pitch, T *out,
@@ -201,7 +250,7 @@ struct Plan {
     int pitch, pieces, width;            // of copies and sums; pieces of the vocabulary
     int split_x, split_w;
     bool slab_x, slab_w;
-    size_t copy_x, copy_w, parts, target, weighed, top, D, sums_x, sums_w, bytes;
+    size_t copy_x, copy_w, parts, target, weighed, top, D, sums_x, sums_w, lost, slot, rest, bytes;
 
     // the loss
     Plan(int n, int d, int vocab, bool aligned) : pitch(round_up(d, 8)) {
@@ -227,6 +276,9 @@ struct Plan {
         sums_w = l.take(slab_w ? (size_t)split_w * width * pitch * sizeof(float) : 0);
         weighed = l.take(head ? (size_t)n * pitch * 2 : 0);
         top = l.take(sizeof(int));
+        lost = l.take((size_t)n * sizeof(float));
+        slot = l.take(head ? (size_t)width * sizeof(int) : 0);
+        rest = l.take(head ? (size_t)n * pitch * sizeof(float) : 0);
         copies(l, n, vocab, aligned);
         bytes = l.bytes;
     }
@@ -283,6 +335,12 @@ struct Call {
             using T = decltype(type);
             return run(copy_rows_kernel<T, true>, ceil_div((int64_t)n * (pitch / 8), 256), 256, static_cast<const T *>(x), ld, n, d,
                        reinterpret_cast<T *>(out), pitch, tokens, g, top);
+        });
+    }
+    cudaError_t lost_rows(const float *lost, const char *x, int pitch, int first, int window, int *slot, float *rest) {
+        return typed([&](auto type) {
+            using T = decltype(type);
+            return run(lost_rows_kernel<T>, n, 256, tokens, lost, reinterpret_cast<const T *>(x), n, d, pitch, first, window, slot, rest);
         });
     }
     cudaError_t sum_splits(const float *slab, int splits, int rows, int pitch, void *out, int64_t ld, const float *g,
@@ -362,6 +420,8 @@ cudaError_t run_grad(Call &c, const void *X, int64_t ldx, const void *W, int64_t
     float *sums_x = p.slab_x ? reinterpret_cast<float *>(c.work + p.sums_x) : nullptr;
     float *sums_w = p.slab_w ? reinterpret_cast<float *>(c.work + p.sums_w) : nullptr;
     int sums = 1;                                    // splits of dX
+    float *lost = reinterpret_cast<float *>(c.work + p.lost), *rest = reinterpret_cast<float *>(c.work + p.rest);
+    int *slot = reinterpret_cast<int *>(c.work + p.slot);
     for (int i = 0; i < p.pieces; ++i) {
         const int v0 = i * p.width, width = std::min(p.width, c.vocab - v0);
         {
@@ -370,6 +430,7 @@ cudaError_t run_grad(Call &c, const void *X, int64_t ldx, const void *W, int64_t
             TRY(tensor_map(&mw, w.row(v0), width, c.d, w.ld, a.cols / 2));
             a.lse = lse, a.g = g, a.first = v0;
             a.out = D, a.ldo = p.width;
+            a.lost = lost;
             TRY(c.product(kLogits, mx, mw, a));
         }
         if (dX) {
@@ -381,6 +442,8 @@ cudaError_t run_grad(Call &c, const void *X, int64_t ldx, const void *W, int64_t
             a.out = dX, a.ldo = lddx;
             a.slab = sums_x, a.pitch = p.pitch;
             a.add = i > 0;
+            a.lost = lost, a.first = v0, a.window = width;
+            a.w = reinterpret_cast<const uint16_t *>(w.row(v0)), a.ldw = w.ld;
             a.last = sums == 1 && i + 1 == p.pieces;
             TRY(c.product(kHidden, md, mb, a));
         }
@@ -393,6 +456,9 @@ cudaError_t run_grad(Call &c, const void *X, int64_t ldx, const void *W, int64_t
             a.slab = sums_w, a.pitch = p.pitch;
             a.last = !p.slab_w;
             a.top = top;
+            a.first = v0, a.count = c.n;
+            a.slot = slot, a.rest = rest, a.rest_pitch = p.pitch;
+            TRY(c.lost_rows(lost, c.work + p.weighed, p.pitch, v0, width, slot, rest));
             TRY(c.product(kHead, md, mb, a));
             if (p.slab_w) TRY(c.sum_splits(sums_w, a.splits, width, p.pitch, out, lddw, nullptr, top));
         }

@@ -313,3 +313,44 @@ def test_two_streams_at_once(jarq):
 def test_a_wait_that_gives_up_is_reported(jarq):
     assert jarq.selftest_stalled_kernel("cross_entropy") == jarq.JARQ_ERR_TIMEOUT
     assert jarq.async_status() == jarq.JARQ_OK
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,d,vocab,px", [(1, 64, 2000, 64), (60, 72, 4000, 72), (60, 77, 4000, 80), (700, 264, 9000, 264),
+                                          (8300, 40, 40000, 40)])
+def test_a_tokens_own_entry_is_not_rounded(jarq, dtype, n, d, vocab, px):
+    """Equal weights whose mantissa lies between two of the type's: rounding the entry of
+    a row's own token, about -g, would move the whole row the same way."""
+    rng = np.random.default_rng(n + d)
+    ulp = 2.0 * HALF[dtype]
+    X = randn(rng, n, d, dtype)
+    W = torch.zeros(vocab, d).to(X.dtype)              # only tokens that occur hold anything
+    known = torch.as_tensor(rng.choice(vocab, 16, replace=False))
+    W[known] = randn(rng, 16, d, dtype, 1 / np.sqrt(d))
+    tok = known[torch.as_tensor(rng.integers(0, 16, n))]
+    if n > 3:
+        tok[1::5] = -1
+    g = torch.full((n,), 2.0 ** -6 * (1 + 0.45 * ulp))
+    x, w = device(X, px, 0), device(W, px, 0)
+    t = tok.cuda()
+    loss, lse = jarq.cross_entropy(x, w, t)
+    dX, dW = jarq.cross_entropy_grad(x, w, t, lse, g.cuda())
+    xn, wn, gn, tn = f64(X), f64(W), f64(g), tok.numpy()
+    logits = xn @ wn.T
+    D = O.logit_gradient(xn, wn, tn, f64(lse), gn)
+    p = np.where((tn >= 0)[:, None], np.exp(logits - f64(lse)[:, None]), 0.0)
+    rel = logit_error(xn, wn)[:, None] + 4 * U * (np.abs(logits) + np.abs(f64(lse))[:, None] + 2)
+    rounded = np.abs(D)
+    rows = np.flatnonzero(tn >= 0)
+    rounded[rows, tn[rows]] = 0                         # these are put right
+    errD = gn[:, None] * (p * rel + FLOOR[dtype]) + rounded * HALF[dtype] + np.abs(D) * 4 * U
+    tiny = float(torch.finfo(X.dtype).tiny) * HALF[dtype]
+    # what is put back: at most HALF |D|, its products and sums in float32
+    back = HALF[dtype] * (n + 2) * U
+    for got, want, err, size in ((dX, D @ wn, errD @ np.abs(wn), np.abs(D) @ np.abs(wn)), (dW, D.T @ xn, errD.T @ np.abs(xn), np.abs(D).T @ np.abs(xn))):
+        k = vocab if got is dX else n
+        near(got, want, 1.01 * (err + (2 * sum_error(k) + back) * size + HALF[dtype] * np.abs(want)) + tiny)
+    again = jarq.cross_entropy_grad(x, w, t, lse, g.cuda())
+    assert torch.equal(again[0], dX) and torch.equal(again[1], dW)
+    assert torch.equal(jarq.cross_entropy_grad(x, w, t, lse, g.cuda(), hidden=False)[1], dW)
+    assert jarq.async_status() == jarq.JARQ_OK
