@@ -36,12 +36,12 @@ struct ProductArgs {
     bool add, last;             // to what slab holds; into out
     const int *top;             // kHead of float16: exponent of the rows' scale
     float *lost;                // [rows of X] what rounding took from D of a row's token, scaled as D is
-    // kHidden, kHead: that much more, of the tokens `first` .. `first` + `window` - 1
-    int window, count;          // count: rows of X
-    const uint16_t *w;          // kHidden: W from token `first` on
+    // kHidden, kHead: that goes into the result; `first` as above
+    int window;                 // kHidden: tokens of the piece
+    const uint16_t *w;          // kHidden: W from token `first` on; kHead: rows of X as the product reads them
     int64_t ldw;
-    const int *slot;            // kHead: a row of `rest` for each token; holds where tokens[slot] is the token
-    const float *rest;          // kHead: [count][rest_pitch]
+    const int2 *tally;          // kHead: a token's first row and number of rows, from token `first` on
+    const float *rest;          // kHead: of a token with several rows, at its first: what goes in
     int rest_pitch;
     int *failed;
 };

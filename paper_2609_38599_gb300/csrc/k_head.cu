@@ -7,10 +7,10 @@
 //
 // D is formed for a piece of the vocabulary (512 MB), which both products then read: dX
 // is added up over the pieces in float32, dW's rows belong to one piece.  A training
-// step's loss and gradients of 8192 x 4096 -> 32000 in bfloat16 take 4.8 to 4.9 ms on the
-// device: 8 n V d operations at 1.75 to 1.8 PFLOP/s.  6 n V d would do if the loss kept its
+// step's loss and gradients of 8192 x 4096 -> 32000 in bfloat16 take 5.0 ms on the device: 8
+// n V d operations at 1.7 PFLOP/s.  6 n V d would do if the loss kept its
 // logits.  The copy of X without its ignored rows, for dW, takes 23 us of that, the
-// join 11.
+// join 9 to 11, what rounding took from dW (below) 47.
 #include <algorithm>
 
 #include "head.cuh"
@@ -78,22 +78,29 @@ __global__ void __launch_bounds__(256) loss_join_kernel(const float2 *parts, int
     }
 }
 
+// A byte of a token, to look for others of it.
+__device__ __forceinline__ uint32_t mark_of(int64_t tok) { return (uint32_t)tok * 0x9E3779B1u >> 24; }
+
 // 16-bit rows of any alignment to rows on 16-byte boundaries, pitch a multiple of 8.
 // WEIGH: those of ignored tokens become zero, whatever they hold, and of float16
-// row r is multiplied by 2^(e_r - top), as head.cuh has D's rows.
+// row r is multiplied by 2^(e_r - top), as head.cuh has D's rows; and each row's token
+// gets its mark, and every token's tally begins.
 template <class T, bool WEIGH>
 __global__ void __launch_bounds__(256) copy_rows_kernel(const T *x, int64_t ld, int n, int d, T *out, int pitch,
-                                                        const int64_t *tokens, const float *g, const int *top) {
+                                                        const int64_t *tokens, const float *g, const int *top, uint8_t *marks, int2 *tally, int vocab) {
     const int per = pitch / 8;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int64_t r = i / per;
     const int k = (int)(i % per) * 8;
     tc::pdl_launch_dependents();
     tc::pdl_wait();
+    if constexpr (WEIGH)
+        for (int64_t v = i; v < vocab; v += (int64_t)gridDim.x * 256) tally[v] = make_int2(0x7FFFFFFF, 0);
     if (r >= n) return;
     const T *p = x + r * ld + k;
     uint4 raw = make_uint4(0, 0, 0, 0);
     const bool live = !WEIGH || tokens[r] >= 0;
+    if (WEIGH && k == 0) marks[r] = (uint8_t)mark_of(tokens[r]);
     if (live) {
         if (((uintptr_t)p & 15) == 0 && k + 8 <= d) {
             raw = *reinterpret_cast<const uint4 *>(p);
@@ -132,51 +139,134 @@ __global__ void __launch_bounds__(1024) top_exponent_kernel(const int64_t *token
     }
 }
 
-// What dW lacks of D's entries of the tokens first .. first + window - 1 that occur: for
-// each the sum of lost_t x_t over its rows t, in their order, which the first of them
-// adds up. No atomics: the same bits every time. x: rows as dW's product reads them.
-// A row's block looks through the tokens before it, and a first one through all: n^2
-// tokens at most, which stay in L2, beside n vocab d products.
-template <class T>
-__global__ void __launch_bounds__(256) lost_rows_kernel(const int64_t *tokens, const float *lost, const T *x, int n, int d, int pitch,
-                                                        int first, int window, int *slot, float *rest) {
-    __shared__ uint32_t found[8];
+// Every token's first row and number of rows, from {INT_MAX, 0}: whole numbers, the same
+// in any order.
+__global__ void __launch_bounds__(256) tally_kernel(const int64_t *tokens, int n, int vocab, int2 *tally) {
+    const int r = blockIdx.x * 256 + threadIdx.x;
     tc::pdl_launch_dependents();
     tc::pdl_wait();
-    const int t = blockIdx.x;
-    const int64_t tok = tokens[t];
-    if (tok < first || tok >= (int64_t)first + window) return;
-    for (int i = 0; i < t; i += 1024) {
-        bool same = false;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int r = i + 256 * j + threadIdx.x;
-            same |= r < t && tokens[r] == tok;
-        }
-        if (__syncthreads_or(same)) return;
+    if (r >= n) return;
+    const int64_t tok = tokens[r];
+    if (tok < 0 || tok >= vocab) return;
+    atomicMin(&tally[tok].x, r);
+    atomicAdd(&tally[tok].y, 1);
+}
+
+// What dW lacks of D's entries of the tokens first .. first + window - 1 that have several
+// rows (of one row, dW's product takes it from there): for each the sum of lost_t x_t
+// over its rows t, in their order, at its first row.  No atomics: the same bits every time.
+// x: rows as dW's product reads them.
+// A block, of 8 rows and 512 columns, takes those that are a token's first in turn: it looks
+// through the rows from there by a byte of each, 4096 at a time, until it has all of the
+// token's, and four groups of its threads add them up, every fourth row each.
+// 8192 rows of 4096 with any of 32000 tokens 44 us.  Such a gradient without this and with
+// it: 3.30 and 3.39 ms, its most frequent token in 610 rows 3.5 to 3.7 and 3.7 to 3.8, one
+// token in all rows 3.3 and 4.4 (they go through 8 blocks), 100000 x 512 -> 32000, in eight pieces, 7.2 and 8.2.
+// On the way: every row's block through all tokens, 8 bytes each, sums in memory 137 us
+// (one token in all rows 13.4 ms); eight tokens a thread at a time 77; a byte each but
+// every row's block and sixteen rows in flight 175 (two blocks an SM); a block a row
+// and 2048 columns 27, but one token in all rows 6.2 ms.
+template <class T>
+__global__ void __launch_bounds__(256) lost_rows_kernel(const int64_t *tokens, const int2 *tally, const uint8_t *marks,
+                                                        const float *lost, const T *x, int n, int d, int pitch, int first,
+                                                        int window, float *rest) {
+    constexpr int kSpan = 4096, kBatch = 8, kGroups = 4;
+    __shared__ int row_of[kSpan];
+    __shared__ int counts[8];
+    __shared__ float parts[kGroups - 1][64][9];
+    tc::pdl_launch_dependents();
+    tc::pdl_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, unit = threadIdx.x & 63, group = threadIdx.x >> 6;
+    const int k = (blockIdx.y * 64 + unit) * 8;
+    // lanes 0 .. 7 of every warp have the block's rows
+    const int own_row = blockIdx.x * 8 + lane;
+    int64_t own_tok = -1;
+    int rows = 0;
+    if (lane < 8 && own_row < n) own_tok = tokens[own_row];
+    if (own_tok >= first && own_tok < (int64_t)first + window) {
+        const int2 all = tally[own_tok];
+        if (all.x == own_row) rows = all.y;
     }
-    if (threadIdx.x == 0) slot[tok - first] = t;
-    float *sum = rest + (size_t)t * pitch;
-    for (int i = t; i < n; i += 256) {
-        const int r = i + threadIdx.x;
-        const uint32_t mine = __ballot_sync(0xffffffffu, r < n && tokens[r] == tok);
-        if ((threadIdx.x & 31) == 0) found[threadIdx.x >> 5] = mine;
-        __syncthreads();
-        for (int w = 0; w < 8; ++w)
-            for (uint32_t left = found[w]; left; left &= left - 1) {
-                const int row = i + 32 * w + __ffs(left) - 1;
-                const float by = lost[row];
-                // a thread's columns are its own from row to row
-                for (int k = 8 * threadIdx.x; k < d; k += 8 * 256) {
-                    float v[8];
-                    unpack(*reinterpret_cast<const uint4 *>(x + (size_t)row * pitch + k), v, T());
+    for (uint32_t todo = __ballot_sync(0xffffffffu, rows > 1); todo; todo &= todo - 1) {
+        const int from = __ffs(todo) - 1, t = blockIdx.x * 8 + from;
+        const int64_t tok = __shfl_sync(0xffffffffu, own_tok, from);
+        const int most = __shfl_sync(0xffffffffu, rows, from);
+        const uint32_t mark = mark_of(tok) * 0x01010101u;
+        float sum[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float y = by != 0.f && fabsf(v[e]) < INFINITY ? by * v[e] : 0.f;
-                        sum[k + e] = row == t ? y : sum[k + e] + y;
-                    }
+        for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+        int had = 0;
+        for (int i = t & ~(kSpan - 1); i < n && had < most; i += kSpan) {
+            // this thread's 16 rows; marks past n are read up to the next 16 and not taken
+            const int r0 = i + 16 * threadIdx.x;
+            uint32_t mine = 0;
+            if (r0 < n) {
+                const uint4 m = *reinterpret_cast<const uint4 *>(marks + r0);
+                const uint32_t w[4] = {m.x, m.y, m.z, m.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t hits = __vcmpeq4(w[j], mark) & 0x08040201u;
+                    hits |= hits >> 16;
+                    mine |= ((hits | hits >> 8) & 15u) << (4 * j);
+                }
+                for (uint32_t left = mine; left; left &= left - 1) {
+                    const int e = __ffs(left) - 1;
+                    if (r0 + e >= n || tokens[r0 + e] != tok) mine &= ~(1u << e);
                 }
             }
+            // their places, in the rows' order
+            const int own = __popc(mine);
+            int upto = own;
+#pragma unroll
+            for (int off = 1; off < 32; off *= 2) {
+                const int v = __shfl_up_sync(0xffffffffu, upto, off);
+                if (lane >= off) upto += v;
+            }
+            if (lane == 31) counts[warp] = upto;
+            __syncthreads();
+            int at = upto - own, total = 0;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) {
+                if (w < warp) at += counts[w];
+                total += counts[w];
+            }
+            for (uint32_t left = mine; left; left &= left - 1, ++at) row_of[at] = r0 + __ffs(left) - 1;
+            had += total;
+            __syncthreads();
+            if (k < d)
+                for (int j0 = group; j0 < total; j0 += kGroups * kBatch) {
+                    uint4 raw[kBatch];
+                    float by[kBatch];
+#pragma unroll
+                    for (int j = 0; j < kBatch; ++j) {
+                        const int at_j = j0 + kGroups * j, r = row_of[min(at_j, total - 1)];
+                        raw[j] = *reinterpret_cast<const uint4 *>(x + (size_t)r * pitch + k);
+                        by[j] = at_j < total ? lost[r] : 0.f;
+                    }
+#pragma unroll
+                    for (int j = 0; j < kBatch; ++j) {
+                        float v[8];
+                        unpack(raw[j], v, T());
+                        // what is not finite has had its effect in the product
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) sum[e] += fabsf(v[e]) < INFINITY ? by[j] * v[e] : 0.f;
+                    }
+                }
+            __syncthreads();
+        }
+        if (group)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) parts[group - 1][unit][e] = sum[e];
+        __syncthreads();
+        if (group == 0 && k < d) {
+#pragma unroll
+            for (int g = 0; g < kGroups - 1; ++g)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += parts[g][unit][e];
+            float4 *to = reinterpret_cast<float4 *>(rest + (size_t)t * pitch + k);
+            to[0] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+            to[1] = make_float4(sum[4], sum[5], sum[6], sum[7]);
+        }
         __syncthreads();
     }
 }
@@ -250,7 +340,7 @@ struct Plan {
     int pitch, pieces, width;            // of copies and sums; pieces of the vocabulary
     int split_x, split_w;
     bool slab_x, slab_w;
-    size_t copy_x, copy_w, parts, target, weighed, top, D, sums_x, sums_w, lost, slot, rest, bytes;
+    size_t copy_x, copy_w, parts, target, weighed, top, D, sums_x, sums_w, lost, tally, rest, marks, bytes;
 
     // the loss
     Plan(int n, int d, int vocab, bool aligned) : pitch(round_up(d, 8)) {
@@ -277,7 +367,8 @@ struct Plan {
         weighed = l.take(head ? (size_t)n * pitch * 2 : 0);
         top = l.take(sizeof(int));
         lost = l.take((size_t)n * sizeof(float));
-        slot = l.take(head ? (size_t)width * sizeof(int) : 0);
+        tally = l.take(head ? (size_t)vocab * sizeof(int2) : 0);
+        marks = l.take(head ? (size_t)round_up(n, 16) : 0);
         rest = l.take(head ? (size_t)n * pitch * sizeof(float) : 0);
         copies(l, n, vocab, aligned);
         bytes = l.bytes;
@@ -327,20 +418,22 @@ struct Call {
             using T = decltype(type);
             return run(copy_rows_kernel<T, false>, ceil_div((int64_t)rows * (pitch / 8), 256), 256, static_cast<const T *>(x), ld,
                        rows, d, reinterpret_cast<T *>(out), pitch, (const int64_t *)nullptr, (const float *)nullptr,
-                       (const int *)nullptr);
+                       (const int *)nullptr, (uint8_t *)nullptr, (int2 *)nullptr, 0);
         });
     }
-    cudaError_t weigh(const void *x, int64_t ld, char *out, int pitch, const float *g, const int *top) {
+    cudaError_t weigh(const void *x, int64_t ld, char *out, int pitch, const float *g, const int *top, uint8_t *marks, int2 *tally) {
         return typed([&](auto type) {
             using T = decltype(type);
             return run(copy_rows_kernel<T, true>, ceil_div((int64_t)n * (pitch / 8), 256), 256, static_cast<const T *>(x), ld, n, d,
-                       reinterpret_cast<T *>(out), pitch, tokens, g, top);
+                       reinterpret_cast<T *>(out), pitch, tokens, g, top, marks, tally, vocab);
         });
     }
-    cudaError_t lost_rows(const float *lost, const char *x, int pitch, int first, int window, int *slot, float *rest) {
+    cudaError_t lost_rows(const int2 *tally, const uint8_t *marks, const float *lost, const char *x, int pitch, int first, int window,
+                          float *rest) {
         return typed([&](auto type) {
             using T = decltype(type);
-            return run(lost_rows_kernel<T>, n, 256, tokens, lost, reinterpret_cast<const T *>(x), n, d, pitch, first, window, slot, rest);
+            return launch_k(lost_rows_kernel<T>, dim3(ceil_div(n, 8), ceil_div(d, 512)), dim3(256), 0, s, launches++ > 0, tokens, tally, marks,
+                            lost, reinterpret_cast<const T *>(x), n, d, pitch, first, window, rest);
         });
     }
     cudaError_t sum_splits(const float *slab, int splits, int rows, int pitch, void *out, int64_t ld, const float *g,
@@ -409,19 +502,21 @@ cudaError_t run_grad(Call &c, const void *X, int64_t ldx, const void *W, int64_t
     TRY(c.readable(X, ldx, c.n, c.work + p.copy_x, p.pitch, &x));
     TRY(c.readable(W, ldw, c.vocab, c.work + p.copy_w, p.pitch, &w));
     int *top = reinterpret_cast<int *>(c.work + p.top);
+    uint8_t *marks = reinterpret_cast<uint8_t *>(c.work + p.marks);
+    int2 *tally = reinterpret_cast<int2 *>(c.work + p.tally);
     CUtensorMap mx, mw, md, mb;
     if (dW) {
         if (c.dtype == JARQ_F16) {
             TRY(c.run(top_exponent_kernel, 1, 1024, c.tokens, g, c.n, top));
         }
-        TRY(c.weigh(X, ldx, c.work + p.weighed, p.pitch, g, top));
+        TRY(c.weigh(X, ldx, c.work + p.weighed, p.pitch, g, top, marks, tally));
+        TRY(c.run(tally_kernel, ceil_div(c.n, 256), 256, c.tokens, c.n, c.vocab, tally));
     }
     char *D = c.work + p.D;
     float *sums_x = p.slab_x ? reinterpret_cast<float *>(c.work + p.sums_x) : nullptr;
     float *sums_w = p.slab_w ? reinterpret_cast<float *>(c.work + p.sums_w) : nullptr;
     int sums = 1;                                    // splits of dX
     float *lost = reinterpret_cast<float *>(c.work + p.lost), *rest = reinterpret_cast<float *>(c.work + p.rest);
-    int *slot = reinterpret_cast<int *>(c.work + p.slot);
     for (int i = 0; i < p.pieces; ++i) {
         const int v0 = i * p.width, width = std::min(p.width, c.vocab - v0);
         {
@@ -456,9 +551,10 @@ cudaError_t run_grad(Call &c, const void *X, int64_t ldx, const void *W, int64_t
             a.slab = sums_w, a.pitch = p.pitch;
             a.last = !p.slab_w;
             a.top = top;
-            a.first = v0, a.count = c.n;
-            a.slot = slot, a.rest = rest, a.rest_pitch = p.pitch;
-            TRY(c.lost_rows(lost, c.work + p.weighed, p.pitch, v0, width, slot, rest));
+            a.first = v0;
+            a.tally = tally + v0, a.rest = rest, a.rest_pitch = p.pitch;
+            a.lost = lost, a.w = reinterpret_cast<const uint16_t *>(c.work + p.weighed), a.ldw = p.pitch;
+            TRY(c.lost_rows(tally, marks, lost, c.work + p.weighed, p.pitch, v0, width, rest));
             TRY(c.product(kHead, md, mb, a));
             if (p.slab_w) TRY(c.sum_splits(sums_w, a.splits, width, p.pitch, out, lddw, nullptr, top));
         }

@@ -281,14 +281,16 @@ struct Lost {
             by = a.lost[row];
             if (by != 0.f) w = a.w + at * a.ldw;
         } else {
-            const int slot = a.slot[row];          // of a token without rows: anything
-            if (slot >= 0 && slot < a.count && a.tokens[slot] == (int64_t)a.first + row) rest = a.rest + (size_t)slot * a.rest_pitch;
+            const int2 of = a.tally[row];
+            if (of.y > 1) rest = a.rest + (size_t)of.x * a.rest_pitch;
+            if (of.y != 1) return;
+            by = a.lost[of.x];
+            if (by != 0.f) w = a.w + of.x * a.ldw;
         }
     }
     // columns k .. k + 31 of a row of n; what is not finite has had its effect
     __device__ void add(float (&x)[32], int k, int n, bool half) const {
-        if constexpr (kRows) {
-            if (!w) return;
+        if (w) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 uint32_t v[4] = {0, 0, 0, 0};
@@ -307,11 +309,15 @@ struct Lost {
                     x[8 * i + e] += fabsf(y) < INFINITY ? by * y : 0.f;
                 }
             }
-        } else {
+        }
+        if constexpr (!kRows) {
             if (!rest) return;
 #pragma unroll
-            for (int e = 0; e < 32; ++e)
-                if (k + e < n) x[e] += rest[k + e];
+            for (int e = 0; e < 32; e += 4) {          // its rows are whole units
+                if (k + e >= n) break;
+                const float4 y = *reinterpret_cast<const float4 *>(rest + k + e);
+                x[e] += y.x, x[e + 1] += y.y, x[e + 2] += y.z, x[e + 3] += y.w;
+            }
         }
     }
 };

@@ -354,3 +354,37 @@ def test_a_tokens_own_entry_is_not_rounded(jarq, dtype, n, d, vocab, px):
     assert torch.equal(again[0], dX) and torch.equal(again[1], dW)
     assert torch.equal(jarq.cross_entropy_grad(x, w, t, lse, g.cuda(), hidden=False)[1], dW)
     assert jarq.async_status() == jarq.JARQ_OK
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_of_the_same_token(jarq, dtype):
+    """Tokens that first occur, and come again, on both sides of 16, 2048 and 4096 rows, tokens
+    whose low bytes agree, and one token in every row."""
+    rng = np.random.default_rng(3)
+    n, d, vocab = 9001, 24, 600
+    X = randn(rng, n, d, dtype)
+    W = randn(rng, vocab, d, dtype, 0.1)
+    g = torch.full((n,), 2.0 ** -6 * (1 + 0.9 * HALF[dtype]))
+    for case in ("borders", "all", "any"):
+        tok = torch.as_tensor(rng.integers(0, vocab, n)) if case == "any" else torch.full((n,), 256 if case == "all" else -1)
+        if case == "borders":
+            tok[[0, 15, 16, 2047, 2048, 4095, 4096, 8191, 8192, 9000]] = torch.as_tensor([0, 256, 0, 512, 256, 0, 512, 1, 0, 257])
+        loss, lse = jarq.cross_entropy(X.cuda(), W.cuda(), tok.cuda())
+        args = (X.cuda(), W.cuda(), tok.cuda(), lse, g.cuda())
+        dX, dW = jarq.cross_entropy_grad(*args)
+        assert torch.equal(jarq.cross_entropy_grad(*args)[1], dW)
+        x, w, t = f64(X), f64(W), tok.numpy()
+        logits = x @ w.T
+        live = np.flatnonzero(t >= 0)
+        D = O.logit_gradient(x, w, t, f64(lse), f64(g))
+        p = np.where((t >= 0)[:, None], np.exp(logits - f64(lse)[:, None]), 0.0)
+        rel = logit_error(x, w)[:, None] + 4 * U * (np.abs(logits) + np.abs(f64(lse))[:, None] + 2)
+        rounded = np.abs(D)
+        rounded[live, t[live]] = 0
+        errD = f64(g)[:, None] * (p * rel + FLOOR[dtype]) + rounded * HALF[dtype] + np.abs(D) * 4 * U
+        tiny = float(torch.finfo(X.dtype).tiny) * HALF[dtype]
+        size = np.abs(D).T @ np.abs(x)
+        err = errD.T @ np.abs(x) + (2 * sum_error(n) + HALF[dtype] * (n + 2) * U) * size
+        want = D.T @ x
+        near(dW, want, 1.01 * (err + HALF[dtype] * np.abs(want)) + tiny)
+
