@@ -94,8 +94,9 @@ __device__ __forceinline__ int adapter_of(const AdapterArgs &a, int t) {
 // The CTAs of a cluster share a token: pieces of its width, then, with the sums of all
 // of them, pieces of its outputs.  Bound by latencies (first loads, cluster's join, B's
 // loads) and, outside a graph, by the host: one token 4096 -> 11008 of rank 16 takes 5.9
-// us on the device, a call 20 us.  In two launches with the sums in memory between them
-// it took 4.6 and 26.  48 tokens 11008 -> 4096 8.1 us, 8.4 in two.
+// to 8.0 us on the device, by the machine, a call 20.  In two launches with the sums in memory
+// between them it took 4.6 and 26.  48 tokens 11008 -> 4096 8.1 to 11.1 us, 8.4 in two on
+// the machine of the 8.1.
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ float load_peer(const float *p, uint32_t rank) {
