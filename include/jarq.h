@@ -425,7 +425,8 @@ jarq_status jarq_rms_norm(const void *X, jarq_dtype dtype, int n, int d, int64_t
  * with u = dY gain,
  *     dX[r][k] = dH[r][k] + rstd (u_k - h_k rstd^2 mean_j u_j h_j)  rounded to T,
  *     dgain[k] = sum_r dY[r][k] h[r][k] rstd[r],
- * dX being the gradient of X and of R alike.
+ * dX being the gradient of X and of R alike, of rows of any size that the norm takes
+ * (h rstd is formed first).
  *   H : the normed rows h (X where there was no residual), pitch ldh.
  *   dY, dX : [n][d] of `dtype`, pitches ldy, ldx.  dH : the gradient that reaches h
  *   by the residual stream, pitch lds, or NULL.  dX may be NULL, and may be dY or dH

@@ -4,8 +4,10 @@
 //   h = round(x + r),  rstd = (mean_k h_k^2 + eps)^(-1/2),  v = h gain,
 //   y = round(v rstd),  a = max_k |v_k|,  scale = (a / 127) rstd,  q = rint(v (127 / a)).
 // rstd is one number a row, so it goes into the row's scale and the integers do
-// not depend on the order of the sum behind it.  With u = dy gain,
-//   dx = dh + rstd (u - h rstd^2 mean_k u_k h_k),   dgain = sum_t dy h rstd.
+// not depend on the order of the sum behind it.  With u = dy gain and z = h rstd,
+//   dx = dh + rstd (u - z mean_k u_k z_k),   dgain = sum_t dy z.
+// (z is of unit size whatever the row's; rstd^2 and dy h are not, and leave float32's
+// range for rows of 1e19 and more or less than its inverse.)
 //
 // One pass over memory.  More than a row an SM: blocks go from row to row with the next
 // rows on their way into shared memory.  Few rows: a block a row, which holds it in
@@ -294,7 +296,8 @@ __global__ void __launch_bounds__(P) norm_grad_kernel(GradArgs a) {
             load_gain<E, T>(a.gain, a.wide_gain, k, a.d, g);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                if constexpr (GAIN) acc[i][e] = fmaf(u[i][e] * hv[i][e], rstd, acc[i][e]);
+                hv[i][e] *= rstd;
+                if constexpr (GAIN) acc[i][e] = fmaf(u[i][e], hv[i][e], acc[i][e]);
                 u[i][e] = __fmul_rn(u[i][e], g[e]);
                 dot = fmaf(u[i][e], hv[i][e], dot);
             }
@@ -307,13 +310,14 @@ __global__ void __launch_bounds__(P) norm_grad_kernel(GradArgs a) {
                 load_gain<E, T>(a.gain, a.wide_gain, (int)k, a.d, g);
 #pragma unroll
                 for (int e = 0; e < E; ++e)
-                    dot = fmaf(__fmul_rn(w[e], g[e]), v[e], dot);
+                    dot = fmaf(__fmul_rn(w[e], g[e]), __fmul_rn(v[e], rstd), dot);
             }
         if (!a.dX) continue;
         // the launch before this one may be reading dY still, where dX is dY
         if (!GAIN && turn == 0) tc::pdl_wait();
         // the two rows of `part` take turns: one is written while the other may still be read
-        const float along = rstd * rstd * (row_sum<P>(dot, part[turn]) / (float)a.d);
+        const float along = row_sum<P>(dot, part[turn]) / (float)a.d;
+        // of z and u
         auto put = [&](int k, const float (&v)[E], const float (&w)[E]) {
             float o[E], s[E];
             if (a.dH) load<E>(dh, k, a.d, s);
@@ -336,7 +340,10 @@ __global__ void __launch_bounds__(P) norm_grad_kernel(GradArgs a) {
                 load<E>(dy, (int)k, a.d, w);
                 load_gain<E, T>(a.gain, a.wide_gain, (int)k, a.d, g);
 #pragma unroll
-                for (int e = 0; e < E; ++e) w[e] = __fmul_rn(w[e], g[e]);
+                for (int e = 0; e < E; ++e) {
+                    v[e] = __fmul_rn(v[e], rstd);
+                    w[e] = __fmul_rn(w[e], g[e]);
+                }
                 put((int)k, v, w);
             }
     }
@@ -373,7 +380,7 @@ __global__ void __launch_bounds__(256) gain_columns_kernel(GradArgs a, int rows_
                 s[j] = in ? a.rstd[r] : 0.f;
             }
 #pragma unroll
-            for (int j = 0; j < kBatch; ++j) acc = fmaf(y[j] * h[j], s[j], acc);
+            for (int j = 0; j < kBatch; ++j) acc = fmaf(y[j], h[j] * s[j], acc);
         }
     }
     part[w][lane] = acc;
@@ -592,13 +599,14 @@ __global__ void __launch_bounds__(P, Ring<P, HELD, 2 + STREAM>::resident) norm_g
             unpack(*R::at(ring, s, 1, i), u, T());
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                acc[i][e] = fmaf(u[e] * h[e], rstd, acc[i][e]);
+                const float z = __fmul_rn(h[e], rstd);
+                acc[i][e] = fmaf(u[e], z, acc[i][e]);
                 // as norm_grad_kernel adds it, so that a row's gradient does not depend on the batch
-                dot = fmaf(__fmul_rn(u[e], g[i][e]), h[e], dot);
+                dot = fmaf(__fmul_rn(u[e], g[i][e]), z, dot);
             }
         }
         if (a.dX) {
-            const float along = rstd * rstd * (row_sum<P>(dot, part[turn]) / (float)a.d);
+            const float along = row_sum<P>(dot, part[turn]) / (float)a.d;
             T *dx = static_cast<T *>(a.dX) + r * a.ldx;
 #pragma unroll
             for (int i = 0; i < HELD; ++i) {
@@ -610,7 +618,7 @@ __global__ void __launch_bounds__(P, Ring<P, HELD, 2 + STREAM>::resident) norm_g
                 if (STREAM) unpack(*R::at(ring, s, 2, i), o, T());
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    const float x = fmaf(-h[e], along, __fmul_rn(u[e], g[i][e]));
+                    const float x = fmaf(-__fmul_rn(h[e], rstd), along, __fmul_rn(u[e], g[i][e]));
                     o[e] = STREAM ? fmaf(x, rstd, o[e]) : x * rstd;
                 }
                 store<E>(dx, k, a.d, o);
