@@ -131,6 +131,17 @@ __device__ __forceinline__ float row_sum(float x, float *part) {
     return x;
 }
 
+// 1 / sqrt(mean + eps) of a sum of squares over a row; `again(by)` is the sum of (by h)^2
+// over the row, which is read once more where sum or eps leave what float32 holds in full
+// (an infinity in the row stays one, and rstd is 0).
+template <class F>
+__device__ __forceinline__ float inverse_rms(float sum, int d, float eps, F again) {
+    const float mean = sum / (float)d + eps;
+    if (isinf(mean)) return 0x1p-80f / sqrtf(again(0x1p-80f) / (float)d + eps * 0x1p-80f * 0x1p-80f);
+    if (mean < 0x1p-100f) return 0x1p64f / sqrtf(again(0x1p64f) / (float)d + eps * 0x1p64f * 0x1p64f);
+    return 1.f / sqrtf(mean);
+}
+
 struct NormArgs {
     const void *X, *R, *gain;
     void *H, *Y;
@@ -204,19 +215,16 @@ __global__ void __launch_bounds__(P == 32 ? 256 : P) norm_kernel(NormArgs a) {
         sum = warp_sum(w < P / 32 ? sums[0][w] : 0.f);
         top = __reduce_max_sync(0xffffffffu, w < P / 32 ? tops[w] : 0u);
     }
-    float rstd = 1.f / sqrtf(sum / (float)a.d + a.eps);
-    if (isinf(sum)) {
-        // squares past float32's range: the row scaled by 2^-80 (the row is read
-        // once more; an infinity in it stays one, and rstd is 0)
-        float small = 0.f;
+    const float rstd = inverse_rms(sum, a.d, a.eps, [&](float by) {
+        float part = 0.f;
         for (int64_t k = (int64_t)t * E; k < a.d; k += P * E) {
             float v[E];
             load<E>(again, (int)k, a.d, v);
 #pragma unroll
-            for (int e = 0; e < E; ++e) small = fmaf(v[e] * 0x1p-80f, v[e] * 0x1p-80f, small);
+            for (int e = 0; e < E; ++e) part = fmaf(v[e] * by, v[e] * by, part);
         }
-        rstd = 0x1p-80f / sqrtf(row_sum<P>(small, sums[1]) / (float)a.d);
-    }
+        return row_sum<P>(part, sums[1]);
+    });
     const quant::RowScale by(top);
     if (t == 0) {
         if (a.rstd) a.rstd[r] = rstd;
@@ -512,10 +520,9 @@ __global__ void __launch_bounds__(P, Ring<P, HELD, 1 + RES>::resident) norm_rows
         __syncthreads();
         sum = warp_sum(w < P / 32 ? sums[turn][w] : 0.f);
         top = __reduce_max_sync(0xffffffffu, w < P / 32 ? tops[turn][w] : 0u);
-        float rstd = 1.f / sqrtf(sum / (float)a.d + a.eps);
-        if (isinf(sum)) {
-            // as in norm_kernel: the row, still in the ring, scaled by 2^-80
-            float small = 0.f;
+        const float rstd = inverse_rms(sum, a.d, a.eps, [&](float by) {
+            // the row is still in the ring
+            float part = 0.f;
 #pragma unroll
             for (int i = 0; i < HELD; ++i) {
                 if ((t + i * P) * E >= a.d) continue;
@@ -525,13 +532,13 @@ __global__ void __launch_bounds__(P, Ring<P, HELD, 1 + RES>::resident) norm_rows
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     if (RES) x[e] = to_float(from_float<T>(x[e] + o[e]));
-                    small = fmaf(x[e] * 0x1p-80f, x[e] * 0x1p-80f, small);
+                    part = fmaf(x[e] * by, x[e] * by, part);
                 }
             }
-            small = row_sum<P>(small, again);
+            part = row_sum<P>(part, again);
             __syncthreads();                       // `again` is free for the next row
-            rstd = 0x1p-80f / sqrtf(small / (float)a.d);
-        }
+            return part;
+        });
         const quant::RowScale by(top);
         if (t == 0) {
             if (a.rstd) a.rstd[r] = rstd;

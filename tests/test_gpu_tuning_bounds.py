@@ -36,3 +36,15 @@ def test_gradient_of_rows_whose_squares_leave_the_range(jarq, dtype, size, n, d)
     row[:, ::2] = 1.0
     h = (row * size).to(h.dtype)
     TN.check_grad(jarq, h, None, jarq.rms_norm(h.cuda(), eps=1e-45).rstd.cpu(), torch.ones_like(h), None)
+
+
+@pytest.mark.parametrize("n,d", [(3, 1000), (200, 4096), (5, 999), (2, 40000)])
+@pytest.mark.parametrize("size,eps", [(3e18, 1e37), (3e18, 3e38), (1e19, 1e38), (1e-3, 3.4e38), (3e-21, 1e-41), (1e-22, 1e-44),
+                                      (1e-20, 1e-45), (0.0, 1e-45)])
+def test_eps_of_any_size_counts(jarq, n, d, size, eps):
+    """Sums of squares above and below float32's numbers, beside an eps of their own size."""
+    eps = float(np.float32(eps))
+    rng = np.random.default_rng(d)
+    for dtype in ("float32", "bfloat16"):
+        r, ref = TN.check(jarq, randn(rng, n, d, dtype, size), None, eps=eps)
+        assert r.rstd.isfinite().all() and (r.rstd > 0).all()
