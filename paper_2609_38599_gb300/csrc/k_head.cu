@@ -31,7 +31,8 @@ constexpr int kMostRows = 1 << 22, kMostWidth = 1 << 20, kMostVocab = 1 << 30;
 
 // loss and lse of a row from the maxima m and sums s of its parts: with M the
 // largest m and S = sum s exp(m - M), lse = M + ln S, and the loss is ln S + (M -
-// logit), neither below 0.  PER: threads of a row, over its parts.
+// logit), neither below 0: S has the largest term, 1, whose two approximate factors may
+// make it less.  PER: threads of a row, over its parts.
 template <int PER>
 __global__ void __launch_bounds__(256) loss_join_kernel(const float2 *parts, int count, const float *target,
                                                         const int64_t *tokens, int n, int vocab, float *loss, float *lse) {
@@ -67,13 +68,14 @@ __global__ void __launch_bounds__(256) loss_join_kernel(const float2 *parts, int
         }
     }
     if (t || r >= n) return;
+    s = s < 1.f ? 1.f : s;                         // NaN stays; with M = -inf it counts for nothing
     const float logs = logf(s);
     if (lse) lse[r] = m + logs;
     if (loss) {
         const int64_t tok = tokens[r];
         float v = 0.f;
         if (tok >= vocab) v = __int_as_float(0x7FC00000);
-        else if (tok >= 0) v = m == -INFINITY ? INFINITY + s : logs + (m - target[r]);   // s: 0, or NaN
+        else if (tok >= 0) v = m == -INFINITY ? INFINITY + s : logs + (m - target[r]);
         loss[r] = v;
     }
 }

@@ -9,8 +9,9 @@ torch = pytest.importorskip("torch")
 pytestmark = [pytest.mark.gpu,
               pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a CUDA GPU")]
 
+import test_gpu_cross_entropy as TC  # noqa: E402
 import test_gpu_norm as TN  # noqa: E402
-from test_gpu_norm import randn  # noqa: E402
+from test_gpu_norm import U, randn  # noqa: E402
 
 
 @pytest.fixture(scope="module")
@@ -48,3 +49,28 @@ def test_eps_of_any_size_counts(jarq, n, d, size, eps):
     for dtype in ("float32", "bfloat16"):
         r, ref = TN.check(jarq, randn(rng, n, d, dtype, size), None, eps=eps)
         assert r.rstd.isfinite().all() and (r.rstd > 0).all()
+
+
+def _sure_rows(dtype):
+    """Rows whose largest logit, of many sizes, is all of their mass, and its token."""
+    top = torch.arange(1, 2048) / 32.0
+    whole = top.floor()
+    X = torch.zeros(len(top), 64)
+    X[:, 0], X[:, 1], X[:, 2] = whole, top - whole, 1.0
+    W = torch.zeros(40, 64)
+    W[:, 2] = -200.0
+    W[7, :3] = torch.tensor([1.0, 1.0, 0.0])
+    t = TN.DT[dtype]
+    return X.to(t), W.to(t), torch.full((len(top),), 7), top
+
+
+@pytest.mark.parametrize("dtype", TC.TYPES)
+def test_a_sure_row_has_no_loss_below_0(jarq, dtype):
+    X, W, tok, top = _sure_rows(dtype)
+    for w, t in ((W, tok), (W[7:8], tok - 7)):
+        loss, lse = jarq.cross_entropy(X.cuda(), w.cuda(), t.cuda())
+        # the sum is 1 but for two exponentials of 2^-22 each and the roundings of two
+        # products, an addition and the logarithm
+        top64 = top.double().cuda()
+        assert (loss >= 0).all() and (loss <= 12 * U).all()
+        assert (lse >= top.cuda()).all() and (lse.double() - top64 <= 12 * U + U * top64).all()
