@@ -49,10 +49,12 @@ constexpr int kPart = 32 * 128;            // bytes that a drain warp stages
 constexpr int kBars = 2 * kStages + 5;     // full, empty, afull[2], aempty[2], closing
 constexpr int kSmem = 1024 + kStages * kStage + kDrainWarps * kPart + 8 * kBars + 16;
 constexpr int kThreads = 32 * (2 + kDrainWarps);
-// Chunks of K in one accumulator of the loss: the tensor cores' float32 additions
+// Chunks of K in one accumulator of the logits: the tensor cores' float32 additions
 // round toward zero, which over a long K moves every logit the same way (K = 4096 in
-// one: lse off by 2e-6 of itself); after 1024 the sum goes to the drain's registers.
-constexpr int kLossChunks = 16;
+// one: lse off by 2e-6 of itself); after 1024 the sum goes to the drain's registers. Those
+// of the gradient have to be the loss's own to the last bits: lse is subtracted, and of a
+// token that has nearly all of the mass 1 as well.
+constexpr int kLogitChunks = 16;
 constexpr int kBand = 9;                   // tiles of rows of a band: with as many columns' tiles at one time, the fewest panels
 static_assert(kSmem <= 227 * 1024, "ring and staged parts must fit an SM's shared memory");
 
@@ -208,8 +210,39 @@ struct RowArgs {
     }
 };
 
+// Where a result's 32 columns from c on come from: an accumulator, or the sums of
+// several in registers (c known to the compiler).
+struct InTmem {
+    uint32_t at;
+    __device__ void load(int c, float (&x)[32]) const { load_columns(at + c, x); }
+};
+struct InRegisters {
+    const tc::F2 (&at)[64];
+    __device__ void load(int c, float (&x)[32]) const {
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) tc::f2_get(at[(c + e) / 2], x[e], x[e + 1]);
+    }
+};
+
+// `f(c)` for c = 0, STEP .. below the limit, a step's code once only where the columns
+// may be any.
+template <int STEP, class F>
+__device__ __forceinline__ void columns(const InTmem &, int limit, F f) {
+#pragma unroll 1
+    for (int c = 0; c < limit; c += STEP) f(c);
+}
+template <int STEP, class F>
+__device__ __forceinline__ void columns(const InRegisters &, int limit, F f) {
+#pragma unroll
+    for (int c = 0; c < 128; c += STEP) {
+        if (c >= limit) break;
+        f(c);
+    }
+}
+
 // `cols` columns of logits to D.
-__device__ __forceinline__ void drain_logits(uint32_t acc, const ProductArgs &a, const RowArgs &of, int row0, int lane, int col,
+template <class From>
+__device__ __forceinline__ void drain_logits(const From &from, const ProductArgs &a, const RowArgs &of, int row0, int lane, int col,
                                              int cols, uint32_t part) {
     const int64_t tok = of.token, at = tok - a.first - col;
     const int mine = at >= 0 && at < cols ? (int)at : -1;
@@ -220,13 +253,12 @@ __device__ __forceinline__ void drain_logits(uint32_t acc, const ProductArgs &a,
     const tc::F2 by = tc::f2(g * exp2_approx(-exps.rho));
     uint16_t *out = static_cast<uint16_t *>(a.out) + (size_t)row0 * a.ldo + col;
     const int limit = min(cols, a.n - col);
-#pragma unroll 1
-    for (int c = 0; c < limit; c += 64) {
+    columns<64>(from, limit, [&](int c) {
         uint32_t w[32];
 #pragma unroll
         for (int h = 0; h < 64; h += 32) {
             float x[32];
-            load_columns(acc + c + h, x);
+            from.load(c + h, x);
             if (near) {
 #pragma unroll
                 for (int e = 0; e < 32; e += 2) tc::f2_get(tc::f2_mul(exps.of(tc::f2(x[e], x[e + 1])), by), x[e], x[e + 1]);
@@ -261,7 +293,7 @@ __device__ __forceinline__ void drain_logits(uint32_t acc, const ProductArgs &a,
             if (row0 + r < a.m && k < limit)
                 *reinterpret_cast<uint4 *>(out + (size_t)r * a.ldo + k) = staged(part, lane, i);
         }
-    }
+    });
 }
 
 // What the one rounding of D took from the tokens' own entries goes back in here. Such an
@@ -404,12 +436,16 @@ __device__ __forceinline__ void drain_sums(uint32_t acc, const ProductArgs &a, c
     }
 }
 
+// kLong: the sums over K are those of several accumulators. (One of the gradient's logits is
+// read straight from where it is: 4286 x 160 -> 36623 with both gradients 334 us, by way of
+// registers 348; 2048 x 512 -> 32000 with dX 156 and 164.)
 // kStalled: for the self-test, the issuer stops after one tile.
-template <Product kWhich, bool kStalled>
+template <Product kWhich, bool kLong, bool kStalled>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     tc_head_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, ProductArgs a) {
     constexpr uint32_t kPolls = tc::wait_polls(kStalled);
     constexpr bool kAmn = kWhich == kHead, kBmn = kWhich == kHead || kWhich == kHidden;
+    constexpr bool kSummed = kWhich == kLoss || kLong;   // accumulators summed in registers
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint64_t *bars = (uint64_t *)(smem + kStages * kStage + kDrainWarps * kPart);
@@ -526,7 +562,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     if (c == first || c == c1) {
                         // an accumulator's chunks of K begin
                         c0 = c;
-                        c1 = kWhich == kLoss ? min(last, c + kLossChunks) : last;
+                        c1 = kSummed ? min(last, c + kLogitChunks) : last;
                         ok = tc::mbar_wait<kPolls>(aempty(acc.s), acc.phase);
                         if (!ok) break;
                     }
@@ -571,12 +607,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const Unit unit(u, a);
             const int row0 = unit.ri * 256 + 128 * rank + 32 * q, col = unit.cj * a.cols + half * cols;
             const bool rows = row0 < a.m;          // else nothing is kept of this warp's rows
-            if constexpr (kWhich == kLoss) {
-                const RowArgs of(a, row0 + lane, false);
+            if constexpr (kSummed) {
+                const RowArgs of(a, row0 + lane, kWhich == kLogits);
                 tc::F2 x[64];
 #pragma unroll
                 for (int e = 0; e < 64; ++e) x[e] = tc::f2(0.f);
-                for (int c = 0; c < a.chunks && ok; c += kLossChunks) {
+                for (int c = 0; c < a.chunks && ok; c += kLogitChunks) {
                     ok = filled();
                     if (!ok) break;
 #pragma unroll
@@ -589,12 +625,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     }
                     release();
                 }
-                if (ok && rows) reduce_loss(x, a, row0 + lane, of.token, col, cols, 2 * unit.cj + half);
+                if (!ok || !rows)
+                    ;
+                else if (kWhich == kLoss)
+                    reduce_loss(x, a, row0 + lane, of.token, col, cols, 2 * unit.cj + half);
+                else
+                    drain_logits(InRegisters{x}, a, of, row0, lane, col, cols, part);
             } else if constexpr (kWhich == kLogits) {
                 const RowArgs of(a, row0 + lane, true);
                 ok = filled();
                 if (!ok) break;
-                if (rows) drain_logits(mine + acc.s * 256, a, of, row0, lane, col, cols, part);
+                if (rows) drain_logits(InTmem{mine + acc.s * 256}, a, of, row0, lane, col, cols, part);
                 release();
             } else {
                 const Lost<kWhich == kHidden> lost(a, row0 + lane, unit.split == 0);
@@ -627,10 +668,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     }
 }
 
-template <Product kWhich, bool kStalled = false>
+template <Product kWhich, bool kLong, bool kStalled = false>
 cudaError_t launch(const CUtensorMap &a, const CUtensorMap &b, const ProductArgs &args, cudaStream_t s, bool pdl) {
     static std::atomic<unsigned long long> done;
-    auto *kernel = tc_head_kernel<kWhich, kStalled>;
+    auto *kernel = tc_head_kernel<kWhich, kLong, kStalled>;
     const cudaError_t e = set_max_dynamic_smem((const void *)kernel, kSmem, done);
     if (e != cudaSuccess) return e;
     const int64_t units = (int64_t)args.mt * args.nt * args.splits;
@@ -642,12 +683,12 @@ cudaError_t launch(const CUtensorMap &a, const CUtensorMap &b, const ProductArgs
 
 cudaError_t launch_product(Product which, const CUtensorMap &a, const CUtensorMap &b, const ProductArgs &args,
                            cudaStream_t s, bool pdl, bool stalled) {
-    if (stalled) return launch<kLoss, true>(a, b, args, s, pdl);
+    if (stalled) return launch<kLoss, true, true>(a, b, args, s, pdl);
     switch (which) {
-        case kLoss: return launch<kLoss>(a, b, args, s, pdl);
-        case kLogits: return launch<kLogits>(a, b, args, s, pdl);
-        case kHidden: return launch<kHidden>(a, b, args, s, pdl);
-        default: return launch<kHead>(a, b, args, s, pdl);
+        case kLoss: return launch<kLoss, true>(a, b, args, s, pdl);
+        case kLogits: return args.chunks > kLogitChunks ? launch<kLogits, true>(a, b, args, s, pdl) : launch<kLogits, false>(a, b, args, s, pdl);
+        case kHidden: return launch<kHidden, false>(a, b, args, s, pdl);
+        default: return launch<kHead, false>(a, b, args, s, pdl);
     }
 }
 

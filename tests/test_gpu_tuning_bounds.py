@@ -11,7 +11,7 @@ pytestmark = [pytest.mark.gpu,
 
 import test_gpu_cross_entropy as TC  # noqa: E402
 import test_gpu_norm as TN  # noqa: E402
-from test_gpu_norm import U, randn  # noqa: E402
+from test_gpu_norm import HALF, U, f64, randn  # noqa: E402
 
 
 @pytest.fixture(scope="module")
@@ -74,3 +74,32 @@ def test_a_sure_row_has_no_loss_below_0(jarq, dtype):
         top64 = top.double().cuda()
         assert (loss >= 0).all() and (loss <= 12 * U).all()
         assert (lse >= top.cuda()).all() and (lse.double() - top64 <= 12 * U + U * top64).all()
+
+
+@pytest.mark.parametrize("dtype", TC.TYPES)
+@pytest.mark.parametrize("rival", [0.82, 0.7])
+@pytest.mark.parametrize("n,d,vocab", [(40, 1024, 300), (60, 4096, 300), (300, 8192, 700), (3, 8200, 300)])
+def test_gradient_of_a_sure_token_is_that_of_its_loss(jarq, dtype, n, d, vocab, rival):
+    """Logits of one sign over a long K, and a token that has all but 1e-4 to 1e-2 of the
+    mass: its entry of D is -(1 - exp(-loss)), so the gradient's logits have to be as good
+    as the loss's own."""
+    rng = np.random.default_rng(d)
+    X = torch.as_tensor(rng.uniform(0.5, 1.0, (n, d)).astype(np.float32)).to(TN.DT[dtype])
+    W = torch.zeros(vocab, d, dtype=X.dtype)
+    W[0] = torch.as_tensor((rng.uniform(0.5, 1.0, d) * 50 / d).astype(np.float32)).to(X.dtype)
+    W[1] = (W[0].float() * rival).to(X.dtype)
+    g = torch.full((n,), 64.0)
+    for r in {0, n // 2, n - 1}:
+        # the only row that counts: the token's row of dW is its entry of D times this row of X
+        tok = torch.full((n,), -1)
+        tok[r] = 0
+        x, w, t = X.cuda(), W.cuda(), tok.cuda()
+        loss, lse = jarq.cross_entropy(x, w, t)
+        dW = jarq.cross_entropy_grad(x, w, t, lse, g.cuda(), hidden=False)[1]
+        entry = -np.expm1(-f64(loss)[r])
+        assert 3e-5 < entry < 2e-2
+        # lse rounded once; the loss's sum and D's exponential, 2^-22 each with their factors
+        # and products
+        err = U * abs(f64(lse)[r]) + 16 * U
+        got = -f64(dW[0]) / (64.0 * f64(X[r]))
+        assert (np.abs(got - entry) <= 1.01 * (err + HALF[dtype] * entry)).all(), (np.abs(got - entry).max(), entry)
