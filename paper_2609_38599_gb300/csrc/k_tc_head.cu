@@ -29,6 +29,7 @@
 // into L2 a kilobyte ahead (42 -> 73), tiles of 160 columns where their waves come out even
 // (1.47 ms for 1.18: the rows' operand is read as often as for 256).
 #include <algorithm>
+#include <type_traits>
 
 #include "head.cuh"
 #include "tc_common.cuh"
@@ -49,12 +50,16 @@ constexpr int kPart = 32 * 128;            // bytes that a drain warp stages
 constexpr int kBars = 2 * kStages + 5;     // full, empty, afull[2], aempty[2], closing
 constexpr int kSmem = 1024 + kStages * kStage + kDrainWarps * kPart + 8 * kBars + 16;
 constexpr int kThreads = 32 * (2 + kDrainWarps);
-// Chunks of K in one accumulator of the logits: the tensor cores' float32 additions
-// round toward zero, which over a long K moves every logit the same way (K = 4096 in
-// one: lse off by 2e-6 of itself); after 1024 the sum goes to the drain's registers. Those
-// of the gradient have to be the loss's own to the last bits: lse is subtracted, and of a
-// token that has nearly all of the mass 1 as well.
-constexpr int kLogitChunks = 16;
+// Chunks of K in one accumulator: the tensor cores' float32 additions round toward zero,
+// which over a long K moves every sum the same way (logits over K = 4096 in one: lse off by
+// 2e-6 of itself; dW over 13000 rows of one sign by 8e-5, dX over 15000 tokens by 1.4e-4).
+// Logits go to the drain's registers after 1024 of it. Those of the gradient have to be the
+// loss's own to the last bits: lse is subtracted, and of a token that has nearly all of the
+// mass 1 as well. dX and dW, which are rounded to 16 bits, do so after 4096: 4e-5 then, a
+// twelfth of float16's rounding (after 1024 a step of 8192 x 4096 -> 32000 took 2 % longer,
+// of 100000 x 512 -> 32000 5 %).
+template <Product kWhich>
+constexpr int kSumChunks = kWhich == kLoss || kWhich == kLogits ? 16 : 64;
 constexpr int kBand = 9;                   // tiles of rows of a band: with as many columns' tiles at one time, the fewest panels
 static_assert(kSmem <= 227 * 1024, "ring and staged parts must fit an SM's shared memory");
 
@@ -436,16 +441,18 @@ __device__ __forceinline__ void drain_sums(uint32_t acc, const ProductArgs &a, c
     }
 }
 
-// kLong: the sums over K are those of several accumulators. (One of the gradient's logits is
-// read straight from where it is: 4286 x 160 -> 36623 with both gradients 334 us, by way of
-// registers 348; 2048 x 512 -> 32000 with dX 156 and 164.)
+// kLong: sums over K are those of several accumulators.  (One of the gradient's logits is
+// read straight from where it is: 4286 x 160 -> 36623 with both gradients 334 us, its logits
+// by way of registers 348; 2048 x 512 -> 32000 with dX 156 and 164.  Several go to D from the
+// registers, so that the next tile has both accumulators: a step of 8192 x 4096 -> 32000 took
+// 1.5 % longer where they were put back into the last, as those of dX and dW are, whose code
+// a step of a tile would else be four times as long: 48 x 2048 -> 50001 with dX 126, 129 and 133 us.)
 // kStalled: for the self-test, the issuer stops after one tile.
 template <Product kWhich, bool kLong, bool kStalled>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     tc_head_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, ProductArgs a) {
     constexpr uint32_t kPolls = tc::wait_polls(kStalled);
     constexpr bool kAmn = kWhich == kHead, kBmn = kWhich == kHead || kWhich == kHidden;
-    constexpr bool kSummed = kWhich == kLoss || kLong;   // accumulators summed in registers
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint64_t *bars = (uint64_t *)(smem + kStages * kStage + kDrainWarps * kPart);
@@ -562,7 +569,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     if (c == first || c == c1) {
                         // an accumulator's chunks of K begin
                         c0 = c;
-                        c1 = kSummed ? min(last, c + kLogitChunks) : last;
+                        c1 = kLong ? min(last, c + kSumChunks<kWhich>) : last;
                         ok = tc::mbar_wait<kPolls>(aempty(acc.s), acc.phase);
                         if (!ok) break;
                     }
@@ -603,16 +610,51 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             if (lane == 0) tc::mbar_arrive_cluster(released + 8 * acc.s);
             acc.next();
         };
+        // a unit's sums, in the last of its accumulators
+        auto summed = [&](int chunks, bool rows) {
+            tc::F2 x[64];
+#pragma unroll
+            for (int e = 0; e < 64; ++e) x[e] = tc::f2(0.f);
+            for (int c = 0;; c += kSumChunks<kWhich>) {
+                if (!filled()) return false;
+                const bool last = c + kSumChunks<kWhich> >= chunks;
+#pragma unroll
+                for (int h = 0; h < 128; h += 32) {
+                    float v[32];
+                    if (h >= cols || !rows) break;
+                    load_columns(mine + acc.s * 256 + h, v);
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) x[(h + e) / 2] = tc::f2_add(x[(h + e) / 2], tc::f2(v[e], v[e + 1]));
+                    if (!last) continue;
+#pragma unroll
+                    for (int i = 0; i < 32; i += 16) {
+                        uint32_t w[16];
+                        if (h + i >= cols) break;          // the other half's
+#pragma unroll
+                        for (int e = 0; e < 16; e += 2) {
+                            float lo, hi;
+                            tc::f2_get(x[(h + i + e) / 2], lo, hi);
+                            w[e] = __float_as_uint(lo), w[e + 1] = __float_as_uint(hi);
+                        }
+                        tc::tmem_st16(mine + acc.s * 256 + h + i, w);
+                    }
+                }
+                if (last) break;
+                release();
+            }
+            tc::tmem_wait_st();
+            return true;
+        };
         for (int64_t u = pair; u < units && ok; u += npairs) {
             const Unit unit(u, a);
             const int row0 = unit.ri * 256 + 128 * rank + 32 * q, col = unit.cj * a.cols + half * cols;
             const bool rows = row0 < a.m;          // else nothing is kept of this warp's rows
-            if constexpr (kSummed) {
+            if constexpr (kWhich == kLoss || (kWhich == kLogits && kLong)) {
                 const RowArgs of(a, row0 + lane, kWhich == kLogits);
                 tc::F2 x[64];
 #pragma unroll
                 for (int e = 0; e < 64; ++e) x[e] = tc::f2(0.f);
-                for (int c = 0; c < a.chunks && ok; c += kLogitChunks) {
+                for (int c = 0; c < a.chunks && ok; c += kSumChunks<kWhich>) {
                     ok = filled();
                     if (!ok) break;
 #pragma unroll
@@ -639,7 +681,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 release();
             } else {
                 const Lost<kWhich == kHidden> lost(a, row0 + lane, unit.split == 0);
-                ok = filled();
+                ok = kLong ? summed(min(a.chunks, (unit.split + 1) * a.per) - unit.split * a.per, rows) : filled();
                 if (!ok) break;
                 if (!rows)
                     ;
@@ -684,11 +726,15 @@ cudaError_t launch(const CUtensorMap &a, const CUtensorMap &b, const ProductArgs
 cudaError_t launch_product(Product which, const CUtensorMap &a, const CUtensorMap &b, const ProductArgs &args,
                            cudaStream_t s, bool pdl, bool stalled) {
     if (stalled) return launch<kLoss, true, true>(a, b, args, s, pdl);
+    auto of = [&](auto product) {
+        constexpr Product kWhich = decltype(product)::value;
+        return args.per > kSumChunks<kWhich> ? launch<kWhich, true>(a, b, args, s, pdl) : launch<kWhich, kWhich == kLoss>(a, b, args, s, pdl);
+    };
     switch (which) {
-        case kLoss: return launch<kLoss, true>(a, b, args, s, pdl);
-        case kLogits: return args.chunks > kLogitChunks ? launch<kLogits, true>(a, b, args, s, pdl) : launch<kLogits, false>(a, b, args, s, pdl);
-        case kHidden: return launch<kHidden, false>(a, b, args, s, pdl);
-        default: return launch<kHead, false>(a, b, args, s, pdl);
+        case kLoss: return of(std::integral_constant<Product, kLoss>());
+        case kLogits: return of(std::integral_constant<Product, kLogits>());
+        case kHidden: return of(std::integral_constant<Product, kHidden>());
+        default: return of(std::integral_constant<Product, kHead>());
     }
 }
 

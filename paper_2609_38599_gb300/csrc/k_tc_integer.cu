@@ -181,15 +181,6 @@ __device__ __forceinline__ uint4 load_shared(uint32_t addr) {
 __device__ __forceinline__ void store_shared(uint32_t addr, const uint4 &v) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
-// 16 columns of this warp's 32 TMEM lanes
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
-        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
-        "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
-        : "memory");
-}
-__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // D (+)= A B^T, A in TMEM; of a pair in the TMEM of both CTAs (128 rows each)
 __device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
@@ -237,7 +228,7 @@ __device__ __forceinline__ void convert_channels(uint32_t raw, uint32_t tmem, in
             uint32_t h[16];
             convert16(v[j], h);
             convert16(v[j + 1], h + 8);
-            tmem_st16(to + 8 * (c + j), h);
+            tc::tmem_st16(to + 8 * (c + j), h);
         }
     }
 }
@@ -610,7 +601,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
                 if (!ok) break;
                 tc::tc_fence_after();
                 convert_channels(raws + in.s * kRaw, tmem_a + out.s * kColsA, warp & 3, lane, 0, kShare ? 4 : 8);
-                tmem_wait_st();
+                tc::tmem_wait_st();
                 tc::tc_fence_before();
                 __syncwarp();
                 if (lane == 0) {
@@ -667,7 +658,7 @@ __global__ void __launch_bounds__(Block<NT, VEC, HALF>::threads, 1)
                 }
                 fence_to_async();
                 if (kShare) {
-                    tmem_wait_st();
+                    tc::tmem_wait_st();
                     tc::tc_fence_before();
                 }
                 __syncwarp();

@@ -103,3 +103,56 @@ def test_gradient_of_a_sure_token_is_that_of_its_loss(jarq, dtype, n, d, vocab, 
         err = U * abs(f64(lse)[r]) + 16 * U
         got = -f64(dW[0]) / (64.0 * f64(X[r]))
         assert (np.abs(got - entry) <= 1.01 * (err + HALF[dtype] * entry)).all(), (np.abs(got - entry).max(), entry)
+
+
+# The tensor cores' additions round toward zero, so a sum of one sign that grows in an
+# accumulator loses a part of itself that grows with the number of its terms.  Over 4096 of K,
+# what one accumulator may hold, that part is measured; longer sums are made up of such ones
+# by float32 additions to nearest, and lose no larger a part of themselves.  What is added
+# for: a dozen roundings of an exponential, its factors and the row's lse, as if all had the
+# same sign, and six deviations of a mean of so many uniform errors of half a step of float16.
+def _noise(count):
+    return 6 * HALF["float16"] / (3 * count) ** 0.5 + 12 * U
+
+
+def _drift_of_rows(jarq, n):
+    """Mean part that entries of dW of n rows, all of one sign, are off by, and its noise."""
+    d, vocab = 1280, 4096
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    X = (0.5 + 0.5 * torch.rand(1 << 17, d, generator=gen, device="cuda")).half()[:n]
+    W = (torch.randn(vocab, d, generator=gen, device="cuda") * 0.01).half()
+    tok = torch.randint(0, 64, (1 << 17,), generator=gen, device="cuda")[:n]
+    loss, lse = jarq.cross_entropy(X, W, tok)
+    dW = jarq.cross_entropy_grad(X, W, tok, lse, torch.ones(n, device="cuda"), hidden=False)[1]
+    want = torch.zeros(vocab, d, dtype=torch.float64, device="cuda")
+    for a, s in zip(X.split(1 << 14), lse.split(1 << 14)):
+        want += torch.exp(a.double() @ W.double().T - s.double()[:, None]).T @ a.double()
+    # rows that are no row's token
+    return abs(((dW[64:].double() - want[64:]) / want[64:]).mean().item()), _noise(dW[64:].numel())
+
+
+def test_sums_over_many_rows_do_not_drift(jarq):
+    """dW over 2^17 rows."""
+    part, noise = _drift_of_rows(jarq, 4096)
+    drift, more = _drift_of_rows(jarq, 1 << 17)
+    assert drift <= part + noise + more
+
+
+def test_sums_over_a_large_vocabulary_do_not_drift(jarq):
+    """dX over 2^17 tokens of a head of one sign."""
+    n, d, vocab = 2048, 1280, 1 << 17
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    X = (torch.randn(n, d, generator=gen, device="cuda") * 0.2 / d ** 0.5).half()
+    W = (0.5 + 0.5 * torch.rand(vocab, d, generator=gen, device="cuda")).half()
+    tok = torch.randint(0, vocab, (n,), generator=gen, device="cuda")
+    loss, lse = jarq.cross_entropy(X, W, tok)
+    dX = jarq.cross_entropy_grad(X, W, tok, lse, torch.ones(n, device="cuda"), head=False)[0]
+    size = torch.zeros(n, d, dtype=torch.float64, device="cuda")
+    for w in W.split(1 << 14):
+        size += torch.exp(X.double() @ w.double().T - lse.double()[:, None]) @ w.double()
+    drift = abs(((dX.double() - (size - W[tok].double())) / size).mean().item())
+    # The part is measured on sums of one sign (a row of D is of both: of 4096 tokens its own
+    # entry would turn the sum's sign).  An addition loses units of the sum so far: 2^-23 to 2^-24
+    # of it, by where in a power of two it lies, and so up to twice what other sums lose.
+    part, noise = _drift_of_rows(jarq, 4096)
+    assert drift <= 2 * part + 2 * noise + _noise(dX.numel())
