@@ -9,8 +9,9 @@
 // tile is too small to fill tcgen05's 128 rows: mma.sync, a warp 16 tokens.  A sum over K
 // does not depend on the order of K, so a lane takes 8 neighbouring elements of a row for
 // its share of two MMAs, and the columns of the expansion are dealt out so that a lane's
-// results are 16 bytes of a token.  u is split into two 16-bit parts for the expansion,
-// three where float32 outputs ask for more than bfloat16's give.
+// results are 16 bytes of a token.  u is split into 16-bit parts for the expansion, two of
+// float16 and three of bfloat16, and so kept to 2^-22 of a token's largest whatever the
+// outputs' type: B's terms may cancel one another or Y0.
 //
 // On the device, cold: 8192 tokens 4096 -> 4096 of rank 16 in bfloat16, six adapters, 47
 // to 49 us (201 MB; each launch alone under a profiler: order 9, sums 15 at 4.4 TB/s, outputs
@@ -421,7 +422,8 @@ __global__ void __launch_bounds__(32 * kSumWarps) sums_kernel(AdapterArgs a) {
     }
 }
 
-// u in 16-bit parts: x = x_0 + x_1 (+ x_2) to 2^-22 (2^-24).
+// u in 16-bit parts, x = x_0 + x_1 + ..: two of float16 keep it to 2^-22, of bfloat16 only to
+// 2^-17, three to 2^-24.
 template <int PARTS, class T>
 __device__ __forceinline__ void split(float lo, float hi, uint32_t (&out)[PARTS]) {
 #pragma unroll
@@ -768,7 +770,7 @@ cudaError_t launch_few(const AdapterArgs &a, cudaStream_t s) {
 
 template <class T, class Out, int KS>
 cudaError_t launch_many_as(const AdapterArgs &a, cudaStream_t s) {
-    constexpr int kParts = std::is_same_v<Out, float> && std::is_same_v<T, __nv_bfloat16> ? 3 : 2;
+    constexpr int kParts = std::is_same_v<T, __nv_bfloat16> ? 3 : 2;
     static std::atomic<unsigned long long> done[2];
     auto *sums = sums_kernel<T, 2 * KS>;
     auto *outputs = outputs_kernel<T, Out, KS, kParts>;

@@ -9,9 +9,11 @@ torch = pytest.importorskip("torch")
 pytestmark = [pytest.mark.gpu,
               pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a CUDA GPU")]
 
+import test_gpu_adapters as TA  # noqa: E402
 import test_gpu_cross_entropy as TC  # noqa: E402
 import test_gpu_norm as TN  # noqa: E402
-from test_gpu_norm import HALF, U, f64, randn  # noqa: E402
+from oracle import jarq_tuning as O  # noqa: E402
+from test_gpu_norm import HALF, U, f64, near, randn  # noqa: E402
 
 
 @pytest.fixture(scope="module")
@@ -156,3 +158,30 @@ def test_sums_over_a_large_vocabulary_do_not_drift(jarq):
     # of it, by where in a power of two it lies, and so up to twice what other sums lose.
     part, noise = _drift_of_rows(jarq, 4096)
     assert drift <= 2 * part + 2 * noise + _noise(dX.numel())
+
+
+@pytest.mark.parametrize("dtype", TA.TYPES)
+@pytest.mark.parametrize("n", [40, 65, 300])
+@pytest.mark.parametrize("din,dout,rank", [(8, 64, 8), (12, 33, 16), (40, 300, 64)])
+def test_adapters_terms_that_cancel(jarq, dtype, n, din, dout, rank):
+    """Terms of B (A x) that cancel all but 2^-14 of themselves: the sums A x are kept to
+    2^-22 of a token's largest, for outputs of the inputs' own type too, whatever the form."""
+    rng = np.random.default_rng(n + din)
+    t = TN.DT[dtype]
+    X = torch.as_tensor(rng.integers(4, 8, (n, din)) / 8.0).to(t)
+    # multiples of 2^-21 below 8: sums A x that any order of float32 additions has exactly
+    A = torch.zeros(3, rank, din, dtype=torch.float64)
+    A[:, ::2, :8] = torch.as_tensor(rng.integers(4, 8, (3, rank // 2, 8)) / 8.0)
+    A[:, 1::2] = A[:, ::2]
+    A[:, :, 3] = torch.as_tensor(rng.integers(64, 128, (3, rank)) * 2.0 ** -18)
+    A = A.to(t)
+    # pairs of rows that differ in that column alone, with opposite powers of two
+    B = torch.as_tensor(2.0 ** rng.integers(-1, 1, (3, dout, rank))).to(t)
+    B[:, :, 1::2] = -B[:, :, ::2]
+    ids = torch.as_tensor(rng.integers(0, 3, n).astype(np.int32))
+    got = jarq.apply_adapters(*(v.cuda() for v in (X, A, B, ids)))
+    x, a, b, i = f64(X), f64(A), f64(B), ids.numpy()
+    want = O.apply_adapters(x, a, b, i)
+    # what is kept of the sums, and an addition a term
+    err = [np.abs(a[k] @ row).max() * (np.abs(b[k]).sum(1) * 2.0 ** -22 + rank * U) for k, row in zip(i, x)]
+    near(got, want, 1.01 * (np.array(err) + HALF[dtype] * np.abs(want)) + float(torch.finfo(t).tiny) * HALF[dtype])
