@@ -185,3 +185,31 @@ def test_adapters_terms_that_cancel(jarq, dtype, n, din, dout, rank):
     # what is kept of the sums, and an addition a term
     err = [np.abs(a[k] @ row).max() * (np.abs(b[k]).sum(1) * 2.0 ** -22 + rank * U) for k, row in zip(i, x)]
     near(got, want, 1.01 * (np.array(err) + HALF[dtype] * np.abs(want)) + float(torch.finfo(t).tiny) * HALF[dtype])
+
+
+@pytest.mark.parametrize("dtype", TA.TYPES)
+@pytest.mark.parametrize("n", [5, 65, 200])
+@pytest.mark.parametrize("scale", [1e-36, 1e-30, 1e28, 1e32, 1e35])
+def test_adapters_scales_of_any_size(jarq, dtype, n, scale):
+    """float32 outputs of scaled sums beyond 2^100 and below 2^-100."""
+    rng = np.random.default_rng(n)
+    X, A, B, ids, s, base = TA.inputs(rng, n, 200, 96, 24, 3, dtype, "float32")
+    TA.check(jarq, X, A, B, ids, s * scale, base * scale)
+
+
+@pytest.mark.parametrize("dtype", TA.TYPES)
+def test_adapters_infinite_sums_are_the_same_in_both_forms(jarq, dtype):
+    """An infinity in a token: its outputs are infinite, or NaN where terms of both signs
+    meet, whatever the number of tokens."""
+    rng = np.random.default_rng(1)
+    X, A, B, ids, s, base = TA.inputs(rng, 80, 64, 40, 16, 3, dtype)
+    X[5, 3], X[60, 9] = float("inf"), -float("inf")
+    ids[5], ids[60] = 1, 2
+    A[1, :, 3], A[2, :, 9] = A[1, :, 3].abs() + 0.01, A[2, :, 9].abs() + 0.01
+    B[1, :20], B[2, 10:] = B[1, :20].abs() + 0.01, -B[2, 10:].abs() - 0.01
+    many = jarq.apply_adapters(*(t.cuda() for t in (X, A, B, ids)), scale=s.cuda(), base=base.cuda())
+    few = torch.cat([jarq.apply_adapters(X[k].cuda(), A.cuda(), B.cuda(), ids[k].contiguous().cuda(), scale=s.cuda(), base=base[k].cuda())
+                     for k in (slice(0, 40), slice(40, 80))])
+    assert (few[5, :20] == float("inf")).all() and (few[60, 10:] == float("inf")).all()
+    for f in (torch.isnan, torch.isposinf, torch.isneginf):
+        assert torch.equal(f(many), f(few))
