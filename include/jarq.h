@@ -466,16 +466,18 @@ jarq_status jarq_cross_entropy(const void *X, jarq_dtype dtype, int n, int d, in
  * hidden states and the head: with D_rv = g_loss[r] (exp(l_rv - lse[r]) - [v =
  * tokens[r]]),  dX = D W  and  dW = D^T X.  The logits are formed once more and D a
  * piece of the vocabulary at a time (of up to 512 MB, at least 4096 tokens), rounded
- * to 16 bits with full relative precision, and what that takes from the tokens' own
- * entries is added to the sums, which are float32 (the tensor cores' own additions, which
- * round toward zero, over 1024 terms of a logit and 4096 of dX and dW).
+ * to 16 bits (float16: entries below 2^-27 of |g_loss[r]| with fewer bits, to multiples of
+ * 2^-37 of it or less), and what that takes from the tokens' own entries is added to the
+ * sums, which are float32 (the tensor cores' own additions, which round toward zero, over
+ * 1024 terms of a logit and 4096 of dX and dW).
  *   X to tokens : as there.  lse : its result.  g_loss : float32 [n].
  *   dX : [n][d], dW : [vocab][d] of `dtype`, pitches lddx, lddw, overwritten (dW with
  *   zeros for n = 0); one of them may be NULL.
  *   workspace, rows_aligned : as there; hidden, head : whether dX, dW are given.
  * An ignored row gets gradient 0 and adds nothing to dW, whatever X holds there; a
- * token >= vocab makes its row of dX, and all of dW, NaN.  For float16, rows whose
- * |g_loss| lies more than 2^14 below the largest lose precision in dW. */
+ * token >= vocab makes its row of dX, and all of dW, NaN.  For float16, entries of X
+ * whose |X g_loss| lies more than 2^28 below the largest lose precision in dW, and a
+ * |g_loss| below 2^-126 counts as 0. */
 size_t jarq_cross_entropy_grad_workspace(int n, int d, int vocab, int rows_aligned, int hidden,
                                          int head);
 jarq_status jarq_cross_entropy_grad(const void *X, jarq_dtype dtype, int n, int d, int64_t ldx,

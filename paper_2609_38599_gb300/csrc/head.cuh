@@ -48,7 +48,8 @@ struct ProductArgs {
 
 // Float16 holds too few exponents for a gradient: row r of D is kept as
 // D_r 2^(14 - e_r) with |g_r| 2^-e_r in [1/2, 1), so |D| <= 2^14, and probabilities
-// down to 2^-29 keep all their bits.  Powers of two are exact, and undone at the end.
+// down to 2^-27 keep all their bits (float16's smallest normal number is 2^-14); smaller
+// ones are rounded to multiples of 2^-38 to 2^-37.  Powers of two are exact, and undone at the end.
 __device__ __forceinline__ int exponent(float g) { return (int)((__float_as_uint(g) >> 23) & 255) - 126; }
 __device__ __forceinline__ float scaled(float g) {
     const int e = exponent(g);

@@ -213,3 +213,44 @@ def test_adapters_infinite_sums_are_the_same_in_both_forms(jarq, dtype):
     assert (few[5, :20] == float("inf")).all() and (few[60, 10:] == float("inf")).all()
     for f in (torch.isnan, torch.isposinf, torch.isneginf):
         assert torch.equal(f(many), f(few))
+
+
+@pytest.mark.parametrize("n,d,vocab,pitch", [(100, 128, 300, 128), (1000, 72, 500, 72), (100, 77, 300, 80)])
+@pytest.mark.parametrize("size,spread", [(1.0, 14), (0.05, 12), (2.0 ** -9, 10), (30.0, 14), (0.05, 0)])
+def test_float16_head_gradient_of_small_states_and_weights(jarq, n, d, vocab, pitch, size, spread):
+    """Rows of small weight that alone have their token, of hidden states of any size: their
+    share of dW keeps all its bits beside rows of large weight."""
+    rng = np.random.default_rng(n)
+    X, W = randn(rng, n, d, "float16", size), randn(rng, vocab, d, "float16", 1 / (size * d ** 0.5))
+    X[:, ::7] = (X[:, ::7].float() * 2.0 ** -3).half()
+    tok = torch.as_tensor(rng.permutation(vocab)[np.arange(n) % vocab])
+    tok[3] = -1
+    g = 2.0 ** -rng.uniform(0, spread, n)
+    g[::9] = 2.0 ** -spread
+    # up to where float16 holds the largest of the results, and the smallest are normal numbers
+    g = torch.as_tensor((g * 2.0 ** (12 - np.ceil(np.log2(size)))).astype(np.float32))
+    x, w, t = TN.device(X, pitch), W.cuda(), tok.cuda()
+    loss, lse = jarq.cross_entropy(x, w, t)
+    # (dX of the same weights would leave float16's range)
+    dW = TC.check_grad(jarq, X, W, tok, lse, g, (x, w, t, lse, g.cuda()), hidden=False)[1]
+    again = jarq.cross_entropy_grad(x, w, t, lse, g.cuda(), hidden=False)[1]
+    assert torch.equal(again, dW)
+
+
+def test_float16_head_gradient_of_states_that_are_zero_or_not_finite(jarq):
+    rng = np.random.default_rng(1)
+    X, W, tok, g = TC.inputs(rng, 70, 64, 300, "float16", ignored=False)
+    for rows in (slice(0, 70), slice(0, 0)):
+        Y = X.clone()
+        Y[rows] = 0
+        Y[5] = 65504.0 if rows.stop == 0 else 0
+        loss, lse = jarq.cross_entropy(Y.cuda(), W.cuda(), tok.cuda())
+        TC.check_grad(jarq, Y, W, tok, lse, g)
+    X[9], tok[9] = float("inf"), -1
+    X[11], g[11] = float("nan"), 0.0
+    tok[11] = -1
+    loss, lse = jarq.cross_entropy(X.cuda(), W.cuda(), tok.cuda())
+    lse[[9, 11]] = 0
+    Y = X.clone()
+    Y[[9, 11]] = 0
+    TC.check_grad(jarq, Y, W, tok, lse, g, (X.cuda(), W.cuda(), tok.cuda(), lse, g.cuda()))
