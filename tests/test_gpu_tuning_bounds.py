@@ -254,3 +254,29 @@ def test_float16_head_gradient_of_states_that_are_zero_or_not_finite(jarq):
     Y = X.clone()
     Y[[9, 11]] = 0
     TC.check_grad(jarq, Y, W, tok, lse, g, (X.cuda(), W.cuda(), tok.cuda(), lse, g.cuda()))
+
+
+@pytest.mark.parametrize("dtype", TC.TYPES)
+@pytest.mark.parametrize("n,d,vocab", [(8200, 1280, 4096), (2048, 1278, 16390), (4100, 2056, 4100), (200, 1100, 60001)])
+def test_sums_of_several_accumulators(jarq, dtype, n, d, vocab):
+    """Every entry of both gradients where sums take more than one accumulator: with and
+    without splits, tiles of any width, edges of rows and columns."""
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    t = TN.DT[dtype]
+    X = torch.randn(n, d, generator=gen, device="cuda").to(t)
+    W = (torch.randn(vocab, d, generator=gen, device="cuda") * 2 / d ** 0.5).to(t)
+    tok = torch.randint(-1, vocab, (n,), generator=gen, device="cuda")
+    g = 0.5 + torch.rand(n, generator=gen, device="cuda")
+    loss, lse = jarq.cross_entropy(X, W, tok)
+    dX, dW = jarq.cross_entropy_grad(X, W, tok, lse, g)
+    x, w = X.double(), W.double()
+    D = torch.exp(x @ w.T - lse.double()[:, None])
+    live = (tok >= 0).nonzero()[:, 0]
+    D[live, tok[live]] -= 1.0
+    D *= torch.where(tok >= 0, g, 0.0).double()[:, None]
+    h = HALF[dtype]
+    for got, want, size in ((dX, D @ w, D.abs() @ w.abs()), (dW, D.T @ x, D.abs().T @ x.abs())):
+        # one rounding of D and one of the result; sums and statistics in float32
+        assert ((got.double() - want).abs() <= 1.01 * h * (size + want.abs()) + 1e-4 * size + 2.0 ** -24).all()
+    again = jarq.cross_entropy_grad(X, W, tok, lse, g)
+    assert torch.equal(again[0], dX) and torch.equal(again[1], dW)
