@@ -467,9 +467,9 @@ jarq_status jarq_cross_entropy(const void *X, jarq_dtype dtype, int n, int d, in
  * tokens[r]]),  dX = D W  and  dW = D^T X.  The logits are formed once more and D a
  * piece of the vocabulary at a time (of up to 512 MB, at least 4096 tokens), rounded
  * to 16 bits (float16: entries below 2^-27 of |g_loss[r]| with fewer bits, to multiples of
- * 2^-37 of it or less), and what that takes from the tokens' own entries is added to the
- * sums, which are float32 (the tensor cores' own additions, which round toward zero, over
- * 1024 terms of a logit and 4096 of dX and dW).
+ * 2^-37 of it or less; a probability below 2^-126 is 0), and what that takes from the
+ * tokens' own entries is added to the sums, which are float32 (the tensor cores' own
+ * additions, which round toward zero, over 1024 terms of a logit and 4096 of dX and dW).
  *   X to tokens : as there.  lse : its result.  g_loss : float32 [n].
  *   dX : [n][d], dW : [vocab][d] of `dtype`, pitches lddx, lddw, overwritten (dW with
  *   zeros for n = 0); one of them may be NULL.

@@ -280,3 +280,37 @@ def test_sums_of_several_accumulators(jarq, dtype, n, d, vocab):
         assert ((got.double() - want).abs() <= 1.01 * h * (size + want.abs()) + 1e-4 * size + 2.0 ** -24).all()
     again = jarq.cross_entropy_grad(X, W, tok, lse, g)
     assert torch.equal(again[0], dX) and torch.equal(again[1], dW)
+
+
+@pytest.mark.parametrize("dtype", TC.TYPES)
+@pytest.mark.parametrize("n,d,vocab", [(1, 1, 1), (3, 1, 5), (5, 3, 300), (1, 7, 40), (300, 2, 1)])
+def test_narrowest_heads(jarq, dtype, n, d, vocab):
+    rng = np.random.default_rng(n + d)
+    X, W, tok, g = TC.inputs(rng, n, d, vocab, dtype)
+    loss, lse = TC.check_loss(jarq, X, W, tok)
+    TC.check_grad(jarq, X, W, tok, lse, g)
+
+
+@pytest.mark.parametrize("dtype", TC.TYPES)
+@pytest.mark.parametrize("size", [40.0, 300.0])
+@pytest.mark.parametrize("d", [64, 1100])
+def test_logits_of_any_size(jarq, monkeypatch, dtype, size, d):
+    """Logits on both sides of 2^16, where the exponentials are formed another way, in the
+    same rows' neighbours too."""
+    # an exponential below 2^-126, float32's smallest normal number, is 0: so much of |g| may be
+    # missing from an entry of D, which bfloat16 would hold (and round by less than 2^-133)
+    monkeypatch.setitem(TC.FLOOR, "bfloat16", 2.0 ** -126 + 2.0 ** -133)
+    rng = np.random.default_rng(d)
+    X, W, tok, g = TC.inputs(rng, 50, d, 700, dtype, scale=2.0, ignored=False)
+    X[::3] = (X[::3].float() * size).to(X.dtype)
+    W = (W.float() * size).to(W.dtype)
+    g[::2] = -g[::2]
+    loss, lse = TC.check_loss(jarq, X, W, tok)
+    TC.check_grad(jarq, X, W, tok, lse, g)
+
+
+@pytest.mark.parametrize("dtype", TA.TYPES)
+@pytest.mark.parametrize("n", [1, 3, 70])
+@pytest.mark.parametrize("din,dout", [(1, 1), (3, 1), (1, 70), (7, 5)])
+def test_narrowest_adapters(jarq, dtype, n, din, dout):
+    TA.check(jarq, *TA.inputs(np.random.default_rng(n), n, din, dout, 8, 3, dtype))
