@@ -288,11 +288,12 @@ jarq_status jarq_pack_codes(const uint8_t *Q, int dout, int din, int bits, uint3
 jarq_status jarq_accumulate_hessian(const void *X, int n, int d, float scale, float *H,
                                     void *stream);
 
-/* ---- running, scoring and tuning a quantized model (device memory only) ----
+/* ---- running and scoring a quantized model (device memory only) ----
  * The paper judges a quantized model by the probabilities that it gives to
  * tokens (Sec. 4, perplexity).  These operators run a layer in integers, norm
  * its inputs and add adapters to it, score logits, and form the loss of an output
- * head with its gradient.  They differ from the calls above in three points, since a
+ * head.  The loss, the norm and the log probabilities have gradients; a layer in
+ * integers and the adapters have none, so a way back ends before them.  They differ from the calls above in three points, since a
  * generation step takes microseconds on the device:
  * - They only enqueue their work on `stream` and return; results are ready in
  *   stream order, and the calls can be captured in a CUDA graph (a process's
@@ -415,7 +416,9 @@ jarq_status jarq_token_logprobs_grad(const void *logits, jarq_dtype dtype, int n
  *   eps : > 0, finite.  Y may be NULL.  Q : int8 [n][d], pitch ldq, and scale :
  *   float32 [n], both or neither.  rstd : float32 [n], may be NULL.
  *   n >= 0, d >= 1, both at most 2^31 - 4096.
- * Sums are float32.  A row's outputs do not depend on the other rows of a call. */
+ * Sums are float32.  A row's outputs do not depend on what the other rows of a call hold,
+ * nor on how many they are where all rows lie on 16-byte boundaries: elsewhere the sums of
+ * a call of one row, whose pitch plays no part, may be added in another order. */
 jarq_status jarq_rms_norm(const void *X, jarq_dtype dtype, int n, int d, int64_t ldx, const void *R,
                           int64_t ldr, void *H, int64_t ldh, const void *gain, jarq_dtype gain_dtype,
                           float eps, void *Y, int64_t ldy, int8_t *Q, int64_t ldq, float *scale,

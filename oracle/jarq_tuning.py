@@ -1,7 +1,7 @@
 """Norms, the loss of an output head and adapters in float64 NumPy, from their
 definitions.
 
-Test infrastructure for the operators that run, score and tune a quantized model:
+Test infrastructure for the operators that run and score a quantized model:
 the root-mean-square norm of rows with its 8-bit integers and its gradient, the
 softmax cross entropy of hidden states under a head with its gradient, and low-rank
 adapters of many requests.

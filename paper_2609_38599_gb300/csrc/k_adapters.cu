@@ -13,10 +13,11 @@
 // float16 and three of bfloat16, and so kept to 2^-22 of a token's largest whatever the
 // outputs' type: B's terms may cancel one another or Y0.
 //
-// On the device, cold: 8192 tokens 4096 -> 4096 of rank 16 in bfloat16, six adapters, 47
+// On the device, cold: 8192 tokens 4096 -> 4096 of rank 16 in bfloat16, six adapters, 48.5
 // to 49 us (201 MB; each launch alone under a profiler: order 9, sums 15 at 4.4 TB/s, outputs
-// 26 at 5.2); 276 x 4236 -> 2009, rank 8, float32 outputs, rows on no boundary 21 us; 2392 x
-// 992 -> 745, rank 64, 38 adapters in any order, float32 38 us.  States on the way, which
+// 25 at 5.2), of rank 64 94; 276 x 4236 -> 2009, rank 8, float32 outputs, rows on no boundary
+// 23 us; 2392 x 992 -> 745, rank 64, 38 adapters in any order, float32 41 us.  With two parts of
+// bfloat16 for three 0.5 us less, of rank 64 7.  States on the way, which
 // differ in more than one thing each: operands straight into a lane's registers 74 to 103
 // us, into places of each lane's own in shared memory 87, tiles of one adapter instead
 // of two walked one after the other (the other blocks had ended) 61, whole lines 53.

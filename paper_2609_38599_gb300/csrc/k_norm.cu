@@ -12,17 +12,17 @@
 // One pass over memory.  More than a row an SM: blocks go from row to row with the next
 // rows on their way into shared memory.  Few rows: a block a row, which holds it in
 // registers from the loads to the outputs, and the gains' gradient by columns beside it.
-// Threads of a row and the order of its sums go by its width alone, so that a row's
-// outputs do not depend on the batch.  Rows are read 16 bytes at a time where every
+// Threads of a row and the order of its sums go by its width and by whether the rows lie on
+// 16-byte boundaries, so that a row's outputs do not depend on the batch.  Rows are read 16 bytes at a time where every
 // array's rows lie on 16-byte boundaries, else an element at a time, neighbouring threads
 // reading neighbouring elements.
 //
 // Bound by memory, near the issue slots (70 % of them in the forward): on the device, cold
-//   8192 x 4096 bfloat16, residual, integers     40.5 us (235 MB, 5.8 TB/s)
+//   8192 x 4096 bfloat16, residual, integers     40 us (235 MB, 5.8 TB/s)
 //   its gradient, with a residual's and gains'   53 us (268 MB, 5.1 TB/s; 47 and the join of
 //                                                the blocks' parts, 7.5 MB, in a launch of its own)
 //   one row of 4096, residual                    3.4 us (a launch and three latencies)
-//   48 x 11008 float16, gradient                 5.9 us
+//   48 x 11008 float16, gradient                 6.0 us
 //   7653 x 997 float16, residual, values         26 us (rows on no boundary: an element a lane)
 // A block of one row each, and of several without a ring, took 65 us and 204.  Two elements
 // an instruction throughout: 41 and 57.

@@ -10,16 +10,17 @@
 //   warp 0      TMA producer: its own 128 rows of A and half of B's columns
 //   warp 1      TMEM allocation; in the even CTA the MMA issuer
 //   warps 2..9  drain: lane quarter w % 4, half of the columns, of one accumulator
-//               while the MMAs of the next tile fill the other
+//               while the MMAs of the next fill the other (of the same tile, over a long K)
 // A row of the loss lies in one thread: its maximum and sum need no exchange.
 // Results leave through 4 KB of shared memory a warp, 128 bytes of a row at a time.
 //
 // Bound by the MMAs where there are many rows, by reading W where there are few:
 //   2048 x 4096 -> 32000 bfloat16, loss    277 us, 1.94 PFLOP/s (in a long loop under the
 //                                          power cap 314, 1.71: a library's product in both)
-//   8192 x 4096 -> 32000, the four products of a step 1.08, 1.11, 1.14 and 1.14 ms; tensor
-//                                          pipes 93 to 97 % active
-//   1000 x 1344 -> 50001 float16           78, 84 and 80 us for logits, D and dX (1.7 PFLOP/s:
+//   8192 x 4096 -> 32000, the four products of a step 1.07, 1.10, 1.16 and 1.17 ms
+//   6144 x 2048 -> 16000, the same          203, 212, 236 and 226 us; tensor pipes 92, 89, 77 and
+//                                          83 % active
+//   1000 x 1344 -> 50001 float16           77, 85 and 87 us for logits, D and dX (1.6 PFLOP/s:
 //                                          21 chunks of K a tile, the last wave's tail)
 //   48 x 2048 -> 50001 float16             40 us (205 MB); one row, 7976 -> 86781 226 us (6.1 TB/s)
 // Rows past the tokens: their boxes, filled with zeros by TMA, held the one row's call to

@@ -497,7 +497,7 @@ def objective(hess: Hessian, W, S, Q, Z, bits: int, out=None):
     return F
 
 
-# ---- running, scoring and tuning a quantized model: device tensors, enqueued on torch's
+# ---- running and scoring a quantized model: device tensors, enqueued on torch's
 # current stream, not waited for.  A call takes a few microseconds on the device,
 # so little is done here: every attribute of a tensor is looked at once. ----
 
