@@ -442,12 +442,12 @@ __device__ __forceinline__ void drain_sums(uint32_t acc, const ProductArgs &a, c
     }
 }
 
-// kLong: sums over K are those of several accumulators.  (One of the gradient's logits is
-// read straight from where it is: 4286 x 160 -> 36623 with both gradients 334 us, its logits
-// by way of registers 348; 2048 x 512 -> 32000 with dX 156 and 164.  Several go to D from the
-// registers, so that the next tile has both accumulators: a step of 8192 x 4096 -> 32000 took
-// 1.5 % longer where they were put back into the last, as those of dX and dW are, whose code
-// a step of a tile would else be four times as long: 48 x 2048 -> 50001 with dX 126, 129 and 133 us.)
+// kLong: sums over K are those of several accumulators.  (One alone is read straight from
+// where it is: 4286 x 160 -> 36623 with both gradients 334 us, its logits by way of registers
+// 348; 2048 x 512 -> 32000 with dX 156 and 164.)  Several logits go to D from the registers, so
+// that the next tile has both accumulators: put back into the last, a step of 8192 x 4096 ->
+// 32000 took 1.5 % longer.  dX and dW are put back: their epilogue from registers, its code
+// unrolled, took 48 x 2048 -> 50001 with dX from 129 to 133 us.
 // kStalled: for the self-test, the issuer stops after one tile.
 template <Product kWhich, bool kLong, bool kStalled>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
